@@ -408,6 +408,129 @@ sd_status sd_sample_logits_noalloc(int32_t n_users, const int32_t* user_ids, con
                                    const float* logits, int32_t mode, uint64_t seed, uint64_t round,
                                    const float* accept_u, int32_t* result, sd_stream stream);
 
+/*
+ * What a request brings of its own: sampling options and an adapter.  The
+ * calls below need no context; sd_user_sampling and sd_user_adapter apply the
+ * same to the users of a verification batch.  All pointers but those said
+ * to be host ones are device pointers on the current device; nothing waits,
+ * allocates or copies, so the calls can be captured into a graph, whose
+ * replays read the arrays' contents of that time.  A workspace belongs to one
+ * call at a time: calls that may overlap (two streams, two graphs) take
+ * one each.  Its contents need not be kept from one call to the next.
+ */
+
+/*
+ * Sampling options of n_rows rows of logits, device arrays [n_rows]; a NULL
+ * array is off for every row (so is a NULL sd_filter).  Every value has a
+ * meaning, so nothing needs to be checked on the device:
+ *   temperature: T > 0; T <= 0 or NaN: the first largest logit alone
+ *   top_k:       <= 0: off
+ *   top_p:       >= 1 or NaN: off; <= 0: the first largest logit alone
+ *   min_p:       <= 0 or NaN: off; >= 1: the logits equal to the largest
+ * A row's eligible tokens are those with a logit above -inf that is not
+ * NaN; where some are +inf, those alone.  With m the largest logit, eligible
+ * tokens weigh w_k = exp((z_k - m) / T).  Ordered by z descending, ties by
+ * index ascending, the token of rank r (from 0) is kept iff r = 0 or all of
+ *   r < top_k,   sum of w over ranks < r  <  top_p * (sum of all w),
+ *   w_r >= min_p
+ * hold: each filter looks at the whole distribution at temperature T, and a
+ * token has to pass all.  Weights and their sums are held in 64 bits
+ * (multiples of at most V 2^-62 of the largest weight): results are the same
+ * on every run.
+ */
+typedef struct sd_filter {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+} sd_filter;
+
+#define SD_FILTER_MAX_ROWS 65535
+#define SD_FILTER_MAX_VOCAB (1 << 20)
+
+/* Bytes of workspace (256-byte aligned device memory) of the two calls that
+ * follow.  Host only.  SD_EINVAL: n_rows or vocab < 1; SD_ELIMIT: beyond the
+ * limits above. */
+sd_status sd_filter_query_size(int32_t n_rows, int32_t vocab, uint64_t* workspace_bytes);
+
+/*
+ * One token a row from given uniforms: the first token in index order whose
+ * running sum of kept weights exceeds u * (sum of kept weights).
+ *   logits:  [n_rows] rows of `vocab` elements of type `dtype` (SD_F32 or
+ *            SD_BF16), row_stride (>= vocab) elements apart
+ *   filter:  host struct of device arrays, or NULL
+ *   u:       fp32 [n_rows] in [0, 1) (clamped to 0 .. 1 - 2^-24; NaN is 0)
+ *   token:   int32 [n_rows]
+ *   prob:    fp32 [n_rows] or NULL: the token's probability among the kept
+ *   kept:    int32 [n_rows] or NULL: number of kept tokens
+ * A row without eligible token gives token -1, prob 0 and kept 0.
+ * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, dtype,
+ * stride), SD_ELIMIT, SD_ENOMEM (workspace too small), SD_EHIP.
+ */
+sd_status sd_sample_filtered(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                             const sd_filter* filter, const float* u, int32_t* token, float* prob, int32_t* kept,
+                             void* workspace, uint64_t workspace_bytes, sd_stream stream);
+
+/*
+ * The rows themselves: out[t][k] = (z_k - m) / T where kept, -inf elsewhere
+ * (T <= 0: 0 at the first largest logit), so that softmax(out[t]) is the
+ * distribution sd_sample_filtered draws from.  These are the logits that
+ * accept/resample (sd_sample_logits and its like) takes to verify drafts
+ * against a target with sampling options.  out: fp32, rows out_stride
+ * (>= vocab) apart; it may be the logits themselves (SD_F32, same stride) and
+ * may not overlap them otherwise (SD_EINVAL).  A row without eligible token
+ * becomes -inf throughout.  Other arguments and errors as above.
+ */
+sd_status sd_filter_logits(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                           const sd_filter* filter, float* out, int64_t out_stride, int32_t* kept, void* workspace,
+                           uint64_t workspace_bytes, sd_stream stream);
+
+/*
+ * Low-rank adapters of one projection y = W x: n_adapters pairs of a down
+ * matrix A [n_seg * rank][d_in] and an up matrix B [d_out][rank], each stacked
+ * over the adapters, in `dtype` (row-major, contiguous; smaller ranks are
+ * filled up with zeros).  A fused projection (q, k and v side by side) has
+ * n_seg segments of columns, seg_off[s] .. seg_off[s+1]-1 (seg_off[0] = 0,
+ * seg_off[n_seg] = d_out, ascending), each with `rank` rows of A of its own.
+ * scale: device fp32 [n_adapters] or NULL (1).
+ */
+#define SD_LORA_MAX_RANK 128
+#define SD_LORA_MAX_SEGS 4
+typedef struct sd_lora {
+    int32_t n_adapters, rank, d_in, d_out, n_seg;
+    int32_t seg_off[SD_LORA_MAX_SEGS + 1];
+    int32_t dtype;
+    const void* a;
+    const void* b;
+    const float* scale;
+} sd_lora;
+
+/* Bytes of workspace (256-byte aligned) of sd_lora_apply for up to n_rows rows.
+ * Host only.  SD_EINVAL: an inconsistent descriptor; SD_ELIMIT: rank above
+ * SD_LORA_MAX_RANK, more than SD_LORA_MAX_SEGS segments, or more than 2^20
+ * rows, d_in or d_out. */
+sd_status sd_lora_query_size(const sd_lora* w, int32_t n_rows, uint64_t* workspace_bytes);
+
+/*
+ * y_out[t] = y_in[t] + scale[a] * B_a (A_a x[t]),  a = adapter[t], for the
+ * rows t = 0 .. n_rows-1 of a batch of many requests.  A row whose adapter is
+ * not in 0 .. n_adapters-1 (-1, say) has none: y_out[t] = y_in[t].
+ *   adapter: int32 [n_rows]; rows that share an adapter share its reads, most
+ *            of all where they follow each other
+ *   x:       [n_rows] rows of d_in elements of w->dtype, x_stride apart
+ *   x_lo:    second plane of x (SD_BF16; x + x_lo is the value), or NULL
+ *   y_in, y_out: rows of d_out elements of y_dtype, y_in_stride and
+ *            y_out_stride apart; y_out may be y_in (same stride) and may not
+ *            overlap it otherwise.  The output of the shared projection W x.
+ * Sums are fp32 (bf16: A x is carried on in two bf16 planes, about 16 bits),
+ * rounded once into y_out, in an order that depends on the sizes alone.
+ * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, dtype,
+ * stride, overlap, x_lo with SD_F32), SD_ELIMIT, SD_ENOMEM, SD_EHIP.
+ */
+sd_status sd_lora_apply(const sd_lora* w, int32_t n_rows, const int32_t* adapter, const void* x, const void* x_lo,
+                        int64_t x_stride, const void* y_in, int64_t y_in_stride, void* y_out, int64_t y_out_stride,
+                        int32_t y_dtype, void* workspace, uint64_t workspace_bytes, sd_stream stream);
+
 /* Kernel classes for sd_profile_begin. */
 enum {
     SD_K_QKV = 1,      /* QKV projection GEMM + fused QK-norm/RoPE/KV append */

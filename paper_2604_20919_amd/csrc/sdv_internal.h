@@ -230,6 +230,48 @@ struct NoallocMeta {  // kernel argument (520 bytes)
 struct NoallocTables {  // device pointers into the scratch array
     int32_t *user_id, *L, *slot_off, *draft_off, *slot_b, *slot_j, *flags;
 };
+// Filtered rows (temperature, top-k, top-p, min-p): a token a row from u, or
+// with out set the rows rewritten (kept: (z - max) / T, others -inf).  temp,
+// topk, topp and minp are device arrays [n_rows] or null (off).
+struct FilterCall {
+    int n_rows, V, bf16;
+    const void* logits;
+    int64_t stride;
+    const float* temp;
+    const int32_t* topk;
+    const float *topp, *minp, *u;
+    int32_t* token;
+    float* prob;
+    int32_t* kept;
+    float* out;
+    int64_t ostride;
+    void* ws;  // filter_workspace bytes
+};
+size_t filter_workspace(int n_rows, int V);
+void launch_filter(const FilterCall& c, hipStream_t s);
+
+// Low-rank adapters: y_out[t] = y_in[t] + scale[a] B_a (A_a x[t]), a = ids[t]
+// (outside 0 .. n_adapters - 1: y_out[t] = y_in[t]).  Columns of segment s (seg[s] ..
+// seg[s+1]-1) take the s-th `rank` rows of A_a.  x_lo: second plane or null.
+constexpr int kLoraSegs = 4;
+constexpr int kLoraRank = 128;
+struct LoraCall {
+    int T, d_in, d_out, rank, n_seg, n_adapters;
+    int seg[kLoraSegs + 1];
+    int bf16, y_bf16;       // types of x, A, B and of y
+    const void *a, *b;      // [n][n_seg * rank][d_in], [n][d_out][rank]
+    const float* scale;     // [n] or null (1)
+    const int32_t* ids;     // [T]
+    const void *x, *x_lo;   // [T][xs]
+    int64_t xs;
+    const void* y_in;       // [T][ys]
+    void* y_out;            // [T][yos]
+    int64_t ys, yos;
+    void* ws;               // lora_workspace bytes
+};
+size_t lora_workspace(int T, int rank, int n_seg);
+void launch_lora(const LoraCall& c, hipStream_t s);
+
 void launch_kv_copy(const Dims& D, const KVPool& kv, const KVCopyPages& pages, int layer,
                     int pos0, int n, const void* k, const void* v, int to_pool, hipStream_t s);
 

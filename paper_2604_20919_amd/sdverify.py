@@ -28,7 +28,10 @@ EXPORTS = ("sd_verify_query_sizes", "sd_verify_init", "sd_verify_destroy", "sd_u
            "sd_user_release", "sd_user_state", "sd_kv_write", "sd_kv_read", "sd_verify_batch",
            "sd_verify_batch_graph", "sd_verify_batch_sparse", "sd_draft_batch", "sd_accept", "sd_sample_logits",
            "sd_sample_logits_noalloc", "sd_debug_logits", "sd_debug_wait_limit", "sd_profile_begin", "sd_profile_end",
-           "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
+           "sd_filter_query_size", "sd_sample_filtered", "sd_filter_logits", "sd_lora_query_size",
+           "sd_lora_apply", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
+SD_FILTER_MAX_ROWS, SD_FILTER_MAX_VOCAB = 65535, 1 << 20
+SD_LORA_MAX_RANK, SD_LORA_MAX_SEGS = 128, 4
 SD_K_QKV, SD_K_ATTN, SD_K_O, SD_K_GATEUP, SD_K_DOWN, SD_K_LMHEAD, SD_K_SAMPLER, SD_K_SMALL = range(1, 9)
 
 
@@ -49,6 +52,16 @@ class sd_layer_weights(ctypes.Structure):
 class sd_weights(ctypes.Structure):
     _fields_ = [("embed", ctypes.c_void_p), ("lm_head", ctypes.c_void_p),
                 ("norm_f", ctypes.c_void_p), ("layers", ctypes.POINTER(sd_layer_weights))]
+
+
+class sd_filter(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class sd_lora(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_adapters", "rank", "d_in", "d_out", "n_seg")] + [
+        ("seg_off", ctypes.c_int32 * (SD_LORA_MAX_SEGS + 1)), ("dtype", ctypes.c_int32),
+        ("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class SdError(RuntimeError):
@@ -90,6 +103,12 @@ def lib() -> ctypes.CDLL:
         L.sd_debug_wait_limit.argtypes = [vp, i32]
         L.sd_profile_begin.argtypes = [vp, i32, i32]
         L.sd_profile_end.argtypes = [vp, P(ctypes.c_double), P(i32)]
+        i64 = ctypes.c_int64
+        L.sd_filter_query_size.argtypes = [i32, i32, P(u64)]
+        L.sd_sample_filtered.argtypes = [i32, i32, vp, i32, i64, P(sd_filter), vp, vp, vp, vp, vp, u64, vp]
+        L.sd_filter_logits.argtypes = [i32, i32, vp, i32, i64, P(sd_filter), vp, i64, vp, vp, u64, vp]
+        L.sd_lora_query_size.argtypes = [P(sd_lora), i32, P(u64)]
+        L.sd_lora_apply.argtypes = [P(sd_lora), i32, vp, vp, vp, i64, vp, i64, vp, i64, i32, vp, u64, vp]
         L.sd_calib_hbm.argtypes = [vp, ctypes.c_size_t, i32, i32, P(ctypes.c_double), vp]
         L.sd_calib_mfma.argtypes = [vp, i32, P(ctypes.c_double), vp]
         for name in EXPORTS:
@@ -240,6 +259,155 @@ def sd_sample_logits_noalloc(user_ids, draft_len, vocab: int, draft_tokens, q, l
     _check("sd_sample_logits_noalloc", lib().sd_sample_logits_noalloc(
         u.size, u.ctypes.data, L.ctypes.data, int(vocab), _dev(draft_tokens), _dev(q), _dev(logits),
         mode, int(seed), int(round_), _dev(accept_u), _dev(result), _stream(stream)))
+
+
+def _dtype(t, what: str) -> int:
+    name = str(t.dtype)
+    if name not in _DTYPES:
+        raise ValueError(f"{what}: float32 or bfloat16, not {name}")
+    return _DTYPES[name]
+
+
+_DTYPES = {"torch.float32": SD_F32, "torch.bfloat16": SD_BF16}
+
+
+def _vec(t, n: int, dtype: str, what: str, at) -> Optional[int]:
+    """Device pointer of a contiguous [n] tensor of one type on device `at`, or None."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype or tuple(t.shape) != (n,) or not t.is_contiguous() or t.device != at:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of {n} on {at}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _matrix(t, cols: Optional[int], what: str, at):
+    """(device pointer, row stride) of a [rows][cols] tensor whose rows are contiguous and apart."""
+    if t.dim() != 2 or t.device != at or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{what}: a matrix{'' if cols is None else f' of {cols} columns'} on {at}, not "
+                         f"{tuple(t.shape)} on {t.device}")
+    n, c = t.shape
+    if (c > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < c):
+        raise ValueError(f"{what}: rows must be contiguous and apart, strides are {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if n > 1 else c)
+
+
+def _on_current_device(t, what: str):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on {t.device}, not on the current GPU")
+    return t.device
+
+
+def _workspace(t, at):
+    if t.device != at or not t.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on {at}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _filter(n: int, at, temperature, top_k, top_p, min_p) -> sd_filter:
+    return sd_filter(_vec(temperature, n, "torch.float32", "temperature", at), _vec(top_k, n, "torch.int32", "top_k", at),
+                     _vec(top_p, n, "torch.float32", "top_p", at), _vec(min_p, n, "torch.float32", "min_p", at))
+
+
+def sd_filter_query_size(n_rows: int, vocab: int) -> int:
+    """Bytes of workspace of sd_sample_filtered and sd_filter_logits."""
+    b = ctypes.c_uint64()
+    _check("sd_filter_query_size", lib().sd_filter_query_size(int(n_rows), int(vocab), ctypes.byref(b)))
+    return b.value
+
+
+def sd_sample_filtered(logits, u, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None,
+                       prob=None, kept=None, stream=None) -> None:
+    """One token a row of logits (float32 or bfloat16 [n][vocab], rows any
+    distance apart) from uniforms u [n] under per-row options (device
+    tensors [n]; None: off).  Writes token int32 [n] and, where given, prob
+    float32 [n] and kept int32 [n]."""
+    at = _on_current_device(logits, "logits")
+    ptr, stride = _matrix(logits, None, "logits", at)
+    n, vocab = logits.shape
+    f = _filter(n, at, temperature, top_k, top_p, min_p)
+    ws, size = _workspace(workspace, at)
+    _check("sd_sample_filtered", lib().sd_sample_filtered(
+        n, vocab, ptr, _dtype(logits, "logits"), stride, ctypes.byref(f), _vec(u, n, "torch.float32", "u", at),
+        _vec(token, n, "torch.int32", "token", at), _vec(prob, n, "torch.float32", "prob", at),
+        _vec(kept, n, "torch.int32", "kept", at), ws, size, _stream(stream)))
+
+
+def sd_filter_logits(logits, out, workspace, temperature=None, top_k=None, top_p=None, min_p=None, kept=None,
+                     stream=None) -> None:
+    """The filtered rows: out float32 [n][vocab] = (logit - largest) / T
+    where a token is kept, -inf elsewhere.  out may be logits."""
+    at = _on_current_device(logits, "logits")
+    ptr, stride = _matrix(logits, None, "logits", at)
+    n, vocab = logits.shape
+    optr, ostride = _matrix(out, vocab, "out", at)
+    if out.shape[0] != n or _dtype(out, "out") != SD_F32:
+        raise ValueError(f"out: float32 of {n} rows, not {out.dtype} of {out.shape[0]}")
+    f = _filter(n, at, temperature, top_k, top_p, min_p)
+    ws, size = _workspace(workspace, at)
+    _check("sd_filter_logits", lib().sd_filter_logits(
+        n, vocab, ptr, _dtype(logits, "logits"), stride, ctypes.byref(f), optr, ostride,
+        _vec(kept, n, "torch.int32", "kept", at), ws, size, _stream(stream)))
+
+
+class Lora:
+    """The adapters of one projection (sd_lora) with the tensors they live in."""
+
+    def __init__(self, desc: sd_lora, a, b, scale):
+        self.desc, self.a, self.b, self.scale = desc, a, b, scale
+        self.ref = ctypes.byref(desc)
+
+
+def make_lora(a, b, scale=None, segs: Optional[Sequence[int]] = None) -> Lora:
+    """Adapters from a [n][n_seg * rank][d_in] and b [n][d_out][rank] (float32
+    or bfloat16, contiguous) and scale float32 [n] (None: 1).  segs: widths
+    of the projection's column segments, each with rows of `a` of its own
+    (None: one)."""
+    at = _on_current_device(a, "a")
+    if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.dtype != b.dtype or b.device != at:
+        raise ValueError("a [n][n_seg * rank][d_in] and b [n][d_out][rank] of one type on one GPU")
+    if not a.is_contiguous() or not b.is_contiguous():
+        raise ValueError("a and b must be contiguous")
+    n, d_out, rank = b.shape
+    segs = [d_out] if segs is None else [int(x) for x in segs]
+    if not 1 <= len(segs) <= SD_LORA_MAX_SEGS or min(segs) < 1 or sum(segs) != d_out or a.shape[1] != len(segs) * rank:
+        raise ValueError(f"segments {segs} do not fit a {tuple(a.shape)} and b {tuple(b.shape)}")
+    off = (ctypes.c_int32 * (SD_LORA_MAX_SEGS + 1))()
+    for i, w in enumerate(segs):
+        off[i + 1] = off[i] + w
+    d = sd_lora(n, rank, a.shape[2], d_out, len(segs), off, _dtype(a, "a"), a.data_ptr(), b.data_ptr(),
+                _vec(scale, n, "torch.float32", "scale", at))
+    return Lora(d, a, b, scale)
+
+
+def sd_lora_query_size(w: Lora, n_rows: int) -> int:
+    """Bytes of workspace of sd_lora_apply for up to n_rows rows."""
+    b = ctypes.c_uint64()
+    _check("sd_lora_query_size", lib().sd_lora_query_size(w.ref, int(n_rows), ctypes.byref(b)))
+    return b.value
+
+
+def sd_lora_apply(w: Lora, adapter, x, y_in, y_out, workspace, x_lo=None, stream=None) -> None:
+    """y_out[t] = y_in[t] + scale[a] B_a (A_a x[t]) with a = adapter[t] (int32
+    [n]; outside the adapters: y_in[t]).  y_out may be y_in."""
+    at = _on_current_device(x, "x")
+    n = x.shape[0]
+    if w.a.device != at:
+        raise ValueError(f"adapters on {w.a.device}, x on {at}")
+    xp, xs = _matrix(x, w.desc.d_in, "x", at)
+    yi, ys = _matrix(y_in, w.desc.d_out, "y_in", at)
+    yo, yos = _matrix(y_out, w.desc.d_out, "y_out", at)
+    lo = None
+    if x_lo is not None:
+        lo, los = _matrix(x_lo, w.desc.d_in, "x_lo", at)
+        if x_lo.shape != x.shape or los != xs or x_lo.dtype != x.dtype:
+            raise ValueError("x_lo: a plane like x")
+    if y_in.shape[0] != n or y_out.shape[0] != n or y_in.dtype != y_out.dtype or x.dtype != w.a.dtype:
+        raise ValueError("x, y_in and y_out: as many rows each, x of the adapters' type, y_out of y_in's")
+    ws, size = _workspace(workspace, at)
+    _check("sd_lora_apply", lib().sd_lora_apply(
+        w.ref, n, _vec(adapter, n, "torch.int32", "adapter", at), xp, lo, xs, yi, ys, yo, yos, _dtype(y_in, "y_in"),
+        ws, size, _stream(stream)))
 
 
 def sd_accept(ctx: int, batch: int, n_users: int, commit: bool = False):
