@@ -17,6 +17,10 @@
 #include "sdv_device.h"
 #include "sdv_internal.h"
 
+// z c and what is subtracted from it are rounded apart everywhere: the largest
+// logit's logarithm has to cancel exactly, however large
+#pragma clang fp contract(off)
+
 namespace sdv {
 namespace {
 
@@ -58,6 +62,7 @@ struct RowOpts {
     double p;      // top_p; off: +inf
     int k;         // top_k; off: INT_MAX
     bool greedy;
+    bool filters;  // any of top-k, top-p, min-p
 };
 __device__ __forceinline__ RowOpts row_opts(const FilterP& p, int row) {
     RowOpts o;
@@ -70,6 +75,7 @@ __device__ __forceinline__ RowOpts row_opts(const FilterP& p, int row) {
     o.p = tp < 1.f ? (double)tp : INFINITY;
     const float mp = p.minp ? p.minp[row] : 0.f;
     o.lmin = mp > 0.f ? log2((double)mp) : -INFINITY;
+    o.filters = k > 0 || tp < 1.f || mp > 0.f;
     return o;
 }
 // log2 of the weight of logit z in a row with maximum m
@@ -80,7 +86,7 @@ __device__ __forceinline__ u64 fixed_weight(double y, int bits) { return (u64)ri
 
 constexpr int kBins = 1024;
 
-struct Shared {
+struct RowShared {
     u64 sum[kBins];
     uint32_t cnt[kBins];
     u64 wsum[16], wpre[17];
@@ -98,14 +104,14 @@ __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
     return v;
 }
 
-// One workgroup a row.  Passes over the row: maximum; weights' total; one a
-// digit of the prefix's last key (10 bits each); the last key's ties if not all
-// of them are kept; the kept weights by wave segments; the segment drawn from,
-// or the rows written.
+// A whole row by one workgroup of 1024 threads, whatever its values: the rows
+// that the chunked kernels below leave (see kModeRow).  Passes over the row:
+// maximum; weights' total; one a digit of the prefix's last key (10 bits
+// each); the last key's ties if not all of them are kept; the kept weights by
+// wave segments; the segment drawn from, or the rows written.
 template <typename T, bool DRAW>
-__global__ __launch_bounds__(1024) void k_filter_row(FilterP p) {
-    __shared__ Shared s;
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+__device__ void filter_row(const FilterP& p, int row, RowShared& s) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const T* z = (const T*)p.z + (size_t)row * p.stride;
     const int V = p.V;
     const RowOpts o = row_opts(p, row);
@@ -302,19 +308,709 @@ __global__ __launch_bounds__(1024) void k_filter_row(FilterP p) {
     }
 }
 
+
+// ---------------------------------------------------------------------------
+// Rows in chunks of kChunk elements, a workgroup each.
+//
+// k_filter_scan reads the row once: a chunk's maximum, its weights' sum and, for
+// rows with a filter, counts and weights by buckets an eighth of an octave wide
+// (in the logarithm of the weight).  Weights are taken relative to 2^G, G the
+// chunk's own largest logarithm rounded up, so that chunks need not know the
+// row's maximum, and buckets lie on one grid for all of them: what another
+// chunk counts moves by whole buckets, its sums by powers of two.
+// k_filter_find merges the chunks of a row and finds the bucket the prefix
+// ends in; k_filter_collect writes that bucket's members out in index order;
+// k_filter_resolve finds the end among them and draws; k_filter_write writes
+// the filtered rows.  The row itself is read by the first and, where a chunk has
+// members of the last bucket, the second kernel, and by the writing one.
+// ---------------------------------------------------------------------------
+constexpr int kChunk = 8192;
+constexpr int kChunkThreads = 512;
+constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
+constexpr int kBuckets = 256;                 // 32 octaves; what lies below is not counted
+constexpr int kList = 16384;                  // most members of the last bucket
+constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G - 50), below 2^63
+
+// What a row still needs after k_filter_find.
+enum { kModeDone = 0, kModeAll = 1, kModeBorder = 2, kModeRow = 3, kModeEmpty = 4 };
+
+struct ChunkRec {
+    double G;      // ceil of the largest log2 weight (z c)
+    u64 S;         // sum of weights, units of 2^(G - kFix)
+    float m;       // largest logit
+    int first;     // its lowest index
+    uint32_t n;    // eligible elements
+    uint32_t off;  // members of the last bucket in the chunks before
+    u64 above;     // kept weights outside the last bucket, units as S
+    int bucket;    // the chunk's number of the last bucket; -1: it has no members
+    int pad;
+};
+struct RowRec {
+    double G, above, P;  // weights above the last bucket and the filter's bound, units of 2^G
+    int mode;
+    float m;
+    uint32_t n_list, above_c;
+    uint32_t cut;        // the prefix's last key and last index among its ties
+    int last;
+};
+
+// Workspace: row records, chunk records, histograms, lists
+struct Work {
+    RowRec* rows;
+    ChunkRec* recs;   // [n][chunks]
+    u64* hsum;        // [n][chunks][kBuckets]
+    uint16_t* hcnt;   // [n][chunks][kBuckets]
+    uint2* list;      // [n][kList] (key, index)
+};
+int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t layout(int n, int V, void* base, Work* w) {
+    const size_t nc = (size_t)n * chunks_of(V);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return (char*)base + at; };
+    char* a = take(n * sizeof(RowRec));
+    char* b = take(nc * sizeof(ChunkRec));
+    char* c = take(nc * kBuckets * 8);
+    char* d = take(nc * kBuckets * 2);
+    char* e = take((size_t)n * kList * 8);
+    if (w) *w = Work{(RowRec*)a, (ChunkRec*)b, (u64*)c, (uint16_t*)d, (uint2*)e};
+    return o;
+}
+
+// Element e (0 .. kPer-1) of a thread: 16-byte pieces, threads next to each other
+template <typename T> __device__ __forceinline__ int elem_at(int tid, int e) {
+    constexpr int W = 16 / sizeof(T);
+    return (e / W) * (kChunkThreads * W) + tid * W + e % W;
+}
+// The thread's elements of the chunk [k0, V) of a row; -inf past the end
+template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int k0, int V, float (&v)[kPer]) {
+    constexpr int W = 16 / sizeof(T);
+    T raw[kPer];
+#pragma unroll
+    for (int g = 0; g < kPer / W; ++g) {
+        const int i = k0 + elem_at<T>(threadIdx.x, g * W);
+        if (i + W <= V) {
+            // (any alignment: the hardware takes 16-byte loads at every address)
+            __builtin_memcpy(&raw[g * W], z + i, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                raw[g * W + e] = 0;
+                if (i + e < V) raw[g * W + e] = z[i + e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        v[e] = k0 + elem_at<T>(threadIdx.x, e) < V ? clean(ld<T>(raw, e)) : -INFINITY;
+}
+
+// 2^y in units of 2^-kFix, y <= 0, rounded to the nearest.  2^f on |f| <= 1/2 by
+// its power series (the first term left out is below 2^-47 of it); the sum
+// with 2^52 leaves the rounded number in the low bits.
+__device__ __forceinline__ double exp2_frac(double f) {
+    // ln(2)^k / k!
+    double r = 4.4455382718708116e-10;  // k = 11
+    r = fma(r, f, 7.0549116208011233e-09);
+    r = fma(r, f, 1.0178086009239699e-07);
+    r = fma(r, f, 1.3215486790144307e-06);
+    r = fma(r, f, 1.5252733804059841e-05);
+    r = fma(r, f, 1.5403530393381608e-04);
+    r = fma(r, f, 1.3333558146428443e-03);
+    r = fma(r, f, 9.6181291076284772e-03);
+    r = fma(r, f, 5.5504108664821580e-02);
+    r = fma(r, f, 2.4022650695910072e-01);
+    r = fma(r, f, 6.9314718055994531e-01);
+    return fma(r, f, 1.0);
+}
+__device__ __forceinline__ u64 fix_weight(double y) {
+    y = fmax(y, -64.0);
+    const double n = rint(y);
+    const double w = ldexp(exp2_frac(y - n), (int)n + kFix);
+    return (u64)__double_as_longlong(w + 0x1p52) & ((1ull << 52) - 1);
+}
+// bucket of a logarithm Y = z c under 2^G: 0 has the largest, widths of 1/8
+__device__ __forceinline__ int bucket_of(double Y, double G) {
+    return (int)fmin(8.0 * G - ceil(8.0 * Y), (double)kBuckets);
+}
+__device__ __forceinline__ double pow2(double d) { return d < -1100.0 ? 0.0 : ldexp(1.0, (int)d); }
+
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
+    __shared__ u64 hs[kBuckets];
+    __shared__ uint32_t hc[kBuckets];
+    __shared__ float sm[8];
+    __shared__ int si[8];
+    __shared__ u64 ss[8];
+    __shared__ uint32_t sn[8];
+    const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    float v[kPer];
+    load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
+    const RowOpts o = row_opts(p, row);
+    const bool hist = !o.greedy && o.filters;
+    if (tid < kBuckets) { hs[tid] = 0; hc[tid] = 0; }
+    float m = v[0];
+    int bi = 0;
+#pragma unroll
+    for (int e = 1; e < kPer; ++e)
+        if (v[e] > m) { m = v[e]; bi = e; }
+    bi = c * kChunk + elem_at<T>(tid, bi);
+    float M = wave_max(m);
+    if (lane == 0) sm[w] = M;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) M = fmaxf(M, sm[i]);
+    int first = m == M ? bi : 0x7fffffff;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+    const double G = ceil((double)M * o.c);
+    u64 S = 0;
+    uint32_t n = 0;
+    if (!o.greedy && M > -INFINITY && M < INFINITY) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if (v[e] == -INFINITY) continue;
+            const double Y = (double)v[e] * o.c;
+            const u64 x = fix_weight(Y - G);
+            S += x;
+            ++n;
+            if (hist) {
+                const int b = bucket_of(Y, G);
+                if (b < kBuckets) {
+                    atomicAdd(&hc[b], 1u);
+                    atomicAdd(&hs[b], x);
+                }
+            }
+        }
+    }
+    S = wave_sum_u64(S);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d, 64);
+    if (lane == 0) { si[w] = first; ss[w] = S; sn[w] = n; }
+    __syncthreads();
+    const size_t at = (size_t)row * nch + c;
+    if (hist && tid < kBuckets) {
+        wk.hsum[at * kBuckets + tid] = hs[tid];
+        wk.hcnt[at * kBuckets + tid] = (uint16_t)hc[tid];
+    }
+    if (tid == 0) {
+        for (int i = 1; i < 8; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
+        ChunkRec r{};
+        r.G = G; r.S = S; r.m = M; r.first = first; r.n = n;
+        r.bucket = -1;
+        wk.recs[at] = r;
+    }
+}
+
+// One workgroup a row; thread b holds bucket b of the row.
+template <bool DRAW>
+__global__ __launch_bounds__(kBuckets) void k_filter_find(FilterP p, Work wk, int nch) {
+    __shared__ double sd[4], sG;
+    __shared__ float sm[4];
+    __shared__ uint32_t su[4];
+    __shared__ int sfound;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    ChunkRec* recs = wk.recs + (size_t)row * nch;
+    const RowOpts o = row_opts(p, row);
+    // the row's maximum, and 2^G that its sums refer to
+    float m = -INFINITY;
+    double G = -INFINITY;
+    for (int c = tid; c < nch; c += kBuckets) {
+        m = fmaxf(m, recs[c].m);
+        if (recs[c].m > -INFINITY) G = fmax(G, recs[c].G);
+    }
+    m = wave_max(m);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) G = fmax(G, __shfl_xor(G, d, 64));
+    if (lane == 0) { sm[w] = m; sd[w] = G; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i]); G = fmax(G, sd[i]); }
+    __syncthreads();
+    RowRec r{};
+    r.G = G;
+    r.m = m;
+    r.last = p.V;
+    r.cut = key_of(-INFINITY) + 1;
+    if (m == -INFINITY || o.greedy || m == INFINITY) {
+        int first = 0x7fffffff;
+        if (m > -INFINITY)
+            for (int c = tid; c < nch; c += kBuckets)
+                if (recs[c].m == m) first = min(first, recs[c].first);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+        if (lane == 0) su[w] = (uint32_t)first;
+        __syncthreads();
+        if (tid == 0) {
+            for (int i = 0; i < 4; ++i) first = min(first, (int)su[i]);
+            r.mode = m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : kModeRow;
+            r.cut = key_of(m);
+            r.last = first;
+            wk.rows[row] = r;
+            if (r.mode != kModeRow) {
+                const bool one = r.mode == kModeDone;
+                if (p.kept) p.kept[row] = one;
+                if (DRAW) {
+                    p.token[row] = one ? first : -1;
+                    if (p.prob) p.prob[row] = one ? 1.f : 0.f;
+                }
+            }
+        }
+        return;
+    }
+    // total weight and number
+    double S = 0.0;
+    uint32_t n = 0;
+    for (int c = tid; c < nch; c += kBuckets) {
+        if (recs[c].m == -INFINITY) continue;
+        S += (double)recs[c].S * pow2(recs[c].G - G - kFix);
+        n += recs[c].n;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) { S += __shfl_xor(S, d, 64); n += __shfl_xor(n, d, 64); }
+    if (lane == 0) { sd[w] = S; su[w] = n; }
+    __syncthreads();
+    S = (sd[0] + sd[1]) + (sd[2] + sd[3]);
+    n = su[0] + su[1] + su[2] + su[3];
+    __syncthreads();
+    r.P = o.p * S;
+    r.mode = kModeAll;
+    int border = kBuckets;
+    double above = 0.0;
+    uint32_t cnt = 0, above_c = 0;
+    if (o.filters) {
+        double sum = 0.0;
+        for (int c = 0; c < nch; ++c) {
+            if (recs[c].m == -INFINITY) continue;
+            const double d = 8.0 * (G - recs[c].G);
+            const int b = d < kBuckets ? tid - (int)d : -1;
+            if (b < 0) continue;
+            const size_t at = ((size_t)row * nch + c) * kBuckets + b;
+            cnt += wk.hcnt[at];
+            sum += (double)wk.hsum[at] * pow2(recs[c].G - G - kFix);
+        }
+        // from the heaviest bucket down, the first where a filter stops
+        uint32_t ic = cnt;
+        double is = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t c2 = __shfl_up(ic, d, 64);
+            const double s2 = __shfl_up(is, d, 64);
+            if (lane >= d) { ic += c2; is += s2; }
+        }
+        if (lane == 63) { su[w] = ic; sd[w] = is; }
+        if (tid == 0) sfound = kBuckets;
+        __syncthreads();
+        for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
+        const int bmin = o.lmin > -INFINITY ? bucket_of((double)m * o.c + fmin(o.lmin, 0.0), G) : kBuckets;
+        if (cnt > 0 && (ic >= (uint32_t)o.k || is >= r.P || tid >= bmin)) atomicMin(&sfound, tid);
+        __syncthreads();
+        border = sfound;
+        if (tid == border) { above_c = ic - cnt; above = is - sum; }
+        if (border == kBuckets) {
+            // all counted ones are kept; if there are more, the whole row decides
+            uint32_t counted = su[0] + su[1] + su[2] + su[3];
+            if (counted < n) r.mode = kModeRow;
+        } else {
+            r.mode = kModeBorder;
+        }
+    }
+    if (r.mode == kModeBorder) {
+        __shared__ uint32_t slist;
+        if (tid == border) {
+            slist = cnt;
+            r.n_list = cnt;
+            r.above = above;
+            r.above_c = above_c;
+            if (cnt > kList) r.mode = kModeRow;
+            wk.rows[row] = r;
+        }
+        __syncthreads();
+        if (slist > kList) return;
+        // members of each chunk before the next, and each chunk's weights above
+        if (w == 0) {
+            uint32_t run = 0;
+            for (int c0 = 0; c0 < nch; c0 += 64) {
+                const int c = c0 + lane;
+                int b = -1;
+                uint32_t k = 0;
+                if (c < nch && recs[c].m > -INFINITY) {
+                    const double d = 8.0 * (G - recs[c].G);
+                    b = d < kBuckets ? border - (int)d : -1;
+                    if (b >= 0) k = wk.hcnt[((size_t)row * nch + c) * kBuckets + b];
+                }
+                uint32_t inc = k;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const uint32_t x = __shfl_up(inc, d, 64);
+                    if (lane >= d) inc += x;
+                }
+                if (c < nch) {
+                    recs[c].bucket = k ? b : -1;
+                    recs[c].off = run + inc - k;
+                }
+                run += __shfl(inc, 63, 64);
+            }
+        }
+        if (DRAW)
+            for (int c = w; c < nch; c += 4) {
+                u64 a = 0;
+                if (recs[c].m > -INFINITY) {
+                    const double d = 8.0 * (G - recs[c].G);
+                    const int b = d < kBuckets ? border - (int)d : -1;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (lane + 64 * e < b) a += wk.hsum[((size_t)row * nch + c) * kBuckets + lane + 64 * e];
+                }
+                a = wave_sum_u64(a);
+                if (lane == 0) recs[c].above = a;
+            }
+        return;
+    }
+    if (r.mode == kModeAll && DRAW)
+        for (int c = tid; c < nch; c += kBuckets) recs[c].above = recs[c].m > -INFINITY ? recs[c].S : 0;
+    if (tid == 0) {
+        wk.rows[row] = r;
+        if (p.kept && r.mode == kModeAll) p.kept[row] = (int)n;
+    }
+}
+
+// The members of the last bucket, in index order.
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Work wk) {
+    constexpr int W = 16 / sizeof(T), NG = kPer / W;
+    __shared__ uint32_t sc[NG][8];
+    const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (wk.rows[row].mode != kModeBorder) return;
+    const ChunkRec r = wk.recs[(size_t)row * nch + c];
+    if (r.bucket < 0) return;
+    const RowOpts o = row_opts(p, row);
+    float v[kPer];
+    load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
+    uint32_t mine = 0;  // bit e: element e is a member
+    uint32_t before[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        uint32_t b = 0, tot = 0;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float x = v[g * W + e];
+            const bool in = x > -INFINITY && bucket_of((double)x * o.c, r.G) == r.bucket;
+            const u64 mask = __ballot(in);
+            mine |= in ? 1u << (g * W + e) : 0u;
+            b += __popcll(mask & ((1ull << lane) - 1));
+            tot += __popcll(mask);
+        }
+        before[g] = b;
+        if (lane == 0) sc[g][w] = tot;
+    }
+    __syncthreads();
+    uint2* list = wk.list + (size_t)row * kList + r.off;
+    uint32_t base = 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        uint32_t at = base + before[g];
+        for (int i = 0; i < 8; ++i) {
+            if (i < w) at += sc[g][i];
+            base += sc[g][i];
+        }
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (mine >> (g * W + e) & 1)
+                list[at++] = uint2{key_of(v[g * W + e]), (uint32_t)(c * kChunk + elem_at<T>(tid, g * W + e))};
+    }
+}
+
+struct ListShared {
+    uint32_t key[kList];
+    double csum[128];  // kept weights of the chunks, units of 2^G
+    u64 cadd[128];     // their part from the last bucket, units of 2^(G_chunk - kFix)
+    int chunk;
+    double before;
+};
+constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
+static_assert(kMaxChunks <= 128, "one array entry a chunk");
+
+// One workgroup a row: the end of the prefix among the last bucket's members,
+// then the chunk and the element drawn.
+template <typename T, bool DRAW>
+__global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int nch) {
+    __shared__ RowShared s;
+    __shared__ ListShared l;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    RowRec r = wk.rows[row];
+    if (r.mode == kModeDone || r.mode == kModeEmpty) return;
+    if (r.mode == kModeRow) {
+        filter_row<T, DRAW>(p, row, s);
+        return;
+    }
+    if (!DRAW && r.mode == kModeAll) return;
+    const RowOpts o = row_opts(p, row);
+    const ChunkRec* recs = wk.recs + (size_t)row * nch;
+    const uint2* list = wk.list + (size_t)row * kList;
+    if (tid < 128) l.cadd[tid] = 0;
+    if (r.mode == kModeBorder) {
+        const int n = (int)r.n_list;
+        uint32_t lo = 0xffffffffu, hi = 0;
+        const double Ymin = o.lmin > -INFINITY ? (double)r.m * o.c + fmin(o.lmin, 0.0) : -INFINITY;
+        auto passes = [&](uint32_t key) { return (double)key_value(key) * o.c >= Ymin; };
+        uint32_t top = 0;
+        for (int i = tid; i < n; i += 1024) {
+            const uint32_t k = list[i].x;
+            l.key[i] = k;
+            top = max(top, k);
+            if (passes(k)) { lo = min(lo, k); hi = max(hi, k); }
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, d, 64));
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
+            top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+        }
+        if (lane == 0) { s.wcnt[w] = lo; s.wsum[w] = (u64)hi << 32 | top; }
+        __syncthreads();
+        for (int i = 0; i < 16; ++i) {
+            lo = min(lo, s.wcnt[i]);
+            hi = max(hi, (uint32_t)(s.wsum[i] >> 32));
+            top = max(top, (uint32_t)s.wsum[i]);
+        }
+        __syncthreads();
+        uint32_t cut, take = 0xffffffffu;
+        int last = p.V;
+        if (lo > hi) {
+            // min-p leaves none of them
+            cut = top;
+            last = -1;
+        } else {
+            const uint32_t first_lo = lo;
+            // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
+            // least: sums of kList stay below 2^63
+            const double Gb = ceil((double)key_value(hi) * o.c) + 1.0;
+            const double need = (r.P - r.above) * ldexp(1.0, (int)fmin(r.G - Gb, 1000.0) + kFix);
+            uint32_t above_c = r.above_c;
+            u64 above_s = 0;
+            bool all = false;
+            for (;;) {
+                const int sh = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 10);
+                s.sum[tid] = 0;
+                s.cnt[tid] = 0;
+                if (tid == 0) s.found = kBins;
+                __syncthreads();
+                for (int i = tid; i < n; i += 1024) {
+                    const uint32_t key = l.key[i];
+                    if (key < lo || key > hi) continue;
+                    atomicAdd(&s.cnt[(key - lo) >> sh], 1u);
+                    atomicAdd(&s.sum[(key - lo) >> sh], fix_weight((double)key_value(key) * o.c - Gb));
+                }
+                __syncthreads();
+                const int b = kBins - 1 - tid;
+                const uint32_t c = s.cnt[b];
+                const u64 ws = s.sum[b];
+                uint32_t ic = c;
+                u64 is = ws;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const uint32_t c2 = __shfl_up(ic, d, 64);
+                    const u64 s2 = __shfl_up(is, d, 64);
+                    if (lane >= d) { ic += c2; is += s2; }
+                }
+                if (lane == 63) { s.wcnt[w] = ic; s.wsum[w] = is; }
+                __syncthreads();
+                ic += above_c;
+                is += above_s;
+                for (int i = 0; i < w; ++i) { ic += s.wcnt[i]; is += s.wsum[i]; }
+                if (c > 0 && (ic >= (uint32_t)o.k || (double)is >= need)) atomicMin(&s.found, tid);
+                __syncthreads();
+                const int found = s.found;
+                if (found == kBins) { all = true; break; }
+                if (tid == found) {
+                    s.above_c = ic - c;
+                    s.above_s = is - ws;
+                    s.lo = lo + ((uint32_t)b << sh);
+                    s.hi = min(hi, s.lo + ((1u << sh) - 1));
+                }
+                __syncthreads();
+                lo = s.lo; hi = s.hi; above_c = s.above_c; above_s = s.above_s;
+                if (sh == 0) break;
+            }
+            if (all) {
+                cut = first_lo;
+            } else {
+                cut = lo;
+                const double wt = (double)fix_weight((double)key_value(lo) * o.c - Gb);
+                double jp = 4e9;
+                if (o.p < INFINITY) {
+                    const double left = need - (double)above_s;
+                    jp = left <= 0.0 ? 0.0 : wt > 0.0 ? fmin(ceil(left / wt), jp) : jp;
+                }
+                take = min((uint32_t)jp, (uint32_t)o.k - above_c);
+                if (above_c == 0) take = max(take, 1u);
+                // the index of the last tie kept
+                if (tid == 0) s.found = p.V;
+                __syncthreads();
+                if (w == 0) {
+                    uint32_t left = take;
+                    for (int i0 = 0; i0 < n; i0 += 64) {
+                        const u64 hit = __ballot(i0 + lane < n && l.key[min(i0 + lane, n - 1)] == cut);
+                        const uint32_t c = __popcll(hit);
+                        if (c >= left) {
+                            if ((hit >> lane & 1) && __popcll(hit & ((2ull << lane) - 1)) == left)
+                                s.found = (int)list[i0 + lane].y;
+                            break;
+                        }
+                        left -= c;
+                    }
+                }
+                __syncthreads();
+                last = s.found;
+            }
+        }
+        // number kept, and the members' weights by chunk
+        __syncthreads();
+        uint32_t kc = 0;
+        for (int i = tid; i < n; i += 1024) {
+            const uint32_t key = l.key[i];
+            if (key < cut || (key == cut && last < p.V && (int)list[i].y > last)) continue;
+            ++kc;
+            if (DRAW) {
+                const int c = (int)(list[i].y / kChunk);
+                atomicAdd(&l.cadd[c], fix_weight((double)key_value(key) * o.c - recs[c].G));
+            }
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) kc += __shfl_xor(kc, d, 64);
+        if (lane == 0) s.wcnt[w] = kc;
+        __syncthreads();
+        if (tid == 0) {
+            uint32_t c = r.above_c;
+            for (int i = 0; i < 16; ++i) c += s.wcnt[i];
+            if (p.kept) p.kept[row] = (int)c;
+            if (!DRAW) {
+                wk.rows[row].cut = cut;
+                wk.rows[row].last = last;
+            }
+        }
+        r.cut = cut;
+        r.last = last;
+    }
+    if (!DRAW) return;
+    __syncthreads();
+    if (tid < nch)
+        l.csum[tid] = recs[tid].m > -INFINITY ? (double)(recs[tid].above + l.cadd[tid]) * pow2(recs[tid].G - r.G - kFix) : 0.0;
+    __syncthreads();
+    float u = p.u[row];
+    u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
+    double K = 0.0;
+    for (int c = 0; c < nch; ++c) K += l.csum[c];
+    const double target = (double)u * K;
+    // the chunk in which the running sum passes the target (the last with weight
+    // if rounding lets none)
+    int ch = -1;
+    double run = 0.0, before = 0.0;
+    for (int c = 0; c < nch; ++c) {
+        if (l.csum[c] > 0.0) {
+            ch = c;
+            before = run;
+            run += l.csum[c];
+            if (run > target) break;
+        }
+    }
+    const ChunkRec cr = recs[ch];
+    const u64 have = cr.above + l.cadd[ch];
+    const u64 goal = min((u64)fmin(fmax((target - before) * pow2(r.G - cr.G + kFix), 0.0), 0x1p63), have - 1);
+    // its elements in index order: the first whose running sum exceeds the goal
+    constexpr int W = 8;
+    const T* z = (const T*)p.z + (size_t)row * p.stride;
+    const int i0 = ch * kChunk + tid * W;
+    u64 x[W], mysum = 0;
+    float vals[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+        const float v = i0 + e < p.V ? row_at(z, i0 + e) : -INFINITY;
+        const uint32_t key = key_of(v);
+        const bool on = v > -INFINITY && (key > r.cut || (key == r.cut && i0 + e <= r.last));
+        vals[e] = v;
+        x[e] = on ? fix_weight((double)v * o.c - cr.G) : 0;
+        mysum += x[e];
+    }
+    u64 inc = mysum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const u64 y = __shfl_up(inc, d, 64);
+        if (lane >= d) inc += y;
+    }
+    if (lane == 63) s.wsum[w] = inc;
+    __syncthreads();
+    u64 at = inc - mysum;
+    for (int i = 0; i < w; ++i) at += s.wsum[i];
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+        if (at <= goal && goal < at + x[e]) {
+            p.token[row] = i0 + e;
+            if (p.prob) p.prob[row] = (float)(exp2((double)vals[e] * o.c - r.G) / K);
+        }
+        at += x[e];
+    }
+}
+static_assert(kChunk == 1024 * 8, "the drawing workgroup's threads take eight elements each");
+
+// The filtered rows from each row's cut.
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work wk) {
+    constexpr int W = 16 / sizeof(T);
+    const int c = blockIdx.x, row = blockIdx.y;
+    const RowRec r = wk.rows[row];
+    if (r.mode == kModeRow) return;  // written by k_filter_resolve
+    float v[kPer];
+    load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
+    const float t = p.temp ? p.temp[row] : 1.f;
+    const double it = t > 0.f ? 1.0 / (double)t : 0.0;
+    float* out = p.out + (size_t)row * p.ostride;
+#pragma unroll
+    for (int g = 0; g < kPer / W; ++g) {
+        const int i = c * kChunk + elem_at<T>(threadIdx.x, g * W);
+        float f[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float x = v[g * W + e];
+            const uint32_t key = key_of(x);
+            const bool on = r.mode != kModeEmpty && x > -INFINITY && (key > r.cut || (key == r.cut && i + e <= r.last));
+            f[e] = on ? (x == r.m ? 0.f : (float)(((double)x - (double)r.m) * it)) : -INFINITY;
+        }
+        if (i + W <= p.V) {
+#pragma unroll
+            for (int e = 0; e < W; e += 4) __builtin_memcpy(out + i + e, f + e, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (i + e < p.V) out[i + e] = f[e];
+        }
+    }
+}
+
 }  // namespace
 
-size_t filter_workspace(int n_rows, int V) {
-    (void)n_rows; (void)V;
-    return 256;
-}
+size_t filter_workspace(int n_rows, int V) { return layout(n_rows, V, nullptr, nullptr); }
 
 template <typename T>
 static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {
-    if (c.out)
-        hipLaunchKernelGGL((k_filter_row<T, false>), dim3(c.n_rows), dim3(1024), 0, s, p);
-    else
-        hipLaunchKernelGGL((k_filter_row<T, true>), dim3(c.n_rows), dim3(1024), 0, s, p);
+    Work wk;
+    layout(c.n_rows, c.V, c.ws, &wk);
+    const int nch = chunks_of(c.V);
+    const dim3 g(nch, c.n_rows);
+    hipLaunchKernelGGL(k_filter_scan<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+    if (c.out) {
+        hipLaunchKernelGGL(k_filter_find<false>, dim3(c.n_rows), dim3(kBuckets), 0, s, p, wk, nch);
+        hipLaunchKernelGGL(k_filter_collect<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+        hipLaunchKernelGGL((k_filter_resolve<T, false>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
+        hipLaunchKernelGGL(k_filter_write<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+    } else {
+        hipLaunchKernelGGL(k_filter_find<true>, dim3(c.n_rows), dim3(kBuckets), 0, s, p, wk, nch);
+        hipLaunchKernelGGL(k_filter_collect<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+        hipLaunchKernelGGL((k_filter_resolve<T, true>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
+    }
 }
 
 void launch_filter(const FilterCall& c, hipStream_t s) {
