@@ -95,6 +95,7 @@ struct RowShared {
     uint32_t above_c;
     u64 above_s;
     float fmax[16];
+    uint32_t ties;
     int found;
 };
 
@@ -322,7 +323,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
 // ends in; k_filter_collect writes that bucket's members out in index order;
 // k_filter_resolve finds the end among them and draws; k_filter_write writes
 // the filtered rows.  The row itself is read by the first and, where a chunk has
-// members of the last bucket, the second kernel, and by the writing one.
+// members of the last bucket, the third kernel, and by the writing one.
 // ---------------------------------------------------------------------------
 constexpr int kChunk = 8192;
 constexpr int kChunkThreads = 512;
@@ -330,26 +331,31 @@ constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
 constexpr int kBuckets = 256;                 // 32 octaves; what lies below is not counted
 constexpr int kList = 16384;                  // most members of the last bucket
 constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G - 50), below 2^63
+constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
+static_assert(kMaxChunks <= 128, "a row's chunks fit the arrays of k_filter_find and k_filter_resolve");
 
 // What a row still needs after k_filter_find.
 enum { kModeDone = 0, kModeAll = 1, kModeBorder = 2, kModeRow = 3, kModeEmpty = 4 };
 
 struct ChunkRec {
-    double G;      // ceil of the largest log2 weight (z c)
-    u64 S;         // sum of weights, units of 2^(G - kFix)
-    float m;       // largest logit
-    int first;     // its lowest index
-    uint32_t n;    // eligible elements
-    uint32_t off;  // members of the last bucket in the chunks before
-    u64 above;     // kept weights outside the last bucket, units as S
-    int bucket;    // the chunk's number of the last bucket; -1: it has no members
-    int pad;
+    double G;       // an integer above the largest log2 weight (z c)
+    u64 S;          // sum of weights, units of 2^(G - kFix)
+    float m;        // largest logit
+    int first;      // its lowest index
+    uint32_t n;     // eligible elements
+    int bucket;     // the chunk's number of the row's last bucket; -1: above all of its own
+    uint32_t off;   // members of the last bucket in the chunks before
+    uint32_t have;  // its own
+    u64 above;      // kept weights outside the last bucket, units as S
 };
 struct RowRec {
     double G, above, P;  // weights above the last bucket and the filter's bound, units of 2^G
+    double c, lmin;      // the row's options (RowOpts)
+    int k;
     int mode;
     float m;
     uint32_t n_list, above_c;
+    uint32_t klo, khi;   // keys of the last bucket's members
     uint32_t cut;        // the prefix's last key and last index among its ties
     int last;
 };
@@ -405,38 +411,60 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int
         v[e] = k0 + elem_at<T>(threadIdx.x, e) < V ? clean(ld<T>(raw, e)) : -INFINITY;
 }
 
-// 2^y in units of 2^-kFix, y <= 0, rounded to the nearest.  2^f on |f| <= 1/2 by
-// its power series (the first term left out is below 2^-47 of it); the sum
-// with 2^52 leaves the rounded number in the low bits.
-__device__ __forceinline__ double exp2_frac(double f) {
-    // ln(2)^k / k!
-    double r = 4.4455382718708116e-10;  // k = 11
-    r = fma(r, f, 7.0549116208011233e-09);
-    r = fma(r, f, 1.0178086009239699e-07);
-    r = fma(r, f, 1.3215486790144307e-06);
-    r = fma(r, f, 1.5252733804059841e-05);
-    r = fma(r, f, 1.5403530393381608e-04);
-    r = fma(r, f, 1.3333558146428443e-03);
-    r = fma(r, f, 9.6181291076284772e-03);
-    r = fma(r, f, 5.5504108664821580e-02);
-    r = fma(r, f, 2.4022650695910072e-01);
-    r = fma(r, f, 6.9314718055994531e-01);
-    return fma(r, f, 1.0);
+// Logarithms on a grid of 2^-32: y = z c - G, -64 <= y < 0, is rounded once, by
+// adding 1.5 2^20 in the same operation; the low word is then the fraction,
+// the high word kGridHi + floor(y).  The grid is the same for every integer G.
+constexpr int kGridHi = 0x41380000;  // high word of 1.5 2^20
+constexpr u64 kFixBias = 0x4330000000000000ull;  // the bits of 2^52
+struct Grid {
+    double c, add;  // add = 1.5 2^20 - G
+    float zmin;     // smaller logits (-inf among them) weigh less than 2^-63: nothing
+};
+// (rows outside of these bounds, which need |z / T| > 2^50 or T > 10^36, take the whole-row path)
+__device__ __forceinline__ bool grid_holds(float m, double c) {
+    return c >= 4e-37 && fabs((double)m * c) < 0x1p50;
 }
-__device__ __forceinline__ u64 fix_weight(double y) {
-    y = fmax(y, -64.0);
-    const double n = rint(y);
-    const double w = ldexp(exp2_frac(y - n), (int)n + kFix);
-    return (u64)__double_as_longlong(w + 0x1p52) & ((1ull << 52) - 1);
+__device__ __forceinline__ Grid grid_of(double G, double c) {
+    return Grid{c, 0x1.8p20 - G, (float)((G - 64.0) / c)};
 }
-// bucket of a logarithm Y = z c under 2^G: 0 has the largest, widths of 1/8
-__device__ __forceinline__ int bucket_of(double Y, double G) {
-    return (int)fmin(8.0 * G - ceil(8.0 * Y), (double)kBuckets);
+__device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)fmaxf(z, g.zmin), g.c, g.add); }
+// an integer above m's logarithm on the grid
+__device__ __forceinline__ double grid_top(float m, double c) {
+    const double G = floor((double)m * c) + 1.0;
+    return __double2hiint(on_grid(grid_of(G, c), m)) >= kGridHi ? G + 1.0 : G;
 }
-__device__ __forceinline__ double pow2(double d) { return d < -1100.0 ? 0.0 : ldexp(1.0, (int)d); }
+// bucket: 0 has the heaviest, widths of 1/8
+__device__ __forceinline__ int grid_bucket(double y) {
+    const uint32_t q = __builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29);
+    return (int)(((uint32_t)kGridHi << 3) - 1u - q);
+}
+// 2^y in units of 2^-kFix plus kFixBias, rounded.  2^f on |f| <= 1/2 by its
+// power series up to f^8 (what is left out is below 2^-32 of it, as is the
+// grid's rounding); the sum with 2^52 leaves the rounded number in the low bits.
+__device__ __forceinline__ u64 grid_weight(double y) {
+    const int lo = __double2loint(y), n = __double2hiint(y) - kGridHi + (int)((uint32_t)lo >> 31);
+    const double f = (double)lo;  // fraction times 2^32
+    // ln(2)^k / k! 2^-32k
+    double r = 1.3215486790144305e-06 * 0x1p-256;
+    r = fma(r, f, 1.5252733804059838e-05 * 0x1p-224);
+    r = fma(r, f, 0.00015403530393381606 * 0x1p-192);
+    r = fma(r, f, 0.0013333558146428441 * 0x1p-160);
+    r = fma(r, f, 0.009618129107628477 * 0x1p-128);
+    r = fma(r, f, 0.055504108664821576 * 0x1p-96);
+    r = fma(r, f, 0.2402265069591007 * 0x1p-64);
+    r = fma(r, f, 0.6931471805599453 * 0x1p-32);
+    r = fma(r, f, 1.0);
+    r = __hiloint2double(__double2hiint(r) + ((n + kFix) << 20), __double2loint(r));
+    return (u64)__double_as_longlong(r + 0x1p52);
+}
+__device__ __forceinline__ double pow2(double d) { return d < -1000.0 ? 0.0 : ldexp(1.0, (int)d); }
+// buckets between a chunk's numbering and the row's
+__device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)fmin(8.0 * (G - Gc), (double)kBuckets); }
 
+// (bound by the vector units beside the read: about 20 64-bit operations an
+// element; see launch_typed for times)
 template <typename T>
-__global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
+__global__ __launch_bounds__(kChunkThreads, 8) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];
     __shared__ uint32_t hc[kBuckets];
     __shared__ float sm[8];
@@ -464,25 +492,28 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     int first = m == M ? bi : 0x7fffffff;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
-    const double G = ceil((double)M * o.c);
     u64 S = 0;
     uint32_t n = 0;
-    if (!o.greedy && M > -INFINITY && M < INFINITY) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) n += v[e] > -INFINITY;
+    double G = floor((double)M * o.c) + 1.0;
+    if (!o.greedy && M > -INFINITY && grid_holds(M, o.c)) {
+        G = grid_top(M, o.c);
+        const Grid g = grid_of(G, o.c);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            if (v[e] == -INFINITY) continue;
-            const double Y = (double)v[e] * o.c;
-            const u64 x = fix_weight(Y - G);
+            const double y = on_grid(g, v[e]);
+            const u64 x = grid_weight(y);
             S += x;
-            ++n;
             if (hist) {
-                const int b = bucket_of(Y, G);
+                const int b = grid_bucket(y);
                 if (b < kBuckets) {
                     atomicAdd(&hc[b], 1u);
                     atomicAdd(&hs[b], x);
                 }
             }
         }
+        S -= (u64)kPer * kFixBias;
     }
     S = wave_sum_u64(S);
 #pragma unroll
@@ -491,59 +522,78 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
     if (hist && tid < kBuckets) {
-        wk.hsum[at * kBuckets + tid] = hs[tid];
+        wk.hsum[at * kBuckets + tid] = hs[tid] - hc[tid] * kFixBias;
         wk.hcnt[at * kBuckets + tid] = (uint16_t)hc[tid];
     }
     if (tid == 0) {
         for (int i = 1; i < 8; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
         ChunkRec r{};
         r.G = G; r.S = S; r.m = M; r.first = first; r.n = n;
-        r.bucket = -1;
         wk.recs[at] = r;
     }
 }
 
-// One workgroup a row; thread b holds bucket b of the row.
+// Smallest key whose logit lies in bucket b or a heavier one of a row, by
+// bisection (the buckets are monotone in the key); one wave, 64 keys at once.
+__device__ __forceinline__ uint32_t bucket_key(const Grid& g, uint32_t top, int b, int lane) {
+    uint32_t lo = key_of(-INFINITY), hi = top;  // lo is lighter or -inf, hi is in
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo + 63) / 64;
+        const uint32_t k = min(lo + step * (lane + 1), hi);
+        const u64 in = __ballot(grid_bucket(on_grid(g, key_value(k))) <= b);
+        const int i = __ffsll(in) - 1;  // (the last lane's key is hi)
+        const uint32_t nlo = i ? min(lo + step * i, hi) : lo;
+        hi = min(lo + step * (i + 1), hi);
+        lo = nlo;
+    }
+    return hi;
+}
+
+// One workgroup a row; four threads hold each bucket of the row and take a
+// quarter of its chunks.
+constexpr int kFindThreads = 4 * kBuckets;
 template <bool DRAW>
-__global__ __launch_bounds__(kBuckets) void k_filter_find(FilterP p, Work wk, int nch) {
-    __shared__ double sd[4], sG;
-    __shared__ float sm[4];
-    __shared__ uint32_t su[4];
+__global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk, int nch) {
+    __shared__ double cG[128], cS[128], bsum[4][kBuckets], sd[16];
+    __shared__ uint32_t bcnt[4][kBuckets], cn[128], cfirst[128], su[16];
+    __shared__ float cm[128];
     __shared__ int sfound;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int bk = tid % kBuckets, part = tid / kBuckets;
     ChunkRec* recs = wk.recs + (size_t)row * nch;
     const RowOpts o = row_opts(p, row);
-    // the row's maximum, and 2^G that its sums refer to
+    if (tid < nch) {
+        const ChunkRec r = recs[tid];
+        cG[tid] = r.G; cS[tid] = (double)r.S; cm[tid] = r.m; cn[tid] = r.n; cfirst[tid] = r.first;
+    }
+    if (tid == 0) sfound = kBuckets;
+    __syncthreads();
+    // the row's maximum, its lowest index and 2^G that its sums refer to (each wave by itself)
     float m = -INFINITY;
     double G = -INFINITY;
-    for (int c = tid; c < nch; c += kBuckets) {
-        m = fmaxf(m, recs[c].m);
-        if (recs[c].m > -INFINITY) G = fmax(G, recs[c].G);
+    for (int c = lane; c < nch; c += 64) {
+        m = fmaxf(m, cm[c]);
+        if (cm[c] > -INFINITY) G = fmax(G, cG[c]);
     }
     m = wave_max(m);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) G = fmax(G, __shfl_xor(G, d, 64));
-    if (lane == 0) { sm[w] = m; sd[w] = G; }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i]); G = fmax(G, sd[i]); }
-    __syncthreads();
     RowRec r{};
     r.G = G;
     r.m = m;
+    r.c = o.c;
+    r.lmin = fmin(o.lmin, 0.0);
+    r.k = o.k;
     r.last = p.V;
     r.cut = key_of(-INFINITY) + 1;
-    if (m == -INFINITY || o.greedy || m == INFINITY) {
+    if (m == -INFINITY || o.greedy || !grid_holds(m, o.c)) {
+        if (w) return;
         int first = 0x7fffffff;
-        if (m > -INFINITY)
-            for (int c = tid; c < nch; c += kBuckets)
-                if (recs[c].m == m) first = min(first, recs[c].first);
+        for (int c = lane; c < nch; c += 64)
+            if (cm[c] == m) first = min(first, (int)cfirst[c]);
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
-        if (lane == 0) su[w] = (uint32_t)first;
-        __syncthreads();
-        if (tid == 0) {
-            for (int i = 0; i < 4; ++i) first = min(first, (int)su[i]);
+        if (lane == 0) {
             r.mode = m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : kModeRow;
             r.cut = key_of(m);
             r.last = first;
@@ -562,37 +612,46 @@ __global__ __launch_bounds__(kBuckets) void k_filter_find(FilterP p, Work wk, in
     // total weight and number
     double S = 0.0;
     uint32_t n = 0;
-    for (int c = tid; c < nch; c += kBuckets) {
-        if (recs[c].m == -INFINITY) continue;
-        S += (double)recs[c].S * pow2(recs[c].G - G - kFix);
-        n += recs[c].n;
+    for (int c = lane; c < nch; c += 64) {
+        if (cm[c] == -INFINITY) continue;
+        S += cS[c] * pow2(cG[c] - G - kFix);
+        n += cn[c];
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) { S += __shfl_xor(S, d, 64); n += __shfl_xor(n, d, 64); }
-    if (lane == 0) { sd[w] = S; su[w] = n; }
-    __syncthreads();
-    S = (sd[0] + sd[1]) + (sd[2] + sd[3]);
-    n = su[0] + su[1] + su[2] + su[3];
-    __syncthreads();
     r.P = o.p * S;
     r.mode = kModeAll;
-    int border = kBuckets;
-    double above = 0.0;
-    uint32_t cnt = 0, above_c = 0;
-    if (o.filters) {
-        double sum = 0.0;
-        for (int c = 0; c < nch; ++c) {
-            if (recs[c].m == -INFINITY) continue;
-            const double d = 8.0 * (G - recs[c].G);
-            const int b = d < kBuckets ? tid - (int)d : -1;
-            if (b < 0) continue;
-            const size_t at = ((size_t)row * nch + c) * kBuckets + b;
-            cnt += wk.hcnt[at];
-            sum += (double)wk.hsum[at] * pow2(recs[c].G - G - kFix);
+    if (!o.filters) {
+        if (tid == 0) {
+            wk.rows[row] = r;
+            if (p.kept) p.kept[row] = (int)n;
         }
-        // from the heaviest bucket down, the first where a filter stops
-        uint32_t ic = cnt;
-        double is = sum;
+        return;
+    }
+    {
+        uint32_t cnt = 0;
+        double sum = 0.0;
+        const size_t at0 = (size_t)row * nch * kBuckets;
+#pragma unroll 8
+        for (int c = part; c < nch; c += 4) {
+            const int b = cm[c] > -INFINITY ? bk - bucket_shift(G, cG[c]) : -1;
+            const size_t at = at0 + (size_t)c * kBuckets + max(b, 0);
+            const uint32_t k = wk.hcnt[at];
+            const u64 x = wk.hsum[at];
+            if (b >= 0) {
+                cnt += k;
+                sum += (double)x * pow2(cG[c] - G - kFix);
+            }
+        }
+        bcnt[part][bk] = cnt;
+        bsum[part][bk] = sum;
+    }
+    __syncthreads();
+    uint32_t cnt = 0, ic = 0;
+    double sum = 0.0, is = 0.0;
+    if (tid < kBuckets) {
+        ic = cnt = bcnt[0][tid] + bcnt[1][tid] + bcnt[2][tid] + bcnt[3][tid];
+        is = sum = (bsum[0][tid] + bsum[1][tid]) + (bsum[2][tid] + bsum[3][tid]);
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t c2 = __shfl_up(ic, d, 64);
@@ -600,93 +659,97 @@ __global__ __launch_bounds__(kBuckets) void k_filter_find(FilterP p, Work wk, in
             if (lane >= d) { ic += c2; is += s2; }
         }
         if (lane == 63) { su[w] = ic; sd[w] = is; }
-        if (tid == 0) sfound = kBuckets;
-        __syncthreads();
-        for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
-        const int bmin = o.lmin > -INFINITY ? bucket_of((double)m * o.c + fmin(o.lmin, 0.0), G) : kBuckets;
-        if (cnt > 0 && (ic >= (uint32_t)o.k || is >= r.P || tid >= bmin)) atomicMin(&sfound, tid);
-        __syncthreads();
-        border = sfound;
-        if (tid == border) { above_c = ic - cnt; above = is - sum; }
-        if (border == kBuckets) {
-            // all counted ones are kept; if there are more, the whole row decides
-            uint32_t counted = su[0] + su[1] + su[2] + su[3];
-            if (counted < n) r.mode = kModeRow;
-        } else {
-            r.mode = kModeBorder;
-        }
     }
-    if (r.mode == kModeBorder) {
-        __shared__ uint32_t slist;
-        if (tid == border) {
-            slist = cnt;
-            r.n_list = cnt;
-            r.above = above;
-            r.above_c = above_c;
-            if (cnt > kList) r.mode = kModeRow;
+    __syncthreads();
+    // from the heaviest bucket down, the first where a filter stops
+    const Grid g = grid_of(G, o.c);
+    if (tid < kBuckets) {
+        for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
+        const double y = on_grid(g, m);
+        const int bmin = o.lmin > -INFINITY
+            ? (int)fmin(-1.0 - floor(8.0 * (y - 0x1.8p20 + r.lmin)), (double)kBuckets) : kBuckets;
+        if (cnt > 0 && (ic >= (uint32_t)o.k || is >= r.P || tid >= bmin)) atomicMin(&sfound, tid);
+    }
+    __syncthreads();
+    const int border = sfound;
+    if (border == kBuckets) {
+        // all counted ones are kept; if there are more, the whole row decides
+        const uint32_t counted = su[0] + su[1] + su[2] + su[3];
+        if (counted < n) r.mode = kModeRow;
+        if (tid == 0) {
             wk.rows[row] = r;
+            if (p.kept && r.mode == kModeAll) p.kept[row] = (int)n;
         }
-        __syncthreads();
-        if (slist > kList) return;
-        // members of each chunk before the next, and each chunk's weights above
-        if (w == 0) {
-            uint32_t run = 0;
-            for (int c0 = 0; c0 < nch; c0 += 64) {
-                const int c = c0 + lane;
-                int b = -1;
-                uint32_t k = 0;
-                if (c < nch && recs[c].m > -INFINITY) {
-                    const double d = 8.0 * (G - recs[c].G);
-                    b = d < kBuckets ? border - (int)d : -1;
-                    if (b >= 0) k = wk.hcnt[((size_t)row * nch + c) * kBuckets + b];
-                }
-                uint32_t inc = k;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t x = __shfl_up(inc, d, 64);
-                    if (lane >= d) inc += x;
-                }
-                if (c < nch) {
-                    recs[c].bucket = k ? b : -1;
-                    recs[c].off = run + inc - k;
-                }
-                run += __shfl(inc, 63, 64);
-            }
-        }
-        if (DRAW)
-            for (int c = w; c < nch; c += 4) {
-                u64 a = 0;
-                if (recs[c].m > -INFINITY) {
-                    const double d = 8.0 * (G - recs[c].G);
-                    const int b = d < kBuckets ? border - (int)d : -1;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (lane + 64 * e < b) a += wk.hsum[((size_t)row * nch + c) * kBuckets + lane + 64 * e];
-                }
-                a = wave_sum_u64(a);
-                if (lane == 0) recs[c].above = a;
-            }
         return;
     }
-    if (r.mode == kModeAll && DRAW)
-        for (int c = tid; c < nch; c += kBuckets) recs[c].above = recs[c].m > -INFINITY ? recs[c].S : 0;
-    if (tid == 0) {
-        wk.rows[row] = r;
-        if (p.kept && r.mode == kModeAll) p.kept[row] = (int)n;
+    if (tid == border) {
+        su[8] = cnt;
+        su[9] = ic - cnt;
+        sd[8] = is - sum;
+    }
+    __syncthreads();
+    if (w == 0) {
+        // members of each chunk before the next
+        uint32_t run = 0;
+        for (int c0 = 0; c0 < nch; c0 += 64) {
+            const int c = c0 + lane;
+            int b = -1;
+            uint32_t k = 0;
+            if (c < nch && cm[c] > -INFINITY) {
+                b = border - bucket_shift(G, cG[c]);
+                if (b >= 0) k = wk.hcnt[((size_t)row * nch + c) * kBuckets + b];
+            }
+            uint32_t inc = k;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t x = __shfl_up(inc, d, 64);
+                if (lane >= d) inc += x;
+            }
+            if (c < nch) {
+                recs[c].bucket = max(b, -1);
+                recs[c].off = run + inc - k;
+                recs[c].have = k;
+            }
+            run += __shfl(inc, 63, 64);
+        }
+    } else if (w == 1) {
+        const uint32_t top = key_of(m);
+        r.klo = bucket_key(g, top, border, lane);
+        r.khi = grid_bucket(on_grid(g, m)) == border ? top : bucket_key(g, top, border - 1, lane) - 1;
+        if (lane == 0) {
+            r.n_list = su[8];
+            r.above_c = su[9];
+            r.above = sd[8];
+            r.mode = r.n_list > kList ? kModeRow : kModeBorder;
+            wk.rows[row] = r;
+        }
     }
 }
 
-// The members of the last bucket, in index order.
-template <typename T>
+// The members of the last bucket, in index order, and (DRAW) each chunk's
+// weights above it.
+template <typename T, bool DRAW>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T), NG = kPer / W;
     __shared__ uint32_t sc[NG][8];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if (wk.rows[row].mode != kModeBorder) return;
-    const ChunkRec r = wk.recs[(size_t)row * nch + c];
-    if (r.bucket < 0) return;
-    const RowOpts o = row_opts(p, row);
+    const RowRec& rr = wk.rows[row];
+    const int mode = rr.mode;
+    if (mode != kModeBorder) return;
+    ChunkRec* rec = wk.recs + (size_t)row * nch + c;
+    const int bucket = rec->bucket;
+    if (DRAW && w == 7) {
+        const u64* h = wk.hsum + ((size_t)row * nch + c) * kBuckets;
+        u64 a = 0;
+#pragma unroll
+        for (int e = 0; e < kBuckets / 64; ++e)
+            if (lane + 64 * e < bucket) a += h[lane + 64 * e];
+        a = wave_sum_u64(a);
+        if (lane == 0) rec->above = a;
+    }
+    if (rec->have == 0) return;
+    const uint32_t klo = rr.klo, khi = rr.khi, off = rec->off;
     float v[kPer];
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
     uint32_t mine = 0;  // bit e: element e is a member
@@ -696,8 +759,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
         uint32_t b = 0, tot = 0;
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-            const float x = v[g * W + e];
-            const bool in = x > -INFINITY && bucket_of((double)x * o.c, r.G) == r.bucket;
+            const uint32_t key = key_of(v[g * W + e]);
+            const bool in = key >= klo && key <= khi;
             const u64 mask = __ballot(in);
             mine |= in ? 1u << (g * W + e) : 0u;
             b += __popcll(mask & ((1ull << lane) - 1));
@@ -707,7 +770,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
         if (lane == 0) sc[g][w] = tot;
     }
     __syncthreads();
-    uint2* list = wk.list + (size_t)row * kList + r.off;
+    uint2* list = wk.list + (size_t)row * kList + off;
     uint32_t base = 0;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -725,13 +788,11 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
 
 struct ListShared {
     uint32_t key[kList];
-    double csum[128];  // kept weights of the chunks, units of 2^G
-    u64 cadd[128];     // their part from the last bucket, units of 2^(G_chunk - kFix)
+    u64 cadd[128];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kFix)
+    double cG[128];
     int chunk;
-    double before;
+    double K, before;
 };
-constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
-static_assert(kMaxChunks <= 128, "one array entry a chunk");
 
 // One workgroup a row: the end of the prefix among the last bucket's members,
 // then the chunk and the element drawn.
@@ -747,62 +808,73 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
         return;
     }
     if (!DRAW && r.mode == kModeAll) return;
-    const RowOpts o = row_opts(p, row);
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
     const uint2* list = wk.list + (size_t)row * kList;
-    if (tid < 128) l.cadd[tid] = 0;
+    // (wave 0 holds the chunks' weights from here to the draw)
+    u64 cabove[2] = {0, 0};
+    double cG[2] = {0, 0};
+    if (DRAW && w == 0) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = lane + 64 * e;
+            if (c < nch && recs[c].m > -INFINITY) {
+                cG[e] = recs[c].G;
+                cabove[e] = r.mode == kModeAll ? recs[c].S : recs[c].above;
+            }
+            l.cG[c] = cG[e];
+            l.cadd[c] = 0;
+        }
+    }
     if (r.mode == kModeBorder) {
         const int n = (int)r.n_list;
         uint32_t lo = 0xffffffffu, hi = 0;
-        const double Ymin = o.lmin > -INFINITY ? (double)r.m * o.c + fmin(o.lmin, 0.0) : -INFINITY;
-        auto passes = [&](uint32_t key) { return (double)key_value(key) * o.c >= Ymin; };
-        uint32_t top = 0;
+        auto passes = [&](uint32_t key) {
+            const float z = key_value(key);
+            return z == r.m || ((double)z - (double)r.m) * r.c >= r.lmin;
+        };
         for (int i = tid; i < n; i += 1024) {
             const uint32_t k = list[i].x;
             l.key[i] = k;
-            top = max(top, k);
             if (passes(k)) { lo = min(lo, k); hi = max(hi, k); }
         }
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
             lo = min(lo, (uint32_t)__shfl_xor((int)lo, d, 64));
             hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
-            top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
         }
-        if (lane == 0) { s.wcnt[w] = lo; s.wsum[w] = (u64)hi << 32 | top; }
+        s.sum[tid] = 0;
+        s.cnt[tid] = 0;
+        if (lane == 0) { s.wcnt[w] = lo; s.wsum[w] = hi; }
+        if (tid == 0) s.found = kBins;
         __syncthreads();
         for (int i = 0; i < 16; ++i) {
             lo = min(lo, s.wcnt[i]);
-            hi = max(hi, (uint32_t)(s.wsum[i] >> 32));
-            top = max(top, (uint32_t)s.wsum[i]);
+            hi = max(hi, (uint32_t)s.wsum[i]);
         }
-        __syncthreads();
-        uint32_t cut, take = 0xffffffffu;
-        int last = p.V;
-        if (lo > hi) {
-            // min-p leaves none of them
-            cut = top;
-            last = -1;
-        } else {
+        uint32_t cut = r.khi, ties = 0, take = 0;
+        int last = -1;  // (min-p leaves none of them)
+        // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
+        // least: sums of kList stay below 2^63
+        const double Gb = floor((double)key_value(r.khi) * r.c) + 2.0;
+        const Grid g = grid_of(Gb, r.c);
+        if (lo <= hi) {
             const uint32_t first_lo = lo;
-            // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
-            // least: sums of kList stay below 2^63
-            const double Gb = ceil((double)key_value(hi) * o.c) + 1.0;
-            const double need = (r.P - r.above) * ldexp(1.0, (int)fmin(r.G - Gb, 1000.0) + kFix);
+            const double need = (r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix);
             uint32_t above_c = r.above_c;
             u64 above_s = 0;
-            bool all = false;
-            for (;;) {
+            for (bool again = false;; again = true) {
                 const int sh = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 10);
-                s.sum[tid] = 0;
-                s.cnt[tid] = 0;
-                if (tid == 0) s.found = kBins;
+                if (again) {
+                    s.sum[tid] = 0;
+                    s.cnt[tid] = 0;
+                    if (tid == 0) s.found = kBins;
+                }
                 __syncthreads();
                 for (int i = tid; i < n; i += 1024) {
                     const uint32_t key = l.key[i];
                     if (key < lo || key > hi) continue;
                     atomicAdd(&s.cnt[(key - lo) >> sh], 1u);
-                    atomicAdd(&s.sum[(key - lo) >> sh], fix_weight((double)key_value(key) * o.c - Gb));
+                    atomicAdd(&s.sum[(key - lo) >> sh], grid_weight(on_grid(g, key_value(key))) - kFixBias);
                 }
                 __syncthreads();
                 const int b = kBins - 1 - tid;
@@ -821,35 +893,42 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
                 ic += above_c;
                 is += above_s;
                 for (int i = 0; i < w; ++i) { ic += s.wcnt[i]; is += s.wsum[i]; }
-                if (c > 0 && (ic >= (uint32_t)o.k || (double)is >= need)) atomicMin(&s.found, tid);
+                if (c > 0 && (ic >= (uint32_t)r.k || (double)is >= need)) {
+                    // (the lanes' sums grow: the first lane of the wave stands for it)
+                    if (lane == __ffsll(__ballot(1)) - 1) atomicMin(&s.found, tid);
+                }
                 __syncthreads();
                 const int found = s.found;
-                if (found == kBins) { all = true; break; }
+                if (found == kBins) {  // min-p alone ends the prefix
+                    cut = first_lo;
+                    last = p.V;
+                    break;
+                }
                 if (tid == found) {
                     s.above_c = ic - c;
                     s.above_s = is - ws;
                     s.lo = lo + ((uint32_t)b << sh);
                     s.hi = min(hi, s.lo + ((1u << sh) - 1));
+                    s.ties = c;
                 }
                 __syncthreads();
                 lo = s.lo; hi = s.hi; above_c = s.above_c; above_s = s.above_s;
-                if (sh == 0) break;
-            }
-            if (all) {
-                cut = first_lo;
-            } else {
+                if (sh) continue;
                 cut = lo;
-                const double wt = (double)fix_weight((double)key_value(lo) * o.c - Gb);
+                ties = s.ties;
                 double jp = 4e9;
-                if (o.p < INFINITY) {
+                if (need < INFINITY) {
+                    const double wt = (double)(grid_weight(on_grid(g, key_value(lo))) - kFixBias);
                     const double left = need - (double)above_s;
                     jp = left <= 0.0 ? 0.0 : wt > 0.0 ? fmin(ceil(left / wt), jp) : jp;
                 }
-                take = min((uint32_t)jp, (uint32_t)o.k - above_c);
+                take = min((uint32_t)jp, (uint32_t)r.k - above_c);
                 if (above_c == 0) take = max(take, 1u);
+                last = p.V;
+                break;
+            }
+            if (take < ties) {
                 // the index of the last tie kept
-                if (tid == 0) s.found = p.V;
-                __syncthreads();
                 if (w == 0) {
                     uint32_t left = take;
                     for (int i0 = 0; i0 < n; i0 += 64) {
@@ -872,11 +951,13 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
         uint32_t kc = 0;
         for (int i = tid; i < n; i += 1024) {
             const uint32_t key = l.key[i];
-            if (key < cut || (key == cut && last < p.V && (int)list[i].y > last)) continue;
+            if (key < cut) continue;
+            const int at = (int)list[i].y;
+            if (key == cut && at > last) continue;
             ++kc;
             if (DRAW) {
-                const int c = (int)(list[i].y / kChunk);
-                atomicAdd(&l.cadd[c], fix_weight((double)key_value(key) * o.c - recs[c].G));
+                const int c = at / kChunk;
+                atomicAdd(&l.cadd[c], grid_weight(on_grid(grid_of(l.cG[c], r.c), key_value(key))) - kFixBias);
             }
         }
 #pragma unroll
@@ -896,43 +977,54 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
         r.last = last;
     }
     if (!DRAW) return;
-    __syncthreads();
-    if (tid < nch)
-        l.csum[tid] = recs[tid].m > -INFINITY ? (double)(recs[tid].above + l.cadd[tid]) * pow2(recs[tid].G - r.G - kFix) : 0.0;
-    __syncthreads();
-    float u = p.u[row];
-    u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
-    double K = 0.0;
-    for (int c = 0; c < nch; ++c) K += l.csum[c];
-    const double target = (double)u * K;
     // the chunk in which the running sum passes the target (the last with weight
-    // if rounding lets none)
-    int ch = -1;
-    double run = 0.0, before = 0.0;
-    for (int c = 0; c < nch; ++c) {
-        if (l.csum[c] > 0.0) {
-            ch = c;
-            before = run;
-            run += l.csum[c];
-            if (run > target) break;
+    // if rounding lets none): wave 0, two chunks a lane
+    if (w == 0) {
+        double x[2], inc[2], tot[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            cabove[e] += l.cadd[lane + 64 * e];
+            inc[e] = x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - kFix) : 0.0;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const double y = __shfl_up(inc[e], d, 64);
+                if (lane >= d) inc[e] += y;
+            }
+            tot[e] = __shfl(inc[e], 63, 64);
+        }
+        const double K = tot[0] + tot[1];
+        float u = p.u[row];
+        u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
+        const double target = (double)u * K;
+        inc[1] += tot[0];
+        const u64 h0 = __ballot(x[0] > 0.0 && inc[0] > target), h1 = __ballot(x[1] > 0.0 && inc[1] > target);
+        const u64 l0 = __ballot(x[0] > 0.0), l1 = __ballot(x[1] > 0.0);
+        const int ch = h0 ? __ffsll(h0) - 1 : h1 ? 63 + __ffsll(h1) : l1 ? 127 - __clzll(l1) : 63 - __clzll(l0);
+        if (lane == (ch & 63)) {
+            const int e = ch >> 6;
+            const u64 have = e ? cabove[1] : cabove[0];
+            const double before = e ? inc[1] - x[1] : inc[0] - x[0];
+            const double local = fmin(fmax((target - before) * pow2(r.G - (e ? cG[1] : cG[0]) + kFix), 0.0), 0x1p63);
+            l.chunk = ch;
+            l.K = K;
+            s.above_s = min((u64)local, have - 1);
         }
     }
-    const ChunkRec cr = recs[ch];
-    const u64 have = cr.above + l.cadd[ch];
-    const u64 goal = min((u64)fmin(fmax((target - before) * pow2(r.G - cr.G + kFix), 0.0), 0x1p63), have - 1);
+    __syncthreads();
+    const int ch = l.chunk;
+    const u64 goal = s.above_s;
     // its elements in index order: the first whose running sum exceeds the goal
-    constexpr int W = 8;
+    constexpr int W = kChunk / 1024;
+    const Grid g = grid_of(l.cG[ch], r.c);
     const T* z = (const T*)p.z + (size_t)row * p.stride;
     const int i0 = ch * kChunk + tid * W;
     u64 x[W], mysum = 0;
-    float vals[W];
 #pragma unroll
     for (int e = 0; e < W; ++e) {
         const float v = i0 + e < p.V ? row_at(z, i0 + e) : -INFINITY;
         const uint32_t key = key_of(v);
-        const bool on = v > -INFINITY && (key > r.cut || (key == r.cut && i0 + e <= r.last));
-        vals[e] = v;
-        x[e] = on ? fix_weight((double)v * o.c - cr.G) : 0;
+        const bool on = key > r.cut || (key == r.cut && i0 + e <= r.last);
+        x[e] = on ? grid_weight(on_grid(g, v)) - kFixBias : 0;
         mysum += x[e];
     }
     u64 inc = mysum;
@@ -949,22 +1041,25 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
     for (int e = 0; e < W; ++e) {
         if (at <= goal && goal < at + x[e]) {
             p.token[row] = i0 + e;
-            if (p.prob) p.prob[row] = (float)(exp2((double)vals[e] * o.c - r.G) / K);
+            if (p.prob) p.prob[row] = (float)(exp2((double)row_at(z, i0 + e) * r.c - r.G) / l.K);
         }
         at += x[e];
     }
 }
-static_assert(kChunk == 1024 * 8, "the drawing workgroup's threads take eight elements each");
 
 // The filtered rows from each row's cut.
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T);
     const int c = blockIdx.x, row = blockIdx.y;
-    const RowRec r = wk.rows[row];
-    if (r.mode == kModeRow) return;  // written by k_filter_resolve
+    const RowRec& rr = wk.rows[row];
+    const int mode = rr.mode;
+    if (mode == kModeRow) return;  // written by k_filter_resolve
     float v[kPer];
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
+    const float m = rr.m;
+    const uint32_t cut = rr.cut;
+    const int last = rr.last;
     const float t = p.temp ? p.temp[row] : 1.f;
     const double it = t > 0.f ? 1.0 / (double)t : 0.0;
     float* out = p.out + (size_t)row * p.ostride;
@@ -976,8 +1071,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work 
         for (int e = 0; e < W; ++e) {
             const float x = v[g * W + e];
             const uint32_t key = key_of(x);
-            const bool on = r.mode != kModeEmpty && x > -INFINITY && (key > r.cut || (key == r.cut && i + e <= r.last));
-            f[e] = on ? (x == r.m ? 0.f : (float)(((double)x - (double)r.m) * it)) : -INFINITY;
+            const bool on = mode != kModeEmpty && (key > cut || (key == cut && i + e <= last));
+            f[e] = on ? (x == m ? 0.f : (float)(((double)x - (double)m) * it)) : -INFINITY;
         }
         if (i + W <= p.V) {
 #pragma unroll
@@ -1002,13 +1097,13 @@ static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {
     const dim3 g(nch, c.n_rows);
     hipLaunchKernelGGL(k_filter_scan<T>, g, dim3(kChunkThreads), 0, s, p, wk);
     if (c.out) {
-        hipLaunchKernelGGL(k_filter_find<false>, dim3(c.n_rows), dim3(kBuckets), 0, s, p, wk, nch);
-        hipLaunchKernelGGL(k_filter_collect<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+        hipLaunchKernelGGL(k_filter_find<false>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_collect<T, false>), g, dim3(kChunkThreads), 0, s, p, wk);
         hipLaunchKernelGGL((k_filter_resolve<T, false>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
         hipLaunchKernelGGL(k_filter_write<T>, g, dim3(kChunkThreads), 0, s, p, wk);
     } else {
-        hipLaunchKernelGGL(k_filter_find<true>, dim3(c.n_rows), dim3(kBuckets), 0, s, p, wk, nch);
-        hipLaunchKernelGGL(k_filter_collect<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+        hipLaunchKernelGGL(k_filter_find<true>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_collect<T, true>), g, dim3(kChunkThreads), 0, s, p, wk);
         hipLaunchKernelGGL((k_filter_resolve<T, true>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
     }
 }

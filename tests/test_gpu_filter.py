@@ -161,6 +161,21 @@ def test_options_that_are_not_given(off):
     check(t.cuda(), host, *o, uniforms(n, 47))
 
 
+@pytest.mark.parametrize("kind", ["masked", "lowest", "nan", "inf", "wide", "coarse"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_stretches_without_a_token(kind, dtype):
+    """All but a few short stretches of a long row masked: whole parts of it
+    hold nothing but -inf or the type's lowest value."""
+    n, V = 10, 40000
+    t, host = values(kind, n, V, dtype, 57)
+    t = t.clone()
+    low = LOWEST[dtype] if kind in ("lowest", "wide") else float("-inf")
+    for a, b in ((0, 8000), (8300, 24500), (24600, 39990)):
+        t[:, a:b] = low
+    check(t.cuda(), t.float().numpy(), *options(n, 58), uniforms(n, 59))
+    check(t.cuda(), t.float().numpy(), None, None, None, None, uniforms(n, 60))
+
+
 @pytest.mark.parametrize("kind", ["normal", "coarse", "flat", "constant", "masked", "two"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_vocabulary(kind, dtype):
