@@ -43,12 +43,19 @@ struct FilterP {
     int64_t ostride;
 };
 
-// NaN becomes -inf (never kept), -0 becomes +0 (equal logits have equal keys)
-__device__ __forceinline__ float clean(float z) { return z == z ? z + 0.0f : -INFINITY; }
+// NaN becomes -inf (never kept)
+__device__ __forceinline__ float clean(float z) { return z == z ? z : -INFINITY; }
 template <typename T> __device__ __forceinline__ float row_at(const T* z, int i) { return clean(ld<T>(z, i)); }
-// larger logit, larger key; -inf has the smallest key that occurs
+// the larger of numbers that are no NaN (fmaxf would first quiet each)
+__device__ __forceinline__ float max_clean(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+// larger logit, larger key, and both zeros the same; -inf has the smallest key
+// that occurs
 __device__ __forceinline__ uint32_t key_of(float z) {
-    const uint32_t b = __float_as_uint(z);
+    const uint32_t b = __float_as_uint(z + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
@@ -392,11 +399,19 @@ template <typename T> __device__ __forceinline__ int elem_at(int tid, int e) {
 template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int k0, int V, float (&v)[kPer]) {
     constexpr int W = 16 / sizeof(T);
     T raw[kPer];
+    // (any alignment: the hardware takes 16-byte loads at every address)
+    if (k0 + kChunk <= V) {
+#pragma unroll
+        for (int g = 0; g < kPer / W; ++g)
+            __builtin_memcpy(&raw[g * W], z + k0 + elem_at<T>(threadIdx.x, g * W), 16);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] = clean(ld<T>(raw, e));
+        return;
+    }
 #pragma unroll
     for (int g = 0; g < kPer / W; ++g) {
         const int i = k0 + elem_at<T>(threadIdx.x, g * W);
         if (i + W <= V) {
-            // (any alignment: the hardware takes 16-byte loads at every address)
             __builtin_memcpy(&raw[g * W], z + i, 16);
         } else {
 #pragma unroll
@@ -414,63 +429,82 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int
 // Logarithms on a grid of 2^-32: y = z c - G, -64 <= y < 0, is rounded once, by
 // adding 1.5 2^20 in the same operation; the low word is then the fraction,
 // the high word kGridHi + floor(y).  The grid is the same for every integer G.
+// (Half a table step is added as well: a weight's table entry is the nearest.)
 constexpr int kGridHi = 0x41380000;  // high word of 1.5 2^20
-constexpr u64 kFixBias = 0x4330000000000000ull;  // the bits of 2^52
+constexpr double kGridAdd = 0x1.8p20 + 0x1p-9;
 struct Grid {
-    double c, add;  // add = 1.5 2^20 - G
+    double c, add;  // add = kGridAdd - G
     float zmin;     // smaller logits (-inf among them) weigh less than 2^-63: nothing
 };
-// (rows outside of these bounds, which need |z / T| > 2^50 or T > 10^36, take the whole-row path)
+// (rows outside of these bounds, which need |z / T| > 2^39 or T > 10^36, take the whole-row path)
 __device__ __forceinline__ bool grid_holds(float m, double c) {
-    return c >= 4e-37 && fabs((double)m * c) < 0x1p50;
+    return c >= 4e-37 && fabs((double)m * c) < 0x1p40;
 }
 __device__ __forceinline__ Grid grid_of(double G, double c) {
-    return Grid{c, 0x1.8p20 - G, (float)((G - 64.0) / c)};
+    return Grid{c, kGridAdd - G, (float)((G - 64.0) / c)};
 }
-__device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)fmaxf(z, g.zmin), g.c, g.add); }
+__device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)max_clean(z, g.zmin), g.c, g.add); }
 // an integer above m's logarithm on the grid
 __device__ __forceinline__ double grid_top(float m, double c) {
     const double G = floor((double)m * c) + 1.0;
-    return __double2hiint(on_grid(grid_of(G, c), m)) >= kGridHi ? G + 1.0 : G;
+    return on_grid(grid_of(G, c), m) >= kGridAdd ? G + 1.0 : G;
 }
 // bucket: 0 has the heaviest, widths of 1/8
 __device__ __forceinline__ int grid_bucket(double y) {
     const uint32_t q = __builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29);
-    return (int)(((uint32_t)kGridHi << 3) - 1u - q);
+    return (int)(((uint32_t)kGridHi << 3) - q);
 }
-// 2^y in units of 2^-kFix plus kFixBias, rounded.  2^f on |f| <= 1/2 by its
-// power series up to f^8 (what is left out is below 2^-32 of it, as is the
-// grid's rounding); the sum with 2^52 leaves the rounded number in the low bits.
-__device__ __forceinline__ u64 grid_weight(double y) {
-    const int lo = __double2loint(y), n = __double2hiint(y) - kGridHi + (int)((uint32_t)lo >> 31);
-    const double f = (double)lo;  // fraction times 2^32
-    // ln(2)^k / k! 2^-32k
-    double r = 1.3215486790144305e-06 * 0x1p-256;
-    r = fma(r, f, 1.5252733804059838e-05 * 0x1p-224);
-    r = fma(r, f, 0.00015403530393381606 * 0x1p-192);
-    r = fma(r, f, 0.0013333558146428441 * 0x1p-160);
-    r = fma(r, f, 0.009618129107628477 * 0x1p-128);
-    r = fma(r, f, 0.055504108664821576 * 0x1p-96);
-    r = fma(r, f, 0.2402265069591007 * 0x1p-64);
-    r = fma(r, f, 0.6931471805599453 * 0x1p-32);
-    r = fma(r, f, 1.0);
-    r = __hiloint2double(__double2hiint(r) + ((n + kFix) << 20), __double2loint(r));
-    return (u64)__double_as_longlong(r + 0x1p52);
+
+// 2^y in units of 2^-kFix, to about 2^-30 of it: 2^(j/256) from a table in LDS
+// (2^30 of it, less the bits of kMagic, and the same as a float) times a second-order series in the rest of
+// the fraction, 1/512 at most, as a 31-bit integer; then a shift.  64-bit
+// floating point takes twice the time of 32-bit here: the power series up to f^8 in
+// it took 43 us of vector work for 256 rows of 151936, this about half.
+constexpr int kTab = 256;
+constexpr float kMagic = 12582912.f;  // 1.5 2^23: the sum's low bits are the rounded number
+constexpr uint32_t kMagicBits = 0x4b400000u;
+constexpr double const_exp2(double x) {
+    double t = 1.0, r = 1.0;
+    for (int k = 1; k < 24; ++k) { t *= x * 0.6931471805599453 / k; r += t; }
+    return r;
+}
+struct Exp2Table {
+    uint2 e[kTab];
+};
+constexpr Exp2Table make_table() {
+    Exp2Table t{};
+    for (int j = 0; j < kTab; ++j) {
+        const double v = const_exp2((double)j / kTab) * 1073741824.0;
+        t.e[j].x = (uint32_t)(v + 0.5) - kMagicBits;
+        t.e[j].y = __builtin_bit_cast(uint32_t, (float)v);
+    }
+    return t;
+}
+__device__ const Exp2Table g_exp2 = make_table();
+__device__ __forceinline__ u64 grid_weight(const uint2* tab, double y) {
+    const uint32_t lo = (uint32_t)__double2loint(y);
+    const uint2 t = tab[lo >> 24];
+    // ln2 2^-32 (u - 2^23) + (ln2 2^-32 (u - 2^23))^2 / 2, expanded in u
+    constexpr double k1 = 0.6931471805599453 * 0x1p-32, k2 = k1 * k1 / 2, h = 8388608.0;
+    const float u = (float)(lo & 0xffffffu);
+    const float p = fmaf(fmaf((float)k2, u, (float)(k1 - 2 * k2 * h)), u, (float)(k2 * h * h - k1 * h));
+    const uint32_t w = t.x + __float_as_uint(fmaf(__uint_as_float(t.y), p, kMagic));
+    const uint32_t s = min((uint32_t)(kGridHi + 62 - kFix) - (uint32_t)__double2hiint(y), 63u);
+    return ((u64)w << 32) >> s;
 }
 __device__ __forceinline__ double pow2(double d) { return d < -1000.0 ? 0.0 : ldexp(1.0, (int)d); }
 // buckets between a chunk's numbering and the row's
 __device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)fmin(8.0 * (G - Gc), (double)kBuckets); }
 
-// (bound by the vector units beside the read: about 20 64-bit operations an
-// element; see launch_typed for times)
 template <typename T>
-__global__ __launch_bounds__(kChunkThreads, 8) void k_filter_scan(FilterP p, Work wk) {
+__global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];
     __shared__ uint32_t hc[kBuckets];
     __shared__ float sm[8];
     __shared__ int si[8];
     __shared__ u64 ss[8];
     __shared__ uint32_t sn[8];
+    __shared__ uint2 tab[kTab];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     float v[kPer];
@@ -478,51 +512,65 @@ __global__ __launch_bounds__(kChunkThreads, 8) void k_filter_scan(FilterP p, Wor
     const RowOpts o = row_opts(p, row);
     const bool hist = !o.greedy && o.filters;
     if (tid < kBuckets) { hs[tid] = 0; hc[tid] = 0; }
-    float m = v[0];
-    int bi = 0;
+    if (tid < kTab) tab[tid] = g_exp2.e[tid];
+    float M = v[0];
 #pragma unroll
-    for (int e = 1; e < kPer; ++e)
-        if (v[e] > m) { m = v[e]; bi = e; }
-    bi = c * kChunk + elem_at<T>(tid, bi);
-    float M = wave_max(m);
+    for (int e = 1; e < kPer; ++e) M = max_clean(M, v[e]);
+    M = wave_max(M);
     if (lane == 0) sm[w] = M;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) M = fmaxf(M, sm[i]);
-    int first = m == M ? bi : 0x7fffffff;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
     u64 S = 0;
-    uint32_t n = 0;
+    uint32_t n = 0;  // of the wave
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) n += v[e] > -INFINITY;
+    for (int e = 0; e < kPer; ++e) n += __popcll(__ballot(v[e] > -INFINITY));
+    int first = 0x7fffffff;
     double G = floor((double)M * o.c) + 1.0;
-    if (!o.greedy && M > -INFINITY && grid_holds(M, o.c)) {
+    if (o.greedy) {
+#pragma unroll
+        for (int e = kPer - 1; e >= 0; --e)
+            if (v[e] == M) first = c * kChunk + elem_at<T>(tid, e);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+    } else if (M > -INFINITY && grid_holds(M, o.c)) {
         G = grid_top(M, o.c);
         const Grid g = grid_of(G, o.c);
+        // (four elements at a time in flight: more take registers from other waves)
+        if (hist) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const double y = on_grid(g, v[e]);
-            const u64 x = grid_weight(y);
-            S += x;
-            if (hist) {
-                const int b = grid_bucket(y);
-                if (b < kBuckets) {
-                    atomicAdd(&hc[b], 1u);
-                    atomicAdd(&hs[b], x);
+            for (int e0 = 0; e0 < kPer; e0 += 4) {
+                u64 x[4];
+                int b[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const double y = on_grid(g, v[e0 + e]);
+                    x[e] = grid_weight(tab, y);
+                    b[e] = grid_bucket(y);
+                    S += x[e];
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (b[e] < kBuckets) {
+                        atomicAdd(&hc[b[e]], 1u);
+                        atomicAdd(&hs[b[e]], x[e]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                S += grid_weight(tab, on_grid(g, v[e]));
+                if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        S -= (u64)kPer * kFixBias;
     }
     S = wave_sum_u64(S);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d, 64);
     if (lane == 0) { si[w] = first; ss[w] = S; sn[w] = n; }
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
     if (hist && tid < kBuckets) {
-        wk.hsum[at * kBuckets + tid] = hs[tid] - hc[tid] * kFixBias;
+        wk.hsum[at * kBuckets + tid] = hs[tid];
         wk.hcnt[at * kBuckets + tid] = (uint16_t)hc[tid];
     }
     if (tid == 0) {
@@ -667,7 +715,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
         const double y = on_grid(g, m);
         const int bmin = o.lmin > -INFINITY
-            ? (int)fmin(-1.0 - floor(8.0 * (y - 0x1.8p20 + r.lmin)), (double)kBuckets) : kBuckets;
+            ? (int)fmin(-floor(8.0 * (y - 0x1.8p20 + r.lmin)), (double)kBuckets) : kBuckets;
         if (cnt > 0 && (ic >= (uint32_t)o.k || is >= r.P || tid >= bmin)) atomicMin(&sfound, tid);
     }
     __syncthreads();
@@ -800,7 +848,9 @@ template <typename T, bool DRAW>
 __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int nch) {
     __shared__ RowShared s;
     __shared__ ListShared l;
+    __shared__ uint2 tab[kTab];
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (tid < kTab) tab[tid] = g_exp2.e[tid];
     RowRec r = wk.rows[row];
     if (r.mode == kModeDone || r.mode == kModeEmpty) return;
     if (r.mode == kModeRow) {
@@ -874,7 +924,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
                     const uint32_t key = l.key[i];
                     if (key < lo || key > hi) continue;
                     atomicAdd(&s.cnt[(key - lo) >> sh], 1u);
-                    atomicAdd(&s.sum[(key - lo) >> sh], grid_weight(on_grid(g, key_value(key))) - kFixBias);
+                    atomicAdd(&s.sum[(key - lo) >> sh], grid_weight(tab, on_grid(g, key_value(key))));
                 }
                 __syncthreads();
                 const int b = kBins - 1 - tid;
@@ -918,7 +968,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
                 ties = s.ties;
                 double jp = 4e9;
                 if (need < INFINITY) {
-                    const double wt = (double)(grid_weight(on_grid(g, key_value(lo))) - kFixBias);
+                    const double wt = (double)(grid_weight(tab, on_grid(g, key_value(lo))));
                     const double left = need - (double)above_s;
                     jp = left <= 0.0 ? 0.0 : wt > 0.0 ? fmin(ceil(left / wt), jp) : jp;
                 }
@@ -957,7 +1007,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
             ++kc;
             if (DRAW) {
                 const int c = at / kChunk;
-                atomicAdd(&l.cadd[c], grid_weight(on_grid(grid_of(l.cG[c], r.c), key_value(key))) - kFixBias);
+                atomicAdd(&l.cadd[c], grid_weight(tab, on_grid(grid_of(l.cG[c], r.c), key_value(key))));
             }
         }
 #pragma unroll
@@ -1024,7 +1074,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
         const float v = i0 + e < p.V ? row_at(z, i0 + e) : -INFINITY;
         const uint32_t key = key_of(v);
         const bool on = key > r.cut || (key == r.cut && i0 + e <= r.last);
-        x[e] = on ? grid_weight(on_grid(g, v)) - kFixBias : 0;
+        x[e] = on ? grid_weight(tab, on_grid(g, v)) : 0;
         mysum += x[e];
     }
     u64 inc = mysum;
