@@ -91,17 +91,19 @@ __device__ __forceinline__ double log2_weight(float z, float m, double c) {
 }
 __device__ __forceinline__ u64 fixed_weight(double y, int bits) { return (u64)rint(ldexp(exp2(y), bits)); }
 
-constexpr int kBins = 1024;
+constexpr int kRowThreads = 512;  // of the kernels that take a row by one workgroup
+constexpr int kRowWaves = kRowThreads / 64;
+constexpr int kBins = kRowThreads;  // a digit of 9 bits
 
 struct RowShared {
     u64 sum[kBins];
     uint32_t cnt[kBins];
-    u64 wsum[16], wpre[17];
-    uint32_t wcnt[16];
+    u64 wsum[kRowWaves], wpre[kRowWaves + 1];
+    uint32_t wcnt[kRowWaves];
     uint32_t lo, hi;
     uint32_t above_c;
     u64 above_s;
-    float fmax[16];
+    float fmax[kRowWaves];
     uint32_t ties;
     int found;
 };
@@ -112,9 +114,9 @@ __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
     return v;
 }
 
-// A whole row by one workgroup of 1024 threads, whatever its values: the rows
+// A whole row by one workgroup, whatever its values: the rows
 // that the chunked kernels below leave (see kModeRow).  Passes over the row:
-// maximum; weights' total; one a digit of the prefix's last key (10 bits
+// maximum; weights' total; one a digit of the prefix's last key (9 bits
 // each); the last key's ties if not all of them are kept; the kept weights by
 // wave segments; the segment drawn from, or the rows written.
 template <typename T, bool DRAW>
@@ -124,11 +126,11 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     const int V = p.V;
     const RowOpts o = row_opts(p, row);
     float m = -INFINITY;
-    for (int i = tid; i < V; i += 1024) m = fmaxf(m, row_at(z, i));
+    for (int i = tid; i < V; i += kRowThreads) m = fmaxf(m, row_at(z, i));
     m = wave_max(m);
     if (lane == 0) s.fmax[w] = m;
     __syncthreads();
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, s.fmax[i]);
+    for (int i = 0; i < kRowWaves; ++i) m = fmaxf(m, s.fmax[i]);
     if (m == -INFINITY) {
         // nothing is eligible
         if (tid == 0) {
@@ -139,7 +141,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
             if (p.kept) p.kept[row] = 0;
         }
         if (!DRAW)
-            for (int i = tid; i < V; i += 1024) p.out[(size_t)row * p.ostride + i] = -INFINITY;
+            for (int i = tid; i < V; i += kRowThreads) p.out[(size_t)row * p.ostride + i] = -INFINITY;
         return;
     }
     // the smallest logit that counts as eligible (an infinite maximum takes all the weight)
@@ -147,7 +149,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     auto eligible = [&](float v) { return alone ? v == m : v > -INFINITY; };
     // total weight
     u64 S = 0;
-    for (int i = tid; i < V; i += 1024) {
+    for (int i = tid; i < V; i += kRowThreads) {
         const float v = row_at(z, i);
         if (eligible(v)) S += fixed_weight(log2_weight(v, m, o.c), p.scale_bits);
     }
@@ -155,7 +157,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     if (lane == 0) s.wsum[w] = S;
     __syncthreads();
     S = 0;
-    for (int i = 0; i < 16; ++i) S += s.wsum[i];
+    for (int i = 0; i < kRowWaves; ++i) S += s.wsum[i];
     // the prefix's last key
     const int k = o.greedy ? 1 : o.k;
     const double P = o.p * (double)S;  // +inf when off
@@ -167,11 +169,11 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     auto passes = [&](float v) { return eligible(v) && log2_weight(v, m, o.c) >= fmin(o.lmin, 0.0); };
     for (;;) {
         const int span = 32 - __clz(hi - lo);  // bits of hi - lo
-        const int sh = hi == lo ? 0 : max(0, span - 10);
+        const int sh = hi == lo ? 0 : max(0, span - 9);
         s.sum[tid] = 0;
         s.cnt[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < V; i += 1024) {
+        for (int i = tid; i < V; i += kRowThreads) {
             const float v = row_at(z, i);
             const uint32_t key = key_of(v);
             if (key < lo || key > hi || !passes(v)) continue;
@@ -227,7 +229,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         take = min(take, (uint32_t)k - above_c);
         if (above_c == 0) take = max(take, 1u);  // rank 0
         // ties in each wave's segment of the row
-        const int seg = (V + 15) / 16, i0 = w * seg, i1 = min(V, i0 + seg);
+        const int seg = (V + kRowWaves - 1) / kRowWaves, i0 = w * seg, i1 = min(V, i0 + seg);
         uint32_t n = 0;
         for (int i = i0 + lane; i < i1; i += 64) n += key_of(row_at(z, i)) == lo;
 #pragma unroll
@@ -237,7 +239,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         if (tid == 0) s.found = V;
         __syncthreads();
         uint32_t before = 0, ties = 0;
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < kRowWaves; ++i) {
             if (i < w) before += s.wcnt[i];
             ties += s.wcnt[i];
         }
@@ -262,7 +264,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         return passes(v) && (key > cut || (key == cut && i <= last));
     };
     // kept weights and number, by wave segments
-    const int seg = (V + 15) / 16, i0 = w * seg, i1 = min(V, i0 + seg);
+    const int seg = (V + kRowWaves - 1) / kRowWaves, i0 = w * seg, i1 = min(V, i0 + seg);
     u64 ks = 0;
     uint32_t kc = 0;
     for (int i = i0 + lane; i < i1; i += 64) {
@@ -282,13 +284,13 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     if (tid == 0) {
         u64 t = 0;
         uint32_t c = 0;
-        for (int i = 0; i < 16; ++i) { s.wpre[i] = t; t += s.wsum[i]; c += s.wcnt[i]; }
-        s.wpre[16] = t;
+        for (int i = 0; i < kRowWaves; ++i) { s.wpre[i] = t; t += s.wsum[i]; c += s.wcnt[i]; }
+        s.wpre[kRowWaves] = t;
         if (p.kept) p.kept[row] = (int)c;
     }
     if (!DRAW) return;
     __syncthreads();
-    const u64 K = s.wpre[16];
+    const u64 K = s.wpre[kRowWaves];
     float u = p.u[row];
     u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
     const u64 target = min((u64)((double)u * (double)K), K - 1);
@@ -338,6 +340,10 @@ constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
 constexpr int kBuckets = 256;                 // 32 octaves; what lies below is not counted
 constexpr int kList = 16384;                  // most members of the last bucket
 constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G - 50), below 2^63
+// A bucket of a chunk is one number: the count from bit kCountBit up, and below it
+// the weights in units of 2^(G - kHistFix), which stay under it.
+constexpr int kCountBit = 50, kHistFix = 37;
+__device__ __forceinline__ u64 hist_weight(u64 w) { return (w + (1ull << (kFix - kHistFix - 1))) >> (kFix - kHistFix); }
 constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
 static_assert(kMaxChunks <= 128, "a row's chunks fit the arrays of k_filter_find and k_filter_resolve");
 
@@ -353,7 +359,7 @@ struct ChunkRec {
     int bucket;     // the chunk's number of the row's last bucket; -1: above all of its own
     uint32_t off;   // members of the last bucket in the chunks before
     uint32_t have;  // its own
-    u64 above;      // kept weights outside the last bucket, units as S
+    u64 above;      // kept weights outside the last bucket, units of 2^(G - kHistFix)
 };
 struct RowRec {
     double G, above, P;  // weights above the last bucket and the filter's bound, units of 2^G
@@ -371,8 +377,7 @@ struct RowRec {
 struct Work {
     RowRec* rows;
     ChunkRec* recs;   // [n][chunks]
-    u64* hsum;        // [n][chunks][kBuckets]
-    uint16_t* hcnt;   // [n][chunks][kBuckets]
+    u64* hist;        // [n][chunks][kBuckets]
     uint2* list;      // [n][kList] (key, index)
 };
 int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
@@ -384,9 +389,8 @@ size_t layout(int n, int V, void* base, Work* w) {
     char* a = take(n * sizeof(RowRec));
     char* b = take(nc * sizeof(ChunkRec));
     char* c = take(nc * kBuckets * 8);
-    char* d = take(nc * kBuckets * 2);
-    char* e = take((size_t)n * kList * 8);
-    if (w) *w = Work{(RowRec*)a, (ChunkRec*)b, (u64*)c, (uint16_t*)d, (uint2*)e};
+    char* d = take((size_t)n * kList * 8);
+    if (w) *w = Work{(RowRec*)a, (ChunkRec*)b, (u64*)c, (uint2*)d};
     return o;
 }
 
@@ -499,7 +503,6 @@ __device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)f
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];
-    __shared__ uint32_t hc[kBuckets];
     __shared__ float sm[8];
     __shared__ int si[8];
     __shared__ u64 ss[8];
@@ -511,7 +514,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
     const RowOpts o = row_opts(p, row);
     const bool hist = !o.greedy && o.filters;
-    if (tid < kBuckets) { hs[tid] = 0; hc[tid] = 0; }
+    if (tid < kBuckets) hs[tid] = 0;
     if (tid < kTab) tab[tid] = g_exp2.e[tid];
     float M = v[0];
 #pragma unroll
@@ -551,10 +554,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (b[e] < kBuckets) {
-                        atomicAdd(&hc[b[e]], 1u);
-                        atomicAdd(&hs[b[e]], x[e]);
-                    }
+                    if (b[e] < kBuckets) atomicAdd(&hs[b[e]], hist_weight(x[e]) + (1ull << kCountBit));
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -569,10 +569,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     if (lane == 0) { si[w] = first; ss[w] = S; sn[w] = n; }
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
-    if (hist && tid < kBuckets) {
-        wk.hsum[at * kBuckets + tid] = hs[tid];
-        wk.hcnt[at * kBuckets + tid] = (uint16_t)hc[tid];
-    }
+    if (hist && tid < kBuckets) wk.hist[at * kBuckets + tid] = hs[tid];
     if (tid == 0) {
         for (int i = 1; i < 8; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
         ChunkRec r{};
@@ -581,17 +578,22 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     }
 }
 
-// Smallest key whose logit lies in bucket b or a heavier one of a row, by
-// bisection (the buckets are monotone in the key); one wave, 64 keys at once.
-__device__ __forceinline__ uint32_t bucket_key(const Grid& g, uint32_t top, int b, int lane) {
-    uint32_t lo = key_of(-INFINITY), hi = top;  // lo is lighter or -inf, hi is in
-    while (hi - lo > 1) {
+// Smallest key whose logit lies in bucket b (0 or more) or a heavier one of a
+// row whose largest key `top` does: buckets are monotone in the key, so one wave
+// narrows a bracket of keys, 64 at once.  It starts around the edge's logit.
+__device__ __forceinline__ uint32_t bucket_key(const Grid& g, double G, uint32_t top, int b, int lane) {
+    auto in = [&](uint32_t k) { return grid_bucket(on_grid(g, key_value(k))) <= b; };
+    const double edge = (G - 0.125 * b - 0x1p-9) / g.c, off = 0x1p-31 / g.c + fabs(edge) * 0x1p-22;
+    uint32_t lo = key_of((float)(edge - off)), hi = key_of((float)(edge + off));
+    const uint32_t least = key_of(-INFINITY);
+    if (!(lo >= least && lo < hi && !in(lo))) lo = least;
+    if (!(hi > lo && hi <= top && in(hi))) hi = top;
+    while (hi - lo > 1) {  // lo is lighter (or -inf), hi is in
         const uint32_t step = (hi - lo + 63) / 64;
         const uint32_t k = min(lo + step * (lane + 1), hi);
-        const u64 in = __ballot(grid_bucket(on_grid(g, key_value(k))) <= b);
-        const int i = __ffsll(in) - 1;  // (the last lane's key is hi)
-        const uint32_t nlo = i ? min(lo + step * i, hi) : lo;
-        hi = min(lo + step * (i + 1), hi);
+        const int i = __ffsll(__ballot(in(k))) - 1;  // (the last lane's key is hi)
+        const uint32_t nlo = lo + step * i;
+        hi = min(nlo + step, hi);
         lo = nlo;
     }
     return hi;
@@ -618,14 +620,9 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     __syncthreads();
     // the row's maximum, its lowest index and 2^G that its sums refer to (each wave by itself)
     float m = -INFINITY;
-    double G = -INFINITY;
-    for (int c = lane; c < nch; c += 64) {
-        m = fmaxf(m, cm[c]);
-        if (cm[c] > -INFINITY) G = fmax(G, cG[c]);
-    }
+    for (int c = lane; c < nch; c += 64) m = fmaxf(m, cm[c]);
     m = wave_max(m);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) G = fmax(G, __shfl_xor(G, d, 64));
+    const double G = grid_top(m, o.c);  // that of the chunk with the maximum
     RowRec r{};
     r.G = G;
     r.m = m;
@@ -684,11 +681,10 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         for (int c = part; c < nch; c += 4) {
             const int b = cm[c] > -INFINITY ? bk - bucket_shift(G, cG[c]) : -1;
             const size_t at = at0 + (size_t)c * kBuckets + max(b, 0);
-            const uint32_t k = wk.hcnt[at];
-            const u64 x = wk.hsum[at];
+            const u64 x = wk.hist[at];
             if (b >= 0) {
-                cnt += k;
-                sum += (double)x * pow2(cG[c] - G - kFix);
+                cnt += (uint32_t)(x >> kCountBit);
+                sum += (double)(x & ((1ull << kCountBit) - 1)) * pow2(cG[c] - G - kHistFix);
             }
         }
         bcnt[part][bk] = cnt;
@@ -745,7 +741,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
             uint32_t k = 0;
             if (c < nch && cm[c] > -INFINITY) {
                 b = border - bucket_shift(G, cG[c]);
-                if (b >= 0) k = wk.hcnt[((size_t)row * nch + c) * kBuckets + b];
+                if (b >= 0) k = (uint32_t)(wk.hist[((size_t)row * nch + c) * kBuckets + b] >> kCountBit);
             }
             uint32_t inc = k;
 #pragma unroll
@@ -761,16 +757,22 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
             run += __shfl(inc, 63, 64);
         }
     } else if (w == 1) {
-        const uint32_t top = key_of(m);
-        r.klo = bucket_key(g, top, border, lane);
-        r.khi = grid_bucket(on_grid(g, m)) == border ? top : bucket_key(g, top, border - 1, lane) - 1;
-        if (lane == 0) {
-            r.n_list = su[8];
-            r.above_c = su[9];
-            r.above = sd[8];
-            r.mode = r.n_list > kList ? kModeRow : kModeBorder;
-            wk.rows[row] = r;
-        }
+        const uint32_t k = bucket_key(g, G, key_of(m), border, lane);
+        if (lane == 0) su[10] = k;
+    } else if (w == 2) {
+        uint32_t k = key_of(m);
+        if (grid_bucket(on_grid(g, m)) != border) k = bucket_key(g, G, k, border - 1, lane) - 1;
+        if (lane == 0) su[11] = k;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        r.n_list = su[8];
+        r.above_c = su[9];
+        r.above = sd[8];
+        r.klo = su[10];
+        r.khi = su[11];
+        r.mode = r.n_list > kList ? kModeRow : kModeBorder;
+        wk.rows[row] = r;
     }
 }
 
@@ -788,11 +790,11 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
     ChunkRec* rec = wk.recs + (size_t)row * nch + c;
     const int bucket = rec->bucket;
     if (DRAW && w == 7) {
-        const u64* h = wk.hsum + ((size_t)row * nch + c) * kBuckets;
+        const u64* h = wk.hist + ((size_t)row * nch + c) * kBuckets;
         u64 a = 0;
 #pragma unroll
         for (int e = 0; e < kBuckets / 64; ++e)
-            if (lane + 64 * e < bucket) a += h[lane + 64 * e];
+            if (lane + 64 * e < bucket) a += h[lane + 64 * e] & ((1ull << kCountBit) - 1);
         a = wave_sum_u64(a);
         if (lane == 0) rec->above = a;
     }
@@ -836,16 +838,16 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
 
 struct ListShared {
     uint32_t key[kList];
-    u64 cadd[128];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kFix)
+    u64 cadd[128];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kHistFix)
     double cG[128];
     int chunk;
-    double K, before;
+    double K;
 };
 
 // One workgroup a row: the end of the prefix among the last bucket's members,
 // then the chunk and the element drawn.
 template <typename T, bool DRAW>
-__global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int nch) {
+__global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Work wk, int nch) {
     __shared__ RowShared s;
     __shared__ ListShared l;
     __shared__ uint2 tab[kTab];
@@ -860,29 +862,33 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
     if (!DRAW && r.mode == kModeAll) return;
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
     const uint2* list = wk.list + (size_t)row * kList;
+    const bool border = r.mode == kModeBorder;
     // (wave 0 holds the chunks' weights from here to the draw)
     u64 cabove[2] = {0, 0};
     double cG[2] = {0, 0};
+    float u = 0.f;
     if (DRAW && w == 0) {
+        u = p.u[row];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int c = lane + 64 * e;
             if (c < nch && recs[c].m > -INFINITY) {
                 cG[e] = recs[c].G;
-                cabove[e] = r.mode == kModeAll ? recs[c].S : recs[c].above;
+                cabove[e] = border ? recs[c].above : recs[c].S;
             }
             l.cG[c] = cG[e];
             l.cadd[c] = 0;
         }
     }
-    if (r.mode == kModeBorder) {
+    if (border) {
         const int n = (int)r.n_list;
         uint32_t lo = 0xffffffffu, hi = 0;
         auto passes = [&](uint32_t key) {
             const float z = key_value(key);
             return z == r.m || ((double)z - (double)r.m) * r.c >= r.lmin;
         };
-        for (int i = tid; i < n; i += 1024) {
+#pragma unroll 8
+        for (int i = tid; i < n; i += kRowThreads) {
             const uint32_t k = list[i].x;
             l.key[i] = k;
             if (passes(k)) { lo = min(lo, k); hi = max(hi, k); }
@@ -897,30 +903,32 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
         if (lane == 0) { s.wcnt[w] = lo; s.wsum[w] = hi; }
         if (tid == 0) s.found = kBins;
         __syncthreads();
-        for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int i = 0; i < kRowWaves; ++i) {
             lo = min(lo, s.wcnt[i]);
             hi = max(hi, (uint32_t)s.wsum[i]);
         }
         uint32_t cut = r.khi, ties = 0, take = 0;
         int last = -1;  // (min-p leaves none of them)
-        // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
-        // least: sums of kList stay below 2^63
-        const double Gb = floor((double)key_value(r.khi) * r.c) + 2.0;
-        const Grid g = grid_of(Gb, r.c);
         if (lo <= hi) {
             const uint32_t first_lo = lo;
+            // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
+            // least: sums of kList stay below 2^63
+            const double Gb = floor((double)key_value(r.khi) * r.c) + 2.0;
+            const Grid g = grid_of(Gb, r.c);
             const double need = (r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix);
             uint32_t above_c = r.above_c;
             u64 above_s = 0;
             for (bool again = false;; again = true) {
-                const int sh = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 10);
+                const int sh = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 9);
                 if (again) {
                     s.sum[tid] = 0;
                     s.cnt[tid] = 0;
                     if (tid == 0) s.found = kBins;
                 }
                 __syncthreads();
-                for (int i = tid; i < n; i += 1024) {
+#pragma unroll 4
+                for (int i = tid; i < n; i += kRowThreads) {
                     const uint32_t key = l.key[i];
                     if (key < lo || key > hi) continue;
                     atomicAdd(&s.cnt[(key - lo) >> sh], 1u);
@@ -944,7 +952,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
                 is += above_s;
                 for (int i = 0; i < w; ++i) { ic += s.wcnt[i]; is += s.wsum[i]; }
                 if (c > 0 && (ic >= (uint32_t)r.k || (double)is >= need)) {
-                    // (the lanes' sums grow: the first lane of the wave stands for it)
+                    // (the first such lane stands for its wave)
                     if (lane == __ffsll(__ballot(1)) - 1) atomicMin(&s.found, tid);
                 }
                 __syncthreads();
@@ -968,7 +976,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
                 ties = s.ties;
                 double jp = 4e9;
                 if (need < INFINITY) {
-                    const double wt = (double)(grid_weight(tab, on_grid(g, key_value(lo))));
+                    const double wt = (double)grid_weight(tab, on_grid(g, key_value(lo)));
                     const double left = need - (double)above_s;
                     jp = left <= 0.0 ? 0.0 : wt > 0.0 ? fmin(ceil(left / wt), jp) : jp;
                 }
@@ -997,26 +1005,25 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
             }
         }
         // number kept, and the members' weights by chunk
-        __syncthreads();
         uint32_t kc = 0;
-        for (int i = tid; i < n; i += 1024) {
-            const uint32_t key = l.key[i];
-            if (key < cut) continue;
-            const int at = (int)list[i].y;
-            if (key == cut && at > last) continue;
+#pragma unroll 8
+        for (int i = tid; i < n; i += kRowThreads) {
+            const uint2 x = list[i];
+            if (x.x < cut || (x.x == cut && (int)x.y > last)) continue;
             ++kc;
             if (DRAW) {
-                const int c = at / kChunk;
-                atomicAdd(&l.cadd[c], grid_weight(tab, on_grid(grid_of(l.cG[c], r.c), key_value(key))));
+                const int c = (int)x.y / kChunk;
+                atomicAdd(&l.cadd[c], hist_weight(grid_weight(tab, on_grid(grid_of(l.cG[c], r.c), key_value(x.x)))));
             }
         }
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) kc += __shfl_xor(kc, d, 64);
+        __syncthreads();
         if (lane == 0) s.wcnt[w] = kc;
         __syncthreads();
         if (tid == 0) {
             uint32_t c = r.above_c;
-            for (int i = 0; i < 16; ++i) c += s.wcnt[i];
+            for (int i = 0; i < kRowWaves; ++i) c += s.wcnt[i];
             if (p.kept) p.kept[row] = (int)c;
             if (!DRAW) {
                 wk.rows[row].cut = cut;
@@ -1029,21 +1036,24 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
     if (!DRAW) return;
     // the chunk in which the running sum passes the target (the last with weight
     // if rounding lets none): wave 0, two chunks a lane
+    const int unit = border ? kHistFix : kFix;
     if (w == 0) {
         double x[2], inc[2], tot[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             cabove[e] += l.cadd[lane + 64 * e];
-            inc[e] = x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - kFix) : 0.0;
+            inc[e] = x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - unit) : 0.0;
+            tot[e] = 0.0;
+            if (64 * e < nch) {
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double y = __shfl_up(inc[e], d, 64);
-                if (lane >= d) inc[e] += y;
+                for (int d = 1; d < 64; d <<= 1) {
+                    const double y = __shfl_up(inc[e], d, 64);
+                    if (lane >= d) inc[e] += y;
+                }
+                tot[e] = __shfl(inc[e], 63, 64);
             }
-            tot[e] = __shfl(inc[e], 63, 64);
         }
         const double K = tot[0] + tot[1];
-        float u = p.u[row];
         u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
         const double target = (double)u * K;
         inc[1] += tot[0];
@@ -1054,7 +1064,7 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
             const int e = ch >> 6;
             const u64 have = e ? cabove[1] : cabove[0];
             const double before = e ? inc[1] - x[1] : inc[0] - x[0];
-            const double local = fmin(fmax((target - before) * pow2(r.G - (e ? cG[1] : cG[0]) + kFix), 0.0), 0x1p63);
+            const double local = fmin(fmax((target - before) * pow2(r.G - (e ? cG[1] : cG[0]) + unit), 0.0), 0x1p63);
             l.chunk = ch;
             l.K = K;
             s.above_s = min((u64)local, have - 1);
@@ -1064,19 +1074,33 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
     const int ch = l.chunk;
     const u64 goal = s.above_s;
     // its elements in index order: the first whose running sum exceeds the goal
-    constexpr int W = kChunk / 1024;
+    constexpr int E = kChunk / kRowThreads, W = 16 / sizeof(T);
     const Grid g = grid_of(l.cG[ch], r.c);
     const T* z = (const T*)p.z + (size_t)row * p.stride;
-    const int i0 = ch * kChunk + tid * W;
-    u64 x[W], mysum = 0;
+    const int i0 = ch * kChunk + tid * E;
+    T raw[E];
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const float v = i0 + e < p.V ? row_at(z, i0 + e) : -INFINITY;
+    for (int q = 0; q < E; q += W) {
+        if (i0 + q + W <= p.V) {
+            __builtin_memcpy(&raw[q], z + i0 + q, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                raw[q + e] = 0;
+                if (i0 + q + e < p.V) raw[q + e] = z[i0 + q + e];
+            }
+        }
+    }
+    auto weight = [&](int e) -> u64 {
+        const float v = i0 + e < p.V ? clean(ld<T>(raw, e)) : -INFINITY;
         const uint32_t key = key_of(v);
         const bool on = key > r.cut || (key == r.cut && i0 + e <= r.last);
-        x[e] = on ? grid_weight(tab, on_grid(g, v)) : 0;
-        mysum += x[e];
-    }
+        const u64 x = grid_weight(tab, on_grid(g, v));
+        return on ? (border ? hist_weight(x) : x) : 0;
+    };
+    u64 mysum = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) mysum += weight(e);
     u64 inc = mysum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -1087,13 +1111,16 @@ __global__ __launch_bounds__(1024) void k_filter_resolve(FilterP p, Work wk, int
     __syncthreads();
     u64 at = inc - mysum;
     for (int i = 0; i < w; ++i) at += s.wsum[i];
+    if (at <= goal && goal < at + mysum) {
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
-        if (at <= goal && goal < at + x[e]) {
-            p.token[row] = i0 + e;
-            if (p.prob) p.prob[row] = (float)(exp2((double)row_at(z, i0 + e) * r.c - r.G) / l.K);
+        for (int e = 0; e < E; ++e) {
+            const u64 x = weight(e);
+            if (at <= goal && goal < at + x) {
+                p.token[row] = i0 + e;
+                if (p.prob) p.prob[row] = (float)(exp2((double)clean(ld<T>(raw, e)) * r.c - r.G) / l.K);
+            }
+            at += x;
         }
-        at += x[e];
     }
 }
 
@@ -1149,12 +1176,12 @@ static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {
     if (c.out) {
         hipLaunchKernelGGL(k_filter_find<false>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
         hipLaunchKernelGGL((k_filter_collect<T, false>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, false>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_resolve<T, false>), dim3(c.n_rows), dim3(kRowThreads), 0, s, p, wk, nch);
         hipLaunchKernelGGL(k_filter_write<T>, g, dim3(kChunkThreads), 0, s, p, wk);
     } else {
         hipLaunchKernelGGL(k_filter_find<true>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
         hipLaunchKernelGGL((k_filter_collect<T, true>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, true>), dim3(c.n_rows), dim3(1024), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_resolve<T, true>), dim3(c.n_rows), dim3(kRowThreads), 0, s, p, wk, nch);
     }
 }
 
