@@ -1,5 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection:
-// y[t] += scale[a] * B_a (A_a x[t]), a the adapter of row t.
+// y[t] += scale[a] * B_a (A_a x[t]), a the adapter of row t.  Two products with
+// the rank between them, both bound by what they read and write: A and B of the
+// adapters in use for few rows, x and y for many.
 #include <algorithm>
 
 #include "../../include/sd_verify.h"
@@ -9,62 +11,339 @@
 namespace sdv {
 namespace {
 
+// Both products run on 16x16 matrix instructions with rows of the batch as the
+// right operand's columns: D[m][n] = sum_k L[m][k] x[n][k], L the rows of A (or
+// of B).  Rows of a tile that have different adapters are computed for each
+// of them, and each row keeps its own: no row is moved, and an adapter's
+// matrices are read once a tile.
+//
+// A lane (row l % 16, group l / 16) loads 16 bytes of a row at a time, kE
+// elements; a step of the product is the four groups' pieces.  Two steps are
+// interleaved so that the groups' pieces make 128 contiguous bytes of a row.
+template <typename T> struct Mma;
+template <> struct Mma<bf16_t> {
+    static constexpr int kE = 8;
+    typedef bf16x8 Frag;
+    static __device__ __forceinline__ f32x4 run(Frag a, Frag b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mma<float> {
+    static constexpr int kE = 4;
+    typedef f32x4 Frag;
+    static __device__ __forceinline__ f32x4 run(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// 16 bytes of a row from element k on, zeros from n on (any alignment: the
+// hardware takes 16-byte loads at every address)
+template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n) {
+    constexpr int E = Mma<T>::kE;
+    typename Mma<T>::Frag f;
+    if (k + E <= n) {
+        __builtin_memcpy(&f, row + k, 16);
+    } else {
+        T v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            v[i] = 0;
+            if (k + i < n) v[i] = row[k + i];
+        }
+        __builtin_memcpy(&f, v, 16);
+    }
+    return f;
+}
+template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k) {
+    typename Mma<T>::Frag f;
+    __builtin_memcpy(&f, row + k, 16);
+    return f;
+}
+
 // one rounding to the output's type (NaN stays NaN)
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(bf16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
 
-// h[t][r] = A_a[r] . x[t], a wave each
-template <typename T>
-__global__ __launch_bounds__(256) void k_lora_down(LoraCall c, float* h) {
-    const int R = c.n_seg * c.rank;
-    const int r = blockIdx.y * 4 + (threadIdx.x >> 6), t = blockIdx.x, lane = threadIdx.x & 63;
-    const int a = c.ids[t];
-    if (r >= R || a < 0 || a >= c.n_adapters) return;
-    const T* A = (const T*)c.a + ((size_t)a * R + r) * c.d_in;
-    const T* x = (const T*)c.x + (size_t)t * c.xs;
-    const T* xl = c.x_lo ? (const T*)c.x_lo + (size_t)t * c.xs : nullptr;
-    float s = 0.f;
-    for (int i = lane; i < c.d_in; i += 64) s += ld<T>(A, i) * (ld<T>(x, i) + (xl ? ld<T>(xl, i) : 0.f));
-    s = wave_sum(s);
-    if (lane == 0) h[(size_t)t * R + r] = s;
+// The adapters of a tile's rows, one a lane (lane n: row n); -1: none
+__device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int rows, int lane) {
+    const int t = t0 + lane;
+    const int a = lane < rows && t < c.T ? c.ids[t] : -1;
+    return a >= 0 && a < c.n_adapters ? a : -1;
 }
 
-template <typename T, typename Y>
-__global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h) {
-    const int col = blockIdx.y * 256 + threadIdx.x, t = blockIdx.x;
-    if (col >= c.d_out) return;
-    const int a = c.ids[t];
-    const Y* yi = (const Y*)c.y_in + (size_t)t * c.ys;
-    Y* yo = (Y*)c.y_out + (size_t)t * c.yos;
-    if (a < 0 || a >= c.n_adapters) {
-        if (yi != yo) yo[col] = yi[col];
-        return;
+// h = A x: one workgroup a tile of 16 NT rows and a range of k, its waves taking
+// 128-byte pieces of the rows in turn, their sums added in LDS and left as
+// plane blockIdx.y of h ([planes][T][R]) that the second product adds up.
+template <typename T, int NT, int NW, bool LO>
+__global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
+    typedef typename Mma<T>::Frag Frag;
+    constexpr int E = Mma<T>::kE, KB = 8 * E, MT = 4;
+    __shared__ f32x4 part[NW][MT * NT][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int t0 = blockIdx.x * 16 * NT, R = c.n_seg * c.rank;
+    const int nkb = (c.d_in + KB - 1) / KB, full = c.d_in / KB;
+    const int kb0 = (int)((int64_t)nkb * blockIdx.y / gridDim.y), kb1 = (int)((int64_t)nkb * (blockIdx.y + 1) / gridDim.y);
+    const T *x[NT], *xl[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const size_t at = (size_t)min(t0 + 16 * j + n, c.T - 1) * c.xs;
+        x[j] = (const T*)c.x + at;
+        xl[j] = LO ? (const T*)c.x_lo + at : nullptr;
     }
-    int seg = 0;
-    while (col >= c.seg[seg + 1]) ++seg;
-    const float* hr = h + ((size_t)t * c.n_seg + seg) * c.rank;
-    const T* B = (const T*)c.b + ((size_t)a * c.d_out + col) * c.rank;
-    float s = 0.f;
-    for (int r = 0; r < c.rank; ++r) s += ld<T>(B, r) * hr[r];
-    put(yo + col, ld<Y>(yi, col) + (c.scale ? c.scale[a] : 1.f) * s);
+    const int id = tile_id(c, t0, 16 * NT, lane);
+    unsigned long long left = __ballot(id >= 0);
+    while (left) {
+        const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
+        left &= ~__ballot(id == a);
+        for (int r0 = 0; r0 < R; r0 += 16 * MT) {
+            const int mt = min(MT, (R - r0 + 15) / 16);
+            const T* A[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) A[m] = (const T*)c.a + ((size_t)a * R + min(r0 + 16 * m + n, R - 1)) * c.d_in;
+            f32x4 acc[MT][NT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto step = [&](int k, auto load) {
+                Frag xf[NT][2], xlf[NT][2];
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        xf[j][e] = load(x[j], k + e * E);
+                        if (LO) xlf[j][e] = load(xl[j], k + e * E);
+                    }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    if (m >= mt) break;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const Frag af = load(A[m], k + e * E);
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) {
+                            acc[m][j] = Mma<T>::run(af, xf[j][e], acc[m][j]);
+                            if (LO) acc[m][j] = Mma<T>::run(af, xlf[j][e], acc[m][j]);
+                        }
+                    }
+                }
+            };
+            const int end = min(kb1, full);
+            int kb = kb0 + w;
+#pragma unroll 2
+            for (; kb < end; kb += NW) step(kb * KB + 2 * E * g, [](const T* p, int k) { return piece(p, k); });
+            if (kb < kb1)  // the row's last, incomplete piece
+                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return piece(p, k, c.d_in); });
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    if (m < mt) part[w][m * NT + j][lane] = acc[m][j];
+            __syncthreads();
+            // (m, j) tiles over the waves
+            for (int q = w; q < mt * NT; q += NW) {
+                const int m = q / NT, j = q % NT;
+                f32x4 s = part[0][q][lane];
+#pragma unroll
+                for (int i = 1; i < NW; ++i) s += part[i][q][lane];
+                const int t = t0 + 16 * j + n, r = r0 + 16 * m + 4 * g;
+                if (__shfl(id, 16 * j + n, 64) == a) {
+                    float* o = h + ((size_t)blockIdx.y * c.T + t) * R + r;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r + i < R) o[i] = s[i];
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// y_out = y_in + scale B h: a wave takes 16 NT rows and 64 columns of one segment.
+// h is the sum of its planes, in bf16 as two planes of its own (hi + lo, about 16
+// bits, two products).
+template <typename T, typename Y, int NT>
+__global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes) {
+    typedef typename Mma<T>::Frag Frag;
+    constexpr int E = Mma<T>::kE, CT = 4;
+    constexpr int W = 16 / sizeof(Y), JW = W / 4;  // columns of a lane next to each other: from JW tiles
+    constexpr bool LO = sizeof(T) == 2;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int t0 = blockIdx.x * 16 * NT, R = c.n_seg * c.rank;
+    // the wave's columns: segments are cut apart
+    int blk = blockIdx.y * 4 + w, seg = 0;
+    while (seg < c.n_seg) {
+        const int nb = (c.seg[seg + 1] - c.seg[seg] + 16 * CT - 1) / (16 * CT);
+        if (blk < nb) break;
+        blk -= nb;
+        ++seg;
+    }
+    if (seg == c.n_seg) return;
+    const int c0 = c.seg[seg] + blk * 16 * CT, c1 = c.seg[seg + 1];
+    const int id = tile_id(c, t0, 16 * NT, lane);
+    unsigned long long left = __ballot(id >= 0);
+    const bool in_place = c.y_in == c.y_out;
+    if (!left && in_place) return;
+    // tile q's row 4 g + i is this lane's column col(q) + i; left operand's row n is column lcol(q)
+    auto col = [&](int q) { return c0 + (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
+    auto lcol = [&](int q) { return c0 + (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
+    f32x4 out[CT][NT];
+#pragma unroll
+    for (int q = 0; q < CT; ++q)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) out[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    while (left) {
+        const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
+        left &= ~__ballot(id == a);
+        f32x4 acc[CT][NT];
+#pragma unroll
+        for (int q = 0; q < CT; ++q)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int r0 = 0; r0 < c.rank; r0 += 4 * E) {
+            const int k = r0 + E * g;
+            Frag hf[NT], lf[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                // (rows of other adapters may hold anything: their columns are not used)
+                const float* hr = h + (size_t)min(t0 + 16 * j + n, c.T - 1) * R + seg * c.rank;
+                float v[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = 0.f;
+                if (k + E <= c.rank) {
+                    for (int p = 0; p < planes; ++p) {
+                        float u[E];
+                        __builtin_memcpy(u, hr + (size_t)p * c.T * R + k, sizeof(u));
+#pragma unroll
+                        for (int i = 0; i < E; ++i) v[i] += u[i];
+                    }
+                } else {
+                    for (int p = 0; p < planes; ++p)
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            if (k + i < c.rank) v[i] += hr[(size_t)p * c.T * R + k + i];
+                }
+                if constexpr (LO) {
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        hf[j][i] = (__bf16)v[i];
+                        lf[j][i] = (__bf16)(v[i] - (float)hf[j][i]);
+                    }
+                } else {
+                    __builtin_memcpy(&hf[j], v, 16);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < CT; ++q) {
+                const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(lcol(q), c1 - 1)) * c.rank;
+                const Frag bf = piece(B, k, c.rank);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    acc[q][j] = Mma<T>::run(bf, hf[j], acc[q][j]);
+                    if constexpr (LO) acc[q][j] = Mma<T>::run(bf, lf[j], acc[q][j]);
+                }
+            }
+        }
+        const float sc = c.scale ? c.scale[a] : 1.f;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const bool mine = __shfl(id, 16 * j + n, 64) == a;
+#pragma unroll
+            for (int q = 0; q < CT; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[q][j][i] = mine ? sc * acc[q][j][i] : out[q][j][i];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int t = t0 + 16 * j + n;
+        if (t >= c.T) continue;
+        const bool on = __shfl(id, 16 * j + n, 64) >= 0;
+        const Y* yi = (const Y*)c.y_in + (size_t)t * c.ys;
+        Y* yo = (Y*)c.y_out + (size_t)t * c.yos;
+        if (!on && in_place) continue;
+#pragma unroll
+        for (int q = 0; q < CT; q += JW) {
+            const int k = col(q);
+            Y v[W];
+            if (k + W <= c1) {
+                __builtin_memcpy(v, yi + k, 16);
+                if (on)
+#pragma unroll
+                    for (int i = 0; i < W; ++i) put(&v[i], as_float(v[i]) + out[q + i / 4][j][i % 4]);
+                __builtin_memcpy(yo + k, v, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (k + i < c1) {
+                        Y x = yi[k + i];
+                        if (on) put(&x, as_float(x) + out[q + i / 4][j][i % 4]);
+                        yo[k + i] = x;
+                    }
+            }
+        }
+    }
+}
+
+// Rows a tile: 64 where there are enough of them to fill the chip with such
+// tiles, else 16.  Ranges of k: about kDownGroups workgroups in all, each with
+// two 128-byte pieces a wave at least.
+constexpr int kWideRows = 2048;
+constexpr int kDownGroups = 512;
+int down_planes(int T, int d_in, int es) {
+    const bool wide = T >= kWideRows;
+    const int tiles = (T + (wide ? 63 : 15)) / (wide ? 64 : 16), nw = wide ? 4 : 8;
+    const int pieces = (d_in * es + 127) / 128;
+    return std::max(1, std::min((kDownGroups + tiles - 1) / tiles, std::min(pieces / (2 * nw), 16)));
+}
+
+template <typename T, int NT, int NW>
+void launch_down(const LoraCall& c, float* h, int planes, hipStream_t s) {
+    const dim3 g((c.T + 16 * NT - 1) / (16 * NT), planes);
+    if constexpr (sizeof(T) == 2) {
+        if (c.x_lo) {
+            hipLaunchKernelGGL((k_lora_down<T, NT, NW, true>), g, dim3(64 * NW), 0, s, c, h);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((k_lora_down<T, NT, NW, false>), g, dim3(64 * NW), 0, s, c, h);
+}
+template <typename T, int NT>
+void launch_up(const LoraCall& c, const float* h, int planes, hipStream_t s) {
+    int blocks = 0;
+    for (int i = 0; i < c.n_seg; ++i) blocks += (c.seg[i + 1] - c.seg[i] + 63) / 64;
+    const dim3 g((c.T + 16 * NT - 1) / (16 * NT), (blocks + 3) / 4);
+    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, NT>), g, dim3(256), 0, s, c, h, planes);
+    else hipLaunchKernelGGL((k_lora_up<T, float, NT>), g, dim3(256), 0, s, c, h, planes);
+}
+template <typename T>
+void launch_typed(const LoraCall& c, hipStream_t s) {
+    float* h = (float*)c.ws;
+    const int planes = down_planes(c.T, c.d_in, sizeof(T));
+    if (c.T >= kWideRows) {
+        launch_down<T, 4, 4>(c, h, planes, s);
+        launch_up<T, 4>(c, h, planes, s);
+    } else {
+        launch_down<T, 1, 8>(c, h, planes, s);
+        launch_up<T, 1>(c, h, planes, s);
+    }
 }
 
 }  // namespace
 
-size_t lora_workspace(int T, int rank, int n_seg) { return ((size_t)T * rank * n_seg * 4 + 255) & ~(size_t)255; }
+// (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
+size_t lora_workspace(int T, int rank, int n_seg) {
+    const size_t rows = std::min((size_t)16 * T, (size_t)64 * (kDownGroups + (T + 15) / 16));
+    return (rows * rank * n_seg * 4 + 255) & ~(size_t)255;
+}
 
 void launch_lora(const LoraCall& c, hipStream_t s) {
-    float* h = (float*)c.ws;
-    const dim3 gd(c.T, (c.n_seg * c.rank + 3) / 4), gu(c.T, (c.d_out + 255) / 256);
-    if (c.bf16) {
-        hipLaunchKernelGGL(k_lora_down<bf16_t>, gd, dim3(256), 0, s, c, h);
-        if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<bf16_t, bf16_t>), gu, dim3(256), 0, s, c, h);
-        else hipLaunchKernelGGL((k_lora_up<bf16_t, float>), gu, dim3(256), 0, s, c, h);
-    } else {
-        hipLaunchKernelGGL(k_lora_down<float>, gd, dim3(256), 0, s, c, h);
-        if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<float, bf16_t>), gu, dim3(256), 0, s, c, h);
-        else hipLaunchKernelGGL((k_lora_up<float, float>), gu, dim3(256), 0, s, c, h);
-    }
+    if (c.bf16) launch_typed<bf16_t>(c, s);
+    else launch_typed<float>(c, s);
 }
 
 }  // namespace sdv

@@ -131,6 +131,7 @@ def test_owners_of_rows(name, ids):
 @pytest.mark.parametrize("T,d_in,segs,rank,n,planes,y_dtype", [
     (80, 25600, [5120], 32, 16, 2, "f32"), (229, 5120, [8192, 1024, 1024], 16, 32, 2, "f32"),
     (1, 2048, [2048, 1024, 1024], 16, 4, 1, "f32"), (700, 5120, [5120], 64, 3, 1, "bf16"),
+    (2500, 1024, [1040], 64, 3, 2, "f32"), (2048, 520, [600, 40], 20, 2, 1, "bf16"), (4111, 256, [130], 8, 40, 1, "f32"),
 ])
 def test_widths_of_the_models(T, d_in, segs, rank, n, planes, y_dtype):
     r = np.random.default_rng(T)
