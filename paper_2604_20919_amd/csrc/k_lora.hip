@@ -75,9 +75,10 @@ __device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int rows, int 
     return a >= 0 && a < c.n_adapters ? a : -1;
 }
 
-// h = A x: one workgroup a tile of 16 NT rows and a range of k, its waves taking
-// 128-byte pieces of the rows in turn, their sums added in LDS and left as
-// plane blockIdx.y of h ([planes][T][R]) that the second product adds up.
+// h = A x: one workgroup a tile of 16 NT rows, a range of k and every gridDim.z-th
+// of the tile's adapters, its waves taking 128-byte pieces of the rows in turn,
+// their sums added in LDS and left as plane blockIdx.y of h ([planes][T][R]) that
+// the second product adds up.
 template <typename T, int NT, int NW, bool LO>
 __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     typedef typename Mma<T>::Frag Frag;
@@ -96,9 +97,10 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     }
     const int id = tile_id(c, t0, 16 * NT, lane);
     unsigned long long left = __ballot(id >= 0);
-    while (left) {
+    for (int ord = 0; left; ++ord) {
         const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
         left &= ~__ballot(id == a);
+        if (ord % gridDim.z != blockIdx.z) continue;
         for (int r0 = 0; r0 < R; r0 += 16 * MT) {
             const int mt = min(MT, (R - r0 + 15) / 16);
             const T* A[MT];
@@ -163,181 +165,232 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     }
 }
 
-// y_out = y_in + scale B h: a wave takes 16 NT rows and 64 columns of one segment.
-// h is the sum of its planes, in bf16 as two planes of its own (hi + lo, about 16
-// bits, two products).
-template <typename T, typename Y, int NT>
-__global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes) {
+// y_out = y_in + scale B h: a wave takes 16 NT rows, `per` blocks of 16 CT columns
+// and every gridDim.z-th of the rows' adapters.  h is the sum of its planes, in
+// bf16 as two planes of its own (hi + lo, about 16 bits, two products), kept
+// in registers over the wave's columns.  RB: steps of the product that hold the rank.
+template <typename T, typename Y, int NT, int RB>
+__global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes, int per) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, CT = 4;
     constexpr int W = 16 / sizeof(Y), JW = W / 4;  // columns of a lane next to each other: from JW tiles
     constexpr bool LO = sizeof(T) == 2;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
     const int t0 = blockIdx.x * 16 * NT, R = c.n_seg * c.rank;
-    // the wave's columns: segments are cut apart
-    int blk = blockIdx.y * 4 + w, seg = 0;
-    while (seg < c.n_seg) {
-        const int nb = (c.seg[seg + 1] - c.seg[seg] + 16 * CT - 1) / (16 * CT);
-        if (blk < nb) break;
-        blk -= nb;
-        ++seg;
-    }
-    if (seg == c.n_seg) return;
-    const int c0 = c.seg[seg] + blk * 16 * CT, c1 = c.seg[seg + 1];
+    // the wave's first block of columns: segments are cut apart
+    int blk = (blockIdx.y * 4 + w) * per, seg0 = 0;
+    auto blocks = [&](int s) { return (c.seg[s + 1] - c.seg[s] + 16 * CT - 1) / (16 * CT); };
+    while (seg0 < c.n_seg && blk >= blocks(seg0)) blk -= blocks(seg0++);
+    if (seg0 == c.n_seg) return;
     const int id = tile_id(c, t0, 16 * NT, lane);
     unsigned long long left = __ballot(id >= 0);
-    const bool in_place = c.y_in == c.y_out;
-    if (!left && in_place) return;
+    int mine[NT];  // the adapter of the lane's row
+#pragma unroll
+    for (int j = 0; j < NT; ++j) mine[j] = __shfl(id, 16 * j + n, 64);
     // tile q's row 4 g + i is this lane's column col(q) + i; left operand's row n is column lcol(q)
-    auto col = [&](int q) { return c0 + (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
-    auto lcol = [&](int q) { return c0 + (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
-    f32x4 out[CT][NT];
-#pragma unroll
-    for (int q = 0; q < CT; ++q)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) out[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    while (left) {
-        const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
-        left &= ~__ballot(id == a);
-        f32x4 acc[CT][NT];
-#pragma unroll
-        for (int q = 0; q < CT; ++q)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int r0 = 0; r0 < c.rank; r0 += 4 * E) {
-            const int k = r0 + E * g;
-            Frag hf[NT], lf[NT];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                // (rows of other adapters may hold anything: their columns are not used)
-                const float* hr = h + (size_t)min(t0 + 16 * j + n, c.T - 1) * R + seg * c.rank;
-                float v[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) v[i] = 0.f;
-                if (k + E <= c.rank) {
-                    for (int p = 0; p < planes; ++p) {
-                        float u[E];
-                        __builtin_memcpy(u, hr + (size_t)p * c.T * R + k, sizeof(u));
-#pragma unroll
-                        for (int i = 0; i < E; ++i) v[i] += u[i];
-                    }
-                } else {
-                    for (int p = 0; p < planes; ++p)
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            if (k + i < c.rank) v[i] += hr[(size_t)p * c.T * R + k + i];
-                }
-                if constexpr (LO) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        hf[j][i] = (__bf16)v[i];
-                        lf[j][i] = (__bf16)(v[i] - (float)hf[j][i]);
-                    }
-                } else {
-                    __builtin_memcpy(&hf[j], v, 16);
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < CT; ++q) {
-                const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(lcol(q), c1 - 1)) * c.rank;
-                const Frag bf = piece(B, k, c.rank);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    acc[q][j] = Mma<T>::run(bf, hf[j], acc[q][j]);
-                    if constexpr (LO) acc[q][j] = Mma<T>::run(bf, lf[j], acc[q][j]);
-                }
+    auto col = [&](int q) { return (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
+    auto lcol = [&](int q) { return (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
+    // blocks of columns from the wave's first on
+    auto each_block = [&](auto f) {
+        int s = seg0, b = blk;
+        for (int i = 0; i < per; ++i) {
+            f(s, c.seg[s] + b * 16 * CT, c.seg[s + 1]);
+            if (++b == blocks(s)) {
+                b = 0;
+                if (++s == c.n_seg) break;
             }
         }
+    };
+    for (int ord = 0; left; ++ord) {
+        const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
+        left &= ~__ballot(id == a);
+        if (ord % gridDim.z != blockIdx.z) continue;
         const float sc = c.scale ? c.scale[a] : 1.f;
+        Frag hf[NT][RB], lf[NT][RB];
+        int have = -1;  // the segment whose h they hold
+        each_block([&](int seg, int c0, int c1) {
+            Frag bf[RB][CT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const bool mine = __shfl(id, 16 * j + n, 64) == a;
+            for (int q = 0; q < CT; ++q) {
+                const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(c0 + lcol(q), c1 - 1)) * c.rank;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) bf[r][q] = piece(B, (4 * r + g) * E, c.rank);
+            }
+            Y y[NT][CT / JW][W];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                if (mine[j] == a) {
+                    const Y* yi = (const Y*)c.y_in + (size_t)(t0 + 16 * j + n) * c.ys;
+#pragma unroll
+                    for (int q = 0; q < CT / JW; ++q) {
+                        const int k = c0 + col(q * JW);
+                        if (k + W <= c1) {
+                            __builtin_memcpy(y[j][q], yi + k, 16);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < W; ++i)
+                                if (k + i < c1) y[j][q][i] = yi[k + i];
+                        }
+                    }
+                }
+            if (have != seg) {
+                have = seg;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    // (rows of other adapters may hold anything: their columns are not used)
+                    const float* hr = h + (size_t)min(t0 + 16 * j + n, c.T - 1) * R + seg * c.rank;
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const int k = (4 * r + g) * E;
+                        float v[E];
+#pragma unroll
+                        for (int i = 0; i < E; ++i) v[i] = 0.f;
+                        if (k + E <= c.rank) {
+#pragma unroll 4
+                            for (int p = 0; p < planes; ++p) {
+                                float u[E];
+                                __builtin_memcpy(u, hr + (size_t)p * c.T * R + k, sizeof(u));
+#pragma unroll
+                                for (int i = 0; i < E; ++i) v[i] += u[i];
+                            }
+                        } else {
+                            for (int p = 0; p < planes; ++p)
+#pragma unroll
+                                for (int i = 0; i < E; ++i)
+                                    if (k + i < c.rank) v[i] += hr[(size_t)p * c.T * R + k + i];
+                        }
+                        if constexpr (LO) {
+#pragma unroll
+                            for (int i = 0; i < E; ++i) {
+                                hf[j][r][i] = (__bf16)v[i];
+                                lf[j][r][i] = (__bf16)(v[i] - (float)hf[j][r][i]);
+                            }
+                        } else {
+                            __builtin_memcpy(&hf[j][r], v, 16);
+                        }
+                    }
+                }
+            }
+            f32x4 acc[CT][NT];
 #pragma unroll
             for (int q = 0; q < CT; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) out[q][j][i] = mine ? sc * acc[q][j][i] : out[q][j][i];
-        }
-    }
+                for (int j = 0; j < NT; ++j) {
+                    acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int t = t0 + 16 * j + n;
-        if (t >= c.T) continue;
-        const bool on = __shfl(id, 16 * j + n, 64) >= 0;
-        const Y* yi = (const Y*)c.y_in + (size_t)t * c.ys;
-        Y* yo = (Y*)c.y_out + (size_t)t * c.yos;
-        if (!on && in_place) continue;
-#pragma unroll
-        for (int q = 0; q < CT; q += JW) {
-            const int k = col(q);
-            Y v[W];
-            if (k + W <= c1) {
-                __builtin_memcpy(v, yi + k, 16);
-                if (on)
-#pragma unroll
-                    for (int i = 0; i < W; ++i) put(&v[i], as_float(v[i]) + out[q + i / 4][j][i % 4]);
-                __builtin_memcpy(yo + k, v, 16);
-            } else {
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-                    if (k + i < c1) {
-                        Y x = yi[k + i];
-                        if (on) put(&x, as_float(x) + out[q + i / 4][j][i % 4]);
-                        yo[k + i] = x;
+                    for (int r = 0; r < RB; ++r) {
+                        acc[q][j] = Mma<T>::run(bf[r][q], hf[j][r], acc[q][j]);
+                        if constexpr (LO) acc[q][j] = Mma<T>::run(bf[r][q], lf[j][r], acc[q][j]);
                     }
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                if (mine[j] == a) {
+                    Y* yo = (Y*)c.y_out + (size_t)(t0 + 16 * j + n) * c.yos;
+#pragma unroll
+                    for (int q = 0; q < CT / JW; ++q) {
+                        const int k = c0 + col(q * JW);
+#pragma unroll
+                        for (int i = 0; i < W; ++i)
+                            put(&y[j][q][i], as_float(y[j][q][i]) + sc * acc[q * JW + i / 4][j][i % 4]);
+                        if (k + W <= c1) {
+                            __builtin_memcpy(yo + k, y[j][q], 16);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < W; ++i)
+                                if (k + i < c1) yo[k + i] = y[j][q][i];
+                        }
+                    }
+                }
+        });
+    }
+    // rows without an adapter
+    if (c.y_in == c.y_out || blockIdx.z) return;
+    each_block([&](int, int c0, int c1) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int t = t0 + 16 * j + n;
+            if (t >= c.T || mine[j] >= 0) continue;
+            const Y* yi = (const Y*)c.y_in + (size_t)t * c.ys;
+            Y* yo = (Y*)c.y_out + (size_t)t * c.yos;
+#pragma unroll
+            for (int q = 0; q < CT / JW; ++q) {
+                const int k = c0 + col(q * JW);
+                if (k + W <= c1) {
+                    __builtin_memcpy(yo + k, yi + k, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        if (k + i < c1) yo[k + i] = yi[k + i];
+                }
             }
         }
-    }
+    });
 }
 
-// Rows a tile: 64 where there are enough of them to fill the chip with such
-// tiles, else 16.  Ranges of k: about kDownGroups workgroups in all, each with
-// two 128-byte pieces a wave at least.
+// Launch shapes.  Few rows: tiles of 16, up to kShare workgroups sharing out a
+// tile's adapters; many: tiles of 32.  Ranges of k: about kDownGroups workgroups
+// in all, a 128-byte piece a wave at least.
 constexpr int kWideRows = 2048;
-constexpr int kDownGroups = 512;
-int down_planes(int T, int d_in, int es) {
+constexpr int kDownGroups = 512, kMaxPlanes = 16, kShare = 8;
+struct Shape {
+    int rows, waves, tiles, share, planes;
+};
+Shape shape_of(int T, int d_in, int es, int n_adapters) {
+    Shape s;
     const bool wide = T >= kWideRows;
-    const int tiles = (T + (wide ? 63 : 15)) / (wide ? 64 : 16), nw = wide ? 4 : 8;
-    const int pieces = (d_in * es + 127) / 128;
-    return std::max(1, std::min((kDownGroups + tiles - 1) / tiles, std::min(pieces / (2 * nw), 16)));
+    s.rows = wide ? 32 : 16;
+    s.waves = 8;
+    s.tiles = (T + s.rows - 1) / s.rows;
+    s.share = wide ? 1 : std::min(std::min(kShare, n_adapters), T);
+    const int pieces = (d_in * es + 127) / 128, groups = s.tiles * std::min(s.share, 4);
+    s.planes = std::max(1, std::min(std::min((kDownGroups + groups - 1) / groups, pieces / s.waves), kMaxPlanes));
+    return s;
 }
 
-template <typename T, int NT, int NW>
-void launch_down(const LoraCall& c, float* h, int planes, hipStream_t s) {
-    const dim3 g((c.T + 16 * NT - 1) / (16 * NT), planes);
+template <typename T, int NT>
+void launch_down(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
+    const dim3 g(sh.tiles, sh.planes, sh.share);
     if constexpr (sizeof(T) == 2) {
         if (c.x_lo) {
-            hipLaunchKernelGGL((k_lora_down<T, NT, NW, true>), g, dim3(64 * NW), 0, s, c, h);
+            hipLaunchKernelGGL((k_lora_down<T, NT, 8, true>), g, dim3(512), 0, s, c, h);
             return;
         }
     }
-    hipLaunchKernelGGL((k_lora_down<T, NT, NW, false>), g, dim3(64 * NW), 0, s, c, h);
+    hipLaunchKernelGGL((k_lora_down<T, NT, 8, false>), g, dim3(512), 0, s, c, h);
 }
-template <typename T, int NT>
-void launch_up(const LoraCall& c, const float* h, int planes, hipStream_t s) {
+template <typename T, int NT, int RB>
+void launch_up(const LoraCall& c, const Shape& sh, const float* h, hipStream_t s) {
     int blocks = 0;
     for (int i = 0; i < c.n_seg; ++i) blocks += (c.seg[i + 1] - c.seg[i] + 63) / 64;
-    const dim3 g((c.T + 16 * NT - 1) / (16 * NT), (blocks + 3) / 4);
-    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, NT>), g, dim3(256), 0, s, c, h, planes);
-    else hipLaunchKernelGGL((k_lora_up<T, float, NT>), g, dim3(256), 0, s, c, h, planes);
+    // as many blocks a wave as leave about 16 waves a CU
+    const int per = std::max(1, (int)std::min<int64_t>((int64_t)blocks * sh.tiles / (16 * cu_count()), 16));
+    const int waves = (blocks + per - 1) / per;
+    const dim3 g(sh.tiles, (waves + 3) / 4, sh.share);
+    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, NT, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
+    else hipLaunchKernelGGL((k_lora_up<T, float, NT, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
+}
+template <typename T, int NT>
+void launch_both(const LoraCall& c, const Shape& sh, hipStream_t s) {
+    float* h = (float*)c.ws;
+    launch_down<T, NT>(c, sh, h, s);
+    constexpr int K = 4 * Mma<T>::kE;  // a step of the product
+    if (c.rank <= 32) launch_up<T, NT, 32 / K>(c, sh, h, s);
+    else if (c.rank <= 64) launch_up<T, NT, 64 / K>(c, sh, h, s);
+    else launch_up<T, NT, 128 / K>(c, sh, h, s);
 }
 template <typename T>
 void launch_typed(const LoraCall& c, hipStream_t s) {
-    float* h = (float*)c.ws;
-    const int planes = down_planes(c.T, c.d_in, sizeof(T));
-    if (c.T >= kWideRows) {
-        launch_down<T, 4, 4>(c, h, planes, s);
-        launch_up<T, 4>(c, h, planes, s);
-    } else {
-        launch_down<T, 1, 8>(c, h, planes, s);
-        launch_up<T, 1>(c, h, planes, s);
-    }
+    const Shape sh = shape_of(c.T, c.d_in, sizeof(T), c.n_adapters);
+    if (sh.rows == 16) launch_both<T, 1>(c, sh, s);
+    else launch_both<T, 2>(c, sh, s);
 }
 
 }  // namespace
 
 // (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
 size_t lora_workspace(int T, int rank, int n_seg) {
-    const size_t rows = std::min((size_t)16 * T, (size_t)64 * (kDownGroups + (T + 15) / 16));
+    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)32 * (kDownGroups + (T + 15) / 16));
     return (rows * rank * n_seg * 4 + 255) & ~(size_t)255;
 }
 
