@@ -68,34 +68,30 @@ __device__ __forceinline__ float as_float(bf16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
 
-// The adapters of a tile's rows, one a lane (lane n: row n); -1: none
-__device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int rows, int lane) {
+// The adapters of a tile's 16 rows, one a lane (lane n: row n); -1: none
+__device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int lane) {
     const int t = t0 + lane;
-    const int a = lane < rows && t < c.T ? c.ids[t] : -1;
+    const int a = lane < 16 && t < c.T ? c.ids[t] : -1;
     return a >= 0 && a < c.n_adapters ? a : -1;
 }
 
-// h = A x: one workgroup a tile of 16 NT rows, a range of k and every gridDim.z-th
+// h = A x: one workgroup a tile of 16 rows, a range of k and every gridDim.z-th
 // of the tile's adapters, its waves taking 128-byte pieces of the rows in turn,
 // their sums added in LDS and left as plane blockIdx.y of h ([planes][T][R]) that
 // the second product adds up.
-template <typename T, int NT, int NW, bool LO>
+template <typename T, int NW, bool LO>
 __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, KB = 8 * E, MT = 4;
-    __shared__ f32x4 part[NW][MT * NT][64];
+    __shared__ f32x4 part[NW][MT][64];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int t0 = blockIdx.x * 16 * NT, R = c.n_seg * c.rank;
+    const int t0 = blockIdx.x * 16, R = c.n_seg * c.rank;
     const int nkb = (c.d_in + KB - 1) / KB, full = c.d_in / KB;
     const int kb0 = (int)((int64_t)nkb * blockIdx.y / gridDim.y), kb1 = (int)((int64_t)nkb * (blockIdx.y + 1) / gridDim.y);
-    const T *x[NT], *xl[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const size_t at = (size_t)min(t0 + 16 * j + n, c.T - 1) * c.xs;
-        x[j] = (const T*)c.x + at;
-        xl[j] = LO ? (const T*)c.x_lo + at : nullptr;
-    }
-    const int id = tile_id(c, t0, 16 * NT, lane);
+    const size_t xrow = (size_t)min(t0 + n, c.T - 1) * c.xs;
+    const T* x = (const T*)c.x + xrow;
+    const T* xl = LO ? (const T*)c.x_lo + xrow : nullptr;
+    const int id = tile_id(c, t0, lane), mine = __shfl(id, n, 64);
     unsigned long long left = __ballot(id >= 0);
     for (int ord = 0; left; ++ord) {
         const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
@@ -106,31 +102,24 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
             const T* A[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) A[m] = (const T*)c.a + ((size_t)a * R + min(r0 + 16 * m + n, R - 1)) * c.d_in;
-            f32x4 acc[MT][NT];
+            f32x4 acc[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
             auto step = [&](int k, auto load) {
-                Frag xf[NT][2], xlf[NT][2];
+                Frag xf[2], xlf[2];
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        xf[j][e] = load(x[j], k + e * E);
-                        if (LO) xlf[j][e] = load(xl[j], k + e * E);
-                    }
+                for (int e = 0; e < 2; ++e) {
+                    xf[e] = load(x, k + e * E);
+                    if (LO) xlf[e] = load(xl, k + e * E);
+                }
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     if (m >= mt) break;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const Frag af = load(A[m], k + e * E);
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) {
-                            acc[m][j] = Mma<T>::run(af, xf[j][e], acc[m][j]);
-                            if (LO) acc[m][j] = Mma<T>::run(af, xlf[j][e], acc[m][j]);
-                        }
+                        acc[m] = Mma<T>::run(af, xf[e], acc[m]);
+                        if (LO) acc[m] = Mma<T>::run(af, xlf[e], acc[m]);
                     }
                 }
             };
@@ -142,19 +131,15 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
                 step(kb * KB + 2 * E * g, [&](const T* p, int k) { return piece(p, k, c.d_in); });
 #pragma unroll
             for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    if (m < mt) part[w][m * NT + j][lane] = acc[m][j];
+                if (m < mt) part[w][m][lane] = acc[m];
             __syncthreads();
-            // (m, j) tiles over the waves
-            for (int q = w; q < mt * NT; q += NW) {
-                const int m = q / NT, j = q % NT;
-                f32x4 s = part[0][q][lane];
+            if (w < mt) {  // the tiles over the waves
+                f32x4 s = part[0][w][lane];
 #pragma unroll
-                for (int i = 1; i < NW; ++i) s += part[i][q][lane];
-                const int t = t0 + 16 * j + n, r = r0 + 16 * m + 4 * g;
-                if (__shfl(id, 16 * j + n, 64) == a) {
-                    float* o = h + ((size_t)blockIdx.y * c.T + t) * R + r;
+                for (int i = 1; i < NW; ++i) s += part[i][w][lane];
+                const int r = r0 + 16 * w + 4 * g;
+                if (mine == a) {
+                    float* o = h + ((size_t)blockIdx.y * c.T + t0 + n) * R + r;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (r + i < R) o[i] = s[i];
@@ -165,232 +150,544 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     }
 }
 
-// y_out = y_in + scale B h: a wave takes 16 NT rows, `per` blocks of 16 CT columns
-// and every gridDim.z-th of the rows' adapters.  h is the sum of its planes, in
-// bf16 as two planes of its own (hi + lo, about 16 bits, two products), kept
-// in registers over the wave's columns.  RB: steps of the product that hold the rank.
-template <typename T, typename Y, int NT, int RB>
+// h of a row's segment as right operand: the sum of its planes, in bf16 carried
+// on in two planes of its own (hi + lo, about 16 bits, two products)
+template <typename T> struct Inner {
+    typedef typename Mma<T>::Frag Frag;
+    Frag hi, lo;
+};
+template <typename T>
+__device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank, size_t stride, int planes) {
+    constexpr int E = Mma<T>::kE;
+    float v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = 0.f;
+    if (k + E <= rank) {
+#pragma unroll 8
+        for (int p = 0; p < planes; ++p) {
+            float u[E];
+            __builtin_memcpy(u, hr + p * stride + k, sizeof(u));
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] += u[i];
+        }
+    } else {
+        for (int p = 0; p < planes; ++p)
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (k + i < rank) v[i] += hr[p * stride + k + i];
+    }
+    Inner<T> r;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            r.hi[i] = (__bf16)v[i];
+            r.lo[i] = (__bf16)(v[i] - (float)r.hi[i]);
+        }
+    } else {
+        __builtin_memcpy(&r.hi, v, 16);
+    }
+    return r;
+}
+
+// y_out = y_in + scale B h: a wave takes 16 rows, `per` blocks of 16 CT columns
+// and every gridDim.z-th of the rows' adapters.  A row's h, y and scale do not
+// wait for the adapters: they are requested first, and each adapter's B while the
+// one before is multiplied.  RB: steps of the product that hold the rank.
+template <typename T, typename Y, int RB>
 __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes, int per) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, CT = 4;
     constexpr int W = 16 / sizeof(Y), JW = W / 4;  // columns of a lane next to each other: from JW tiles
-    constexpr bool LO = sizeof(T) == 2;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int t0 = blockIdx.x * 16 * NT, R = c.n_seg * c.rank;
+    const int t0 = blockIdx.x * 16, t = t0 + n, R = c.n_seg * c.rank;
     // the wave's first block of columns: segments are cut apart
-    int blk = (blockIdx.y * 4 + w) * per, seg0 = 0;
-    auto blocks = [&](int s) { return (c.seg[s + 1] - c.seg[s] + 16 * CT - 1) / (16 * CT); };
-    while (seg0 < c.n_seg && blk >= blocks(seg0)) blk -= blocks(seg0++);
-    if (seg0 == c.n_seg) return;
-    const int id = tile_id(c, t0, 16 * NT, lane);
-    unsigned long long left = __ballot(id >= 0);
-    int mine[NT];  // the adapter of the lane's row
-#pragma unroll
-    for (int j = 0; j < NT; ++j) mine[j] = __shfl(id, 16 * j + n, 64);
+    int b = (blockIdx.y * 4 + w) * per, s = 0;
+    auto blocks = [&](int i) { return (c.seg[i + 1] - c.seg[i] + 16 * CT - 1) / (16 * CT); };
+    while (s < c.n_seg && b >= blocks(s)) b -= blocks(s++);
+    if (s == c.n_seg) return;
+    const int id = tile_id(c, t0, lane);
+    const size_t row = (size_t)min(t, c.T - 1);
+    const Y* yi = (const Y*)c.y_in + row * c.ys;
+    Y* yo = (Y*)c.y_out + row * c.yos;
     // tile q's row 4 g + i is this lane's column col(q) + i; left operand's row n is column lcol(q)
     auto col = [&](int q) { return (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
     auto lcol = [&](int q) { return (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
-    // blocks of columns from the wave's first on
-    auto each_block = [&](auto f) {
-        int s = seg0, b = blk;
-        for (int i = 0; i < per; ++i) {
-            f(s, c.seg[s] + b * 16 * CT, c.seg[s + 1]);
-            if (++b == blocks(s)) {
-                b = 0;
-                if (++s == c.n_seg) break;
+    Inner<T> hv[RB];
+    Y y[CT / JW][W];
+    int have = -1;  // the segment of hv
+    unsigned long long todo = 0;  // first rows of the adapters that are this workgroup's
+    int mine = -1;
+    bool write = false;
+    float sc = 1.f;
+    for (int i = 0; i < per; ++i) {
+        const int c0 = c.seg[s] + b * 16 * CT, c1 = c.seg[s + 1];
+        if (have != s) {
+            have = s;
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                hv[r] = inner_piece<T>(h + row * R + s * c.rank, (4 * r + g) * E, c.rank, (size_t)c.T * R, planes);
+        }
+#pragma unroll
+        for (int q = 0; q < CT / JW; ++q) {
+            const int k = c0 + col(q * JW);
+            if (k + W <= c1) {
+                __builtin_memcpy(y[q], yi + k, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; ++e) y[q][e] = k + e < c1 ? yi[k + e] : (Y)0;
             }
         }
-    };
-    for (int ord = 0; left; ++ord) {
-        const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
-        left &= ~__ballot(id == a);
-        if (ord % gridDim.z != blockIdx.z) continue;
-        const float sc = c.scale ? c.scale[a] : 1.f;
-        Frag hf[NT][RB], lf[NT][RB];
-        int have = -1;  // the segment whose h they hold
-        each_block([&](int seg, int c0, int c1) {
-            Frag bf[RB][CT];
+        if (i == 0) {
+            mine = __shfl(id, n, 64);
+            write = mine < 0 && t < c.T && blockIdx.z == 0 && c.y_in != c.y_out;
+            unsigned long long left = __ballot(id >= 0);
+            for (int ord = 0; left; ++ord) {
+                const int f = __ffsll(left) - 1, a = __builtin_amdgcn_readlane(id, f);
+                left &= ~__ballot(id == a);
+                if (ord % gridDim.z != blockIdx.z) continue;
+                todo |= 1ull << f;
+                write |= mine == a;
+            }
+            if (!__ballot(write)) return;
+            if (c.scale && mine >= 0) sc = c.scale[mine];
+        }
+        f32x4 out[CT];
+#pragma unroll
+        for (int q = 0; q < CT; ++q) out[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Frag bf[RB][CT];
+        auto fetch = [&](int a) {
 #pragma unroll
             for (int q = 0; q < CT; ++q) {
                 const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(c0 + lcol(q), c1 - 1)) * c.rank;
 #pragma unroll
                 for (int r = 0; r < RB; ++r) bf[r][q] = piece(B, (4 * r + g) * E, c.rank);
             }
-            Y y[NT][CT / JW][W];
+        };
+        unsigned long long left = todo;
+        int a = left ? __builtin_amdgcn_readlane(id, __ffsll(left) - 1) : -1;
+        if (a >= 0) fetch(a);
+        while (a >= 0) {
+            left &= left - 1;
+            const int next = left ? __builtin_amdgcn_readlane(id, __ffsll(left) - 1) : -1;
+            f32x4 acc[CT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (mine[j] == a) {
-                    const Y* yi = (const Y*)c.y_in + (size_t)(t0 + 16 * j + n) * c.ys;
+            for (int q = 0; q < CT; ++q) {
+                acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int q = 0; q < CT / JW; ++q) {
-                        const int k = c0 + col(q * JW);
-                        if (k + W <= c1) {
-                            __builtin_memcpy(y[j][q], yi + k, 16);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < W; ++i)
-                                if (k + i < c1) y[j][q][i] = yi[k + i];
-                        }
-                    }
-                }
-            if (have != seg) {
-                have = seg;
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    // (rows of other adapters may hold anything: their columns are not used)
-                    const float* hr = h + (size_t)min(t0 + 16 * j + n, c.T - 1) * R + seg * c.rank;
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        const int k = (4 * r + g) * E;
-                        float v[E];
-#pragma unroll
-                        for (int i = 0; i < E; ++i) v[i] = 0.f;
-                        if (k + E <= c.rank) {
-#pragma unroll 4
-                            for (int p = 0; p < planes; ++p) {
-                                float u[E];
-                                __builtin_memcpy(u, hr + (size_t)p * c.T * R + k, sizeof(u));
-#pragma unroll
-                                for (int i = 0; i < E; ++i) v[i] += u[i];
-                            }
-                        } else {
-                            for (int p = 0; p < planes; ++p)
-#pragma unroll
-                                for (int i = 0; i < E; ++i)
-                                    if (k + i < c.rank) v[i] += hr[(size_t)p * c.T * R + k + i];
-                        }
-                        if constexpr (LO) {
-#pragma unroll
-                            for (int i = 0; i < E; ++i) {
-                                hf[j][r][i] = (__bf16)v[i];
-                                lf[j][r][i] = (__bf16)(v[i] - (float)hf[j][r][i]);
-                            }
-                        } else {
-                            __builtin_memcpy(&hf[j][r], v, 16);
-                        }
-                    }
+                for (int r = 0; r < RB; ++r) {
+                    acc[q] = Mma<T>::run(bf[r][q], hv[r].hi, acc[q]);
+                    if constexpr (sizeof(T) == 2) acc[q] = Mma<T>::run(bf[r][q], hv[r].lo, acc[q]);
                 }
             }
-            f32x4 acc[CT][NT];
+            if (next >= 0) fetch(next);
 #pragma unroll
             for (int q = 0; q < CT; ++q)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int e = 0; e < 4; ++e) out[q][e] = mine == a ? acc[q][e] : out[q][e];
+            a = next;
+        }
+        if (write) {
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        acc[q][j] = Mma<T>::run(bf[r][q], hf[j][r], acc[q][j]);
-                        if constexpr (LO) acc[q][j] = Mma<T>::run(bf[r][q], lf[j][r], acc[q][j]);
+            for (int q = 0; q < CT / JW; ++q) {
+                const int k = c0 + col(q * JW);
+                if (mine >= 0)
+#pragma unroll
+                    for (int e = 0; e < W; ++e) put(&y[q][e], as_float(y[q][e]) + sc * out[q * JW + e / 4][e % 4]);
+                if (k + W <= c1) {
+                    __builtin_memcpy(yo + k, y[q], 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        if (k + e < c1) yo[k + e] = y[q][e];
+                }
+            }
+        }
+        if (++b == blocks(s)) {
+            b = 0;
+            if (++s == c.n_seg) return;
+        }
+    }
+}
+
+// Many rows: a workgroup takes kWideTile of them, a wave 16, and the adapter's
+// rows go through LDS once for all waves (each wave loading them by itself took
+// as long as x: 8192 rows of 8192, rank 64, 92 us against 46 without).
+// Row tiles of the workgroup that have no row of the adapter skip the products.
+constexpr int kWideWaves = 8, kWideTile = 16 * kWideWaves;
+
+// The adapters of the workgroup's rows, one at a time: the lowest that is above
+// `after`; -1: no more.  `ids`: the rows' adapters in LDS.
+__device__ __forceinline__ int next_id(const int* ids, int after, int lane) {
+    int best = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < kWideTile / 64; ++i) {
+        const int v = ids[64 * i + lane];
+        if (v > after) best = min(best, v);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) best = min(best, __shfl_xor(best, d, 64));
+    return best == 0x7fffffff ? -1 : best;
+}
+
+template <typename T, bool LO>
+__global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, float* h) {
+    typedef typename Mma<T>::Frag Frag;
+    constexpr int E = Mma<T>::kE, ST = 4, KC = 4 * E * ST, MT = 4;  // ST steps of the product a chunk
+    constexpr int P = KC + E;  // elements between the rows in LDS: 16 rows' pieces in different banks
+    __shared__ __align__(16) T as[2][16 * MT * P];
+    __shared__ int ids[kWideTile];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int t0 = blockIdx.x * kWideTile, R = c.n_seg * c.rank;
+    const int nch = (c.d_in + KC - 1) / KC;
+    const int ch0 = (int)((int64_t)nch * blockIdx.y / gridDim.y), ch1 = (int)((int64_t)nch * (blockIdx.y + 1) / gridDim.y);
+    for (int i = tid; i < kWideTile; i += 64 * kWideWaves) {
+        const int t = t0 + i, a = t < c.T ? c.ids[t] : -1;
+        ids[i] = a >= 0 && a < c.n_adapters ? a : -1;
+    }
+    __syncthreads();
+    const int t = t0 + 16 * w + n, mine = ids[16 * w + n];
+    const T* x = (const T*)c.x + (size_t)min(t, c.T - 1) * c.xs;
+    const T* xl = LO ? (const T*)c.x_lo + (size_t)min(t, c.T - 1) * c.xs : nullptr;
+    for (int a = -1; (a = next_id(ids, a, lane)) >= 0;) {
+        const bool part = __ballot(mine == a) != 0;
+        for (int r0 = 0; r0 < R; r0 += 16 * MT) {
+            const int rows = min(16 * MT, R - r0), mt = (rows + 15) / 16;
+            const T* A = (const T*)c.a + ((size_t)a * R + r0) * c.d_in;
+            // a chunk of A: 16 MT rows of ST * 4 pieces, two a thread
+            constexpr int PP = 16 * MT * ST * 4 / (64 * kWideWaves);
+            Frag st[PP];
+            auto fetch = [&](int ch) {
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {
+                    const int q = tid + 64 * kWideWaves * i, r = q / (ST * 4), k = ch * KC + (q % (ST * 4)) * E;
+                    st[i] = piece(A + (size_t)min(r, rows - 1) * c.d_in, k, c.d_in);
+                }
+            };
+            auto store = [&](int b) {
+#pragma unroll
+                for (int i = 0; i < PP; ++i) {
+                    const int q = tid + 64 * kWideWaves * i;
+                    *(Frag*)&as[b][(q / (ST * 4)) * P + (q % (ST * 4)) * E] = st[i];
+                }
+            };
+            Frag xf[ST], xlf[ST];
+            auto fetch_x = [&](int ch) {
+                if (!part) return;
+#pragma unroll
+                for (int e = 0; e < ST; ++e) {
+                    const int k = ch * KC + (ST * g + e) * E;
+                    xf[e] = piece(x, k, c.d_in);
+                    if (LO) xlf[e] = piece(xl, k, c.d_in);
+                }
+            };
+            f32x4 acc[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (ch0 < ch1) {
+                fetch(ch0);
+                fetch_x(ch0);
+                store(0);
+            }
+            __syncthreads();
+            for (int ch = ch0; ch < ch1; ++ch) {
+                const int b = (ch - ch0) & 1;
+                Frag xc[ST], xlc[ST];
+#pragma unroll
+                for (int e = 0; e < ST; ++e) {
+                    xc[e] = xf[e];
+                    if (LO) xlc[e] = xlf[e];
+                }
+                if (ch + 1 < ch1) {
+                    fetch(ch + 1);
+                    fetch_x(ch + 1);
+                }
+                if (part) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        if (m >= mt) break;
+#pragma unroll
+                        for (int e = 0; e < ST; ++e) {
+                            const Frag af = *(const Frag*)&as[b][(16 * m + n) * P + (ST * g + e) * E];
+                            acc[m] = Mma<T>::run(af, xc[e], acc[m]);
+                            if (LO) acc[m] = Mma<T>::run(af, xlc[e], acc[m]);
+                        }
                     }
                 }
+                if (ch + 1 < ch1) store(b ^ 1);
+                __syncthreads();
+            }
+            if (mine == a) {
+                float* o = h + ((size_t)blockIdx.y * c.T + t) * R + r0;
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (mine[j] == a) {
-                    Y* yo = (Y*)c.y_out + (size_t)(t0 + 16 * j + n) * c.yos;
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (16 * m + 4 * g + i < rows) o[16 * m + 4 * g + i] = acc[m][i];
+            }
+        }
+    }
+}
+
+// The planes of h added up, into the first; in bf16 as two bf16 planes, hi and
+// lo, in the place of the float that they make (about 16 of its bits).
+template <typename T>
+__global__ __launch_bounds__(256) void k_lora_join(float* h, size_t n, int planes) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < planes; ++p) v += h[p * n + i];
+    if constexpr (sizeof(T) == 2) {
+        const __bf16 hi = (__bf16)v, lo = (__bf16)(v - (float)hi);
+        ((uint32_t*)h)[i] = (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16 | __builtin_bit_cast(uint16_t, lo);
+    } else {
+        h[i] = v;
+    }
+}
+
+template <typename T, typename Y, int RB>
+__global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, const float* h, int per) {
+    typedef typename Mma<T>::Frag Frag;
+    constexpr int E = Mma<T>::kE, CT = 4;
+    constexpr int W = 16 / sizeof(Y), JW = W / 4;
+    constexpr bool LO = sizeof(T) == 2;
+    constexpr int P = 4 * RB * E + E;  // elements between the columns' rows of B in LDS
+    __shared__ __align__(16) T bs[2][16 * CT * P];
+    __shared__ int ids[kWideTile];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int t0 = blockIdx.x * kWideTile, R = c.n_seg * c.rank;
+    int blk = blockIdx.y * per, seg0 = 0;
+    auto blocks = [&](int s) { return (c.seg[s + 1] - c.seg[s] + 16 * CT - 1) / (16 * CT); };
+    while (seg0 < c.n_seg && blk >= blocks(seg0)) blk -= blocks(seg0++);
+    if (seg0 == c.n_seg) return;
+    for (int i = tid; i < kWideTile; i += 64 * kWideWaves) {
+        const int t = t0 + i, a = t < c.T ? c.ids[t] : -1;
+        ids[i] = a >= 0 && a < c.n_adapters ? a : -1;
+    }
+    __syncthreads();
+    const int t = t0 + 16 * w + n, mine = ids[16 * w + n];
+    const Y* yi = (const Y*)c.y_in + (size_t)min(t, c.T - 1) * c.ys;
+    Y* yo = (Y*)c.y_out + (size_t)min(t, c.T - 1) * c.yos;
+    auto col = [&](int q) { return (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
+    auto lcol = [&](int q) { return (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
+    // the next block of columns in place of (s, b); false: the wave's last, or the projection's
+    int left = per;
+    auto next_block = [&](int& s, int& b) {
+        if (--left <= 0) return false;
+        if (++b == blocks(s)) {
+            b = 0;
+            ++s;
+        }
+        return s < c.n_seg;
+    };
+    for (int a = -1; (a = next_id(ids, a, lane)) >= 0;) {
+        const bool part = __ballot(mine == a) != 0;
+        const float sc = c.scale ? c.scale[a] : 1.f;
+        Frag hf[RB], lf[RB];
+        // B of a block of columns: 16 CT rows of 4 RB pieces
+        constexpr int N = 16 * CT * 4 * RB, PP = (N + 64 * kWideWaves - 1) / (64 * kWideWaves);
+        Frag st[PP];
+        auto fetch = [&](int s, int b) {
+            const int c0 = c.seg[s] + b * 16 * CT, c1 = c.seg[s + 1];
+#pragma unroll
+            for (int i = 0; i < PP; ++i) {
+                const int q = tid + 64 * kWideWaves * i;
+                if (N % (64 * kWideWaves) && q >= N) break;
+                st[i] = piece((const T*)c.b + ((size_t)a * c.d_out + min(c0 + q / (4 * RB), c1 - 1)) * c.rank, (q % (4 * RB)) * E, c.rank);
+            }
+        };
+        auto store = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < PP; ++i) {
+                const int q = tid + 64 * kWideWaves * i;
+                if (N % (64 * kWideWaves) && q >= N) break;
+                *(Frag*)&bs[buf][(q / (4 * RB)) * P + (q % (4 * RB)) * E] = st[i];
+            }
+        };
+        Y y[CT / JW][W];
+        auto fetch_y = [&](int s, int b) {
+            if (mine != a) return;
+            const int c0 = c.seg[s] + b * 16 * CT, c1 = c.seg[s + 1];
+#pragma unroll
+            for (int q = 0; q < CT / JW; ++q) {
+                const int k = c0 + col(q * JW);
+                if (k + W <= c1) {
+                    __builtin_memcpy(y[q], yi + k, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        if (k + i < c1) y[q][i] = yi[k + i];
+                }
+            }
+        };
+        int s = seg0, b = blk, have = -1;
+        left = per;
+        fetch(s, b);
+        fetch_y(s, b);
+        store(0);
+        __syncthreads();
+        for (int buf = 0;; buf ^= 1) {
+            const int c0 = c.seg[s] + b * 16 * CT, c1 = c.seg[s + 1];
+            if (have != s && part) {
+                have = s;
+                const float* hr = h + (size_t)min(t, c.T - 1) * R + s * c.rank;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const int k = (4 * r + g) * E;
+                    uint32_t v[E];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) v[i] = 0;
+                    if (k + E <= c.rank) {
+                        __builtin_memcpy(v, hr + k, sizeof(v));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            if (k + i < c.rank) v[i] = __float_as_uint(hr[k + i]);
+                    }
+                    if constexpr (LO) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            hf[r][i] = __builtin_bit_cast(__bf16, (uint16_t)(v[i] >> 16));
+                            lf[r][i] = __builtin_bit_cast(__bf16, (uint16_t)v[i]);
+                        }
+                    } else {
+                        __builtin_memcpy(&hf[r], v, 16);
+                    }
+                }
+            }
+            Y yc[CT / JW][W];
+            __builtin_memcpy(yc, y, sizeof(y));
+            const bool more = next_block(s, b);
+            if (more) {
+                fetch(s, b);
+                fetch_y(s, b);
+            }
+            if (part) {
+                f32x4 acc[CT];
+#pragma unroll
+                for (int q = 0; q < CT; ++q) {
+                    acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const Frag bf = *(const Frag*)&bs[buf][lcol(q) * P + (4 * r + g) * E];
+                        acc[q] = Mma<T>::run(bf, hf[r], acc[q]);
+                        if constexpr (LO) acc[q] = Mma<T>::run(bf, lf[r], acc[q]);
+                    }
+                }
+                if (mine == a) {
 #pragma unroll
                     for (int q = 0; q < CT / JW; ++q) {
                         const int k = c0 + col(q * JW);
 #pragma unroll
                         for (int i = 0; i < W; ++i)
-                            put(&y[j][q][i], as_float(y[j][q][i]) + sc * acc[q * JW + i / 4][j][i % 4]);
+                            put(&yc[q][i], as_float(yc[q][i]) + sc * acc[q * JW + i / 4][i % 4]);
                         if (k + W <= c1) {
-                            __builtin_memcpy(yo + k, y[j][q], 16);
+                            __builtin_memcpy(yo + k, yc[q], 16);
                         } else {
 #pragma unroll
                             for (int i = 0; i < W; ++i)
-                                if (k + i < c1) yo[k + i] = y[j][q][i];
+                                if (k + i < c1) yo[k + i] = yc[q][i];
                         }
                     }
                 }
-        });
+            }
+            if (more) store(buf ^ 1);
+            __syncthreads();
+            if (!more) break;
+        }
     }
     // rows without an adapter
-    if (c.y_in == c.y_out || blockIdx.z) return;
-    each_block([&](int, int c0, int c1) {
+    if (c.y_in == c.y_out || t >= c.T || mine >= 0) return;
+    int s = seg0, b = blk;
+    left = per;
+    do {
+        const int c0 = c.seg[s] + b * 16 * CT, c1 = c.seg[s + 1];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int t = t0 + 16 * j + n;
-            if (t >= c.T || mine[j] >= 0) continue;
-            const Y* yi = (const Y*)c.y_in + (size_t)t * c.ys;
-            Y* yo = (Y*)c.y_out + (size_t)t * c.yos;
+        for (int q = 0; q < CT / JW; ++q) {
+            const int k = c0 + col(q * JW);
+            if (k + W <= c1) {
+                __builtin_memcpy(yo + k, yi + k, 16);
+            } else {
 #pragma unroll
-            for (int q = 0; q < CT / JW; ++q) {
-                const int k = c0 + col(q * JW);
-                if (k + W <= c1) {
-                    __builtin_memcpy(yo + k, yi + k, 16);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i)
-                        if (k + i < c1) yo[k + i] = yi[k + i];
-                }
+                for (int i = 0; i < W; ++i)
+                    if (k + i < c1) yo[k + i] = yi[k + i];
             }
         }
-    });
+    } while (next_block(s, b));
 }
 
 // Launch shapes.  Few rows: tiles of 16, up to kShare workgroups sharing out a
-// tile's adapters; many: tiles of 32.  Ranges of k: about kDownGroups workgroups
-// in all, a 128-byte piece a wave at least.
+// tile's adapters; many: tiles of kWideTile.  Ranges of k: about kDownGroups
+// workgroups in all, a 128-byte piece a wave (a chunk of 256 bytes) at least.
 constexpr int kWideRows = 2048;
-constexpr int kDownGroups = 512, kMaxPlanes = 16, kShare = 8;
+constexpr int kDownGroups = 512, kMaxPlanes = 8, kShare = 8;
 struct Shape {
-    int rows, waves, tiles, share, planes;
+    bool wide;
+    int tiles, share, planes;
 };
 Shape shape_of(int T, int d_in, int es, int n_adapters) {
     Shape s;
-    const bool wide = T >= kWideRows;
-    s.rows = wide ? 32 : 16;
-    s.waves = 8;
-    s.tiles = (T + s.rows - 1) / s.rows;
-    s.share = wide ? 1 : std::min(std::min(kShare, n_adapters), T);
-    const int pieces = (d_in * es + 127) / 128, groups = s.tiles * std::min(s.share, 4);
-    s.planes = std::max(1, std::min(std::min((kDownGroups + groups - 1) / groups, pieces / s.waves), kMaxPlanes));
+    s.wide = T >= kWideRows;
+    const int rows = s.wide ? kWideTile : 16;
+    s.tiles = (T + rows - 1) / rows;
+    s.share = s.wide ? 1 : std::min(std::min(kShare, n_adapters), T);
+    const int pieces = s.wide ? (d_in * es + 255) / 256 : (d_in * es + 127) / 128 / 8;
+    const int groups = s.tiles * s.share;
+    s.planes = std::max(1, std::min(std::min((kDownGroups + groups - 1) / groups, pieces), kMaxPlanes));
     return s;
 }
 
-template <typename T, int NT>
+template <typename T, bool LO>
 void launch_down(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     const dim3 g(sh.tiles, sh.planes, sh.share);
-    if constexpr (sizeof(T) == 2) {
-        if (c.x_lo) {
-            hipLaunchKernelGGL((k_lora_down<T, NT, 8, true>), g, dim3(512), 0, s, c, h);
-            return;
-        }
-    }
-    hipLaunchKernelGGL((k_lora_down<T, NT, 8, false>), g, dim3(512), 0, s, c, h);
+    if (sh.wide) hipLaunchKernelGGL((k_lora_down_wide<T, LO>), g, dim3(64 * kWideWaves), 0, s, c, h);
+    else hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h);
 }
-template <typename T, int NT, int RB>
-void launch_up(const LoraCall& c, const Shape& sh, const float* h, hipStream_t s) {
+template <typename T, int RB>
+void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     int blocks = 0;
     for (int i = 0; i < c.n_seg; ++i) blocks += (c.seg[i + 1] - c.seg[i] + 63) / 64;
-    // as many blocks a wave as leave about 16 waves a CU
-    const int per = std::max(1, (int)std::min<int64_t>((int64_t)blocks * sh.tiles / (16 * cu_count()), 16));
+    const int64_t units = (int64_t)blocks * sh.tiles;
+    if (sh.wide) {
+        const size_t n = (size_t)c.T * c.n_seg * c.rank;
+        hipLaunchKernelGGL(k_lora_join<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, h, n, sh.planes);
+        // as many blocks a workgroup as leave about four workgroups a CU
+        const int per = std::max(1, (int)std::min<int64_t>(units / (4 * cu_count()), 16));
+        const dim3 g(sh.tiles, (blocks + per - 1) / per);
+        if (c.y_bf16) hipLaunchKernelGGL((k_lora_up_wide<T, bf16_t, RB>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
+        else hipLaunchKernelGGL((k_lora_up_wide<T, float, RB>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
+        return;
+    }
+    // as many blocks a wave as leave about 16 waves a CU; with fewer than 8 a CU the
+    // adapters of a tile are shared out as well
+    const int per = std::max(1, (int)std::min<int64_t>(units / (16 * cu_count()), 16));
+    const int share = std::max(1, std::min(sh.share, (int)(8 * cu_count() / units)));
     const int waves = (blocks + per - 1) / per;
-    const dim3 g(sh.tiles, (waves + 3) / 4, sh.share);
-    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, NT, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
-    else hipLaunchKernelGGL((k_lora_up<T, float, NT, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
-}
-template <typename T, int NT>
-void launch_both(const LoraCall& c, const Shape& sh, hipStream_t s) {
-    float* h = (float*)c.ws;
-    launch_down<T, NT>(c, sh, h, s);
-    constexpr int K = 4 * Mma<T>::kE;  // a step of the product
-    if (c.rank <= 32) launch_up<T, NT, 32 / K>(c, sh, h, s);
-    else if (c.rank <= 64) launch_up<T, NT, 64 / K>(c, sh, h, s);
-    else launch_up<T, NT, 128 / K>(c, sh, h, s);
+    const dim3 g(sh.tiles, (waves + 3) / 4, share);
+    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
+    else hipLaunchKernelGGL((k_lora_up<T, float, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
 }
 template <typename T>
 void launch_typed(const LoraCall& c, hipStream_t s) {
     const Shape sh = shape_of(c.T, c.d_in, sizeof(T), c.n_adapters);
-    if (sh.rows == 16) launch_both<T, 1>(c, sh, s);
-    else launch_both<T, 2>(c, sh, s);
+    float* h = (float*)c.ws;
+    if constexpr (sizeof(T) == 2) {
+        if (c.x_lo) launch_down<T, true>(c, sh, h, s);
+        else launch_down<T, false>(c, sh, h, s);
+    } else {
+        launch_down<T, false>(c, sh, h, s);
+    }
+    constexpr int K = 4 * Mma<T>::kE;  // a step of the product
+    if (c.rank <= 32) launch_up<T, 32 / K>(c, sh, h, s);
+    else if (c.rank <= 64) launch_up<T, 64 / K>(c, sh, h, s);
+    else launch_up<T, 128 / K>(c, sh, h, s);
 }
 
 }  // namespace
 
 // (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
 size_t lora_workspace(int T, int rank, int n_seg) {
-    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)32 * (kDownGroups + (T + 15) / 16));
+    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)kWideTile * (kDownGroups + (T + 15) / 16));
     return (rows * rank * n_seg * 4 + 255) & ~(size_t)255;
 }
 
