@@ -39,21 +39,29 @@ template <> struct Mma<float> {
 };
 
 // 16 bytes of a row from element k on, zeros from n on (any alignment: the
-// hardware takes 16-byte loads at every address)
-template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n) {
+// hardware takes 16-byte loads at every address).  WHOLE: rows are whole pieces,
+// and lanes past the end read the row's start and drop it (a branch for them
+// would wait for the loads of the others, one piece after the other); what they
+// read is dropped by `inside` where it is used, so that nothing waits before.
+template <bool WHOLE, typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n) {
     constexpr int E = Mma<T>::kE;
     typename Mma<T>::Frag f;
-    if (k + E <= n) {
-        __builtin_memcpy(&f, row + k, 16);
+    if constexpr (WHOLE) {
+        __builtin_memcpy(&f, row + (k < n ? k : 0), 16);
     } else {
         T v[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            v[i] = 0;
-            if (k + i < n) v[i] = row[k + i];
+            const T x = row[k + i < n ? k + i : 0];
+            v[i] = k + i < n ? x : (T)0;
         }
         __builtin_memcpy(&f, v, 16);
     }
+    return f;
+}
+template <typename F> __device__ __forceinline__ F inside(F f, bool in) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(F) / sizeof(f[0])); ++i) f[i] = in ? f[i] : 0;
     return f;
 }
 template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k) {
@@ -84,7 +92,7 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, KB = 8 * E, MT = 4;
     __shared__ f32x4 part[NW][MT][64];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int t0 = blockIdx.x * 16, R = c.n_seg * c.rank;
     const int nkb = (c.d_in + KB - 1) / KB, full = c.d_in / KB;
     const int kb0 = (int)((int64_t)nkb * blockIdx.y / gridDim.y), kb1 = (int)((int64_t)nkb * (blockIdx.y + 1) / gridDim.y);
@@ -128,7 +136,7 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
 #pragma unroll 2
             for (; kb < end; kb += NW) step(kb * KB + 2 * E * g, [](const T* p, int k) { return piece(p, k); });
             if (kb < kb1)  // the row's last, incomplete piece
-                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return piece(p, k, c.d_in); });
+                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return piece<false>(p, k, c.d_in); });
 #pragma unroll
             for (int m = 0; m < MT; ++m)
                 if (m < mt) part[w][m][lane] = acc[m];
@@ -140,9 +148,13 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
                 const int r = r0 + 16 * w + 4 * g;
                 if (mine == a) {
                     float* o = h + ((size_t)blockIdx.y * c.T + t0 + n) * R + r;
+                    if (r + 4 <= R) {
+                        __builtin_memcpy(o, &s, 16);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (r + i < R) o[i] = s[i];
+                        for (int i = 0; i < 4; ++i)
+                            if (r + i < R) o[i] = s[i];
+                    }
                 }
             }
             __syncthreads();
@@ -156,26 +168,29 @@ template <typename T> struct Inner {
     typedef typename Mma<T>::Frag Frag;
     Frag hi, lo;
 };
-template <typename T>
+template <bool WHOLE, typename T>
 __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank, size_t stride, int planes) {
     constexpr int E = Mma<T>::kE;
     float v[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = 0.f;
-    if (k + E <= rank) {
+    if constexpr (WHOLE) {
+        const float* from = hr + (k < rank ? k : 0);
 #pragma unroll 8
         for (int p = 0; p < planes; ++p) {
             float u[E];
-            __builtin_memcpy(u, hr + p * stride + k, sizeof(u));
+            __builtin_memcpy(u, from + p * stride, sizeof(u));
 #pragma unroll
             for (int i = 0; i < E; ++i) v[i] += u[i];
         }
     } else {
+#pragma unroll 2
         for (int p = 0; p < planes; ++p)
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (k + i < rank) v[i] += hr[p * stride + k + i];
+            for (int i = 0; i < E; ++i) v[i] += hr[p * stride + (k + i < rank ? k + i : 0)];
     }
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = k + i < rank ? v[i] : 0.f;
     Inner<T> r;
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -193,12 +208,12 @@ __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank
 // and every gridDim.z-th of the rows' adapters.  A row's h, y and scale do not
 // wait for the adapters: they are requested first, and each adapter's B while the
 // one before is multiplied.  RB: steps of the product that hold the rank.
-template <typename T, typename Y, int RB>
+template <typename T, typename Y, int RB, bool WHOLE>
 __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes, int per) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, CT = 4;
     constexpr int W = 16 / sizeof(Y), JW = W / 4;  // columns of a lane next to each other: from JW tiles
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int t0 = blockIdx.x * 16, t = t0 + n, R = c.n_seg * c.rank;
     // the wave's first block of columns: segments are cut apart
     int b = (blockIdx.y * 4 + w) * per, s = 0;
@@ -225,7 +240,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
             have = s;
 #pragma unroll
             for (int r = 0; r < RB; ++r)
-                hv[r] = inner_piece<T>(h + row * R + s * c.rank, (4 * r + g) * E, c.rank, (size_t)c.T * R, planes);
+                hv[r] = inner_piece<WHOLE, T>(h + row * R + s * c.rank, (4 * r + g) * E, c.rank, (size_t)c.T * R, planes);
         }
 #pragma unroll
         for (int q = 0; q < CT / JW; ++q) {
@@ -260,7 +275,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
             for (int q = 0; q < CT; ++q) {
                 const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(c0 + lcol(q), c1 - 1)) * c.rank;
 #pragma unroll
-                for (int r = 0; r < RB; ++r) bf[r][q] = piece(B, (4 * r + g) * E, c.rank);
+                for (int r = 0; r < RB; ++r) bf[r][q] = piece<WHOLE>(B, (4 * r + g) * E, c.rank);
             }
         };
         unsigned long long left = todo;
@@ -275,8 +290,9 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
                 acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    acc[q] = Mma<T>::run(bf[r][q], hv[r].hi, acc[q]);
-                    if constexpr (sizeof(T) == 2) acc[q] = Mma<T>::run(bf[r][q], hv[r].lo, acc[q]);
+                    const Frag f = WHOLE ? inside(bf[r][q], (4 * r + g) * E < c.rank) : bf[r][q];
+                    acc[q] = Mma<T>::run(f, hv[r].hi, acc[q]);
+                    if constexpr (sizeof(T) == 2) acc[q] = Mma<T>::run(f, hv[r].lo, acc[q]);
                 }
             }
             if (next >= 0) fetch(next);
@@ -336,7 +352,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
     constexpr int P = KC + E;  // elements between the rows in LDS: 16 rows' pieces in different banks
     __shared__ __align__(16) T as[2][16 * MT * P];
     __shared__ int ids[kWideTile];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int t0 = blockIdx.x * kWideTile, R = c.n_seg * c.rank;
     const int nch = (c.d_in + KC - 1) / KC;
     const int ch0 = (int)((int64_t)nch * blockIdx.y / gridDim.y), ch1 = (int)((int64_t)nch * (blockIdx.y + 1) / gridDim.y);
@@ -356,12 +372,23 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
             // a chunk of A: 16 MT rows of ST * 4 pieces, two a thread
             constexpr int PP = 16 * MT * ST * 4 / (64 * kWideWaves);
             Frag st[PP];
-            auto fetch = [&](int ch) {
+            Frag xf[ST], xlf[ST];
+            auto load = [&](int ch, auto get) {
 #pragma unroll
                 for (int i = 0; i < PP; ++i) {
-                    const int q = tid + 64 * kWideWaves * i, r = q / (ST * 4), k = ch * KC + (q % (ST * 4)) * E;
-                    st[i] = piece(A + (size_t)min(r, rows - 1) * c.d_in, k, c.d_in);
+                    const int q = tid + 64 * kWideWaves * i, r = q / (ST * 4);
+                    st[i] = get(A + (size_t)min(r, rows - 1) * c.d_in, ch * KC + (q % (ST * 4)) * E);
                 }
+                if (!part) return;
+#pragma unroll
+                for (int e = 0; e < ST; ++e) {
+                    xf[e] = get(x, ch * KC + (ST * g + e) * E);
+                    if (LO) xlf[e] = get(xl, ch * KC + (ST * g + e) * E);
+                }
+            };
+            auto fetch = [&](int ch) {
+                if ((ch + 1) * KC <= c.d_in) load(ch, [](const T* p, int k) { return piece(p, k); });
+                else load(ch, [&](const T* p, int k) { return piece<false>(p, k, c.d_in); });
             };
             auto store = [&](int b) {
 #pragma unroll
@@ -370,22 +397,16 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
                     *(Frag*)&as[b][(q / (ST * 4)) * P + (q % (ST * 4)) * E] = st[i];
                 }
             };
-            Frag xf[ST], xlf[ST];
-            auto fetch_x = [&](int ch) {
-                if (!part) return;
-#pragma unroll
-                for (int e = 0; e < ST; ++e) {
-                    const int k = ch * KC + (ST * g + e) * E;
-                    xf[e] = piece(x, k, c.d_in);
-                    if (LO) xlf[e] = piece(xl, k, c.d_in);
-                }
-            };
             f32x4 acc[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // (tiles begin at different chunks: rows are often a power of two apart, and
+            // everyone reading the same columns at once meets in few memory channels,
+            // 62 against 50 us for 8192 rows of 8192)
+            const int cn = ch1 - ch0, turn = cn > 0 ? (int)(blockIdx.x % cn) : 0;
+            auto at = [&](int ch) { return ch + turn < ch1 ? ch + turn : ch + turn - cn; };
             if (ch0 < ch1) {
-                fetch(ch0);
-                fetch_x(ch0);
+                fetch(at(ch0));
                 store(0);
             }
             __syncthreads();
@@ -397,10 +418,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
                     xc[e] = xf[e];
                     if (LO) xlc[e] = xlf[e];
                 }
-                if (ch + 1 < ch1) {
-                    fetch(ch + 1);
-                    fetch_x(ch + 1);
-                }
+                if (ch + 1 < ch1) fetch(at(ch + 1));
                 if (part) {
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
@@ -419,10 +437,16 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
             if (mine == a) {
                 float* o = h + ((size_t)blockIdx.y * c.T + t) * R + r0;
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int m = 0; m < MT; ++m) {
+                    const int r = 16 * m + 4 * g;
+                    if (r + 4 <= rows) {
+                        __builtin_memcpy(o + r, &acc[m], 16);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (16 * m + 4 * g + i < rows) o[16 * m + 4 * g + i] = acc[m][i];
+                        for (int i = 0; i < 4; ++i)
+                            if (r + i < rows) o[r + i] = acc[m][i];
+                    }
+                }
             }
         }
     }
@@ -445,7 +469,7 @@ __global__ __launch_bounds__(256) void k_lora_join(float* h, size_t n, int plane
     }
 }
 
-template <typename T, typename Y, int RB>
+template <typename T, typename Y, int RB, bool WHOLE>
 __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, const float* h, int per) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, CT = 4;
@@ -454,7 +478,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
     constexpr int P = 4 * RB * E + E;  // elements between the columns' rows of B in LDS
     __shared__ __align__(16) T bs[2][16 * CT * P];
     __shared__ int ids[kWideTile];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int t0 = blockIdx.x * kWideTile, R = c.n_seg * c.rank;
     int blk = blockIdx.y * per, seg0 = 0;
     auto blocks = [&](int s) { return (c.seg[s + 1] - c.seg[s] + 16 * CT - 1) / (16 * CT); };
@@ -493,7 +517,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
             for (int i = 0; i < PP; ++i) {
                 const int q = tid + 64 * kWideWaves * i;
                 if (N % (64 * kWideWaves) && q >= N) break;
-                st[i] = piece((const T*)c.b + ((size_t)a * c.d_out + min(c0 + q / (4 * RB), c1 - 1)) * c.rank, (q % (4 * RB)) * E, c.rank);
+                st[i] = piece<WHOLE>((const T*)c.b + ((size_t)a * c.d_out + min(c0 + q / (4 * RB), c1 - 1)) * c.rank, (q % (4 * RB)) * E, c.rank);
             }
         };
         auto store = [&](int buf) {
@@ -501,7 +525,8 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
             for (int i = 0; i < PP; ++i) {
                 const int q = tid + 64 * kWideWaves * i;
                 if (N % (64 * kWideWaves) && q >= N) break;
-                *(Frag*)&bs[buf][(q / (4 * RB)) * P + (q % (4 * RB)) * E] = st[i];
+                *(Frag*)&bs[buf][(q / (4 * RB)) * P + (q % (4 * RB)) * E] =
+                    WHOLE ? inside(st[i], (q % (4 * RB)) * E < c.rank) : st[i];
             }
         };
         Y y[CT / JW][W];
@@ -617,10 +642,13 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
 }
 
 // Launch shapes.  Few rows: tiles of 16, up to kShare workgroups sharing out a
-// tile's adapters; many: tiles of kWideTile.  Ranges of k: about kDownGroups
-// workgroups in all, a 128-byte piece a wave (a chunk of 256 bytes) at least.
+// tile's adapters; many: tiles of kWideTile.  Ranges of k: about kGroups
+// (kWideGroups) workgroups in all, a 128-byte piece a wave (a chunk of 256
+// bytes) at least.  More ranges make the first product shorter and the second
+// longer, which adds them up (229 rows qkv 32B, 512 / 1024 groups: 13.3 + 10.9 /
+// 10.7 + 11.7 us; 8192 rows, 256 / 512 groups: 53 + 5 / 45 + 5.6 us).
 constexpr int kWideRows = 2048;
-constexpr int kDownGroups = 512, kMaxPlanes = 8, kShare = 8;
+constexpr int kGroups = 1024, kWideGroups = 512, kMaxPlanes = 8, kShare = 8;
 struct Shape {
     bool wide;
     int tiles, share, planes;
@@ -632,18 +660,18 @@ Shape shape_of(int T, int d_in, int es, int n_adapters) {
     s.tiles = (T + rows - 1) / rows;
     s.share = s.wide ? 1 : std::min(std::min(kShare, n_adapters), T);
     const int pieces = s.wide ? (d_in * es + 255) / 256 : (d_in * es + 127) / 128 / 8;
-    const int groups = s.tiles * s.share;
-    s.planes = std::max(1, std::min(std::min((kDownGroups + groups - 1) / groups, pieces), kMaxPlanes));
+    const int groups = s.tiles * s.share, want = s.wide ? kWideGroups : kGroups;
+    s.planes = std::max(1, std::min(std::min((want + groups - 1) / groups, pieces), kMaxPlanes));
     return s;
 }
 
 template <typename T, bool LO>
 void launch_down(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
-    const dim3 g(sh.tiles, sh.planes, sh.share);
-    if (sh.wide) hipLaunchKernelGGL((k_lora_down_wide<T, LO>), g, dim3(64 * kWideWaves), 0, s, c, h);
+    const dim3 g(sh.tiles, sh.planes, sh.share), wide(64 * kWideWaves);
+    if (sh.wide) hipLaunchKernelGGL((k_lora_down_wide<T, LO>), g, wide, 0, s, c, h);
     else hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h);
 }
-template <typename T, int RB>
+template <typename T, typename Y, int RB, bool WHOLE>
 void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     int blocks = 0;
     for (int i = 0; i < c.n_seg; ++i) blocks += (c.seg[i + 1] - c.seg[i] + 63) / 64;
@@ -654,8 +682,7 @@ void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
         // as many blocks a workgroup as leave about four workgroups a CU
         const int per = std::max(1, (int)std::min<int64_t>(units / (4 * cu_count()), 16));
         const dim3 g(sh.tiles, (blocks + per - 1) / per);
-        if (c.y_bf16) hipLaunchKernelGGL((k_lora_up_wide<T, bf16_t, RB>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
-        else hipLaunchKernelGGL((k_lora_up_wide<T, float, RB>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
+        hipLaunchKernelGGL((k_lora_up_wide<T, Y, RB, WHOLE>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
         return;
     }
     // as many blocks a wave as leave about 16 waves a CU; with fewer than 8 a CU the
@@ -664,8 +691,15 @@ void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     const int share = std::max(1, std::min(sh.share, (int)(8 * cu_count() / units)));
     const int waves = (blocks + per - 1) / per;
     const dim3 g(sh.tiles, (waves + 3) / 4, share);
-    if (c.y_bf16) hipLaunchKernelGGL((k_lora_up<T, bf16_t, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
-    else hipLaunchKernelGGL((k_lora_up<T, float, RB>), g, dim3(256), 0, s, c, h, sh.planes, per);
+    hipLaunchKernelGGL((k_lora_up<T, Y, RB, WHOLE>), g, dim3(256), 0, s, c, h, sh.planes, per);
+}
+template <typename T, typename Y>
+void launch_up_rank(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
+    constexpr int K = 4 * Mma<T>::kE;  // a step of the product
+    if (c.rank % Mma<T>::kE) launch_up<T, Y, 128 / K, false>(c, sh, h, s);
+    else if (c.rank <= 32) launch_up<T, Y, 32 / K, true>(c, sh, h, s);
+    else if (c.rank <= 64) launch_up<T, Y, 64 / K, true>(c, sh, h, s);
+    else launch_up<T, Y, 128 / K, true>(c, sh, h, s);
 }
 template <typename T>
 void launch_typed(const LoraCall& c, hipStream_t s) {
@@ -677,17 +711,15 @@ void launch_typed(const LoraCall& c, hipStream_t s) {
     } else {
         launch_down<T, false>(c, sh, h, s);
     }
-    constexpr int K = 4 * Mma<T>::kE;  // a step of the product
-    if (c.rank <= 32) launch_up<T, 32 / K>(c, sh, h, s);
-    else if (c.rank <= 64) launch_up<T, 64 / K>(c, sh, h, s);
-    else launch_up<T, 128 / K>(c, sh, h, s);
+    if (c.y_bf16) launch_up_rank<T, bf16_t>(c, sh, h, s);
+    else launch_up_rank<T, float>(c, sh, h, s);
 }
 
 }  // namespace
 
 // (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
 size_t lora_workspace(int T, int rank, int n_seg) {
-    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)kWideTile * (kDownGroups + (T + 15) / 16));
+    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
     return (rows * rank * n_seg * 4 + 255) & ~(size_t)255;
 }
 
