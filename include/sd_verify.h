@@ -531,6 +531,50 @@ sd_status sd_lora_apply(const sd_lora* w, int32_t n_rows, const int32_t* adapter
                         int64_t x_stride, const void* y_in, int64_t y_in_stride, void* y_out, int64_t y_out_stride,
                         int32_t y_dtype, void* workspace, uint64_t workspace_bytes, sd_stream stream);
 
+/*
+ * The same for the users of a context's batches.
+ *
+ * sd_user_sampling: user `user`'s sampling options from the next
+ * sd_verify_batch, sd_verify_batch_graph, sd_verify_batch_sparse,
+ * sd_sample_logits or sd_draft_batch on (host values, as in sd_filter;
+ * temperature 0: the largest logit alone; top_k 0, top_p 1, min_p 0: off).  A
+ * new user has 1, 0, 1, 0.  In a SD_STOCHASTIC pass with such a user every
+ * slot's logits are replaced by their filtered rows (sd_filter_logits)
+ * before accept/resample: the user's drafts are verified against, and its
+ * tokens drawn from, the filtered distribution, which sd_draft_batch's probs
+ * and sd_debug_logits then show.  SD_GREEDY and SD_FORCE passes, whose
+ * tokens the filters never drop, take no notice.  The options stay over
+ * sd_user_reset and end with sd_user_release.
+ * SD_EINVAL: user or an option out of range (temperature finite and >= 0,
+ * top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1); SD_ESTATE: user pending.
+ */
+sd_status sd_user_sampling(sd_ctx* ctx, int32_t user, float temperature, int32_t top_k, float top_p, float min_p);
+
+/*
+ * sd_adapters_set: n_adapters adapters for every layer's projections (host
+ * array of n_layers entries, copied; a NULL sd_lora.a leaves that projection
+ * without), in the context's dtype: qkv beside the fused q, k and v
+ * projection (d_in = d_model, d_out = (n_q_heads + 2 n_kv_heads) * head_dim
+ * columns in that order), o beside the output projection (d_in =
+ * n_q_heads * head_dim, d_out = d_model), down beside the down projection
+ * (d_in = d_ffn, d_out = d_model).  The matrices are read in place until the
+ * next call or sd_verify_destroy.  0 and NULL take them away.  Every user is
+ * without adapter afterwards.
+ * SD_EINVAL: an adapter does not fit (SD_ELIMIT: rank or segments beyond
+ * sd_lora's); SD_ESTATE: a batch is pending.
+ *
+ * sd_user_adapter: user `user`'s slots of the batches that follow take
+ * adapter `adapter` (-1: none) in every pass, cached keys and values as
+ * they then come out included.  Passes without such a user are what they
+ * were.  Stays over sd_user_reset, ends with sd_user_release.
+ * SD_EINVAL: user or adapter out of range; SD_ESTATE: user pending.
+ */
+typedef struct sd_layer_adapters {
+    sd_lora qkv, o, down;
+} sd_layer_adapters;
+sd_status sd_adapters_set(sd_ctx* ctx, int32_t n_adapters, const sd_layer_adapters* layers);
+sd_status sd_user_adapter(sd_ctx* ctx, int32_t user, int32_t adapter);
+
 /* Kernel classes for sd_profile_begin. */
 enum {
     SD_K_QKV = 1,      /* QKV projection GEMM + fused QK-norm/RoPE/KV append */

@@ -36,10 +36,11 @@ int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 struct Layout {
     // staging block (int32 offsets within the block)
     size_t st_user, st_prefix, st_L, st_root, st_soff, st_doff, st_sb, st_sj, st_pt, st_items,
-        st_ioff, st_flags, st_prow, st_bytes;
+        st_ioff, st_flags, st_prow, st_temp, st_topk, st_topp, st_minp, st_adapter, st_bytes;
     // slot buffers (byte offsets within the slot)
     size_t stage, tok, cs, x, ssq, h, ffn, qbuf, attn, apart, aml, gpart, logits, sstat, spart,
-        spartB, lstat, zd, dnext, skcnt, result, slot_bytes;
+        spartB, lstat, zd, dnext, skcnt, result, filter, lora, slot_bytes;
+    size_t filter_bytes, lora_bytes;
     size_t gpart_floats;
     int nsq;
     // global region after the slots
@@ -125,6 +126,12 @@ Layout plan(const sd_config& c) {
     L.st_ioff = take_i(L.Bmax + 1);
     L.st_flags = take_i(4);
     L.st_prow = take_i(L.Bmax);
+    // per slot: its user's sampling options and adapter
+    L.st_temp = take_i(L.Tmax);
+    L.st_topk = take_i(L.Tmax);
+    L.st_topp = take_i(L.Tmax);
+    L.st_minp = take_i(L.Tmax);
+    L.st_adapter = take_i(L.Tmax);
     L.st_bytes = o;
     // slot
     size_t s = 0;
@@ -157,6 +164,10 @@ Layout plan(const sd_config& c) {
     L.dnext = take((size_t)L.Tmax * 4);
     L.skcnt = take((size_t)kSkCounters * 4);
     L.result = take((size_t)(2 * L.Bmax + 4) * 4);
+    L.filter_bytes = filter_workspace(L.Tmax, D.V);
+    L.filter = take(L.filter_bytes);
+    L.lora_bytes = lora_workspace(L.Tmax, kLoraRank, kLoraSegs);
+    L.lora = take(L.lora_bytes);
     L.slot_bytes = s;
     L.total = align_up(L.slot_bytes * (size_t)c.max_pending);
     return L;
@@ -186,6 +197,11 @@ struct User {
     int root = 0;
     std::vector<int> pages;
     int pending_slot = -1;
+    // sampling options (sd_user_sampling) and adapter (sd_user_adapter)
+    float temperature = 1.f, top_p = 1.f, min_p = 0.f;
+    int top_k = 0;
+    int adapter = -1;
+    bool filtered() const { return temperature != 1.f || top_k != 0 || top_p != 1.f || min_p != 0.f; }
 };
 
 struct Slot {
@@ -197,6 +213,8 @@ struct Slot {
     std::vector<int> users;  // global ids in batch order
     std::vector<int> L;
     std::vector<int> prow;   // decode steps: destination row of each user's probabilities
+    bool filtered = false;   // some user of a stochastic pass has sampling options
+    bool adapted = false;    // some user of the pass has an adapter
     hipEvent_t done = nullptr;
     char* stage_host = nullptr;  // pinned
     int32_t* result_host = nullptr;  // pinned
@@ -226,6 +244,9 @@ struct sd_ctx {
     int device = 0;
     int attn_cap = 512;  // attention work items that run in one wave of workgroups
     int sk_polls = kSkPollsDefault;  // bound of the stream-K waits
+    std::vector<sd_layer_adapters> adapters;  // [n_layers], or empty
+    int n_adapters = 0;
+    int64_t adapters_set = 0;  // counts sd_adapters_set calls (graph signatures)
     // diagnostic timing of one kernel class
     int prof_class = 0;
     int prof_used = 0;
@@ -411,8 +432,14 @@ void build_stage(sd_ctx* c, Slot& s, int mode, bool with_items, int* n_items, in
         soff[b + 1] = soff[b] + s.L[b] + 1;
         doff[b + 1] = doff[b] + s.L[b];
         for (int j = 0; j <= s.L[b]; ++j) {
-            sb[soff[b] + j] = b;
-            sj[soff[b] + j] = j;
+            const int t = soff[b] + j;
+            sb[t] = b;
+            sj[t] = j;
+            ((float*)(st + L.st_temp))[t] = u.temperature;
+            ((int32_t*)(st + L.st_topk))[t] = u.top_k;
+            ((float*)(st + L.st_topp))[t] = u.top_p;
+            ((float*)(st + L.st_minp))[t] = u.min_p;
+            ((int32_t*)(st + L.st_adapter))[t] = u.adapter;
         }
         for (int i = 0; i < L.max_pages; ++i)
             pt[(size_t)b * L.max_pages + i] = i < (int)u.pages.size() ? u.pages[i] : 0;
@@ -496,6 +523,31 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
         else
             launch_resid_norm(D, T, sb.gpart, S, sb.x, gamma, sb.h, st);
     };
+    // the users' adapters beside one projection: y += scale B (A x), x the
+    // projection's input (planes T * d_in apart) and y what its sums are in
+    auto adapters = [&](const sd_lora& w, const void* x, float* y) {
+        if (!w.a) return;
+        LoraCall a{};
+        a.T = T;
+        a.d_in = w.d_in;
+        a.d_out = w.d_out;
+        a.rank = w.rank;
+        a.n_seg = w.n_seg;
+        a.n_adapters = w.n_adapters;
+        for (int i = 0; i <= kLoraSegs; ++i) a.seg[i] = w.seg_off[std::min(i, w.n_seg)];
+        a.bf16 = D.bf16;
+        a.a = w.a;
+        a.b = w.b;
+        a.scale = w.scale;
+        a.ids = (const int32_t*)(s.base + c->lay.stage + c->lay.st_adapter);
+        a.x = x;
+        a.x_lo = D.bf16 ? (const char*)x + (size_t)T * w.d_in * 2 : nullptr;
+        a.xs = w.d_in;
+        a.y_in = a.y_out = y;
+        a.ys = a.yos = w.d_out;
+        a.ws = s.base + c->lay.lora;
+        launch_lora(a, st);
+    };
     for (int l = 0; l < D.L; ++l) {
         const sd_layer_weights& w = c->layers[l];
         const size_t lbase = (size_t)l * c->pl.layer * 2;
@@ -517,6 +569,9 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
             g.sk_cnt = sb.skcnt;
             g.sk_polls = c->sk_polls;
             const int S = launch_gemm(D, g, sb, st);
+            // (into the first plane of the raw sums: the row factor of the norm, which
+            // the finish applies, then covers the adapter's part too)
+            if (s.adapted) adapters(c->adapters[l].qkv, sb.h, sb.gpart);
             launch_qkv_finish(D, bv, sb, c->kv, l, sb.gpart, S, nnb, w.qnorm, w.knorm, st);
         }
         {
@@ -526,6 +581,7 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
         {
             // output projection, then residual add fused with the pre-FFN norm
             ProfScope ps(c, SD_K_O, st);
+            if (s.adapted) adapters(c->adapters[l].o, sb.attn, sb.x);
             GemmCall o{};
             o.X = sb.attn;
             o.Wp = c->wpack + lbase + c->pl.o * 2;
@@ -565,6 +621,7 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
             // down projection, then residual add fused with the next norm
             // (next layer's pre-attention gain, or the final norm)
             ProfScope ps(c, SD_K_DOWN, st);
+            if (s.adapted) adapters(c->adapters[l].down, sb.ffn, sb.x);
             GemmCall dn{};
             dn.X = sb.ffn;
             dn.Wp = c->wpack + lbase + c->pl.down * 2;
@@ -849,9 +906,62 @@ sd_status sd_user_release(sd_ctx* c, int32_t user) {
     User& u = c->users[user];
     if (u.pending_slot >= 0) return SD_ESTATE;
     release_to(c, u, 0);
-    u.active = false;
-    u.prefix = 0;
-    u.root = 0;
+    u = User{};
+    return SD_OK;
+}
+
+sd_status sd_user_sampling(sd_ctx* c, int32_t user, float temperature, int32_t top_k, float top_p, float min_p) {
+    if (!c || user < 0 || user >= c->cfg.max_users) return SD_EINVAL;
+    if (!(temperature >= 0.f) || !std::isfinite(temperature) || top_k < 0 || !(top_p > 0.f && top_p <= 1.f) ||
+        !(min_p >= 0.f && min_p <= 1.f))
+        return SD_EINVAL;
+    User& u = c->users[user];
+    if (u.pending_slot >= 0) return SD_ESTATE;
+    u.temperature = temperature;
+    u.top_k = top_k;
+    u.top_p = top_p;
+    u.min_p = min_p;
+    return SD_OK;
+}
+
+sd_status sd_adapters_set(sd_ctx* c, int32_t n_adapters, const sd_layer_adapters* layers) {
+    if (!c || n_adapters < 0 || (n_adapters > 0) != (layers != nullptr)) return SD_EINVAL;
+    for (const User& u : c->users)
+        if (u.pending_slot >= 0) return SD_ESTATE;
+    const Dims& D = c->D;
+    for (int l = 0; l < D.L && n_adapters; ++l) {
+        const sd_lora* w[3] = {&layers[l].qkv, &layers[l].o, &layers[l].down};
+        const int in[3] = {D.d, D.nq(), D.F}, out[3] = {D.nqkv(), D.d, D.d};
+        for (int i = 0; i < 3; ++i) {
+            if (!w[i]->a) continue;
+            uint64_t bytes = 0;
+            const sd_status r = sd_lora_query_size(w[i], c->lay.Tmax, &bytes);
+            if (r != SD_OK) return r;
+            const uintptr_t es = c->cfg.dtype == SD_BF16 ? 2 : 4;
+            if (!w[i]->b || w[i]->n_adapters != n_adapters || w[i]->d_in != in[i] || w[i]->d_out != out[i] ||
+                w[i]->dtype != c->cfg.dtype || ((uintptr_t)w[i]->a | (uintptr_t)w[i]->b) % es ||
+                (uintptr_t)w[i]->scale % 4 || bytes > c->lay.lora_bytes)
+                return SD_EINVAL;
+        }
+    }
+    std::vector<sd_layer_adapters> next;
+    try {
+        if (n_adapters) next.assign(layers, layers + D.L);
+    } catch (const std::bad_alloc&) {
+        return SD_ENOMEM;
+    }
+    c->adapters.swap(next);
+    c->n_adapters = n_adapters;
+    ++c->adapters_set;
+    for (User& u : c->users) u.adapter = -1;
+    return SD_OK;
+}
+
+sd_status sd_user_adapter(sd_ctx* c, int32_t user, int32_t adapter) {
+    if (!c || user < 0 || user >= c->cfg.max_users || adapter < -1 || adapter >= c->n_adapters) return SD_EINVAL;
+    User& u = c->users[user];
+    if (u.pending_slot >= 0) return SD_ESTATE;
+    u.adapter = adapter;
     return SD_OK;
 }
 
@@ -921,16 +1031,38 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
                               hipStream_t st, float* probs = nullptr) {
     sd_status rs = hip_status(hipMemcpyAsync(s.base + c->lay.stage, s.stage_host, c->lay.st_bytes,
                                              hipMemcpyHostToDevice, st));
+    // users with sampling options: every slot's row of logits is filtered (into the
+    // slot's own rows), and the sampler takes its statistics from there
+    auto filter = [&](const float* from) {
+        const char* stage = s.base + c->lay.stage;
+        FilterCall f{};
+        f.n_rows = bv.T;
+        f.V = c->D.V;
+        f.logits = from;
+        f.stride = f.ostride = c->D.V;
+        f.temp = (const float*)(stage + c->lay.st_temp);
+        f.topk = (const int32_t*)(stage + c->lay.st_topk);
+        f.topp = (const float*)(stage + c->lay.st_topp);
+        f.minp = (const float*)(stage + c->lay.st_minp);
+        f.out = s.bufs.logits;
+        f.ws = s.base + c->lay.filter;
+        launch_filter(f, st);
+    };
     if (rs == SD_OK) {
         if (logits) {
             launch_prepare(c->D, bv, s.bufs, st);
-            launch_sampler(c->D, bv, s.bufs, logits, st);
+            if (s.filtered) filter(logits);
+            launch_sampler(c->D, bv, s.bufs, s.filtered ? s.bufs.logits : logits, st);
             rs = hip_status(hipGetLastError());
         } else {
             int groups = 0;
             rs = enqueue_forward(c, s, bv, st, pass_writes_logits(c, bv.mode, probs), &groups);
             if (rs == SD_OK) {
                 ProfScope ps(c, SD_K_SAMPLER, st);
+                if (s.filtered) {
+                    filter(s.bufs.logits);
+                    groups = 0;
+                }
                 launch_sampler(c->D, bv, s.bufs, s.bufs.logits, st, groups);
                 if (probs) launch_probs(c->D, bv, s.bufs, s.bufs.logits, probs, st);
                 rs = hip_status(hipGetLastError());
@@ -951,7 +1083,8 @@ static std::vector<int64_t> launch_key(sd_ctx* c, const Slot& s, const BatchView
     std::vector<int64_t> k = {bv.B, bv.T, bv.nd, bv.mode, (int64_t)bv.seed, (int64_t)bv.round,
                               bv.n_items, bv.rows_max, bv.combine, bv.few, (int64_t)(intptr_t)bv.drafts,
                               (int64_t)(intptr_t)bv.q, (int64_t)(intptr_t)bv.accept_u,
-                              (int64_t)(intptr_t)st, c->sk_polls};
+                              (int64_t)(intptr_t)st, c->sk_polls, s.filtered,
+                              s.adapted ? c->adapters_set : 0};
     for (int b = 0; b < s.B; ++b) {
         k.push_back(s.users[b]);
         k.push_back(s.L[b]);
@@ -1054,6 +1187,11 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     s.batch = batch;
     s.sample_only = sample_only;
     s.logits_ok = sample_only || pass_writes_logits(c, mode, probs);
+    s.filtered = s.adapted = false;
+    for (int m : users) {
+        s.filtered |= mode == SD_STOCHASTIC && c->users[m].filtered();
+        s.adapted |= c->users[m].adapter >= 0;
+    }
     int n_items = 0, rows_max = 0, combine = 0, few = 0;
     build_stage(c, s, mode, !sample_only, &n_items, &rows_max, &combine, &few);
     BatchView bv = make_view(c, s);

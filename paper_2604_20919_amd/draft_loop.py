@@ -65,6 +65,13 @@ class DraftLoop:
         self.dv.reset_user(user, prefix_len, root)
         self.tv.reset_user(user, prefix_len, root)
 
+    def user_sampling(self, user: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                      min_p: float = 0.0):
+        """Sampling options of a user in both models: drafts are drawn from, and
+        verified against, distributions filtered alike."""
+        for v in (self.dv, self.tv):
+            v.user_sampling(user, temperature, top_k, top_p, min_p)
+
     def round(self, batch: int, assign: Sequence[int], draft_len: Sequence[int], rnd: int,
               commit: bool = True) -> RoundResult:
         assign = np.asarray(assign, np.int32)

@@ -29,7 +29,7 @@ EXPORTS = ("sd_verify_query_sizes", "sd_verify_init", "sd_verify_destroy", "sd_u
            "sd_verify_batch_graph", "sd_verify_batch_sparse", "sd_draft_batch", "sd_accept", "sd_sample_logits",
            "sd_sample_logits_noalloc", "sd_debug_logits", "sd_debug_wait_limit", "sd_profile_begin", "sd_profile_end",
            "sd_filter_query_size", "sd_sample_filtered", "sd_filter_logits", "sd_lora_query_size",
-           "sd_lora_apply", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
+           "sd_lora_apply", "sd_user_sampling", "sd_adapters_set", "sd_user_adapter", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
 SD_FILTER_MAX_ROWS, SD_FILTER_MAX_VOCAB = 65535, 1 << 20
 SD_LORA_MAX_RANK, SD_LORA_MAX_SEGS = 128, 4
 SD_K_QKV, SD_K_ATTN, SD_K_O, SD_K_GATEUP, SD_K_DOWN, SD_K_LMHEAD, SD_K_SAMPLER, SD_K_SMALL = range(1, 9)
@@ -62,6 +62,10 @@ class sd_lora(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_adapters", "rank", "d_in", "d_out", "n_seg")] + [
         ("seg_off", ctypes.c_int32 * (SD_LORA_MAX_SEGS + 1)), ("dtype", ctypes.c_int32),
         ("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class sd_layer_adapters(ctypes.Structure):
+    _fields_ = [(n, sd_lora) for n in ("qkv", "o", "down")]
 
 
 class SdError(RuntimeError):
@@ -109,6 +113,10 @@ def lib() -> ctypes.CDLL:
         L.sd_filter_logits.argtypes = [i32, i32, vp, i32, i64, P(sd_filter), vp, i64, vp, vp, u64, vp]
         L.sd_lora_query_size.argtypes = [P(sd_lora), i32, P(u64)]
         L.sd_lora_apply.argtypes = [P(sd_lora), i32, vp, vp, vp, i64, vp, i64, vp, i64, i32, vp, u64, vp]
+        f32 = ctypes.c_float
+        L.sd_user_sampling.argtypes = [vp, i32, f32, i32, f32, f32]
+        L.sd_adapters_set.argtypes = [vp, i32, P(sd_layer_adapters)]
+        L.sd_user_adapter.argtypes = [vp, i32, i32]
         L.sd_calib_hbm.argtypes = [vp, ctypes.c_size_t, i32, i32, P(ctypes.c_double), vp]
         L.sd_calib_mfma.argtypes = [vp, i32, P(ctypes.c_double), vp]
         for name in EXPORTS:
@@ -408,6 +416,34 @@ def sd_lora_apply(w: Lora, adapter, x, y_in, y_out, workspace, x_lo=None, stream
     _check("sd_lora_apply", lib().sd_lora_apply(
         w.ref, n, _vec(adapter, n, "torch.int32", "adapter", at), xp, lo, xs, yi, ys, yo, yos, _dtype(y_in, "y_in"),
         ws, size, _stream(stream)))
+
+
+def sd_user_sampling(ctx: int, user: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                     min_p: float = 0.0) -> None:
+    _check("sd_user_sampling", lib().sd_user_sampling(ctx, user, float(temperature), int(top_k), float(top_p),
+                                                      float(min_p)))
+
+
+def sd_adapters_set(ctx: int, layers) -> None:
+    """layers: per layer a dict of Lora under "qkv", "o", "down" (any of them
+    left out), or None to take all adapters away.  The caller keeps the
+    tensors alive until the next call or sd_verify_destroy."""
+    if layers is None:
+        _check("sd_adapters_set", lib().sd_adapters_set(ctx, 0, None))
+        return
+    arr = (sd_layer_adapters * len(layers))()
+    n = 0
+    for dst, src in zip(arr, layers):
+        for name, w in src.items():
+            if name not in ("qkv", "o", "down"):
+                raise ValueError(f"no adapters beside {name}")
+            setattr(dst, name, w.desc)
+            n = w.desc.n_adapters
+    _check("sd_adapters_set", lib().sd_adapters_set(ctx, n, arr))
+
+
+def sd_user_adapter(ctx: int, user: int, adapter: int) -> None:
+    _check("sd_user_adapter", lib().sd_user_adapter(ctx, user, int(adapter)))
 
 
 def sd_accept(ctx: int, batch: int, n_users: int, commit: bool = False):

@@ -64,6 +64,23 @@ class Verifier:
     def user_state(self, user: int):
         return sv.sd_user_state(self.ctx, user)
 
+    def user_sampling(self, user: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                      min_p: float = 0.0):
+        """Sampling options of a user's stochastic passes (sd_user_sampling)."""
+        sv.sd_user_sampling(self.ctx, user, temperature, top_k, top_p, min_p)
+
+    def set_adapters(self, layers):
+        """Adapters of every layer (sd_adapters_set): per layer a dict of
+        sdverify.Lora under "qkv", "o", "down"; None: no adapters."""
+        if layers is not None and len(layers) != self.cfg.n_layers:
+            raise ValueError(f"adapters of {len(layers)} layers, the model has {self.cfg.n_layers}")
+        sv.sd_adapters_set(self.ctx, layers)
+        self._adapters = layers  # the library reads them in place
+
+    def user_adapter(self, user: int, adapter: int):
+        """The adapter of a user's slots, -1: none (sd_user_adapter)."""
+        sv.sd_user_adapter(self.ctx, user, adapter)
+
     def write_kv(self, user: int, layer: int, pos0: int, k: torch.Tensor, v: torch.Tensor, stream=None):
         sv.sd_kv_write(self.ctx, user, layer, pos0, k.shape[0], k, v, stream)
 
