@@ -108,10 +108,49 @@ struct RowShared {
     int found;
 };
 
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Scans over the lanes of a wave by moves within the vector registers (a
+// shuffle through LDS takes about ten times as long): shifts by 1, 2, 4 and 8
+// within rows of 16, then the last lane of rows 0 and 2, and of 1, to the rest.
+template <int CTRL, int ROWS, typename T> __device__ __forceinline__ T lane_move(T v, T other) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other),
+                                                                 __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    } else {
+        const u64 a = __builtin_bit_cast(u64, v), b = __builtin_bit_cast(u64, other);
+        const uint32_t lo = __builtin_amdgcn_update_dpp((int)(uint32_t)b, (int)(uint32_t)a, CTRL, ROWS, 0xf, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp((int)(b >> 32), (int)(a >> 32), CTRL, ROWS, 0xf, false);
+        return __builtin_bit_cast(T, (u64)hi << 32 | lo);
+    }
+}
+// inclusive scan; `none` leaves a value as it is
+template <typename T, typename Op> __device__ __forceinline__ T wave_scan(T v, T none, Op op) {
+    v = op(v, lane_move<0x111, 0xf>(v, none));
+    v = op(v, lane_move<0x112, 0xf>(v, none));
+    v = op(v, lane_move<0x114, 0xf>(v, none));
+    v = op(v, lane_move<0x118, 0xf>(v, none));
+    v = op(v, lane_move<0x142, 0xa>(v, none));
+    v = op(v, lane_move<0x143, 0xc>(v, none));
     return v;
+}
+template <typename T> __device__ __forceinline__ T last_lane(T v) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    } else {
+        const u64 a = __builtin_bit_cast(u64, v);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)a, 63);
+        const uint32_t hi = __builtin_amdgcn_readlane((int)(a >> 32), 63);
+        return __builtin_bit_cast(T, (u64)hi << 32 | lo);
+    }
+}
+template <typename T> __device__ __forceinline__ T scan_add(T v) {
+    return wave_scan(v, (T)0, [](T a, T b) { return a + b; });
+}
+template <typename T> __device__ __forceinline__ T wave_add(T v) { return last_lane(scan_add(v)); }
+__device__ __forceinline__ float wave_top(float v) {
+    return last_lane(wave_scan(v, -INFINITY, [](float a, float b) { return max_clean(a, b); }));
+}
+__device__ __forceinline__ uint32_t wave_least(uint32_t v) {
+    return last_lane(wave_scan(v, 0xffffffffu, [](uint32_t a, uint32_t b) { return min(a, b); }));
 }
 
 // A whole row by one workgroup, whatever its values: the rows
@@ -127,7 +166,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
     const RowOpts o = row_opts(p, row);
     float m = -INFINITY;
     for (int i = tid; i < V; i += kRowThreads) m = fmaxf(m, row_at(z, i));
-    m = wave_max(m);
+    m = wave_top(m);
     if (lane == 0) s.fmax[w] = m;
     __syncthreads();
     for (int i = 0; i < kRowWaves; ++i) m = fmaxf(m, s.fmax[i]);
@@ -153,7 +192,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         const float v = row_at(z, i);
         if (eligible(v)) S += fixed_weight(log2_weight(v, m, o.c), p.scale_bits);
     }
-    S = wave_sum_u64(S);
+    S = wave_add(S);
     if (lane == 0) s.wsum[w] = S;
     __syncthreads();
     S = 0;
@@ -185,14 +224,8 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         const int b = kBins - 1 - tid;
         const uint32_t c = s.cnt[b];
         const u64 ws = s.sum[b];
-        uint32_t ic = c;
-        u64 is = ws;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t c2 = __shfl_up(ic, d, 64);
-            const u64 s2 = __shfl_up(is, d, 64);
-            if (lane >= d) { ic += c2; is += s2; }
-        }
+        uint32_t ic = scan_add(c);
+        u64 is = scan_add(ws);
         if (lane == 63) { s.wcnt[w] = ic; s.wsum[w] = is; }
         if (tid == 0) s.found = kBins;
         __syncthreads();
@@ -232,8 +265,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         const int seg = (V + kRowWaves - 1) / kRowWaves, i0 = w * seg, i1 = min(V, i0 + seg);
         uint32_t n = 0;
         for (int i = i0 + lane; i < i1; i += 64) n += key_of(row_at(z, i)) == lo;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d, 64);
+        n = wave_add(n);
         __syncthreads();
         if (lane == 0) s.wcnt[w] = n;
         if (tid == 0) s.found = V;
@@ -275,9 +307,8 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         ++kc;
         if (DRAW) ks += fixed_weight(log2_weight(v, m, o.c), p.scale_bits);
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) kc += __shfl_xor(kc, d, 64);
-    ks = wave_sum_u64(ks);
+    kc = wave_add(kc);
+    ks = wave_add(ks);
     __syncthreads();
     if (lane == 0) { s.wcnt[w] = kc; s.wsum[w] = ks; }
     __syncthreads();
@@ -300,12 +331,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
         const float v = i + lane < i1 ? row_at(z, i + lane) : -INFINITY;
         const bool on = i + lane < i1 && keeps(v, i + lane);
         const u64 wt = on ? fixed_weight(log2_weight(v, m, o.c), p.scale_bits) : 0;
-        u64 inc = wt;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const u64 x = __shfl_up(inc, d, 64);
-            if (lane >= d) inc += x;
-        }
+        const u64 inc = scan_add(wt);
         const u64 hit = __ballot(base + inc > target);
         if (hit) {
             if (lane == __ffsll(hit) - 1) {
@@ -314,7 +340,7 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
             }
             return;
         }
-        base += __shfl(inc, 63, 64);
+        base += last_lane(inc);
     }
 }
 
@@ -343,6 +369,11 @@ constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G -
 // A bucket of a chunk is one number: the count from bit kCountBit up, and below it
 // the weights in units of 2^(G - kHistFix), which stay under it.
 constexpr int kCountBit = 50, kHistFix = 37;
+// (the count's one rides through the same shift)
+__device__ __forceinline__ u64 hist_entry(u64 w) {
+    static_assert(kCountBit + kFix - kHistFix == 63, "the count's one is the top bit before the shift");
+    return (w + (1ull << 63) + (1ull << (kFix - kHistFix - 1))) >> (kFix - kHistFix);
+}
 __device__ __forceinline__ u64 hist_weight(u64 w) { return (w + (1ull << (kFix - kHistFix - 1))) >> (kFix - kHistFix); }
 constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
 static_assert(kMaxChunks <= 128, "a row's chunks fit the arrays of k_filter_find and k_filter_resolve");
@@ -369,6 +400,7 @@ struct RowRec {
     float m;
     uint32_t n_list, above_c;
     uint32_t klo, khi;   // keys of the last bucket's members
+    uint32_t kmin;       // smallest key that min-p lets pass
     uint32_t cut;        // the prefix's last key and last index among its ties
     int last;
 };
@@ -519,7 +551,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     float M = v[0];
 #pragma unroll
     for (int e = 1; e < kPer; ++e) M = max_clean(M, v[e]);
-    M = wave_max(M);
+    M = wave_top(M);
     if (lane == 0) sm[w] = M;
     __syncthreads();
 #pragma unroll
@@ -534,8 +566,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
 #pragma unroll
         for (int e = kPer - 1; e >= 0; --e)
             if (v[e] == M) first = c * kChunk + elem_at<T>(tid, e);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+        first = (int)wave_least((uint32_t)first);
     } else if (M > -INFINITY && grid_holds(M, o.c)) {
         G = grid_top(M, o.c);
         const Grid g = grid_of(G, o.c);
@@ -554,7 +585,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (b[e] < kBuckets) atomicAdd(&hs[b[e]], hist_weight(x[e]) + (1ull << kCountBit));
+                    if (b[e] < kBuckets) atomicAdd(&hs[b[e]], hist_entry(x[e]));
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -565,7 +596,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
             }
         }
     }
-    S = wave_sum_u64(S);
+    S = wave_add(S);
     if (lane == 0) { si[w] = first; ss[w] = S; sn[w] = n; }
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
@@ -578,23 +609,20 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     }
 }
 
-// Smallest key whose logit lies in bucket b (0 or more) or a heavier one of a
-// row whose largest key `top` does: buckets are monotone in the key, so one wave
-// narrows a bracket of keys, 64 at once.  It starts around the edge's logit.
-__device__ __forceinline__ uint32_t bucket_key(const Grid& g, double G, uint32_t top, int b, int lane) {
-    auto in = [&](uint32_t k) { return grid_bucket(on_grid(g, key_value(k))) <= b; };
-    const double edge = (G - 0.125 * b - 0x1p-9) / g.c, off = 0x1p-31 / g.c + fabs(edge) * 0x1p-22;
-    uint32_t lo = key_of((float)(edge - off)), hi = key_of((float)(edge + off));
+// Smallest key for which `in`, monotone in the key, holds; it does for `top`.
+// One wave narrows a bracket of keys, 64 at once, from the keys around the logit
+// `edge` that the border should have.
+template <typename F>
+__device__ __forceinline__ uint32_t first_key(F in, double edge, double off, uint32_t top, int lane) {
     const uint32_t least = key_of(-INFINITY);
+    uint32_t lo = key_of((float)(edge - off)), hi = key_of((float)(edge + off));
     if (!(lo >= least && lo < hi && !in(lo))) lo = least;
     if (!(hi > lo && hi <= top && in(hi))) hi = top;
-    while (hi - lo > 1) {  // lo is lighter (or -inf), hi is in
+    while (hi - lo > 1) {  // lo is out (or -inf), hi is in
         const uint32_t step = (hi - lo + 63) / 64;
-        const uint32_t k = min(lo + step * (lane + 1), hi);
-        const int i = __ffsll(__ballot(in(k))) - 1;  // (the last lane's key is hi)
-        const uint32_t nlo = lo + step * i;
-        hi = min(nlo + step, hi);
-        lo = nlo;
+        const int i = __ffsll(__ballot(in(min(lo + step * (lane + 1), hi)))) - 1;  // (the last lane's key is hi)
+        lo += step * i;
+        hi = min(lo + step, hi);
     }
     return hi;
 }
@@ -621,7 +649,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     // the row's maximum, its lowest index and 2^G that its sums refer to (each wave by itself)
     float m = -INFINITY;
     for (int c = lane; c < nch; c += 64) m = fmaxf(m, cm[c]);
-    m = wave_max(m);
+    m = wave_top(m);
     const double G = grid_top(m, o.c);  // that of the chunk with the maximum
     RowRec r{};
     r.G = G;
@@ -636,8 +664,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         int first = 0x7fffffff;
         for (int c = lane; c < nch; c += 64)
             if (cm[c] == m) first = min(first, (int)cfirst[c]);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+        first = (int)wave_least((uint32_t)first);
         if (lane == 0) {
             r.mode = m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : kModeRow;
             r.cut = key_of(m);
@@ -662,8 +689,8 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         S += cS[c] * pow2(cG[c] - G - kFix);
         n += cn[c];
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) { S += __shfl_xor(S, d, 64); n += __shfl_xor(n, d, 64); }
+    S = wave_add(S);
+    n = wave_add(n);
     r.P = o.p * S;
     r.mode = kModeAll;
     if (!o.filters) {
@@ -696,12 +723,8 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     if (tid < kBuckets) {
         ic = cnt = bcnt[0][tid] + bcnt[1][tid] + bcnt[2][tid] + bcnt[3][tid];
         is = sum = (bsum[0][tid] + bsum[1][tid]) + (bsum[2][tid] + bsum[3][tid]);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t c2 = __shfl_up(ic, d, 64);
-            const double s2 = __shfl_up(is, d, 64);
-            if (lane >= d) { ic += c2; is += s2; }
-        }
+        ic = scan_add(ic);
+        is = scan_add(is);
         if (lane == 63) { su[w] = ic; sd[w] = is; }
     }
     __syncthreads();
@@ -743,26 +766,31 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
                 b = border - bucket_shift(G, cG[c]);
                 if (b >= 0) k = (uint32_t)(wk.hist[((size_t)row * nch + c) * kBuckets + b] >> kCountBit);
             }
-            uint32_t inc = k;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t x = __shfl_up(inc, d, 64);
-                if (lane >= d) inc += x;
-            }
+            const uint32_t inc = scan_add(k);
             if (c < nch) {
                 recs[c].bucket = max(b, -1);
                 recs[c].off = run + inc - k;
                 recs[c].have = k;
             }
-            run += __shfl(inc, 63, 64);
+            run += last_lane(inc);
         }
-    } else if (w == 1) {
-        const uint32_t k = bucket_key(g, G, key_of(m), border, lane);
-        if (lane == 0) su[10] = k;
-    } else if (w == 2) {
-        uint32_t k = key_of(m);
-        if (grid_bucket(on_grid(g, m)) != border) k = bucket_key(g, G, k, border - 1, lane) - 1;
-        if (lane == 0) su[11] = k;
+    } else if (w < 4) {
+        // waves 1 and 2: the border bucket's keys; wave 3: min-p's
+        const uint32_t top = key_of(m);
+        uint32_t k = 0;
+        if (w < 3) {
+            const int b = border + 1 - w;
+            k = top + 1;  // (no bucket above the maximum's)
+            if (grid_bucket(on_grid(g, m)) <= b)
+                k = first_key([&](uint32_t x) { return grid_bucket(on_grid(g, key_value(x))) <= b; },
+                              (G - 0.125 * b - 0x1p-9) / o.c, 0x1p-31 / o.c + fabs(G / o.c) * 0x1p-22, top, lane);
+        } else if (o.lmin > -INFINITY) {
+            k = first_key([&](uint32_t x) {
+                const float z = key_value(x);
+                return z == m || ((double)z - (double)m) * o.c >= r.lmin;
+            }, (double)m + r.lmin / o.c, (fabs((double)m) + fabs(r.lmin / o.c)) * 0x1p-22, top, lane);
+        }
+        if (lane == 0) su[9 + w] = k;
     }
     __syncthreads();
     if (tid == 0) {
@@ -770,7 +798,8 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         r.above_c = su[9];
         r.above = sd[8];
         r.klo = su[10];
-        r.khi = su[11];
+        r.khi = su[11] - 1;
+        r.kmin = su[12];
         r.mode = r.n_list > kList ? kModeRow : kModeBorder;
         wk.rows[row] = r;
     }
@@ -795,7 +824,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
 #pragma unroll
         for (int e = 0; e < kBuckets / 64; ++e)
             if (lane + 64 * e < bucket) a += h[lane + 64 * e] & ((1ull << kCountBit) - 1);
-        a = wave_sum_u64(a);
+        a = wave_add(a);
         if (lane == 0) rec->above = a;
     }
     if (rec->have == 0) return;
@@ -836,38 +865,97 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
     }
 }
 
-struct ListShared {
-    uint32_t key[kList];
+struct ResolveShared {
+    u64 sum[4][kBins];      // a digit's weights and counts
+    uint32_t cnt[4][kBins];
+    u64 wsum[kRowWaves];
+    uint32_t wcnt[kRowWaves];
+    uint32_t ties_of[64];
+    uint32_t lo, hi, above_c, ties, kept;
+    u64 above_s, goal;
+    int found, last, chunk;
+    double K;
     u64 cadd[128];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kHistFix)
     double cG[128];
-    int chunk;
-    double K;
+    RowRec r;
 };
+constexpr int kHeld = 8;                        // members of the last bucket that a thread holds
+constexpr int kHeldAll = kHeld * kRowThreads;   // at once; longer lists are read again for each pass
 
 // One workgroup a row: the end of the prefix among the last bucket's members,
-// then the chunk and the element drawn.
-template <typename T, bool DRAW>
+// then the chunk and the element drawn.  PLAIN: no row has a filter, and the
+// chunks are merged here.
+template <typename T, bool DRAW, bool PLAIN>
 __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Work wk, int nch) {
-    __shared__ RowShared s;
-    __shared__ ListShared l;
+    __shared__ union { RowShared row; ResolveShared s; } sh;
     __shared__ uint2 tab[kTab];
+    ResolveShared& s = sh.s;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if (tid < kTab) tab[tid] = g_exp2.e[tid];
-    RowRec r = wk.rows[row];
-    if (r.mode == kModeDone || r.mode == kModeEmpty) return;
-    if (r.mode == kModeRow) {
-        filter_row<T, DRAW>(p, row, s);
-        return;
-    }
-    if (!DRAW && r.mode == kModeAll) return;
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
-    const uint2* list = wk.list + (size_t)row * kList;
-    const bool border = r.mode == kModeBorder;
     // (wave 0 holds the chunks' weights from here to the draw)
     u64 cabove[2] = {0, 0};
     double cG[2] = {0, 0};
     float u = 0.f;
-    if (DRAW && w == 0) {
+    RowRec r;
+    if (PLAIN) {
+        if (w == 0) {
+            const RowOpts o = row_opts(p, row);
+            u = p.u[row];
+            float cm[2] = {-INFINITY, -INFINITY};
+            uint32_t n = 0, first = 0xffffffffu, cf[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = lane + 64 * e;
+                if (c < nch) {
+                    cm[e] = recs[c].m;
+                    cf[e] = (uint32_t)recs[c].first;
+                    n += recs[c].n;
+                    if (cm[e] > -INFINITY) {
+                        cG[e] = recs[c].G;
+                        cabove[e] = recs[c].S;
+                    }
+                }
+                s.cG[c] = cG[e];
+                s.cadd[c] = 0;
+            }
+            r = RowRec{};
+            r.m = wave_top(max_clean(cm[0], cm[1]));
+            r.c = o.c;
+            r.cut = key_of(-INFINITY) + 1;
+            r.last = p.V;
+            r.mode = r.m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : grid_holds(r.m, o.c) ? kModeAll : kModeRow;
+            if (r.mode == kModeAll) r.G = grid_top(r.m, o.c);
+            n = wave_add(n);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (cm[e] == r.m) first = min(first, cf[e]);
+            first = wave_least(first);
+            if (lane == 0) {
+                s.r = r;
+                if (r.mode != kModeRow) {
+                    if (p.kept) p.kept[row] = r.mode == kModeAll ? (int)n : r.mode == kModeDone;
+                    if (r.mode != kModeAll) {
+                        p.token[row] = r.mode == kModeDone ? (int)first : -1;
+                        if (p.prob) p.prob[row] = r.mode == kModeDone ? 1.f : 0.f;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        r = s.r;
+        __syncthreads();  // (the whole-row path takes the same memory)
+    } else {
+        r = wk.rows[row];
+    }
+    if (r.mode == kModeDone || r.mode == kModeEmpty) return;
+    if (r.mode == kModeRow) {
+        filter_row<T, DRAW>(p, row, sh.row);
+        return;
+    }
+    if (!DRAW && r.mode == kModeAll) return;
+    const bool border = !PLAIN && r.mode == kModeBorder;
+    if (tid < kTab) tab[tid] = g_exp2.e[tid];
+    if (!PLAIN && DRAW && w == 0) {
         u = p.u[row];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -876,102 +964,80 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                 cG[e] = recs[c].G;
                 cabove[e] = border ? recs[c].above : recs[c].S;
             }
-            l.cG[c] = cG[e];
-            l.cadd[c] = 0;
+            s.cG[c] = cG[e];
+            s.cadd[c] = 0;
         }
     }
     if (border) {
+        const uint2* list = wk.list + (size_t)row * kList;
         const int n = (int)r.n_list;
-        uint32_t lo = 0xffffffffu, hi = 0;
-        auto passes = [&](uint32_t key) {
-            const float z = key_value(key);
-            return z == r.m || ((double)z - (double)r.m) * r.c >= r.lmin;
+        uint2 held[kHeld];
+        auto hold = [&](int i0) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                const int i = i0 + j * kRowThreads + tid;
+                held[j] = i < n ? list[i] : uint2{0, 0};  // (no member has key 0)
+            }
         };
-#pragma unroll 8
-        for (int i = tid; i < n; i += kRowThreads) {
-            const uint32_t k = list[i].x;
-            l.key[i] = k;
-            if (passes(k)) { lo = min(lo, k); hi = max(hi, k); }
-        }
+        hold(0);
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            lo = min(lo, (uint32_t)__shfl_xor((int)lo, d, 64));
-            hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
-        }
-        s.sum[tid] = 0;
-        s.cnt[tid] = 0;
-        if (lane == 0) { s.wcnt[w] = lo; s.wsum[w] = hi; }
-        if (tid == 0) s.found = kBins;
+        for (int i = 0; i < 4; ++i) { s.sum[i][tid] = 0; s.cnt[i][tid] = 0; }
+        if (tid == 0) { s.found = 0; s.kept = 0; }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kRowWaves; ++i) {
-            lo = min(lo, s.wcnt[i]);
-            hi = max(hi, (uint32_t)s.wsum[i]);
-        }
-        uint32_t cut = r.khi, ties = 0, take = 0;
+        uint32_t lo = max(r.klo, r.kmin), hi = r.khi, cut = hi, ties = 0, take = 0;
         int last = -1;  // (min-p leaves none of them)
         if (lo <= hi) {
-            const uint32_t first_lo = lo;
             // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
             // least: sums of kList stay below 2^63
-            const double Gb = floor((double)key_value(r.khi) * r.c) + 2.0;
+            const double Gb = floor((double)key_value(hi) * r.c) + 2.0;
             const Grid g = grid_of(Gb, r.c);
-            const double need = (r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix);
+            // (a bound of nothing stops at the first: rank 0 is kept)
+            const double need = fmax((r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix), 0.5);
             uint32_t above_c = r.above_c;
             u64 above_s = 0;
-            for (bool again = false;; again = true) {
-                const int sh = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 9);
-                if (again) {
-                    s.sum[tid] = 0;
-                    s.cnt[tid] = 0;
-                    if (tid == 0) s.found = kBins;
-                }
-                __syncthreads();
-#pragma unroll 4
-                for (int i = tid; i < n; i += kRowThreads) {
-                    const uint32_t key = l.key[i];
-                    if (key < lo || key > hi) continue;
-                    atomicAdd(&s.cnt[(key - lo) >> sh], 1u);
-                    atomicAdd(&s.sum[(key - lo) >> sh], grid_weight(tab, on_grid(g, key_value(key))));
+            for (int it = 0; it < 4; ++it) {
+                const int sf = hi == lo ? 0 : max(0, 32 - __clz(hi - lo) - 9);
+                for (int i0 = 0; i0 < n; i0 += kHeldAll) {
+                    if (n > kHeldAll) hold(i0);
+#pragma unroll
+                    for (int j = 0; j < kHeld; ++j) {
+                        const uint32_t key = held[j].x;
+                        if (key < lo || key > hi) continue;
+                        atomicAdd(&s.cnt[it][(key - lo) >> sf], 1u);
+                        atomicAdd(&s.sum[it][(key - lo) >> sf], grid_weight(tab, on_grid(g, key_value(key))));
+                    }
                 }
                 __syncthreads();
                 const int b = kBins - 1 - tid;
-                const uint32_t c = s.cnt[b];
-                const u64 ws = s.sum[b];
-                uint32_t ic = c;
-                u64 is = ws;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t c2 = __shfl_up(ic, d, 64);
-                    const u64 s2 = __shfl_up(is, d, 64);
-                    if (lane >= d) { ic += c2; is += s2; }
-                }
+                const uint32_t c = s.cnt[it][b];
+                const u64 ws = s.sum[it][b];
+                uint32_t ic = scan_add(c);
+                u64 is = scan_add(ws);
                 if (lane == 63) { s.wcnt[w] = ic; s.wsum[w] = is; }
                 __syncthreads();
                 ic += above_c;
                 is += above_s;
-                for (int i = 0; i < w; ++i) { ic += s.wcnt[i]; is += s.wsum[i]; }
-                if (c > 0 && (ic >= (uint32_t)r.k || (double)is >= need)) {
-                    // (the first such lane stands for its wave)
-                    if (lane == __ffsll(__ballot(1)) - 1) atomicMin(&s.found, tid);
+#pragma unroll
+                for (int i = 0; i < kRowWaves - 1; ++i)
+                    if (i < w) { ic += s.wcnt[i]; is += s.wsum[i]; }
+                // the bin in which a filter stops: the sums grow, so there is one
+                if (c > 0 && (ic >= (uint32_t)r.k || (double)is >= need) &&
+                    !(ic - c >= (uint32_t)r.k || (double)(is - ws) >= need)) {
+                    s.above_c = ic - c;
+                    s.above_s = is - ws;
+                    s.lo = lo + ((uint32_t)b << sf);
+                    s.hi = min(hi, lo + ((uint32_t)b << sf) + ((1u << sf) - 1));
+                    s.ties = c;
+                    s.found = it + 1;
                 }
                 __syncthreads();
-                const int found = s.found;
-                if (found == kBins) {  // min-p alone ends the prefix
-                    cut = first_lo;
+                if (s.found != it + 1) {  // min-p alone ends the prefix
+                    cut = lo;
                     last = p.V;
                     break;
                 }
-                if (tid == found) {
-                    s.above_c = ic - c;
-                    s.above_s = is - ws;
-                    s.lo = lo + ((uint32_t)b << sh);
-                    s.hi = min(hi, s.lo + ((1u << sh) - 1));
-                    s.ties = c;
-                }
-                __syncthreads();
                 lo = s.lo; hi = s.hi; above_c = s.above_c; above_s = s.above_s;
-                if (sh) continue;
+                if (sf) continue;
                 cut = lo;
                 ties = s.ties;
                 double jp = 4e9;
@@ -986,45 +1052,62 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                 break;
             }
             if (take < ties) {
-                // the index of the last tie kept
-                if (w == 0) {
-                    uint32_t left = take;
-                    for (int i0 = 0; i0 < n; i0 += 64) {
-                        const u64 hit = __ballot(i0 + lane < n && l.key[min(i0 + lane, n - 1)] == cut);
-                        const uint32_t c = __popcll(hit);
-                        if (c >= left) {
-                            if ((hit >> lane & 1) && __popcll(hit & ((2ull << lane) - 1)) == left)
-                                s.found = (int)list[i0 + lane].y;
-                            break;
+                // the index of the last tie kept: ties by wave and piece of the list
+                uint32_t left = take;
+                for (int i0 = 0; i0 < n; i0 += kHeldAll) {
+                    if (n > kHeldAll) hold(i0);
+#pragma unroll
+                    for (int j = 0; j < kHeld; ++j) {
+                        const u64 hit = __ballot(held[j].x == cut);
+                        if (lane == 0) s.ties_of[j * kRowWaves + w] = __popcll(hit);
+                    }
+                    __syncthreads();
+                    const uint32_t c = s.ties_of[lane], inc = scan_add(c);
+                    const u64 past = __ballot(inc >= left);
+                    if (past) {
+                        const int at = __ffsll(past) - 1;
+                        const uint32_t nth = left - (__shfl(inc, at, 64) - __shfl(c, at, 64));
+#pragma unroll
+                        for (int j = 0; j < kHeld; ++j) {
+                            if (at != j * kRowWaves + w) continue;
+                            const u64 hit = __ballot(held[j].x == cut);
+                            if ((hit >> lane & 1) && __popcll(hit & ((2ull << lane) - 1)) == nth) s.last = (int)held[j].y;
                         }
-                        left -= c;
+                        __syncthreads();
+                        break;
+                    }
+                    left -= last_lane(inc);
+                    __syncthreads();
+                }
+                last = s.last;
+            }
+        }
+        // number kept, and the members' weights by chunk (those of a wave mostly lie in one)
+        for (int i0 = 0; i0 < n; i0 += kHeldAll) {
+            if (n > kHeldAll) hold(i0);
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                if (i0 + j * kRowThreads + (tid & ~63) >= n) break;
+                const uint2 x = held[j];
+                const bool on = x.x > cut || (x.x == cut && (int)x.y <= last);
+                const u64 who = __ballot(on);
+                if (!who) continue;
+                if (lane == 0) atomicAdd(&s.kept, (uint32_t)__popcll(who));
+                if (DRAW) {
+                    const int c = (int)x.y / kChunk, c0 = __builtin_amdgcn_readlane(c, __ffsll(who) - 1);
+                    const u64 wt = on ? hist_weight(grid_weight(tab, on_grid(grid_of(s.cG[c], r.c), key_value(x.x)))) : 0;
+                    if (__ballot(on && c != c0)) {
+                        if (on) atomicAdd(&s.cadd[c], wt);
+                    } else {
+                        const u64 sum = wave_add(wt);
+                        if (lane == 0) atomicAdd(&s.cadd[c0], sum);
                     }
                 }
-                __syncthreads();
-                last = s.found;
             }
         }
-        // number kept, and the members' weights by chunk
-        uint32_t kc = 0;
-#pragma unroll 8
-        for (int i = tid; i < n; i += kRowThreads) {
-            const uint2 x = list[i];
-            if (x.x < cut || (x.x == cut && (int)x.y > last)) continue;
-            ++kc;
-            if (DRAW) {
-                const int c = (int)x.y / kChunk;
-                atomicAdd(&l.cadd[c], hist_weight(grid_weight(tab, on_grid(grid_of(l.cG[c], r.c), key_value(x.x)))));
-            }
-        }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) kc += __shfl_xor(kc, d, 64);
-        __syncthreads();
-        if (lane == 0) s.wcnt[w] = kc;
         __syncthreads();
         if (tid == 0) {
-            uint32_t c = r.above_c;
-            for (int i = 0; i < kRowWaves; ++i) c += s.wcnt[i];
-            if (p.kept) p.kept[row] = (int)c;
+            if (p.kept) p.kept[row] = (int)(r.above_c + s.kept);
             if (!DRAW) {
                 wk.rows[row].cut = cut;
                 wk.rows[row].last = last;
@@ -1041,17 +1124,10 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
         double x[2], inc[2], tot[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            cabove[e] += l.cadd[lane + 64 * e];
-            inc[e] = x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - unit) : 0.0;
-            tot[e] = 0.0;
-            if (64 * e < nch) {
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const double y = __shfl_up(inc[e], d, 64);
-                    if (lane >= d) inc[e] += y;
-                }
-                tot[e] = __shfl(inc[e], 63, 64);
-            }
+            cabove[e] += s.cadd[lane + 64 * e];
+            x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - unit) : 0.0;
+            inc[e] = scan_add(x[e]);
+            tot[e] = last_lane(inc[e]);
         }
         const double K = tot[0] + tot[1];
         u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
@@ -1065,62 +1141,57 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             const u64 have = e ? cabove[1] : cabove[0];
             const double before = e ? inc[1] - x[1] : inc[0] - x[0];
             const double local = fmin(fmax((target - before) * pow2(r.G - (e ? cG[1] : cG[0]) + unit), 0.0), 0x1p63);
-            l.chunk = ch;
-            l.K = K;
-            s.above_s = min((u64)local, have - 1);
+            s.chunk = ch;
+            s.K = K;
+            s.goal = min((u64)local, have - 1);
         }
     }
     __syncthreads();
-    const int ch = l.chunk;
-    const u64 goal = s.above_s;
+    const int ch = s.chunk;
+    const u64 goal = s.goal;
     // its elements in index order: the first whose running sum exceeds the goal
     constexpr int E = kChunk / kRowThreads, W = 16 / sizeof(T);
-    const Grid g = grid_of(l.cG[ch], r.c);
+    const Grid g = grid_of(s.cG[ch], r.c);
     const T* z = (const T*)p.z + (size_t)row * p.stride;
     const int i0 = ch * kChunk + tid * E;
     T raw[E];
+    if ((ch + 1) * kChunk <= p.V) {
 #pragma unroll
-    for (int q = 0; q < E; q += W) {
-        if (i0 + q + W <= p.V) {
-            __builtin_memcpy(&raw[q], z + i0 + q, 16);
-        } else {
+        for (int q = 0; q < E; q += W) __builtin_memcpy(&raw[q], z + i0 + q, 16);
+    } else {
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                raw[q + e] = 0;
-                if (i0 + q + e < p.V) raw[q + e] = z[i0 + q + e];
-            }
-        }
+        for (int e = 0; e < E; ++e) raw[e] = z[min(i0 + e, p.V - 1)];
     }
-    auto weight = [&](int e) -> u64 {
+    u64 x[E], mysum = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
         const float v = i0 + e < p.V ? clean(ld<T>(raw, e)) : -INFINITY;
         const uint32_t key = key_of(v);
         const bool on = key > r.cut || (key == r.cut && i0 + e <= r.last);
-        const u64 x = grid_weight(tab, on_grid(g, v));
-        return on ? (border ? hist_weight(x) : x) : 0;
-    };
-    u64 mysum = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) mysum += weight(e);
-    u64 inc = mysum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 y = __shfl_up(inc, d, 64);
-        if (lane >= d) inc += y;
+        const u64 t = grid_weight(tab, on_grid(g, v));
+        x[e] = on ? (border ? hist_weight(t) : t) : 0;
+        mysum += x[e];
     }
+    const u64 inc = scan_add(mysum);
     if (lane == 63) s.wsum[w] = inc;
     __syncthreads();
     u64 at = inc - mysum;
-    for (int i = 0; i < w; ++i) at += s.wsum[i];
+#pragma unroll
+    for (int i = 0; i < kRowWaves - 1; ++i)
+        if (i < w) at += s.wsum[i];
     if (at <= goal && goal < at + mysum) {
+        int hit = 0;
+        float v = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const u64 x = weight(e);
-            if (at <= goal && goal < at + x) {
-                p.token[row] = i0 + e;
-                if (p.prob) p.prob[row] = (float)(exp2((double)clean(ld<T>(raw, e)) * r.c - r.G) / l.K);
+            if (at <= goal && goal < at + x[e]) {
+                hit = e;
+                v = ld<T>(raw, e);
             }
-            at += x;
+            at += x[e];
         }
+        p.token[row] = i0 + hit;
+        if (p.prob) p.prob[row] = (float)(exp2((double)v * r.c - r.G) / s.K);
     }
 }
 
@@ -1173,15 +1244,18 @@ static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {
     const int nch = chunks_of(c.V);
     const dim3 g(nch, c.n_rows);
     hipLaunchKernelGGL(k_filter_scan<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+    const dim3 rows(c.n_rows), of_row(kRowThreads);
     if (c.out) {
-        hipLaunchKernelGGL(k_filter_find<false>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL(k_filter_find<false>, rows, dim3(kFindThreads), 0, s, p, wk, nch);
         hipLaunchKernelGGL((k_filter_collect<T, false>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, false>), dim3(c.n_rows), dim3(kRowThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_resolve<T, false, false>), rows, of_row, 0, s, p, wk, nch);
         hipLaunchKernelGGL(k_filter_write<T>, g, dim3(kChunkThreads), 0, s, p, wk);
+    } else if (!c.topk && !c.topp && !c.minp) {
+        hipLaunchKernelGGL((k_filter_resolve<T, true, true>), rows, of_row, 0, s, p, wk, nch);
     } else {
-        hipLaunchKernelGGL(k_filter_find<true>, dim3(c.n_rows), dim3(kFindThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL(k_filter_find<true>, rows, dim3(kFindThreads), 0, s, p, wk, nch);
         hipLaunchKernelGGL((k_filter_collect<T, true>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, true>), dim3(c.n_rows), dim3(kRowThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_resolve<T, true, false>), rows, of_row, 0, s, p, wk, nch);
     }
 }
 
