@@ -360,9 +360,10 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
 // the filtered rows.  The row itself is read by the first and, where a chunk has
 // members of the last bucket, the third kernel, and by the writing one.
 // ---------------------------------------------------------------------------
-constexpr int kChunk = 8192;
-constexpr int kChunkThreads = 512;
+constexpr int kChunk = 4096;
+constexpr int kChunkThreads = 256, kChunkWaves = kChunkThreads / 64;
 constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
+static_assert(kPer <= 32, "k_filter_collect marks them in 32 bits");
 constexpr int kBuckets = 256;                 // 32 octaves; what lies below is not counted
 constexpr int kList = 16384;                  // most members of the last bucket
 constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G - 50), below 2^63
@@ -376,7 +377,8 @@ __device__ __forceinline__ u64 hist_entry(u64 w) {
 }
 __device__ __forceinline__ u64 hist_weight(u64 w) { return (w + (1ull << (kFix - kHistFix - 1))) >> (kFix - kHistFix); }
 constexpr int kMaxChunks = SD_FILTER_MAX_VOCAB / kChunk;
-static_assert(kMaxChunks <= 128, "a row's chunks fit the arrays of k_filter_find and k_filter_resolve");
+constexpr int kLaneChunks = kMaxChunks / 64;  // of a row, a lane
+static_assert(kMaxChunks % 64 == 0 && kMaxChunks <= 4 * kBuckets, "chunks over the lanes and over k_filter_find's threads");
 
 // What a row still needs after k_filter_find.
 enum { kModeDone = 0, kModeAll = 1, kModeBorder = 2, kModeRow = 3, kModeEmpty = 4 };
@@ -535,10 +537,10 @@ __device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)f
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];
-    __shared__ float sm[8];
-    __shared__ int si[8];
-    __shared__ u64 ss[8];
-    __shared__ uint32_t sn[8];
+    __shared__ float sm[kChunkWaves];
+    __shared__ int si[kChunkWaves];
+    __shared__ u64 ss[kChunkWaves];
+    __shared__ uint32_t sn[kChunkWaves];
     __shared__ uint2 tab[kTab];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -546,8 +548,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
     const RowOpts o = row_opts(p, row);
     const bool hist = !o.greedy && o.filters;
-    if (tid < kBuckets) hs[tid] = 0;
-    if (tid < kTab) tab[tid] = g_exp2.e[tid];
+    for (int i = tid; i < kBuckets; i += kChunkThreads) hs[i] = 0;
+    for (int i = tid; i < kTab; i += kChunkThreads) tab[i] = g_exp2.e[i];
     float M = v[0];
 #pragma unroll
     for (int e = 1; e < kPer; ++e) M = max_clean(M, v[e]);
@@ -555,7 +557,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     if (lane == 0) sm[w] = M;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) M = fmaxf(M, sm[i]);
+    for (int i = 0; i < kChunkWaves; ++i) M = fmaxf(M, sm[i]);
     u64 S = 0;
     uint32_t n = 0;  // of the wave
 #pragma unroll
@@ -600,9 +602,10 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     if (lane == 0) { si[w] = first; ss[w] = S; sn[w] = n; }
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
-    if (hist && tid < kBuckets) wk.hist[at * kBuckets + tid] = hs[tid];
+    if (hist)
+        for (int i = tid; i < kBuckets; i += kChunkThreads) wk.hist[at * kBuckets + i] = hs[i];
     if (tid == 0) {
-        for (int i = 1; i < 8; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
+        for (int i = 1; i < kChunkWaves; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
         ChunkRec r{};
         r.G = G; r.S = S; r.m = M; r.first = first; r.n = n;
         wk.recs[at] = r;
@@ -632,9 +635,9 @@ __device__ __forceinline__ uint32_t first_key(F in, double edge, double off, uin
 constexpr int kFindThreads = 4 * kBuckets;
 template <bool DRAW>
 __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk, int nch) {
-    __shared__ double cG[128], cS[128], bsum[4][kBuckets], sd[16];
-    __shared__ uint32_t bcnt[4][kBuckets], cn[128], cfirst[128], su[16];
-    __shared__ float cm[128];
+    __shared__ double cG[kMaxChunks], cS[kMaxChunks], bsum[4][kBuckets], sd[16];
+    __shared__ uint32_t bcnt[4][kBuckets], cn[kMaxChunks], cfirst[kMaxChunks], su[16];
+    __shared__ float cm[kMaxChunks];
     __shared__ int sfound;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int bk = tid % kBuckets, part = tid / kBuckets;
@@ -704,14 +707,21 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         uint32_t cnt = 0;
         double sum = 0.0;
         const size_t at0 = (size_t)row * nch * kBuckets;
-#pragma unroll 8
-        for (int c = part; c < nch; c += 4) {
-            const int b = cm[c] > -INFINITY ? bk - bucket_shift(G, cG[c]) : -1;
-            const size_t at = at0 + (size_t)c * kBuckets + max(b, 0);
-            const u64 x = wk.hist[at];
-            if (b >= 0) {
-                cnt += (uint32_t)(x >> kCountBit);
-                sum += (double)(x & ((1ull << kCountBit) - 1)) * pow2(cG[c] - G - kHistFix);
+        constexpr int kAhead = 12;  // loads at once
+        for (int c0 = part; c0 < nch; c0 += 4 * kAhead) {
+            u64 x[kAhead];
+            int b[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int c = c0 + 4 * j;
+                b[j] = c < nch && cm[c] > -INFINITY ? bk - bucket_shift(G, cG[c]) : -1;
+                x[j] = wk.hist[at0 + (size_t)min(c, nch - 1) * kBuckets + max(b[j], 0)];
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (b[j] < 0) continue;
+                cnt += (uint32_t)(x[j] >> kCountBit);
+                sum += (double)(x[j] & ((1ull << kCountBit) - 1)) * pow2(cG[c0 + 4 * j] - G - kHistFix);
             }
         }
         bcnt[part][bk] = cnt;
@@ -810,7 +820,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
 template <typename T, bool DRAW>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T), NG = kPer / W;
-    __shared__ uint32_t sc[NG][8];
+    __shared__ uint32_t sc[NG][kChunkWaves];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const RowRec& rr = wk.rows[row];
@@ -818,7 +828,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
     if (mode != kModeBorder) return;
     ChunkRec* rec = wk.recs + (size_t)row * nch + c;
     const int bucket = rec->bucket;
-    if (DRAW && w == 7) {
+    if (DRAW && w == kChunkWaves - 1) {
         const u64* h = wk.hist + ((size_t)row * nch + c) * kBuckets;
         u64 a = 0;
 #pragma unroll
@@ -854,7 +864,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         uint32_t at = base + before[g];
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kChunkWaves; ++i) {
             if (i < w) at += sc[g][i];
             base += sc[g][i];
         }
@@ -875,8 +885,8 @@ struct ResolveShared {
     u64 above_s, goal;
     int found, last, chunk;
     double K;
-    u64 cadd[128];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kHistFix)
-    double cG[128];
+    u64 cadd[kMaxChunks];  // chunks' kept weights from the last bucket, units of 2^(G_chunk - kHistFix)
+    double cG[kMaxChunks];
     RowRec r;
 };
 constexpr int kHeld = 8;                        // members of the last bucket that a thread holds
@@ -893,19 +903,26 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
     // (wave 0 holds the chunks' weights from here to the draw)
-    u64 cabove[2] = {0, 0};
-    double cG[2] = {0, 0};
+    u64 cabove[kLaneChunks];
+    double cG[kLaneChunks];
+#pragma unroll
+    for (int e = 0; e < kLaneChunks; ++e) {
+        cabove[e] = 0;
+        cG[e] = 0.0;
+    }
     float u = 0.f;
     RowRec r;
     if (PLAIN) {
         if (w == 0) {
             const RowOpts o = row_opts(p, row);
             u = p.u[row];
-            float cm[2] = {-INFINITY, -INFINITY};
-            uint32_t n = 0, first = 0xffffffffu, cf[2] = {0, 0};
+            float cm[kLaneChunks], top = -INFINITY;
+            uint32_t n = 0, first = 0xffffffffu, cf[kLaneChunks];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < kLaneChunks; ++e) {
                 const int c = lane + 64 * e;
+                cm[e] = -INFINITY;
+                cf[e] = 0;
                 if (c < nch) {
                     cm[e] = recs[c].m;
                     cf[e] = (uint32_t)recs[c].first;
@@ -915,11 +932,12 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                         cabove[e] = recs[c].S;
                     }
                 }
+                top = max_clean(top, cm[e]);
                 s.cG[c] = cG[e];
                 s.cadd[c] = 0;
             }
             r = RowRec{};
-            r.m = wave_top(max_clean(cm[0], cm[1]));
+            r.m = wave_top(top);
             r.c = o.c;
             r.cut = key_of(-INFINITY) + 1;
             r.last = p.V;
@@ -927,7 +945,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             if (r.mode == kModeAll) r.G = grid_top(r.m, o.c);
             n = wave_add(n);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+            for (int e = 0; e < kLaneChunks; ++e)
                 if (cm[e] == r.m) first = min(first, cf[e]);
             first = wave_least(first);
             if (lane == 0) {
@@ -958,7 +976,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     if (!PLAIN && DRAW && w == 0) {
         u = p.u[row];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < kLaneChunks; ++e) {
             const int c = lane + 64 * e;
             if (c < nch && recs[c].m > -INFINITY) {
                 cG[e] = recs[c].G;
@@ -1118,33 +1136,37 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     }
     if (!DRAW) return;
     // the chunk in which the running sum passes the target (the last with weight
-    // if rounding lets none): wave 0, two chunks a lane
+    // if rounding lets none): wave 0, kLaneChunks a lane
     const int unit = border ? kHistFix : kFix;
     if (w == 0) {
-        double x[2], inc[2], tot[2];
+        double x[kLaneChunks], inc[kLaneChunks], K = 0.0;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < kLaneChunks; ++e) {
+            inc[e] = x[e] = 0.0;
+            if (64 * e >= nch) continue;
             cabove[e] += s.cadd[lane + 64 * e];
             x[e] = cabove[e] ? (double)cabove[e] * pow2(cG[e] - r.G - unit) : 0.0;
-            inc[e] = scan_add(x[e]);
-            tot[e] = last_lane(inc[e]);
+            inc[e] = K + scan_add(x[e]);
+            K = last_lane(inc[e]);
         }
-        const double K = tot[0] + tot[1];
         u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
         const double target = (double)u * K;
-        inc[1] += tot[0];
-        const u64 h0 = __ballot(x[0] > 0.0 && inc[0] > target), h1 = __ballot(x[1] > 0.0 && inc[1] > target);
-        const u64 l0 = __ballot(x[0] > 0.0), l1 = __ballot(x[1] > 0.0);
-        const int ch = h0 ? __ffsll(h0) - 1 : h1 ? 63 + __ffsll(h1) : l1 ? 127 - __clzll(l1) : 63 - __clzll(l0);
-        if (lane == (ch & 63)) {
-            const int e = ch >> 6;
-            const u64 have = e ? cabove[1] : cabove[0];
-            const double before = e ? inc[1] - x[1] : inc[0] - x[0];
-            const double local = fmin(fmax((target - before) * pow2(r.G - (e ? cG[1] : cG[0]) + unit), 0.0), 0x1p63);
-            s.chunk = ch;
-            s.K = K;
-            s.goal = min((u64)local, have - 1);
+        int ch = -1, last = 0;
+#pragma unroll
+        for (int e = 0; e < kLaneChunks; ++e) {
+            const u64 past = __ballot(x[e] > 0.0 && inc[e] > target), some = __ballot(x[e] > 0.0);
+            if (ch < 0 && past) ch = 64 * e + __ffsll(past) - 1;
+            if (some) last = 64 * e + 63 - __clzll(some);
         }
+        if (ch < 0) ch = last;
+#pragma unroll
+        for (int e = 0; e < kLaneChunks; ++e)
+            if (lane + 64 * e == ch) {
+                const double local = fmin(fmax((target - (inc[e] - x[e])) * pow2(r.G - cG[e] + unit), 0.0), 0x1p63);
+                s.chunk = ch;
+                s.K = K;
+                s.goal = min((u64)local, cabove[e] - 1);
+            }
     }
     __syncthreads();
     const int ch = s.chunk;
