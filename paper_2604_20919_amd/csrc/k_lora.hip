@@ -38,35 +38,48 @@ template <> struct Mma<float> {
     }
 };
 
-// 16 bytes of a row from element k on, zeros from n on (any alignment: the
-// hardware takes 16-byte loads at every address).  WHOLE: rows are whole pieces,
-// and lanes past the end read the row's start and drop it (a branch for them
-// would wait for the loads of the others, one piece after the other); what they
-// read is dropped by `inside` where it is used, so that nothing waits before.
-template <bool WHOLE, typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n) {
+// 16 bytes of a row of n elements from element k on, with what lies past its end
+// to be dropped by `inside`, where they are used, so that nothing waits before:
+// a branch for the lanes past the end would wait for the loads of the others, one
+// piece after the other.  (Any alignment: the hardware takes 16-byte loads at
+// every address.)  Lanes past the end read the row's start.  WHOLE: rows are whole
+// pieces; else a piece may reach into what follows the row, up to `end`.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n, const T* end) {
     constexpr int E = Mma<T>::kE;
     typename Mma<T>::Frag f;
-    if constexpr (WHOLE) {
-        __builtin_memcpy(&f, row + (k < n ? k : 0), 16);
+    const T* from = row + (k < n ? k : 0);
+    if (WHOLE || __all(from + E <= end)) {
+        __builtin_memcpy(&f, from, 16);
     } else {
         T v[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const T x = row[k + i < n ? k + i : 0];
-            v[i] = k + i < n ? x : (T)0;
-        }
+        for (int i = 0; i < E; ++i) v[i] = row[k + i < n ? k + i : 0];
         __builtin_memcpy(&f, v, 16);
     }
     return f;
 }
-template <typename F> __device__ __forceinline__ F inside(F f, bool in) {
+template <bool WHOLE, typename F> __device__ __forceinline__ F inside(F f, int k, int n) {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(F) / sizeof(f[0])); ++i) f[i] = in ? f[i] : 0;
+    for (int i = 0; i < (int)(sizeof(F) / sizeof(f[0])); ++i) f[i] = k + (WHOLE ? 0 : i) < n ? f[i] : 0;
     return f;
 }
 template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k) {
     typename Mma<T>::Frag f;
     __builtin_memcpy(&f, row + k, 16);
+    return f;
+}
+// one by one, zeros past the end: the incomplete last piece of a row
+template <typename T> __device__ __forceinline__ typename Mma<T>::Frag last_piece(const T* row, int k, int n) {
+    constexpr int E = Mma<T>::kE;
+    typename Mma<T>::Frag f;
+    T v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const T x = row[k + i < n ? k + i : 0];
+        v[i] = k + i < n ? x : (T)0;
+    }
+    __builtin_memcpy(&f, v, 16);
     return f;
 }
 
@@ -136,7 +149,7 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
 #pragma unroll 2
             for (; kb < end; kb += NW) step(kb * KB + 2 * E * g, [](const T* p, int k) { return piece(p, k); });
             if (kb < kb1)  // the row's last, incomplete piece
-                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return piece<false>(p, k, c.d_in); });
+                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return last_piece(p, k, c.d_in); });
 #pragma unroll
             for (int m = 0; m < MT; ++m)
                 if (m < mt) part[w][m][lane] = acc[m];
@@ -168,26 +181,20 @@ template <typename T> struct Inner {
     typedef typename Mma<T>::Frag Frag;
     Frag hi, lo;
 };
-template <bool WHOLE, typename T>
+// (pieces may reach past the row, the last one past the planes: the workspace does too)
+template <typename T>
 __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank, size_t stride, int planes) {
     constexpr int E = Mma<T>::kE;
     float v[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = 0.f;
-    if constexpr (WHOLE) {
-        const float* from = hr + (k < rank ? k : 0);
+    const float* from = hr + (k < rank ? k : 0);
 #pragma unroll 8
-        for (int p = 0; p < planes; ++p) {
-            float u[E];
-            __builtin_memcpy(u, from + p * stride, sizeof(u));
+    for (int p = 0; p < planes; ++p) {
+        float u[E];
+        __builtin_memcpy(u, from + p * stride, sizeof(u));
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[i] += u[i];
-        }
-    } else {
-#pragma unroll 2
-        for (int p = 0; p < planes; ++p)
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[i] += hr[p * stride + (k + i < rank ? k + i : 0)];
+        for (int i = 0; i < E; ++i) v[i] += u[i];
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = k + i < rank ? v[i] : 0.f;
@@ -227,6 +234,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
     // tile q's row 4 g + i is this lane's column col(q) + i; left operand's row n is column lcol(q)
     auto col = [&](int q) { return (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
     auto lcol = [&](int q) { return (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
+    const T* b_end = (const T*)c.b + (size_t)c.n_adapters * c.d_out * c.rank;
     Inner<T> hv[RB];
     Y y[CT / JW][W];
     int have = -1;  // the segment of hv
@@ -240,7 +248,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
             have = s;
 #pragma unroll
             for (int r = 0; r < RB; ++r)
-                hv[r] = inner_piece<WHOLE, T>(h + row * R + s * c.rank, (4 * r + g) * E, c.rank, (size_t)c.T * R, planes);
+                hv[r] = inner_piece<T>(h + row * R + s * c.rank, (4 * r + g) * E, c.rank, (size_t)c.T * R, planes);
         }
 #pragma unroll
         for (int q = 0; q < CT / JW; ++q) {
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
             for (int q = 0; q < CT; ++q) {
                 const T* B = (const T*)c.b + ((size_t)a * c.d_out + min(c0 + lcol(q), c1 - 1)) * c.rank;
 #pragma unroll
-                for (int r = 0; r < RB; ++r) bf[r][q] = piece<WHOLE>(B, (4 * r + g) * E, c.rank);
+                for (int r = 0; r < RB; ++r) bf[r][q] = piece<WHOLE>(B, (4 * r + g) * E, c.rank, b_end);
             }
         };
         unsigned long long left = todo;
@@ -290,7 +298,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
                 acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    const Frag f = WHOLE ? inside(bf[r][q], (4 * r + g) * E < c.rank) : bf[r][q];
+                    const Frag f = inside<WHOLE>(bf[r][q], (4 * r + g) * E, c.rank);
                     acc[q] = Mma<T>::run(f, hv[r].hi, acc[q]);
                     if constexpr (sizeof(T) == 2) acc[q] = Mma<T>::run(f, hv[r].lo, acc[q]);
                 }
@@ -388,7 +396,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
             };
             auto fetch = [&](int ch) {
                 if ((ch + 1) * KC <= c.d_in) load(ch, [](const T* p, int k) { return piece(p, k); });
-                else load(ch, [&](const T* p, int k) { return piece<false>(p, k, c.d_in); });
+                else load(ch, [&](const T* p, int k) { return last_piece(p, k, c.d_in); });
             };
             auto store = [&](int b) {
 #pragma unroll
@@ -494,6 +502,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
     Y* yo = (Y*)c.y_out + (size_t)min(t, c.T - 1) * c.yos;
     auto col = [&](int q) { return (q / JW) * 16 * JW + W * g + 4 * (q % JW); };
     auto lcol = [&](int q) { return (q / JW) * 16 * JW + W * (n / 4) + 4 * (q % JW) + n % 4; };
+    const T* b_end = (const T*)c.b + (size_t)c.n_adapters * c.d_out * c.rank;
     // the next block of columns in place of (s, b); false: the wave's last, or the projection's
     int left = per;
     auto next_block = [&](int& s, int& b) {
@@ -517,7 +526,8 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
             for (int i = 0; i < PP; ++i) {
                 const int q = tid + 64 * kWideWaves * i;
                 if (N % (64 * kWideWaves) && q >= N) break;
-                st[i] = piece<WHOLE>((const T*)c.b + ((size_t)a * c.d_out + min(c0 + q / (4 * RB), c1 - 1)) * c.rank, (q % (4 * RB)) * E, c.rank);
+                const T* row = (const T*)c.b + ((size_t)a * c.d_out + min(c0 + q / (4 * RB), c1 - 1)) * c.rank;
+                st[i] = piece<WHOLE>(row, (q % (4 * RB)) * E, c.rank, b_end);
             }
         };
         auto store = [&](int buf) {
@@ -526,7 +536,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
                 const int q = tid + 64 * kWideWaves * i;
                 if (N % (64 * kWideWaves) && q >= N) break;
                 *(Frag*)&bs[buf][(q / (4 * RB)) * P + (q % (4 * RB)) * E] =
-                    WHOLE ? inside(st[i], (q % (4 * RB)) * E < c.rank) : st[i];
+                    inside<WHOLE>(st[i], (q % (4 * RB)) * E, c.rank);
             }
         };
         Y y[CT / JW][W];
@@ -560,15 +570,9 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
                 for (int r = 0; r < RB; ++r) {
                     const int k = (4 * r + g) * E;
                     uint32_t v[E];
+                    __builtin_memcpy(v, hr + (k < c.rank ? k : 0), sizeof(v));
 #pragma unroll
-                    for (int i = 0; i < E; ++i) v[i] = 0;
-                    if (k + E <= c.rank) {
-                        __builtin_memcpy(v, hr + k, sizeof(v));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            if (k + i < c.rank) v[i] = __float_as_uint(hr[k + i]);
-                    }
+                    for (int i = 0; i < E; ++i) v[i] = k + i < c.rank ? v[i] : 0;
                     if constexpr (LO) {
 #pragma unroll
                         for (int i = 0; i < E; ++i) {
@@ -693,13 +697,12 @@ void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     const dim3 g(sh.tiles, (waves + 3) / 4, share);
     hipLaunchKernelGGL((k_lora_up<T, Y, RB, WHOLE>), g, dim3(256), 0, s, c, h, sh.planes, per);
 }
-template <typename T, typename Y>
+template <typename T, typename Y, bool WHOLE>
 void launch_up_rank(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     constexpr int K = 4 * Mma<T>::kE;  // a step of the product
-    if (c.rank % Mma<T>::kE) launch_up<T, Y, 128 / K, false>(c, sh, h, s);
-    else if (c.rank <= 32) launch_up<T, Y, 32 / K, true>(c, sh, h, s);
-    else if (c.rank <= 64) launch_up<T, Y, 64 / K, true>(c, sh, h, s);
-    else launch_up<T, Y, 128 / K, true>(c, sh, h, s);
+    if (c.rank <= 32) launch_up<T, Y, 32 / K, WHOLE>(c, sh, h, s);
+    else if (c.rank <= 64) launch_up<T, Y, 64 / K, WHOLE>(c, sh, h, s);
+    else launch_up<T, Y, 128 / K, WHOLE>(c, sh, h, s);
 }
 template <typename T>
 void launch_typed(const LoraCall& c, hipStream_t s) {
@@ -711,8 +714,13 @@ void launch_typed(const LoraCall& c, hipStream_t s) {
     } else {
         launch_down<T, false>(c, sh, h, s);
     }
-    if (c.y_bf16) launch_up_rank<T, bf16_t>(c, sh, h, s);
-    else launch_up_rank<T, float>(c, sh, h, s);
+    if (c.rank % Mma<T>::kE == 0) {
+        if (c.y_bf16) launch_up_rank<T, bf16_t, true>(c, sh, h, s);
+        else launch_up_rank<T, float, true>(c, sh, h, s);
+    } else {
+        if (c.y_bf16) launch_up_rank<T, bf16_t, false>(c, sh, h, s);
+        else launch_up_rank<T, float, false>(c, sh, h, s);
+    }
 }
 
 }  // namespace
@@ -720,7 +728,8 @@ void launch_typed(const LoraCall& c, hipStream_t s) {
 // (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
 size_t lora_workspace(int T, int rank, int n_seg) {
     const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
-    return (rows * rank * n_seg * 4 + 255) & ~(size_t)255;
+    // (and a piece of 32 bytes past the end)
+    return (rows * rank * n_seg * 4 + 32 + 255) & ~(size_t)255;
 }
 
 void launch_lora(const LoraCall& c, hipStream_t s) {
