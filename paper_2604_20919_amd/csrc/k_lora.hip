@@ -96,12 +96,12 @@ __device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int lane) {
     return a >= 0 && a < c.n_adapters ? a : -1;
 }
 
-// h = A x: one workgroup a tile of 16 rows, a range of k and every gridDim.z-th
-// of the tile's adapters, its waves taking 128-byte pieces of the rows in turn,
+// h = A x: one workgroup a tile of 16 rows, a range of k, 64 of A's rows and every
+// share-th of the tile's adapters (both in blockIdx.z), its waves taking 128-byte pieces of the rows in turn,
 // their sums added in LDS and left as plane blockIdx.y of h ([planes][T][R]) that
 // the second product adds up.
 template <typename T, int NW, bool LO>
-__global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
+__global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h, int share) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, KB = 8 * E, MT = 4;
     __shared__ f32x4 part[NW][MT][64];
@@ -117,61 +117,59 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h) {
     for (int ord = 0; left; ++ord) {
         const int a = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
         left &= ~__ballot(id == a);
-        if (ord % gridDim.z != blockIdx.z) continue;
-        for (int r0 = 0; r0 < R; r0 += 16 * MT) {
-            const int mt = min(MT, (R - r0 + 15) / 16);
-            const T* A[MT];
+        if (ord % share != (int)blockIdx.z % share) continue;
+        const int r0 = (int)blockIdx.z / share * 16 * MT, mt = min(MT, (R - r0 + 15) / 16);
+        const T* A[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) A[m] = (const T*)c.a + ((size_t)a * R + min(r0 + 16 * m + n, R - 1)) * c.d_in;
-            f32x4 acc[MT];
+        for (int m = 0; m < MT; ++m) A[m] = (const T*)c.a + ((size_t)a * R + min(r0 + 16 * m + n, R - 1)) * c.d_in;
+        f32x4 acc[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-            auto step = [&](int k, auto load) {
-                Frag xf[2], xlf[2];
+        for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto step = [&](int k, auto load) {
+            Frag xf[2], xlf[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                xf[e] = load(x, k + e * E);
+                if (LO) xlf[e] = load(xl, k + e * E);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if (m >= mt) break;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    xf[e] = load(x, k + e * E);
-                    if (LO) xlf[e] = load(xl, k + e * E);
-                }
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (m >= mt) break;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const Frag af = load(A[m], k + e * E);
-                        acc[m] = Mma<T>::run(af, xf[e], acc[m]);
-                        if (LO) acc[m] = Mma<T>::run(af, xlf[e], acc[m]);
-                    }
-                }
-            };
-            const int end = min(kb1, full);
-            int kb = kb0 + w;
-#pragma unroll 2
-            for (; kb < end; kb += NW) step(kb * KB + 2 * E * g, [](const T* p, int k) { return piece(p, k); });
-            if (kb < kb1)  // the row's last, incomplete piece
-                step(kb * KB + 2 * E * g, [&](const T* p, int k) { return last_piece(p, k, c.d_in); });
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-                if (m < mt) part[w][m][lane] = acc[m];
-            __syncthreads();
-            if (w < mt) {  // the tiles over the waves
-                f32x4 s = part[0][w][lane];
-#pragma unroll
-                for (int i = 1; i < NW; ++i) s += part[i][w][lane];
-                const int r = r0 + 16 * w + 4 * g;
-                if (mine == a) {
-                    float* o = h + ((size_t)blockIdx.y * c.T + t0 + n) * R + r;
-                    if (r + 4 <= R) {
-                        __builtin_memcpy(o, &s, 16);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (r + i < R) o[i] = s[i];
-                    }
+                    const Frag af = load(A[m], k + e * E);
+                    acc[m] = Mma<T>::run(af, xf[e], acc[m]);
+                    if (LO) acc[m] = Mma<T>::run(af, xlf[e], acc[m]);
                 }
             }
-            __syncthreads();
+        };
+        const int end = min(kb1, full);
+        int kb = kb0 + w;
+#pragma unroll 2
+        for (; kb < end; kb += NW) step(kb * KB + 2 * E * g, [](const T* p, int k) { return piece(p, k); });
+        if (kb < kb1)  // the row's last, incomplete piece
+            step(kb * KB + 2 * E * g, [&](const T* p, int k) { return last_piece(p, k, c.d_in); });
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            if (m < mt) part[w][m][lane] = acc[m];
+        __syncthreads();
+        if (w < mt) {  // the tiles over the waves
+            f32x4 s = part[0][w][lane];
+#pragma unroll
+            for (int i = 1; i < NW; ++i) s += part[i][w][lane];
+            const int r = r0 + 16 * w + 4 * g;
+            if (mine == a) {
+                float* o = h + ((size_t)blockIdx.y * c.T + t0 + n) * R + r;
+                if (r + 4 <= R) {
+                    __builtin_memcpy(o, &s, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (r + i < R) o[i] = s[i];
+                }
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -655,25 +653,26 @@ constexpr int kWideRows = 2048;
 constexpr int kGroups = 1024, kWideGroups = 512, kMaxPlanes = 8, kShare = 8;
 struct Shape {
     bool wide;
-    int tiles, share, planes;
+    int tiles, share, blocks, planes;  // blocks: of 64 of A's rows, apart
 };
-Shape shape_of(int T, int d_in, int es, int n_adapters) {
+Shape shape_of(int T, int d_in, int es, int n_adapters, int R) {
     Shape s;
     s.wide = T >= kWideRows;
     const int rows = s.wide ? kWideTile : 16;
     s.tiles = (T + rows - 1) / rows;
     s.share = s.wide ? 1 : std::min(std::min(kShare, n_adapters), T);
     const int pieces = s.wide ? (d_in * es + 255) / 256 : (d_in * es + 127) / 128 / 8;
-    const int groups = s.tiles * s.share, want = s.wide ? kWideGroups : kGroups;
+    s.blocks = s.wide ? 1 : (R + 63) / 64;
+    const int groups = s.tiles * s.share * s.blocks, want = s.wide ? kWideGroups : kGroups;
     s.planes = std::max(1, std::min(std::min((want + groups - 1) / groups, pieces), kMaxPlanes));
     return s;
 }
 
 template <typename T, bool LO>
 void launch_down(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
-    const dim3 g(sh.tiles, sh.planes, sh.share), wide(64 * kWideWaves);
+    const dim3 g(sh.tiles, sh.planes, sh.share * sh.blocks), wide(64 * kWideWaves);
     if (sh.wide) hipLaunchKernelGGL((k_lora_down_wide<T, LO>), g, wide, 0, s, c, h);
-    else hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h);
+    else hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h, sh.share);
 }
 template <typename T, typename Y, int RB, bool WHOLE>
 void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
@@ -706,7 +705,7 @@ void launch_up_rank(const LoraCall& c, const Shape& sh, float* h, hipStream_t s)
 }
 template <typename T>
 void launch_typed(const LoraCall& c, hipStream_t s) {
-    const Shape sh = shape_of(c.T, c.d_in, sizeof(T), c.n_adapters);
+    const Shape sh = shape_of(c.T, c.d_in, sizeof(T), c.n_adapters, c.n_seg * c.rank);
     float* h = (float*)c.ws;
     if constexpr (sizeof(T) == 2) {
         if (c.x_lo) launch_down<T, true>(c, sh, h, s);
