@@ -9,8 +9,8 @@
 // no larger.  So nothing is sorted: the end is found by histograms of counts
 // and weights, digit by digit of an order-preserving integer key of the logit.
 //
-// Weights are 64-bit fixed-point numbers (rounded once from a double), so sums
-// of them are exact and the same in every order, LDS atomics included.
+// Weights are rounded to 64-bit fixed-point numbers, so sums of them are exact
+// and the same in every order, LDS atomics included.
 #include <algorithm>
 
 #include "../../include/sd_verify.h"
@@ -870,7 +870,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
         }
 #pragma unroll
         for (int e = 0; e < W; ++e)
-            if (mine >> (g * W + e) & 1)
+            // (there is room for every member; the bound holds if someone writes the logits meanwhile)
+            if ((mine >> (g * W + e) & 1) && at < kList - off)
                 list[at++] = uint2{key_of(v[g * W + e]), (uint32_t)(c * kChunk + elem_at<T>(tid, g * W + e))};
     }
 }

@@ -322,3 +322,12 @@ def test_refusals_of_tensors():
     with pytest.raises(sv.SdError) as e:
         sv.sd_sample_filtered(z, u, token, ws[:0])
     assert e.value.status in (sv.SD_EINVAL, sv.SD_ENOMEM)
+
+
+def test_rows_beyond_32_bit_offsets():
+    n, V, stride = 3, 4099, (1 << 30) + 7
+    t, host = values("normal", n, V, "bf16", 111)
+    buf = torch.empty(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    z = buf.as_strided((n, V), (stride, 1))
+    z.copy_(t)
+    check(z, host, *options(n, 113), uniforms(n, 115))

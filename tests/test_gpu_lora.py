@@ -217,3 +217,18 @@ def test_refusals_of_tensors():
         buf = torch.zeros(6 * 48 + 48, device="cuda")
         sv.sd_lora_apply(w, ids, x, buf[:288].view(6, 48), buf[48:].view(6, 48), ws)
     assert e.value.status == sv.SD_EINVAL
+
+
+def test_rows_beyond_32_bit_offsets():
+    c = make(3, 72, [40], 8, 2, ids=[1, -1, 0], seed=6)
+    stride = (1 << 30) + 9
+    far = lambda t: torch.empty(2 * stride + t.shape[1], dtype=t.dtype, device="cuda").as_strided(t.shape, (stride, 1))
+    w = sv.make_lora(c["a"].cuda(), c["b"].cuda(), c["scale"].cuda(), c["segs"])
+    x, y = far(c["x"]), far(c["y"].bfloat16())
+    c["y"] = c["y"].bfloat16()
+    x.copy_(c["x"])
+    y.copy_(c["y"])
+    ws = torch.empty(sv.sd_lora_query_size(w, 3), dtype=torch.uint8, device="cuda")
+    sv.sd_lora_apply(w, torch.from_numpy(c["ids"]).cuda(), x, y, y, ws)
+    torch.cuda.synchronize()
+    expect(c, y.cpu())

@@ -345,3 +345,74 @@ def test_refusals():
     v.accept(0, 2)
     v.set_adapters(None)
     v.close()
+
+
+def test_sparse_draft_rows_with_options_and_adapters():
+    """Sparse draft rows against the dense rows they stand for, in a pass whose
+    users have options and adapters: the same decisions."""
+    prefix, L = [12, 70, 5], [3, 5, 2]
+    w, dw, v = context("tiny-bf16", prefix, L, seed=91)
+    b = w.batch(0)
+    sp = wl.sparsify(b, 16, 7)
+    q = oracle.expand_sparse_q(sp.idx, sp.val, sp.rest, w.model.vocab)
+    ad = Adapters(w.model, 2, 128, seed=3, sigma=0.02)
+    v.set_adapters(ad.layers)
+    for u, (o, a) in enumerate(zip(OPTIONS, (1, -1, 0))):
+        v.user_sampling(u, *o)
+        v.user_adapter(u, a)
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    drafts, idx, val, rest, dense = dev(b.drafts), dev(sp.idx), dev(sp.val), dev(sp.rest), dev(q)
+    for seed in range(4):
+        for i, u in enumerate(b.users):
+            v.reset_user(int(u), int(b.prefix_len[i]), int(b.root[i]))
+        v.verify_sparse(0, w.assign, w.draft_len, drafts, idx, val, rest, seed=seed)
+        a = v.accept(0, 3)
+        v.verify(0, w.assign, w.draft_len, drafts, dense, seed=seed)
+        d = v.accept(0, 3)
+        assert np.array_equal(a[0], d[0]) and np.array_equal(a[1], d[1])
+    v.close()
+
+
+def test_two_batches_at_once():
+    """Two pending batches on two streams, users of both with options and adapters,
+    give what each gives alone."""
+    prefix, L = [30, 5, 90, 17, 64, 2], [4, 2, 6, 3, 5, 1]
+    w = wl.custom_workload("tiny-bf16", prefix, L, seed=97, assign=[0, 1, 0, 1, 0, 1])
+    dw = DeviceWeights(w.model, w.seed)
+    v = make_verifier(w, dw, extra_ctx=32)
+    load_synthetic_kv(v, w)
+    ad = Adapters(w.model, 3, 12, seed=13)
+    v.set_adapters(ad.layers)
+    ins = []
+    for n in range(2):
+        b = w.batch(n)
+        ins.append((b, batch_to_device(b)))
+        for i, u in enumerate(b.users):
+            v.reset_user(int(u), int(b.prefix_len[i]), int(b.root[i]))
+    for u in range(6):
+        v.user_sampling(u, *OPTIONS[u])
+        v.user_adapter(u, u % 4 - 1)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+
+    def go(n):
+        b, (d, q, au) = ins[n]
+        v.verify(n, w.assign, w.draft_len, d, q, "stochastic", seed=4, accept_u=au, stream=streams[n])
+
+    alone = []
+    for n in range(2):
+        go(n)
+        lg = v.logits(n, ins[n][0].T, streams[n])
+        acc, tok = v.accept(n, 6)
+        torch.cuda.synchronize()
+        alone.append((lg.cpu().numpy(), acc, tok))
+    for rep in range(4):
+        go(0)
+        go(1)
+        for n in (1, 0):
+            lg = v.logits(n, ins[n][0].T, streams[n])
+            acc, tok = v.accept(n, 6)
+            torch.cuda.synchronize()
+            assert np.array_equal(lg.cpu().numpy(), alone[n][0])
+            assert np.array_equal(acc, alone[n][1]) and np.array_equal(tok, alone[n][2])
+    v.close()
