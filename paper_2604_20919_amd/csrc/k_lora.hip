@@ -69,6 +69,12 @@ template <typename T> __device__ __forceinline__ typename Mma<T>::Frag piece(con
     __builtin_memcpy(&f, row + k, 16);
     return f;
 }
+// 16 bytes that no one else reads, past what the caches keep for others
+template <typename T> __device__ __forceinline__ void load_once(T* to, const T* from) {
+    typedef f32x4 Any __attribute__((aligned(2)));  // (at any address, as above)
+    const f32x4 v = __builtin_nontemporal_load((const Any*)from);
+    __builtin_memcpy(to, &v, 16);
+}
 // one by one, zeros past the end: the incomplete last piece of a row
 template <typename T> __device__ __forceinline__ typename Mma<T>::Frag last_piece(const T* row, int k, int n) {
     constexpr int E = Mma<T>::kE;
@@ -475,6 +481,10 @@ __global__ __launch_bounds__(256) void k_lora_join(float* h, size_t n, int plane
     }
 }
 
+// Workgroups next to each other in launch order take the same rows' next columns:
+// those that run together then have whole rows between them, not one piece of
+// each row (8192 rows of 5120 columns, rank 64: 66 -> 60 us), and y passes by what
+// the caches keep of B and h (60 -> 56 us).
 template <typename T, typename Y, int RB, bool WHOLE>
 __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, const float* h, int per) {
     typedef typename Mma<T>::Frag Frag;
@@ -485,8 +495,8 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
     __shared__ __align__(16) T bs[2][16 * CT * P];
     __shared__ int ids[kWideTile];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int t0 = blockIdx.x * kWideTile, R = c.n_seg * c.rank;
-    int blk = blockIdx.y * per, seg0 = 0;
+    const int t0 = blockIdx.y * kWideTile, R = c.n_seg * c.rank;
+    int blk = blockIdx.x * per, seg0 = 0;
     auto blocks = [&](int s) { return (c.seg[s + 1] - c.seg[s] + 16 * CT - 1) / (16 * CT); };
     while (seg0 < c.n_seg && blk >= blocks(seg0)) blk -= blocks(seg0++);
     if (seg0 == c.n_seg) return;
@@ -545,7 +555,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
             for (int q = 0; q < CT / JW; ++q) {
                 const int k = c0 + col(q * JW);
                 if (k + W <= c1) {
-                    __builtin_memcpy(y[q], yi + k, 16);
+                    load_once(y[q], yi + k);
                 } else {
 #pragma unroll
                     for (int i = 0; i < W; ++i)
@@ -684,7 +694,7 @@ void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
         hipLaunchKernelGGL(k_lora_join<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, h, n, sh.planes);
         // as many blocks a workgroup as leave about four workgroups a CU
         const int per = std::max(1, (int)std::min<int64_t>(units / (4 * cu_count()), 16));
-        const dim3 g(sh.tiles, (blocks + per - 1) / per);
+        const dim3 g((blocks + per - 1) / per, sh.tiles);
         hipLaunchKernelGGL((k_lora_up_wide<T, Y, RB, WHOLE>), g, dim3(64 * kWideWaves), 0, s, c, h, per);
         return;
     }
