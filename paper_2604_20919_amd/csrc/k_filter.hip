@@ -64,7 +64,7 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 
 // What a row's filters are, with every value defined.
 struct RowOpts {
-    double c;      // log2(e) / T; greedy: unused
+    double c, rc;  // log2(e) / T and its inverse; greedy: 0
     double lmin;   // log2 of min_p, or -inf
     double p;      // top_p; off: +inf
     int k;         // top_k; off: INT_MAX
@@ -76,6 +76,7 @@ __device__ __forceinline__ RowOpts row_opts(const FilterP& p, int row) {
     const float t = p.temp ? p.temp[row] : 1.f;
     o.greedy = !(t > 0.f);
     o.c = o.greedy ? 0.0 : 1.4426950408889634 / (double)t;
+    o.rc = o.greedy ? 0.0 : (double)t * 0.6931471805599453;
     const int k = p.topk ? p.topk[row] : 0;
     o.k = k > 0 ? k : 0x7fffffff;
     const float tp = p.topp ? p.topp[row] : 1.f;
@@ -396,7 +397,7 @@ struct ChunkRec {
 };
 struct RowRec {
     double G, above, P;  // weights above the last bucket and the filter's bound, units of 2^G
-    double c, lmin;      // the row's options (RowOpts)
+    double c, rc, lmin;  // the row's options (RowOpts)
     int k;
     int mode;
     float m;
@@ -478,14 +479,14 @@ struct Grid {
 __device__ __forceinline__ bool grid_holds(float m, double c) {
     return c >= 4e-37 && fabs((double)m * c) < 0x1p40;
 }
-__device__ __forceinline__ Grid grid_of(double G, double c) {
-    return Grid{c, kGridAdd - G, (float)((G - 64.0) / c)};
+__device__ __forceinline__ Grid grid_of(double G, double c, double rc) {
+    return Grid{c, kGridAdd - G, (float)((G - 64.0) * rc)};
 }
 __device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)max_clean(z, g.zmin), g.c, g.add); }
 // an integer above m's logarithm on the grid
-__device__ __forceinline__ double grid_top(float m, double c) {
+__device__ __forceinline__ double grid_top(float m, double c, double rc) {
     const double G = floor((double)m * c) + 1.0;
-    return on_grid(grid_of(G, c), m) >= kGridAdd ? G + 1.0 : G;
+    return on_grid(grid_of(G, c, rc), m) >= kGridAdd ? G + 1.0 : G;
 }
 // bucket: 0 has the heaviest, widths of 1/8
 __device__ __forceinline__ int grid_bucket(double y) {
@@ -542,12 +543,20 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __shared__ u64 ss[kChunkWaves];
     __shared__ uint32_t sn[kChunkWaves];
     __shared__ uint2 tab[kTab];
+    __shared__ RowOpts opts;
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     float v[kPer];
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
-    const RowOpts o = row_opts(p, row);
-    const bool hist = !o.greedy && o.filters;
+    if (w == 0) {  // (divisions in 64 bits: for all waves they were an eighth of the work)
+        const RowOpts o = row_opts(p, row);
+        if (lane == 0) {
+            opts.c = o.c;
+            opts.rc = o.rc;
+            opts.greedy = o.greedy;
+            opts.filters = o.filters;
+        }
+    }
     for (int i = tid; i < kBuckets; i += kChunkThreads) hs[i] = 0;
     for (int i = tid; i < kTab; i += kChunkThreads) tab[i] = g_exp2.e[i];
     float M = v[0];
@@ -558,20 +567,22 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kChunkWaves; ++i) M = fmaxf(M, sm[i]);
+    const double oc = opts.c, orc = opts.rc;
+    const bool greedy = opts.greedy, hist = !greedy && opts.filters;
     u64 S = 0;
     uint32_t n = 0;  // of the wave
 #pragma unroll
     for (int e = 0; e < kPer; ++e) n += __popcll(__ballot(v[e] > -INFINITY));
     int first = 0x7fffffff;
-    double G = floor((double)M * o.c) + 1.0;
-    if (o.greedy) {
+    double G = floor((double)M * oc) + 1.0;
+    if (greedy) {
 #pragma unroll
         for (int e = kPer - 1; e >= 0; --e)
             if (v[e] == M) first = c * kChunk + elem_at<T>(tid, e);
         first = (int)wave_least((uint32_t)first);
-    } else if (M > -INFINITY && grid_holds(M, o.c)) {
-        G = grid_top(M, o.c);
-        const Grid g = grid_of(G, o.c);
+    } else if (M > -INFINITY && grid_holds(M, oc)) {
+        G = grid_top(M, oc, orc);
+        const Grid g = grid_of(G, oc, orc);
         // (four elements at a time in flight: more take registers from other waves)
         if (hist) {
 #pragma unroll
@@ -635,9 +646,10 @@ __device__ __forceinline__ uint32_t first_key(F in, double edge, double off, uin
 constexpr int kFindThreads = 4 * kBuckets;
 template <bool DRAW>
 __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk, int nch) {
-    __shared__ double cG[kMaxChunks], cS[kMaxChunks], bsum[4][kBuckets], sd[16];
+    __shared__ double cG[kMaxChunks], cS[kMaxChunks], unit[kMaxChunks], bsum[4][kBuckets], sd[16];
     __shared__ uint32_t bcnt[4][kBuckets], cn[kMaxChunks], cfirst[kMaxChunks], su[16];
     __shared__ float cm[kMaxChunks];
+    __shared__ int shift[kMaxChunks];  // from a chunk's buckets to the row's; kBuckets: none is shared
     __shared__ int sfound;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int bk = tid % kBuckets, part = tid / kBuckets;
@@ -653,11 +665,12 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     float m = -INFINITY;
     for (int c = lane; c < nch; c += 64) m = fmaxf(m, cm[c]);
     m = wave_top(m);
-    const double G = grid_top(m, o.c);  // that of the chunk with the maximum
+    const double G = grid_top(m, o.c, o.rc);  // that of the chunk with the maximum
     RowRec r{};
     r.G = G;
     r.m = m;
     r.c = o.c;
+    r.rc = o.rc;
     r.lmin = fmin(o.lmin, 0.0);
     r.k = o.k;
     r.last = p.V;
@@ -684,6 +697,11 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         }
         return;
     }
+    // the chunks' places and units in the row's histogram, once for all threads
+    if (tid < nch) {
+        shift[tid] = cm[tid] > -INFINITY ? bucket_shift(G, cG[tid]) : kBuckets;
+        unit[tid] = cm[tid] > -INFINITY ? pow2(cG[tid] - G - kHistFix) : 0.0;
+    }
     // total weight and number
     double S = 0.0;
     uint32_t n = 0;
@@ -703,6 +721,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         }
         return;
     }
+    __syncthreads();
     {
         uint32_t cnt = 0;
         double sum = 0.0;
@@ -714,14 +733,14 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int c = c0 + 4 * j;
-                b[j] = c < nch && cm[c] > -INFINITY ? bk - bucket_shift(G, cG[c]) : -1;
+                b[j] = c < nch ? bk - shift[c] : -1;
                 x[j] = wk.hist[at0 + (size_t)min(c, nch - 1) * kBuckets + max(b[j], 0)];
             }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 if (b[j] < 0) continue;
                 cnt += (uint32_t)(x[j] >> kCountBit);
-                sum += (double)(x[j] & ((1ull << kCountBit) - 1)) * pow2(cG[c0 + 4 * j] - G - kHistFix);
+                sum += (double)(x[j] & ((1ull << kCountBit) - 1)) * unit[c0 + 4 * j];
             }
         }
         bcnt[part][bk] = cnt;
@@ -739,7 +758,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     }
     __syncthreads();
     // from the heaviest bucket down, the first where a filter stops
-    const Grid g = grid_of(G, o.c);
+    const Grid g = grid_of(G, o.c, o.rc);
     if (tid < kBuckets) {
         for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
         const double y = on_grid(g, m);
@@ -772,8 +791,8 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
             const int c = c0 + lane;
             int b = -1;
             uint32_t k = 0;
-            if (c < nch && cm[c] > -INFINITY) {
-                b = border - bucket_shift(G, cG[c]);
+            if (c < nch) {
+                b = border - shift[c];
                 if (b >= 0) k = (uint32_t)(wk.hist[((size_t)row * nch + c) * kBuckets + b] >> kCountBit);
             }
             const uint32_t inc = scan_add(k);
@@ -882,7 +901,7 @@ struct ResolveShared {
     u64 wsum[kRowWaves];
     uint32_t wcnt[kRowWaves];
     uint32_t ties_of[64];
-    uint32_t lo, hi, above_c, ties, kept;
+    uint32_t lo, hi, above_c, ties, kept, key;
     u64 above_s, goal;
     int found, last, chunk;
     double K;
@@ -940,10 +959,11 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             r = RowRec{};
             r.m = wave_top(top);
             r.c = o.c;
+            r.rc = o.rc;
             r.cut = key_of(-INFINITY) + 1;
             r.last = p.V;
             r.mode = r.m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : grid_holds(r.m, o.c) ? kModeAll : kModeRow;
-            if (r.mode == kModeAll) r.G = grid_top(r.m, o.c);
+            if (r.mode == kModeAll) r.G = grid_top(r.m, o.c, o.rc);
             n = wave_add(n);
 #pragma unroll
             for (int e = 0; e < kLaneChunks; ++e)
@@ -989,13 +1009,14 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     }
     if (border) {
         const uint2* list = wk.list + (size_t)row * kList;
-        const int n = (int)r.n_list;
+        const int n = (int)r.n_list, w0 = __builtin_amdgcn_readfirstlane(tid & ~63);
         uint2 held[kHeld];
         auto hold = [&](int i0) {
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
                 const int i = i0 + j * kRowThreads + tid;
-                held[j] = i < n ? list[i] : uint2{0, 0};  // (no member has key 0)
+                held[j] = list[min(i, n - 1)];
+                if (i >= n) held[j].x = 0;  // (no member has key 0)
             }
         };
         hold(0);
@@ -1009,7 +1030,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
             // least: sums of kList stay below 2^63
             const double Gb = floor((double)key_value(hi) * r.c) + 2.0;
-            const Grid g = grid_of(Gb, r.c);
+            const Grid g = grid_of(Gb, r.c, r.rc);
             // (a bound of nothing stops at the first: rank 0 is kept)
             const double need = fmax((r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix), 0.5);
             uint32_t above_c = r.above_c;
@@ -1020,6 +1041,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                     if (n > kHeldAll) hold(i0);
 #pragma unroll
                     for (int j = 0; j < kHeld; ++j) {
+                        if (i0 + j * kRowThreads + w0 >= n) break;
                         const uint32_t key = held[j].x;
                         if (key < lo || key > hi) continue;
                         atomicAdd(&s.cnt[it][(key - lo) >> sf], 1u);
@@ -1056,9 +1078,20 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                     break;
                 }
                 lo = s.lo; hi = s.hi; above_c = s.above_c; above_s = s.above_s;
+                ties = s.ties;
+                if (sf && ties == 1 && n <= kHeldAll) {
+                    // one member: its key is the last, and it is kept (a filter stops at it, not before)
+#pragma unroll
+                    for (int j = 0; j < kHeld; ++j)
+                        if (held[j].x >= lo && held[j].x <= hi) s.key = held[j].x;
+                    __syncthreads();
+                    cut = s.key;
+                    take = ties;
+                    last = p.V;
+                    break;
+                }
                 if (sf) continue;
                 cut = lo;
-                ties = s.ties;
                 double jp = 4e9;
                 if (need < INFINITY) {
                     const double wt = (double)grid_weight(tab, on_grid(g, key_value(lo)));
@@ -1106,7 +1139,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             if (n > kHeldAll) hold(i0);
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
-                if (i0 + j * kRowThreads + (tid & ~63) >= n) break;
+                if (i0 + j * kRowThreads + w0 >= n) break;
                 const uint2 x = held[j];
                 const bool on = x.x > cut || (x.x == cut && (int)x.y <= last);
                 const u64 who = __ballot(on);
@@ -1114,7 +1147,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                 if (lane == 0) atomicAdd(&s.kept, (uint32_t)__popcll(who));
                 if (DRAW) {
                     const int c = (int)x.y / kChunk, c0 = __builtin_amdgcn_readlane(c, __ffsll(who) - 1);
-                    const u64 wt = on ? hist_weight(grid_weight(tab, on_grid(grid_of(s.cG[c], r.c), key_value(x.x)))) : 0;
+                    const u64 wt = on ? hist_weight(grid_weight(tab, on_grid(grid_of(s.cG[c], r.c, r.rc), key_value(x.x)))) : 0;
                     if (__ballot(on && c != c0)) {
                         if (on) atomicAdd(&s.cadd[c], wt);
                     } else {
@@ -1174,7 +1207,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     const u64 goal = s.goal;
     // its elements in index order: the first whose running sum exceeds the goal
     constexpr int E = kChunk / kRowThreads, W = 16 / sizeof(T);
-    const Grid g = grid_of(s.cG[ch], r.c);
+    const Grid g = grid_of(s.cG[ch], r.c, r.rc);
     const T* z = (const T*)p.z + (size_t)row * p.stride;
     const int i0 = ch * kChunk + tid * E;
     T raw[E];
