@@ -44,12 +44,17 @@ struct FilterP {
 };
 
 // NaN becomes -inf (never kept)
-__device__ __forceinline__ float clean(float z) { return z == z ? z : -INFINITY; }
+__device__ __forceinline__ float clean(float z) { return z > -INFINITY ? z : -INFINITY; }
 template <typename T> __device__ __forceinline__ float row_at(const T* z, int i) { return clean(ld<T>(z, i)); }
 // the larger of numbers that are no NaN (fmaxf would first quiet each)
 __device__ __forceinline__ float max_clean(float a, float b) {
     float r;
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float max_clean(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 // larger logit, larger key, and both zeros the same; -inf has the smallest key
@@ -488,11 +493,11 @@ __device__ __forceinline__ double grid_top(float m, double c, double rc) {
     const double G = floor((double)m * c) + 1.0;
     return on_grid(grid_of(G, c, rc), m) >= kGridAdd ? G + 1.0 : G;
 }
-// bucket: 0 has the heaviest, widths of 1/8
-__device__ __forceinline__ int grid_bucket(double y) {
-    const uint32_t q = __builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29);
-    return (int)(((uint32_t)kGridHi << 3) - q);
+// eighths, and bucket: 0 has the heaviest
+__device__ __forceinline__ uint32_t grid_eighths(double y) {
+    return __builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29);
 }
+__device__ __forceinline__ int grid_bucket(double y) { return (int)(((uint32_t)kGridHi << 3) - grid_eighths(y)); }
 
 // 2^y in units of 2^-kFix, to about 2^-30 of it: 2^(j/256) from a table in LDS
 // (2^30 of it, less the bits of kMagic, and the same as a float) times a second-order series in the rest of
@@ -537,7 +542,7 @@ __device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)f
 
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
-    __shared__ u64 hs[kBuckets];
+    __shared__ u64 hs[kBuckets];  // (the lightest first: one instruction less an element)
     __shared__ float sm[kChunkWaves];
     __shared__ int si[kChunkWaves];
     __shared__ u64 ss[kChunkWaves];
@@ -561,7 +566,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     for (int i = tid; i < kTab; i += kChunkThreads) tab[i] = g_exp2.e[i];
     float M = v[0];
 #pragma unroll
-    for (int e = 1; e < kPer; ++e) M = max_clean(M, v[e]);
+    for (int e = 1; e < kPer; e += 2) M = max_clean(M, v[e], v[min(e + 1, kPer - 1)]);
     M = wave_top(M);
     if (lane == 0) sm[w] = M;
     __syncthreads();
@@ -588,17 +593,17 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
 #pragma unroll
             for (int e0 = 0; e0 < kPer; e0 += 4) {
                 u64 x[4];
-                int b[4];
+                uint32_t b[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const double y = on_grid(g, v[e0 + e]);
                     x[e] = grid_weight(tab, y);
-                    b[e] = grid_bucket(y);
+                    b[e] = grid_eighths(y) - (((uint32_t)kGridHi << 3) - (kBuckets - 1));
                     S += x[e];
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (b[e] < kBuckets) atomicAdd(&hs[b[e]], hist_entry(x[e]));
+                    if (b[e] < (uint32_t)kBuckets) atomicAdd(&hs[b[e]], hist_entry(x[e]));
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -614,7 +619,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __syncthreads();
     const size_t at = (size_t)row * nch + c;
     if (hist)
-        for (int i = tid; i < kBuckets; i += kChunkThreads) wk.hist[at * kBuckets + i] = hs[i];
+        for (int i = tid; i < kBuckets; i += kChunkThreads) wk.hist[at * kBuckets + i] = hs[kBuckets - 1 - i];
     if (tid == 0) {
         for (int i = 1; i < kChunkWaves; ++i) { first = min(first, si[i]); S += ss[i]; n += sn[i]; }
         ChunkRec r{};
