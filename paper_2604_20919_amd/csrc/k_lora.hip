@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
     }
 }
 
-// Many rows: a workgroup takes kWideTile of them, a wave 16, and the adapter's
+// Many rows: a workgroup takes kWideTile of them, a wave 16, and 16 MT of the adapter's
 // rows go through LDS once for all waves (each wave loading them by itself took
 // as long as x: 8192 rows of 8192, rank 64, 92 us against 46 without).
 // Row tiles of the workgroup that have no row of the adapter skip the products.
@@ -360,10 +360,10 @@ __device__ __forceinline__ int next_id(const int* ids, int after, int lane) {
 // Workgroups next to each other in launch order take the same rows' next ranges
 // of k; up to eight of them, one on each of the chip's dies, so that a die's L2
 // holds its range of A (46 -> 42 us).
-template <typename T, bool LO>
+template <typename T, bool LO, int MT, int ST>
 __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, float* h) {
     typedef typename Mma<T>::Frag Frag;
-    constexpr int E = Mma<T>::kE, ST = 4, KC = 4 * E * ST, MT = 4;  // ST steps of the product a chunk
+    constexpr int E = Mma<T>::kE, KC = 4 * E * ST;  // ST steps of the product a chunk
     constexpr int P = KC + E;  // elements between the rows in LDS: 16 rows' pieces in different banks
     __shared__ __align__(16) T as[2][16 * MT * P];
     __shared__ int ids[kWideTile];
@@ -684,8 +684,23 @@ Shape shape_of(int T, int d_in, int es, int n_adapters, int R) {
 template <typename T, bool LO>
 void launch_down(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     const dim3 g(sh.tiles, sh.planes, sh.share * sh.blocks), wide(64 * kWideWaves);
-    if (sh.wide) hipLaunchKernelGGL((k_lora_down_wide<T, LO>), dim3(sh.planes, sh.tiles), wide, 0, s, c, h);
-    else hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h, sh.share);
+    if (sh.wide) {
+        const dim3 gw(sh.planes, sh.tiles);
+        if constexpr (LO) {
+            // x is read once for each block of A's rows: 128 of them, in chunks half as
+            // long (the registers), where there are more than 64 (8192 rows of 5120, two
+            // planes: 96 of A's rows 281 -> 253 us with the second product, 192 rows 328 -> 314;
+            // 63 rows, one block either way, 239 us with chunks half as long against 244, but
+            // 2805 rows 98 against 94; x in one plane, 192 rows: 283 against 260)
+            if (c.n_seg * c.rank > 64) {
+                hipLaunchKernelGGL((k_lora_down_wide<T, true, 8, 2>), gw, wide, 0, s, c, h);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((k_lora_down_wide<T, LO, 4, 4>), gw, wide, 0, s, c, h);
+        return;
+    }
+    hipLaunchKernelGGL((k_lora_down<T, 8, LO>), g, dim3(512), 0, s, c, h, sh.share);
 }
 template <typename T, typename Y, int RB, bool WHOLE>
 void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {

@@ -118,6 +118,18 @@ def test_strides_and_alignments(pad, offset, dtype, y_dtype):
     expect(c, apply(c, pad, offset, in_place=True))
 
 
+@pytest.mark.parametrize("T,d_in,segs,rank,dtype,y_dtype,planes", [
+    (2049, 333, [130, 40, 70], 33, "bf16", "f32", 2), (2500, 640, [200, 64, 64], 64, "bf16", "f32", 2),
+    (2177, 1000, [72], 128, "bf16", "bf16", 2), (2300, 129, [100, 30], 65, "bf16", "f32", 1),
+    (2048, 1, [1], 1, "bf16", "bf16", 1), (2100, 70, [66, 3], 5, "f32", "bf16", 1), (2200, 257, [140, 64, 64], 43, "f32", "f32", 1),
+])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (3, 1)])
+def test_many_rows(T, d_in, segs, rank, dtype, y_dtype, planes, pad, offset):
+    c = make(T, d_in, segs, rank, 4, dtype, y_dtype, planes, seed=T + pad)
+    expect(c, apply(c, pad, offset))
+    expect(c, apply(c, pad, offset, in_place=True))
+
+
 @pytest.mark.parametrize("name,ids", [
     ("none", [-1] * 40), ("one", [2] * 40), ("runs", [0] * 17 + [-1] * 3 + [3] * 16 + [1] * 4),
     ("alternating", [0, 1] * 20), ("all apart", list(range(40))), ("out of range", [0, 40, -2, 1 << 30, -(1 << 31), 39] * 6 + [0] * 4),
