@@ -46,7 +46,7 @@ enum {
                          bounded wait of one workgroup for another gave up */
     SD_ENOTIMPL = -6, /* configuration the library does not implement */
     SD_ENODEV = -7,   /* no usable gfx950 device */
-    SD_ELIMIT = -8    /* input beyond the fixed limits of sd_sample_logits_noalloc */
+    SD_ELIMIT = -8    /* input beyond a call's fixed limits */
 };
 
 enum { SD_F32 = 0, SD_BF16 = 1 };
@@ -546,7 +546,9 @@ sd_status sd_lora_apply(const sd_lora* w, int32_t n_rows, const int32_t* adapter
  * tokens the filters never drop, take no notice.  The options stay over
  * sd_user_reset and end with sd_user_release.
  * SD_EINVAL: user or an option out of range (temperature finite and >= 0,
- * top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1); SD_ESTATE: user pending.
+ * top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1); SD_ESTATE: user pending;
+ * SD_ELIMIT: a context whose vocab is above SD_FILTER_MAX_VOCAB or whose
+ * max_batch_tokens is above SD_FILTER_MAX_ROWS.
  */
 sd_status sd_user_sampling(sd_ctx* ctx, int32_t user, float temperature, int32_t top_k, float top_p, float min_p);
 

@@ -40,7 +40,7 @@ struct Layout {
     // slot buffers (byte offsets within the slot)
     size_t stage, tok, cs, x, ssq, h, ffn, qbuf, attn, apart, aml, gpart, logits, sstat, spart,
         spartB, lstat, zd, dnext, skcnt, result, filter, lora, slot_bytes;
-    size_t filter_bytes, lora_bytes;
+    size_t lora_bytes;
     size_t gpart_floats;
     int nsq;
     // global region after the slots
@@ -164,8 +164,7 @@ Layout plan(const sd_config& c) {
     L.dnext = take((size_t)L.Tmax * 4);
     L.skcnt = take((size_t)kSkCounters * 4);
     L.result = take((size_t)(2 * L.Bmax + 4) * 4);
-    L.filter_bytes = filter_workspace(L.Tmax, D.V);
-    L.filter = take(L.filter_bytes);
+    L.filter = take(D.V > SD_FILTER_MAX_VOCAB || L.Tmax > SD_FILTER_MAX_ROWS ? 0 : filter_workspace(L.Tmax, D.V));
     L.lora_bytes = lora_workspace(L.Tmax, kLoraRank, kLoraSegs);
     L.lora = take(L.lora_bytes);
     L.slot_bytes = s;
@@ -915,6 +914,8 @@ sd_status sd_user_sampling(sd_ctx* c, int32_t user, float temperature, int32_t t
     if (!(temperature >= 0.f) || !std::isfinite(temperature) || top_k < 0 || !(top_p > 0.f && top_p <= 1.f) ||
         !(min_p >= 0.f && min_p <= 1.f))
         return SD_EINVAL;
+    // the filter's kernels hold a row's chunks in LDS, and rows in a grid's y
+    if (c->D.V > SD_FILTER_MAX_VOCAB || c->lay.Tmax > SD_FILTER_MAX_ROWS) return SD_ELIMIT;
     User& u = c->users[user];
     if (u.pending_slot >= 0) return SD_ESTATE;
     u.temperature = temperature;

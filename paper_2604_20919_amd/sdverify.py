@@ -420,8 +420,8 @@ def sd_lora_apply(w: Lora, adapter, x, y_in, y_out, workspace, x_lo=None, stream
 
 def sd_user_sampling(ctx: int, user: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
                      min_p: float = 0.0) -> None:
-    _check("sd_user_sampling", lib().sd_user_sampling(ctx, user, float(temperature), int(top_k), float(top_p),
-                                                      float(min_p)))
+    top_k = max(-1, min(int(top_k), 2**31 - 1))  # (more than any vocab is off as well)
+    _check("sd_user_sampling", lib().sd_user_sampling(ctx, user, float(temperature), top_k, float(top_p), float(min_p)))
 
 
 def sd_adapters_set(ctx: int, layers) -> None:

@@ -416,3 +416,14 @@ def test_two_batches_at_once():
             assert np.array_equal(lg.cpu().numpy(), alone[n][0])
             assert np.array_equal(acc, alone[n][1]) and np.array_equal(tok, alone[n][2])
     v.close()
+
+
+def test_options_of_a_vocabulary_beyond_the_filters():
+    v = _sampler_verifier(sv.SD_FILTER_MAX_VOCAB + 4, 1, 1, 2)
+    with pytest.raises(sv.SdError) as e:
+        v.user_sampling(0, 0.5)
+    assert e.value.status == sv.SD_ELIMIT
+    v.close()
+    v = _sampler_verifier(sv.SD_FILTER_MAX_VOCAB, 1, 1, 2)
+    v.user_sampling(0, 0.5, top_k=1 << 40)
+    v.close()
