@@ -656,28 +656,40 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
     } while (next_block(s, b));
 }
 
-// Launch shapes.  Few rows: tiles of 16, up to kShare workgroups sharing out a
-// tile's adapters; many: tiles of kWideTile.  Ranges of k: about kGroups
-// (kWideGroups) workgroups in all, a 128-byte piece a wave (a chunk of 256
-// bytes) at least.  More ranges make the first product shorter and the second
-// longer, which adds them up (229 rows qkv 32B, 512 / 1024 groups: 13.3 + 10.9 /
-// 10.7 + 11.7 us; 8192 rows, 256 / 512 groups: 53 + 5 / 45 + 5.6 us).
-constexpr int kWideRows = 2048;
-constexpr int kGroups = 1024, kWideGroups = 512, kMaxPlanes = 8, kShare = 8;
+// Launch shapes.  Tiles of 16 rows with up to kShare workgroups sharing out a
+// tile's adapters, or (wide) of kWideTile rows, whose workgroup takes its adapters one after
+// the other.  Wide is the faster the more rows, the more inner results a row and
+// the longer the runs of one adapter, of which the host only knows the number of
+// adapters there are; from kWideWork rows x inner results an adapter on (16 adapters
+// at most) it mostly is.  us a call, tiles of 16 against wide, d_in 5120 / d_out
+// 10240 in three segments or 8192 / 5120 in one:
+//   one or two adapters, 24 inner results: 640 rows 24 / 28, 2047 rows 70 / 62
+//   one or two adapters, 64: 400 rows 21 / 18, 1024 rows 42 / 26, 4096 rows 120 / 68
+//   8 adapters in runs of 30, 16: 2047 rows 37 / 46; 64: 640 rows 40 / 35, 4096 rows 135 / 98
+//   32 adapters in runs of 7, 16: 4096 rows 101 / 174; 64: 2047 rows 122 / 149, 4096 rows 239 / 233
+// Ranges of k: about kGroups (kWideGroups) workgroups in all, a 128-byte piece a wave (a
+// chunk of 256 bytes) at least.  More ranges make the first product shorter and the
+// second longer, which adds them up (229 rows qkv 32B, 512 / 1024 groups: 13.3 +
+// 10.9 / 10.7 + 11.7 us; wide, 8192 rows of 64, 512 / 1024 groups: 104 / 114 us; 32 ranges
+// at most against 16: 640 rows of 64 23.5 / 26 us, but 2047 rows of 192 105 / 95).
+constexpr int kWideRows = 384, kWideWork = 8192, kWideFew = 2, kWideMany = 16, kWideInner = 16;
+constexpr int kGroups = 1024, kWideGroups = 512, kMaxPlanes = 8, kWidePlanes = 32, kShare = 8;
 struct Shape {
     bool wide;
     int tiles, share, blocks, planes;  // blocks: of 64 of A's rows, apart
 };
 Shape shape_of(int T, int d_in, int es, int n_adapters, int R) {
     Shape s;
-    s.wide = T >= kWideRows;
+    s.wide = T >= kWideRows && (int64_t)T * std::max(R, kWideInner) >=
+                                   (int64_t)kWideWork * std::max(kWideFew, std::min(n_adapters, kWideMany));
     const int rows = s.wide ? kWideTile : 16;
     s.tiles = (T + rows - 1) / rows;
     s.share = s.wide ? 1 : std::min(std::min(kShare, n_adapters), T);
     const int pieces = s.wide ? (d_in * es + 255) / 256 : (d_in * es + 127) / 128 / 8;
     s.blocks = s.wide ? 1 : (R + 63) / 64;
     const int groups = s.tiles * s.share * s.blocks, want = s.wide ? kWideGroups : kGroups;
-    s.planes = std::max(1, std::min(std::min((want + groups - 1) / groups, pieces), kMaxPlanes));
+    const int most = !s.wide ? kMaxPlanes : R <= 64 ? kWidePlanes : kWidePlanes / 2;
+    s.planes = std::max(1, std::min(std::min((want + groups - 1) / groups, pieces), most));
     return s;
 }
 
@@ -754,7 +766,7 @@ void launch_typed(const LoraCall& c, hipStream_t s) {
 
 // (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
 size_t lora_workspace(int T, int rank, int n_seg) {
-    const size_t rows = std::min((size_t)kMaxPlanes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
+    const size_t rows = std::min((size_t)kWidePlanes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
     // (and a piece of 32 bytes past the end)
     return (rows * rank * n_seg * 4 + 32 + 255) & ~(size_t)255;
 }

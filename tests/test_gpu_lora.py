@@ -130,6 +130,15 @@ def test_many_rows(T, d_in, segs, rank, dtype, y_dtype, planes, pad, offset):
     expect(c, apply(c, pad, offset, in_place=True))
 
 
+@pytest.mark.parametrize("T", [383, 384, 385, 640, 1023])
+@pytest.mark.parametrize("n,rank,segs,planes", [(1, 48, [136], 1), (3, 64, [100], 2), (3, 40, [64, 30, 33], 2), (17, 64, [72], 1)])
+def test_rows_between_few_and_many(T, n, rank, segs, planes):
+    c = make(T, 1160, segs, rank, n, planes=planes, seed=T + n)
+    expect(c, apply(c))
+    c = make(T, 5000, segs, rank, n, "f32", "bf16", seed=T + n, ids=np.sort(np.random.default_rng(T).integers(-1, n, T)))
+    expect(c, apply(c, in_place=True))
+
+
 @pytest.mark.parametrize("name,ids", [
     ("none", [-1] * 40), ("one", [2] * 40), ("runs", [0] * 17 + [-1] * 3 + [3] * 16 + [1] * 4),
     ("alternating", [0, 1] * 20), ("all apart", list(range(40))), ("out of range", [0, 40, -2, 1 << 30, -(1 << 31), 39] * 6 + [0] * 4),
