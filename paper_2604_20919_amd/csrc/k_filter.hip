@@ -160,7 +160,9 @@ __device__ __forceinline__ uint32_t wave_least(uint32_t v) {
 }
 
 // A whole row by one workgroup, whatever its values: the rows
-// that the chunked kernels below leave (see kModeRow).  Passes over the row:
+// that the chunked kernels below leave (see kModeRow).  Bound by its passes' latencies: 0.2 to
+// 0.9 ms for 1 to 32 rows of 151936 (equal logits, which meet in one bin, the
+// longest) against 0.03 ms for rows in chunks; such rows are rare.  Passes over the row:
 // maximum; weights' total; one a digit of the prefix's last key (9 bits
 // each); the last key's ties if not all of them are kept; the kept weights by
 // wave segments; the segment drawn from, or the rows written.
@@ -366,6 +368,8 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
 // the filtered rows.  The row itself is read by the first and, where a chunk has
 // members of the last bucket, the third kernel, and by the writing one.
 // ---------------------------------------------------------------------------
+// (Chunks of 8192 make half the records, but a chunk with a member of the last
+// bucket is read again whole: 416 rows of 151936, 146 against 130 us in all.)
 constexpr int kChunk = 4096;
 constexpr int kChunkThreads = 256, kChunkWaves = kChunkThreads / 64;
 constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
@@ -540,6 +544,10 @@ __device__ __forceinline__ double pow2(double d) { return d < -1000.0 ? 0.0 : ld
 // buckets between a chunk's numbering and the row's
 __device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)fmin(8.0 * (G - Gc), (double)kBuckets); }
 
+// Bound by vector instructions, about 30 an element: 416 rows of 151936 fp32 take
+// 64 us (4.0 TB/s; reading alone takes 40), rows without filters 34 us for 256 (4.5 TB/s).
+// One LDS atomic an element carries count and weight; copies of the histogram
+// against bank conflicts changed nothing (64 / 68 us with 2 / 4).
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];  // (the lightest first: one instruction less an element)
@@ -647,7 +655,8 @@ __device__ __forceinline__ uint32_t first_key(F in, double edge, double off, uin
 }
 
 // One workgroup a row; four threads hold each bucket of the row and take a
-// quarter of its chunks.
+// quarter of its chunks.  Bound by its chain of loads and barriers: 9 us for 1 to
+// 130 rows of 151936, 14 us for 416.
 constexpr int kFindThreads = 4 * kBuckets;
 template <bool DRAW>
 __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk, int nch) {
@@ -840,7 +849,9 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
 }
 
 // The members of the last bucket, in index order, and (DRAW) each chunk's
-// weights above it.
+// weights above it.  Chunks without members are not read: 4.5 us for one row of
+// 151936, 27 us for 416, whose chunks all have some (9.4 TB/s, most of it from the
+// caches).
 template <typename T, bool DRAW>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T), NG = kPer / W;
@@ -918,8 +929,10 @@ constexpr int kHeld = 8;                        // members of the last bucket th
 constexpr int kHeldAll = kHeld * kRowThreads;   // at once; longer lists are read again for each pass
 
 // One workgroup a row: the end of the prefix among the last bucket's members,
-// then the chunk and the element drawn.  PLAIN: no row has a filter, and the
-// chunks are merged here.
+// then the chunk and the element drawn.  Bound by its chain of passes over the
+// members: 11 us for one row of 151936, 26 us for 416.  PLAIN: no row has a
+// filter, and the chunks are merged here: 6.5 us for 256 rows and no more kernels,
+// against find, collect and resolve, 30 us together.
 template <typename T, bool DRAW, bool PLAIN>
 __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Work wk, int nch) {
     __shared__ union { RowShared row; ResolveShared s; } sh;
