@@ -43,7 +43,8 @@ template <> struct Mma<float> {
 // a branch for the lanes past the end would wait for the loads of the others, one
 // piece after the other.  (Any alignment: the hardware takes 16-byte loads at
 // every address.)  Lanes past the end read the row's start.  WHOLE: rows are whole
-// pieces; else a piece may reach into what follows the row, up to `end`.
+// pieces (229 rows, rank 16: 11.9 us, 12.5 without the difference); else a piece may
+// reach into what follows the row, up to `end` (rank 12: 17 us, element by element 109).
 template <bool WHOLE, typename T>
 __device__ __forceinline__ typename Mma<T>::Frag piece(const T* row, int k, int n, const T* end) {
     constexpr int E = Mma<T>::kE;
@@ -103,9 +104,13 @@ __device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int lane) {
 }
 
 // h = A x: one workgroup a tile of 16 rows, a range of k, 64 of A's rows and every
-// share-th of the tile's adapters (both in blockIdx.z), its waves taking 128-byte pieces of the rows in turn,
-// their sums added in LDS and left as plane blockIdx.y of h ([planes][T][R]) that
-// the second product adds up.
+// share-th of the tile's adapters (both in blockIdx.z), its waves taking 128-byte pieces
+// of the rows in turn, their sums added in LDS and left as plane blockIdx.y of h
+// ([planes][T][R]) that the second product adds up.  Bound by what it reads: 80 rows of
+// 25600 in two planes with 16 adapters of rank 32, 34 MB, 16 us (one workgroup taking
+// all of a tile's adapters: 52 us), 229 rows of 5120, 11 us (19); a plain read of 29 MB takes 13 us
+// on the card, most of it to get under way.  Deeper unrolling, other orders of the
+// pieces, twice the ranges of k or half the waves left both where they are.
 template <typename T, int NW, bool LO>
 __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h, int share) {
     typedef typename Mma<T>::Frag Frag;
@@ -218,7 +223,8 @@ __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank
 // y_out = y_in + scale B h: a wave takes 16 rows, `per` blocks of 16 CT columns
 // and every gridDim.z-th of the rows' adapters.  A row's h, y and scale do not
 // wait for the adapters: they are requested first, and each adapter's B while the
-// one before is multiplied.  RB: steps of the product that hold the rank.
+// one before is multiplied.  RB: steps of the product that hold the rank.  Bound by y
+// and B: 229 rows of 10240 columns, 27 MB, 12 us; 80 rows of 5120, 8 us.
 template <typename T, typename Y, int RB, bool WHOLE>
 __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int planes, int per) {
     typedef typename Mma<T>::Frag Frag;
