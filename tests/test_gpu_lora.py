@@ -253,3 +253,24 @@ def test_rows_beyond_32_bit_offsets():
     sv.sd_lora_apply(w, torch.from_numpy(c["ids"]).cuda(), x, y, y, ws)
     torch.cuda.synchronize()
     expect(c, y.cpu())
+
+
+@pytest.mark.parametrize("T,n", [(1 << 20, 1), (1 << 20, 40), (8191, 40)])
+def test_most_rows(T, n):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T + n)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")
+    a, b, scale, x, y = r(n, 2, 8), r(n, 8, 2), r(n), r(T, 8), r(T, 8)
+    ids = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    w = sv.make_lora(a, b, scale)
+    out = torch.empty_like(y)
+    ws = torch.empty(sv.sd_lora_query_size(w, T), dtype=torch.uint8, device="cuda")
+    sv.sd_lora_apply(w, ids, x, y, out, ws)
+    on, i = (ids >= 0)[:, None], ids.clamp(min=0).long()
+    d = lambda t: t.double()
+    f = lambda a, x, b, s: (b[i] * (a[i] * x[:, None, :]).sum(2)[:, None, :]).sum(2) * s[i][:, None]
+    ref = torch.where(on, d(y) + f(d(a), d(x), d(b), d(scale)), d(y))
+    size = torch.where(on, f(d(a).abs(), d(x).abs(), d(b).abs(), d(scale).abs()), 0.0)
+    # (as in expect: an fp32 sum of 8 and 2 products and its rounding)
+    tol = size * (8 + 2 + 8) * 2.0 ** -24 + ref.abs() * 2.0 ** -23
+    assert bool(((d(out) - ref).abs() <= tol).all())
