@@ -183,6 +183,50 @@ def test_other_rows_and_adapters_do_not_leak():
     assert torch.equal(got[rows], clean[rows])
 
 
+@pytest.mark.parametrize("rank,planes,dtype", [(64, 1, "bf16"), (50, 2, "bf16"), (64, 1, "f32")])
+def test_many_rows_do_not_leak(rank, planes, dtype):
+    T = 1030
+    ids = np.arange(T) // 7 % 3
+    c = make(T, 136, [96, 40], rank, 4, dtype, planes=planes, ids=ids, seed=rank)
+    clean = apply(c)
+    c["x"][[5, 700]] = float("nan")
+    c["a"][3] = float("nan")
+    c["b"][3] = float("inf")
+    got = apply(c)
+    on = np.ones(T, bool)
+    on[[5, 700]] = False
+    assert torch.equal(got[torch.from_numpy(on)], clean[torch.from_numpy(on)]) and torch.isnan(got[[5, 700]]).all()
+    c["a"][2] = float("inf")
+    c["b"][2] = float("nan")
+    got = apply(c, in_place=True)
+    on &= ids != 2
+    assert torch.equal(got[torch.from_numpy(on)], clean[torch.from_numpy(on)])
+
+
+def test_many_rows_in_a_graph_and_on_two_streams():
+    """Replays follow their inputs, with a run of the same sizes beside them."""
+    c = make(1300, 512, [256, 128], 40, 3, planes=2, seed=4)
+    w = sv.make_lora(c["a"].cuda(), c["b"].cuda(), c["scale"].cuda(), c["segs"])
+    ids, x, lo, y = torch.from_numpy(c["ids"]).cuda(), c["x"].cuda(), c["x_lo"].cuda(), c["y"].cuda()
+    out, beside = torch.empty_like(y), torch.empty_like(y)
+    ws, ws2 = (torch.empty(sv.sd_lora_query_size(w, 1300), dtype=torch.uint8, device="cuda") for _ in range(2))
+    s, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        sv.sd_lora_apply(w, ids, x, y, out, ws, x_lo=lo, stream=s)
+    for rep in range(4):
+        ids.copy_(torch.from_numpy(np.roll(c["ids"], 5 * rep)))
+        x.copy_(c["x"] * (1 + rep))
+        torch.cuda.synchronize()
+        g.replay()
+        sv.sd_lora_apply(w, ids, x, y, beside, ws2, x_lo=lo, stream=s2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, beside), rep
+        d = dict(c, ids=np.roll(c["ids"], 5 * rep), x=c["x"] * (1 + rep))
+        expect(d, out.cpu())
+
+
 def test_same_bits_alone_and_on_every_run():
     """A run gives the same bits again, in place too, and on another stream
     while one runs beside it."""
