@@ -147,6 +147,28 @@ def test_logits_with_adapters(model, prefix, L, ids):
     v.close()
 
 
+def test_adapters_of_high_rank_over_many_slots():
+    """396 slots and three adapters of rank 64: the adapters' 128-row kernels."""
+    ids = [i % 4 - 1 for i in range(33)]
+    w, dw, v = context("tiny-bf16", [8] * 33, [11] * 33, seed=63)
+    b = w.batch(0)
+    plain, _, _ = verify(v, w, b)
+    ad = Adapters(w.model, 3, 64, seed=5, sigma=0.03)
+    v.set_adapters(ad.layers)
+    for u, a in zip(b.users, ids):
+        v.user_adapter(int(u), a)
+    got, _, _ = verify(v, w, b)
+    err = logit_rel_err(got, reference(w, b, ad, ids))
+    assert err.max() < 2.3e-3, err.max()
+    mine = np.repeat(np.asarray(ids) >= 0, b.n_slots)
+    assert np.array_equal(got[~mine], plain[~mine])
+    st = torch.cuda.Stream()
+    for rep in range(3):
+        again, _, _ = verify(v, w, b, graph=True, stream=st)
+        assert np.array_equal(again, got), rep
+    v.close()
+
+
 @pytest.mark.parametrize("target", ["qkv", "o", "down"])
 def test_adapters_beside_one_projection(target):
     w, dw, v = context("tiny-bf16", [30, 4], [4, 2], seed=67)
