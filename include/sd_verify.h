@@ -434,9 +434,10 @@ sd_status sd_sample_logits_noalloc(int32_t n_users, const int32_t* user_ids, con
  *   r < top_k,   sum of w over ranks < r  <  top_p * (sum of all w),
  *   w_r >= min_p
  * hold: each filter looks at the whole distribution at temperature T, and a
- * token has to pass all.  Weights are computed to about 2^-30 of each and
- * summed as 64-bit integers: results are the same on every run, and those of
- * exact arithmetic unless a sum comes that near to its border.
+ * token has to pass all.  Weights are computed to about 2^-30 of each, or 2^-36
+ * of the row's largest where that is more, and summed as 64-bit integers:
+ * results are the same on every run, and those of exact arithmetic unless a sum
+ * comes that near to its border (a draw at u = 0 passes by tokens whose weights vanish).
  */
 typedef struct sd_filter {
     const float* temperature;

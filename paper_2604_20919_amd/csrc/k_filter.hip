@@ -488,8 +488,11 @@ struct Grid {
 __device__ __forceinline__ bool grid_holds(float m, double c) {
     return c >= 4e-37 && fabs((double)m * c) < 0x1p40;
 }
+// (zmin's rounding may only make it smaller: far from zero its steps are many
+// octaves, up to 2^18 of them, which the grid still holds)
 __device__ __forceinline__ Grid grid_of(double G, double c, double rc) {
-    return Grid{c, kGridAdd - G, (float)((G - 64.0) * rc)};
+    const double z = (G - 64.0) * rc;
+    return Grid{c, kGridAdd - G, (float)(z - fabs(z) * 0x1p-23)};
 }
 __device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)max_clean(z, g.zmin), g.c, g.add); }
 // an integer above m's logarithm on the grid
@@ -1265,7 +1268,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             at += x[e];
         }
         p.token[row] = i0 + hit;
-        if (p.prob) p.prob[row] = (float)(exp2((double)v * r.c - r.G) / s.K);
+        if (p.prob) p.prob[row] = (float)(exp2(fma((double)v, r.c, -r.G)) / s.K);  // (as the weights: one rounding)
     }
 }
 

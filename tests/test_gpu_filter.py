@@ -82,8 +82,14 @@ def padded(t, pad, offset=0):
     return view
 
 
-def check(z, host, t, k, p, m, u, stream=None, workspace=None):
-    """Both calls on device rows z (host: their values), against the oracle."""
+def check(z, host, t, k, p, m, u, stream=None, workspace=None, near=False):
+    """Both calls on device rows z (host: their values), against the oracle.
+
+    near: rows with weights so small that they vanish beside the largest, drawn
+    from at u = 0 too.  A weight is a multiple of 2^-37 of 2^G, G at most two
+    above the largest's logarithm: it is off by 2^-36 of the largest at most, and
+    a running sum by that times the number kept.  The token drawn is one whose
+    interval u comes that near to."""
     n, V = host.shape
     dev = lambda a: None if a is None else torch.from_numpy(a).cuda()
     token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
@@ -112,6 +118,12 @@ def check(z, host, t, k, p, m, u, stream=None, workspace=None):
         on = got[i, :V] > -np.inf
         ref = lw[on]
         assert np.all(np.abs(got[i, :V][on] - ref) <= 2 * 2.0 ** -24 * np.abs(ref) + 2.0 ** -149), where
+        if near and token[i] != tok:
+            w = np.exp(lw.astype(np.longdouble))
+            cum = np.cumsum(w)
+            x, eps = min(max(float(np.nan_to_num(u[i])), 0.0), 1.0 - 2.0 ** -24) * cum[-1], keep.sum() * 2.0 ** -36
+            tok, pr = token[i], float(w[token[i]] / cum[-1])
+            assert keep[tok] and cum[tok] - w[tok] - eps <= x <= cum[tok] + eps, where
         assert token[i] == tok, (where, token[i], tok)
         assert abs(prob[i] - pr) <= 2 * 2.0 ** -24 * pr, (where, prob[i], pr)
 
@@ -182,6 +194,26 @@ def test_large_vocabulary(kind, dtype):
     n, V = 8, 151936
     t, host = values(kind, n, V, dtype, 51)
     check(t.cuda(), host, *options(n, 53), uniforms(n, 55))
+
+
+@pytest.mark.parametrize("big", [-1e9, 1e10, 3e11, -7.5e7, 1e6])
+def test_masked_beside_logits_far_from_zero(big):
+    """Logits so far from zero that one step of fp32 is many octaves of weight,
+    with -inf and not-a-numbers beside them: those weigh nothing."""
+    n, V = 12, 9001
+    r = np.random.default_rng(81)
+    z = np.full((n, V), -np.inf, np.float32)
+    at = r.integers(0, V, (n, 40))
+    for i in range(n):
+        z[i, at[i]] = np.nextafter(np.float32(big), np.float32(-np.inf if i % 2 else big))
+        z[i, at[i, :3]] = np.float32(big)
+        z[i, at[i, 20:25]] = np.nan
+    t, host = torch.from_numpy(z), z
+    T = np.array([1.0, 0.5, 0.3, 2.0] * 3, np.float32)
+    check(t.cuda(), host, T, None, None, None, uniforms(n, 83), near=True)
+    check(t.cuda(), host, T, np.array([0, 2, 5, 100] * 3, np.int32), np.array([0.9, 0.5, 1.0, 0.999] * 3, np.float32),
+          np.array([0.0, 0.0, 0.5, 0.0] * 3, np.float32), uniforms(n, 85),
+          near=True)
 
 
 def test_largest_vocabulary():
