@@ -67,12 +67,14 @@ __device__ __forceinline__ float key_value(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
+constexpr int kMaxShift = 12;  // (2^17 octaves in all, which the logarithms' grid still holds)
 // What a row's filters are, with every value defined.
 struct RowOpts {
     double c, rc;  // log2(e) / T and its inverse; greedy: 0
     double lmin;   // log2 of min_p, or -inf
     double p;      // top_p; off: +inf
     int k;         // top_k; off: INT_MAX
+    int sh;        // buckets are 2^sh eighths of an octave wide
     bool greedy;
     bool filters;  // any of top-k, top-p, min-p
 };
@@ -82,6 +84,12 @@ __device__ __forceinline__ RowOpts row_opts(const FilterP& p, int row) {
     o.greedy = !(t > 0.f);
     o.c = o.greedy ? 0.0 : 1.4426950408889634 / (double)t;
     o.rc = o.greedy ? 0.0 : (double)t * 0.6931471805599453;
+    // (the lower the temperature, the more octaves a logit makes: the buckets of a row
+    // together are 13 to 27 wide in logits from T = 0.6 down, 22 at T = 1.  With eighths
+    // at every temperature the prefix of the 50 largest at T = 0.1 ended below them,
+    // and the whole-row path took 600 us for one row of 151936 and 1220 for 416, against 26
+    // and 104; the shift costs the first read 65 -> 68 us for 416 rows.)
+    o.sh = o.greedy ? 0 : min(max(-ilogbf(t * (1.f / 0.6f)), 0), kMaxShift);
     const int k = p.topk ? p.topk[row] : 0;
     o.k = k > 0 ? k : 0x7fffffff;
     const float tp = p.topp ? p.topp[row] : 1.f;
@@ -358,7 +366,8 @@ __device__ void filter_row(const FilterP& p, int row, RowShared& s) {
 //
 // k_filter_scan reads the row once: a chunk's maximum, its weights' sum and, for
 // rows with a filter, counts and weights by buckets an eighth of an octave wide
-// (in the logarithm of the weight).  Weights are taken relative to 2^G, G the
+// (in the logarithm of the weight; at low temperatures, where a step of the logit
+// is many octaves, 2, 4, 8 .. eighths).  Weights are taken relative to 2^G, G the
 // chunk's own largest logarithm rounded up, so that chunks need not know the
 // row's maximum, and buckets lie on one grid for all of them: what another
 // chunk counts moves by whole buckets, its sums by powers of two.
@@ -374,7 +383,7 @@ constexpr int kChunk = 4096;
 constexpr int kChunkThreads = 256, kChunkWaves = kChunkThreads / 64;
 constexpr int kPer = kChunk / kChunkThreads;  // elements a thread
 static_assert(kPer <= 32, "k_filter_collect marks them in 32 bits");
-constexpr int kBuckets = 256;                 // 32 octaves; what lies below is not counted
+constexpr int kBuckets = 256;                 // 32 octaves times 2^sh; what lies below is not counted
 constexpr int kList = 16384;                  // most members of the last bucket
 constexpr int kFix = 50;                      // chunk sums: multiples of 2^(G - 50), below 2^63
 // A bucket of a chunk is one number: the count from bit kCountBit up, and below it
@@ -407,7 +416,7 @@ struct ChunkRec {
 struct RowRec {
     double G, above, P;  // weights above the last bucket and the filter's bound, units of 2^G
     double c, rc, lmin;  // the row's options (RowOpts)
-    int k;
+    int k, sh;
     int mode;
     float m;
     uint32_t n_list, above_c;
@@ -490,8 +499,8 @@ __device__ __forceinline__ bool grid_holds(float m, double c) {
 }
 // (zmin's rounding may only make it smaller: far from zero its steps are many
 // octaves, up to 2^18 of them, which the grid still holds)
-__device__ __forceinline__ Grid grid_of(double G, double c, double rc) {
-    const double z = (G - 64.0) * rc;
+__device__ __forceinline__ Grid grid_of(double G, double c, double rc, int sh = 0) {
+    const double z = (G - (double)(32 + (32 << sh))) * rc;
     return Grid{c, kGridAdd - G, (float)(z - fabs(z) * 0x1p-23)};
 }
 __device__ __forceinline__ double on_grid(const Grid& g, float z) { return fma((double)max_clean(z, g.zmin), g.c, g.add); }
@@ -500,11 +509,14 @@ __device__ __forceinline__ double grid_top(float m, double c, double rc) {
     const double G = floor((double)m * c) + 1.0;
     return on_grid(grid_of(G, c, rc), m) >= kGridAdd ? G + 1.0 : G;
 }
-// eighths, and bucket: 0 has the heaviest
-__device__ __forceinline__ uint32_t grid_eighths(double y) {
-    return __builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29);
+// Buckets, 0 the heaviest, are 2^sh eighths of an octave wide and begin at
+// multiples of that, whatever G is: `rest` eighths of G are over.
+__device__ __forceinline__ int grid_eighths(double y) {
+    return (int)(__builtin_amdgcn_alignbit((uint32_t)__double2hiint(y), (uint32_t)__double2loint(y), 29) -
+                 ((uint32_t)kGridHi << 3));
 }
-__device__ __forceinline__ int grid_bucket(double y) { return (int)(((uint32_t)kGridHi << 3) - grid_eighths(y)); }
+__device__ __forceinline__ int grid_rest(double G, int sh) { return (int)((long long)(8.0 * G) & ((1ll << sh) - 1)); }
+__device__ __forceinline__ int grid_bucket(double y, int rest, int sh) { return -((grid_eighths(y) + rest) >> sh); }
 
 // 2^y in units of 2^-kFix, to about 2^-30 of it: 2^(j/256) from a table in LDS
 // (2^30 of it, less the bits of kMagic, and the same as a float) times a second-order series in the rest of
@@ -545,10 +557,13 @@ __device__ __forceinline__ u64 grid_weight(const uint2* tab, double y) {
 }
 __device__ __forceinline__ double pow2(double d) { return d < -1000.0 ? 0.0 : ldexp(1.0, (int)d); }
 // buckets between a chunk's numbering and the row's
-__device__ __forceinline__ int bucket_shift(double G, double Gc) { return (int)fmin(8.0 * (G - Gc), (double)kBuckets); }
+__device__ __forceinline__ int bucket_shift(double G, double Gc, int sh) {
+    const double e = ldexp(8.0, -sh);
+    return (int)fmin(floor(e * G) - floor(e * Gc), (double)kBuckets);
+}
 
 // Bound by vector instructions, about 30 an element: 416 rows of 151936 fp32 take
-// 64 us (4.0 TB/s; reading alone takes 40), rows without filters 34 us for 256 (4.5 TB/s).
+// 68 us (3.7 TB/s; reading alone takes 40), rows without filters 34 us for 256 (4.5 TB/s).
 // One LDS atomic an element carries count and weight; copies of the histogram
 // against bank conflicts changed nothing (64 / 68 us with 2 / 4).
 template <typename T>
@@ -569,6 +584,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
         if (lane == 0) {
             opts.c = o.c;
             opts.rc = o.rc;
+            opts.sh = o.sh;
             opts.greedy = o.greedy;
             opts.filters = o.filters;
         }
@@ -598,23 +614,24 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
         first = (int)wave_least((uint32_t)first);
     } else if (M > -INFINITY && grid_holds(M, oc)) {
         G = grid_top(M, oc, orc);
-        const Grid g = grid_of(G, oc, orc);
+        const int sh = __builtin_amdgcn_readfirstlane(opts.sh), rest = grid_rest(G, sh);
+        const Grid g = grid_of(G, oc, orc, sh);
         // (four elements at a time in flight: more take registers from other waves)
         if (hist) {
 #pragma unroll
             for (int e0 = 0; e0 < kPer; e0 += 4) {
                 u64 x[4];
-                uint32_t b[4];
+                int b[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const double y = on_grid(g, v[e0 + e]);
                     x[e] = grid_weight(tab, y);
-                    b[e] = grid_eighths(y) - (((uint32_t)kGridHi << 3) - (kBuckets - 1));
+                    b[e] = (grid_eighths(y) + rest) >> sh;
                     S += x[e];
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (b[e] < (uint32_t)kBuckets) atomicAdd(&hs[b[e]], hist_entry(x[e]));
+                    if (b[e] > -kBuckets) atomicAdd(&hs[b[e] + (kBuckets - 1)], hist_entry(x[e]));
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -690,6 +707,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     r.rc = o.rc;
     r.lmin = fmin(o.lmin, 0.0);
     r.k = o.k;
+    r.sh = o.sh;
     r.last = p.V;
     r.cut = key_of(-INFINITY) + 1;
     if (m == -INFINITY || o.greedy || !grid_holds(m, o.c)) {
@@ -716,7 +734,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     }
     // the chunks' places and units in the row's histogram, once for all threads
     if (tid < nch) {
-        shift[tid] = cm[tid] > -INFINITY ? bucket_shift(G, cG[tid]) : kBuckets;
+        shift[tid] = cm[tid] > -INFINITY ? bucket_shift(G, cG[tid], o.sh) : kBuckets;
         unit[tid] = cm[tid] > -INFINITY ? pow2(cG[tid] - G - kHistFix) : 0.0;
     }
     // total weight and number
@@ -775,12 +793,13 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     }
     __syncthreads();
     // from the heaviest bucket down, the first where a filter stops
-    const Grid g = grid_of(G, o.c, o.rc);
+    const int rest = grid_rest(G, o.sh);
+    const Grid g = grid_of(G, o.c, o.rc, o.sh);
     if (tid < kBuckets) {
         for (int i = 0; i < w; ++i) { ic += su[i]; is += sd[i]; }
         const double y = on_grid(g, m);
         const int bmin = o.lmin > -INFINITY
-            ? (int)fmin(-floor(8.0 * (y - 0x1.8p20 + r.lmin)), (double)kBuckets) : kBuckets;
+            ? (int)fmin(-floor(ldexp(floor(8.0 * (y - 0x1.8p20 + r.lmin)) + rest, -o.sh)), (double)kBuckets) : kBuckets;
         if (cnt > 0 && (ic >= (uint32_t)o.k || is >= r.P || tid >= bmin)) atomicMin(&sfound, tid);
     }
     __syncthreads();
@@ -827,9 +846,10 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         if (w < 3) {
             const int b = border + 1 - w;
             k = top + 1;  // (no bucket above the maximum's)
-            if (grid_bucket(on_grid(g, m)) <= b)
-                k = first_key([&](uint32_t x) { return grid_bucket(on_grid(g, key_value(x))) <= b; },
-                              (G - 0.125 * b - 0x1p-9) / o.c, 0x1p-31 / o.c + fabs(G / o.c) * 0x1p-22, top, lane);
+            if (grid_bucket(on_grid(g, m), rest, o.sh) <= b)
+                k = first_key([&](uint32_t x) { return grid_bucket(on_grid(g, key_value(x)), rest, o.sh) <= b; },
+                              (G - 0.125 * (ldexp((double)b, o.sh) + rest) - 0x1p-9) * o.rc,
+                              0x1p-31 * o.rc + fabs(G * o.rc) * 0x1p-22, top, lane);
         } else if (o.lmin > -INFINITY) {
             k = first_key([&](uint32_t x) {
                 const float z = key_value(x);
@@ -981,6 +1001,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             r.m = wave_top(top);
             r.c = o.c;
             r.rc = o.rc;
+            r.sh = o.sh;
             r.cut = key_of(-INFINITY) + 1;
             r.last = p.V;
             r.mode = r.m == -INFINITY ? kModeEmpty : o.greedy ? kModeDone : grid_holds(r.m, o.c) ? kModeAll : kModeRow;
@@ -1051,7 +1072,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
             // weights in units of 2^(Gb - kFix), Gb above the bucket's logarithms by one at
             // least: sums of kList stay below 2^63
             const double Gb = floor((double)key_value(hi) * r.c) + 2.0;
-            const Grid g = grid_of(Gb, r.c, r.rc);
+            const Grid g = grid_of(Gb, r.c, r.rc, r.sh);
             // (a bound of nothing stops at the first: rank 0 is kept)
             const double need = fmax((r.P - r.above) * ldexp(1.0, (int)fmin(fmax(r.G - Gb, -100.0), 100.0) + kFix), 0.5);
             uint32_t above_c = r.above_c;
@@ -1168,7 +1189,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
                 if (lane == 0) atomicAdd(&s.kept, (uint32_t)__popcll(who));
                 if (DRAW) {
                     const int c = (int)x.y / kChunk, c0 = __builtin_amdgcn_readlane(c, __ffsll(who) - 1);
-                    const u64 wt = on ? hist_weight(grid_weight(tab, on_grid(grid_of(s.cG[c], r.c, r.rc), key_value(x.x)))) : 0;
+                    const u64 wt = on ? hist_weight(grid_weight(tab, on_grid(grid_of(s.cG[c], r.c, r.rc, r.sh), key_value(x.x)))) : 0;
                     if (__ballot(on && c != c0)) {
                         if (on) atomicAdd(&s.cadd[c], wt);
                     } else {
@@ -1228,7 +1249,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     const u64 goal = s.goal;
     // its elements in index order: the first whose running sum exceeds the goal
     constexpr int E = kChunk / kRowThreads, W = 16 / sizeof(T);
-    const Grid g = grid_of(s.cG[ch], r.c, r.rc);
+    const Grid g = grid_of(s.cG[ch], r.c, r.rc, r.sh);
     const T* z = (const T*)p.z + (size_t)row * p.stride;
     const int i0 = ch * kChunk + tid * E;
     T raw[E];

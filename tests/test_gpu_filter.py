@@ -196,6 +196,21 @@ def test_large_vocabulary(kind, dtype):
     check(t.cuda(), host, *options(n, 53), uniforms(n, 55))
 
 
+@pytest.mark.parametrize("V,dtype", [(9001, "f32"), (40000, "bf16"), (151936, "f32")])
+@pytest.mark.parametrize("kind", ["normal", "coarse", "masked"])
+def test_low_temperatures(V, dtype, kind):
+    """Prefixes that end far below the largest weight."""
+    n = 16
+    t, host = values(kind, n, V, dtype, 91)
+    T = np.array([0.61, 0.59, 0.3, 0.29, 0.15, 0.1, 0.05, 0.02, 0.01, 1e-3, 3e-4, 1e-4, 1e-5, 1e-8, 0.2, 0.1], np.float32)
+    k = np.array([50, 1000, 50, 2000, 50, 1000, 100, 64, 5, 1000, 50, 700, 50, 50, 0, 0], np.int32)
+    p = np.array([1.0, 0.999, 1.0, 1.0] * 4, np.float32)
+    m = np.zeros(n, np.float32)
+    m[14:] = 1e-20, 1e-30
+    check(t.cuda(), host, T, k, p, m, uniforms(n, 93), near=True)
+    check(t.cuda(), host, T, k, None, m, uniforms(n, 95), near=True)
+
+
 @pytest.mark.parametrize("big", [-1e9, 1e10, 3e11, -7.5e7, 1e6])
 def test_masked_beside_logits_far_from_zero(big):
     """Logits so far from zero that one step of fp32 is many octaves of weight,
