@@ -563,9 +563,9 @@ __device__ __forceinline__ int bucket_shift(double G, double Gc, int sh) {
 }
 
 // Bound by vector instructions, about 30 an element: 416 rows of 151936 fp32 take
-// 68 us (3.7 TB/s; reading alone takes 40), rows without filters 34 us for 256 (4.5 TB/s).
+// 68 us (3.7 TB/s; reading alone takes 40), rows without filters 35 us for 256 (4.4 TB/s).
 // One LDS atomic an element carries count and weight; copies of the histogram
-// against bank conflicts changed nothing (64 / 68 us with 2 / 4).
+// against bank conflicts changed nothing (2 or 4 of them: -1 or +3 us).
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];  // (the lightest first: one instruction less an element)
