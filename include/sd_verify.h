@@ -304,7 +304,8 @@ sd_status sd_verify_batch_sparse(sd_ctx* ctx, int32_t batch, int32_t n_users,
  *   probs: device fp32 [rows][vocab], or NULL.  Receives p of each user's
  *          slot, evaluated with the same expression the race uses, so the
  *          drawn token is a draw from exactly these rows; pass them as
- *          sd_verify_batch's q.
+ *          sd_verify_batch's q.  A slot with no token to draw (see sd_accept)
+ *          gives a row of zeros.
  *   probs_row: host int32 [n_users] or NULL: the row of `probs` that
  *          receives user m's distribution (entries of users outside the
  *          batch are ignored; the caller guarantees the rows exist and are
@@ -328,10 +329,13 @@ sd_status sd_draft_batch(sd_ctx* ctx, int32_t batch, int32_t n_users, const int3
  *   n_accepted: host [M] (M of the sd_verify_batch call); entry m of every
  *               batch user receives a_m, the number of leading drafts accepted
  *   out_token:  host [M]; entry m receives the resampled token (a_m < l_m) or
- *               the bonus token (a_m == l_m)
+ *               the bonus token (a_m == l_m); -1 where an SD_STOCHASTIC pass
+ *               had no token to draw, the logits of slot a_m being -inf
+ *               throughout or their softmax NaN
  *   commit:     1 = advance each user (Sec. II-A step 4): i_m += 1 + a_m, root
- *               := out_token, pages trimmed to the new length; 0 = leave the
- *               user state unchanged (repeatable measurements)
+ *               := out_token, pages trimmed to the new length; a user whose
+ *               out_token is -1 stays where it was; 0 = leave the user state
+ *               unchanged (repeatable measurements)
  * Entries of users outside the batch are not touched.  Returns SD_EDEVICE,
  * without committing, if the GPU saw a token id >= vocab, or if a workgroup
  * of the split gate/up product stopped waiting for the partial sums of
@@ -387,7 +391,8 @@ sd_status sd_debug_wait_limit(sd_ctx* ctx, int32_t max_polls);
  *   logits:       device [T][V] fp32, rows user by user, slot 0 first
  *   mode, seed, round, accept_u: as for sd_verify_batch
  *   result:       device int32 [2*B + 1], written on `stream`: n_acc[B],
- *                 then token[B], then a flag word (nonzero: a draft token
+ *                 then token[B] (-1: no token to draw, as in sd_accept),
+ *                 then a flag word (nonzero: a draft token
  *                 was outside [0, V); n_acc and token are then undefined)
  * Decisions and tokens are those of sd_sample_logits on the same inputs
  * (the same kernels).  Asynchronous on `stream`; nothing waits.  Every call

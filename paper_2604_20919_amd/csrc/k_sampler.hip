@@ -426,6 +426,7 @@ __global__ __launch_bounds__(256) void k_samp_b2(SampP p, int chunks) {
             if (p2 > BP || (p2 == BP && ip2 < IP)) { BP = p2; IP = ip2; }
         }
         tok = (a < bv.L[b] && BR > 0.f) ? IR : IP;
+        if (tok == 0x7fffffff) tok = -1;  // the row has no token to draw: all -inf, or NaN
     }
     if (lane != 0) return;
     p.result[b] = a;
@@ -434,7 +435,8 @@ __global__ __launch_bounds__(256) void k_samp_b2(SampP p, int chunks) {
 
 // Decode-step output: the target distribution p of every slot, written
 // with the expression phase B's race evaluates, so a token drawn by the
-// race is a draw from exactly these rows.  One thread per four entries.
+// race is a draw from exactly these rows (what it passes by is 0: the whole row
+// where there is no token to draw).  One thread per four entries.
 __global__ __launch_bounds__(256) void k_probs(BatchView bv, const float* logits, const float* sstat,
                                                float* probs, int V) {
     const int t = blockIdx.y;
@@ -445,7 +447,10 @@ __global__ __launch_bounds__(256) void k_probs(BatchView bv, const float* logits
     float* o = probs + (size_t)bv.prow[bv.slot_b[t]] * V;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (k + e < V) o[k + e] = expf(z[k + e] - M) / S;
+        if (k + e < V) {
+            const float pk = expf(z[k + e] - M) / S;
+            o[k + e] = pk > 0.f ? pk : 0.f;
+        }
 }
 
 void launch_probs(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,

@@ -1299,7 +1299,8 @@ sd_status sd_accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_
             out_token[s.users[b]] = s.result_host[Bmax + b];
         }
         if (!s.sample_only) {
-            if (ok && commit) {
+            // (a user whose row gave no token stays where it is)
+            if (ok && commit && s.result_host[Bmax + b] >= 0) {
                 u.prefix += 1 + s.result_host[b];
                 u.root = s.result_host[Bmax + b];
             }

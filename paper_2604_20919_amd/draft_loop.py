@@ -38,7 +38,7 @@ from .verifier import Verifier
 @dataclass
 class RoundResult:
     n_acc: np.ndarray        # accepted drafts per batch user
-    token: np.ndarray        # target's output token per batch user
+    token: np.ndarray        # target's output token per batch user (-1: none, the user stays)
     drafts: np.ndarray       # the drafts of this round, users ascending
     draft_ms: float          # wall time of the drafting steps (host clock)
     verify_ms: float         # wall time of verify + accept
@@ -94,6 +94,11 @@ class DraftLoop:
             for i, u in enumerate(users):
                 if L[u] > j:
                     drafts[doff[i] + j] = tok[u]
+            none = [int(u) for u in users if L[u] > j and tok[u] < 0]
+            if none:  # nothing can be verified: back to where the round began
+                for u, (P0, root) in start.items():
+                    self.dv.reset_user(u, P0, root)
+                raise RuntimeError(f"drafting model: no token to draw for users {none} (logits -inf or NaN)")
         t1 = time.perf_counter()
         self.drafts[:drafts.size].copy_(torch.from_numpy(drafts))
         torch.cuda.synchronize()
@@ -107,7 +112,7 @@ class DraftLoop:
             u = int(u)
             P0, _ = start[u]
             a = int(n_acc[u])
-            if not commit:
+            if not commit or tok[u] < 0:  # (without a token the target has not advanced either)
                 self.dv.reset_user(u, P0, start[u][1])
                 continue
             if a == int(L[u]):

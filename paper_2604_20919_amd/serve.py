@@ -172,7 +172,8 @@ class GpuVerify:
         for m in users:
             self.accepted.append(int(n_acc[m]))
             self.drafted.append(self.l[m])
-        return int(sum(int(n_acc[m]) + 1 for m in users))
+        # (a user without a token, out_token -1, has not advanced)
+        return int(sum(int(n_acc[m]) + 1 for m in users if tok[m] >= 0))
 
     @property
     def acceptance(self) -> float:
