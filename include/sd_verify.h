@@ -160,8 +160,8 @@ sd_status sd_verify_query_sizes(const sd_config* cfg, uint64_t* kv_pool_bytes,
  * kv_pool / workspace / weight_pack: device buffers of at least the queried
  *   sizes, 256-byte aligned, owned by the caller, kept until destroy
  *   (weight_pack may be NULL when its size is 0).  The KV pool is zero-filled
- *   here (attention reads whole blocks past a context's end and needs those
- *   rows finite); KV contents written later must be finite too.
+ *   here.  Rows past a context's end, whatever a page's earlier user left in
+ *   them, have no part in its attention.
  *   Initialisation work runs on the null stream and is synchronised before
  *   returning.
  * out: receives the context.  Errors: SD_EINVAL (cfg, NULL pointer),

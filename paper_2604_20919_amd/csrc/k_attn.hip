@@ -117,6 +117,22 @@ __device__ __forceinline__ void lds_read8(bf16x8 (&f)[8], uint32_t a) {
         : "memory");
 }
 
+// V^T fragments (a lane: 8 tokens) with all tokens but the first n of the lane's
+// zero: rows of a page past a user's context may hold anything -- what another
+// user, or a pass that was not committed, left there -- and p = 0 times an
+// infinity would not be 0.  Only a context's last block has such rows.
+__device__ __forceinline__ void zero_past(bf16x8 (&vf)[8], int n) {
+    uint32_t keep[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) keep[w] = n > 2 * w + 1 ? 0xffffffffu : n > 2 * w ? 0xffffu : 0u;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        uint4 v = __builtin_bit_cast(uint4, vf[dt]);
+        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+        vf[dt] = __builtin_bit_cast(bf16x8, v);
+    }
+}
+
 // One 32-token block (its K and V^T fragments) for one row tile.  Scores stay
 // in the raw (unscaled) domain until the exponent, which folds the scale in:
 // p = 2^(s*c - m*c) with c = log2(e)/sqrt(hd).  Blocks that every row sees
@@ -229,9 +245,8 @@ __device__ __forceinline__ void attn_ring(const AttnP& p, const AttnItem& ac, At
     typedef __attribute__((address_space(3))) void lds_void;
     // Requests block blk into LDS buffer buf: four 16-byte direct loads per
     // thread.  Tokens past the chunk end are read from the chunk's last page
-    // (the page index is clamped); their scores are masked, and V there is
-    // finite (pool zeroed at init, later only model values), so p = 0
-    // contributes exactly 0.
+    // (the page index is clamped); their scores are masked and V there is
+    // taken as 0 (zero_past).
     auto issue = [&](int blk, uint4* buf) __attribute__((always_inline)) {
         const int t0 = c0 + blk * 32;
         const uint32_t pb0 = (uint32_t)pt[min(t0, c1 - 1) >> 4] * page_bytes;
@@ -265,10 +280,12 @@ __device__ __forceinline__ void attn_ring(const AttnP& p, const AttnItem& ac, At
         for (int i = 0; i < RT_MAX; ++i) {
             if (!act[i]) continue;
             attn_block(kfr, vfr, qf[i], ql[i], m[i], l[i], o[i], lim[i], t0, c1, lg, full, p.scale_log2, [&]() {
-                if (i == 0)
+                if (i == 0) {
                     asm volatile("s_waitcnt lgkmcnt(0)"
                                  : "+v"(vfr[0]), "+v"(vfr[1]), "+v"(vfr[2]), "+v"(vfr[3]), "+v"(vfr[4]),
                                    "+v"(vfr[5]), "+v"(vfr[6]), "+v"(vfr[7]));
+                    if (t0 + 32 > c1) zero_past(vfr, c1 - t0 - 8 * lg);
+                }
             });
         }
     };
@@ -343,7 +360,7 @@ __device__ __forceinline__ void attn_few(const AttnP& p, const AttnItem& ac, int
     const uint32_t ko1 = gk + (uint32_t)(((kt1 & 15) * HD + 8 * lg) * 2);
     const uint32_t vo = gv + (uint32_t)((lr * kPageTokens + 8 * (lg & 1)) * 2);
     auto load = [&](bf16x8 (&kf)[8], bf16x8 (&vf)[8], int blk) __attribute__((always_inline)) {
-        // tokens past the chunk end: the chunk's last page (masked, V finite)
+        // tokens past the chunk end: the chunk's last page (masked, V zeroed)
         const int t0 = c0 + blk * 32;
         const uint32_t pb0 = (uint32_t)pt[min(t0, c1 - 1) >> 4] * page_bytes;
         const uint32_t pb1 = (uint32_t)pt[min(t0 + 16, c1 - 1) >> 4] * page_bytes;
@@ -377,8 +394,9 @@ __device__ __forceinline__ void attn_few(const AttnP& p, const AttnItem& ac, int
     f32x4 o[8];
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto block = [&](const bf16x8 (&kf)[8], const bf16x8 (&vf)[8], int k) __attribute__((always_inline)) {
+    auto block = [&](const bf16x8 (&kf)[8], bf16x8 (&vf)[8], int k) __attribute__((always_inline)) {
         const int t0 = c0 + k * 32;
+        if (t0 + 32 > c1) zero_past(vf, c1 - t0 - 8 * lg);
         attn_block(kf, vf, qf, ql, m, l, o, lim, t0, c1, lg, t0 + 32 <= c1 && t0 + 31 <= prefix, p.scale_log2, [] {});
     };
     if (stripe < nblk) block(ka, va, stripe);

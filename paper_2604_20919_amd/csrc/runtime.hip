@@ -827,9 +827,7 @@ sd_status sd_verify_init(const sd_config* cfg, const sd_weights* w, void* kv_poo
         b.bmax = L.Bmax;
     }
     if (ok) {
-        // The attention kernel reads whole 32-token blocks and multiplies the
-        // value rows past a user's context by an exact 0; zeroing the pool
-        // once keeps never-written rows finite (0 * NaN would not be 0).
+        // every row of the pool holds a number from the start
         const Dims& D = c->D;
         const size_t kv_bytes = (size_t)D.L * cfg->n_pages * 2 * D.hkv * kPageTokens * D.hd * c->kv.esize;
         ok &= hipMemset(kv_pool, 0, kv_bytes) == hipSuccess;
