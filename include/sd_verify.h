@@ -544,13 +544,16 @@ sd_status sd_lora_apply(const sd_lora* w, int32_t n_rows, const int32_t* adapter
  * sd_verify_batch, sd_verify_batch_graph, sd_verify_batch_sparse,
  * sd_sample_logits or sd_draft_batch on (host values, as in sd_filter;
  * temperature 0: the largest logit alone; top_k 0, top_p 1, min_p 0: off).  A
- * new user has 1, 0, 1, 0.  In a SD_STOCHASTIC pass with such a user every
- * slot's logits are replaced by their filtered rows (sd_filter_logits)
- * before accept/resample: the user's drafts are verified against, and its
- * tokens drawn from, the filtered distribution, which sd_draft_batch's probs
- * and sd_debug_logits then show.  SD_GREEDY and SD_FORCE passes, whose
- * tokens the filters never drop, take no notice.  The options stay over
- * sd_user_reset and end with sd_user_release.
+ * new user has 1, 0, 1, 0, which is without options.  In a SD_STOCHASTIC pass
+ * the logits of such a user's slots are replaced by their filtered rows
+ * (sd_filter_logits) before accept/resample: its drafts are verified against,
+ * and its tokens drawn from, the filtered distribution, which
+ * sd_draft_batch's probs then show.  Users without options get the decisions,
+ * tokens and probs of a pass without such users, bit for bit; sd_debug_logits
+ * shows all rows of the pass relative to their largest, as sd_filter_logits
+ * writes them (not-a-numbers of users without options stay).  SD_GREEDY and
+ * SD_FORCE passes, whose tokens the filters never drop, take no notice.  The
+ * options stay over sd_user_reset and end with sd_user_release.
  * SD_EINVAL: user or an option out of range (temperature finite and >= 0,
  * top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1); SD_ESTATE: user pending;
  * SD_ELIMIT: a context whose vocab is above SD_FILTER_MAX_VOCAB or whose

@@ -41,7 +41,9 @@ struct FilterP {
     int32_t* kept;
     float* out;          // [n][ostride] (filtered rows)
     int64_t ostride;
+    const int32_t* only; // [n] or null: rows where it is 0 are left as they are
 };
+__device__ __forceinline__ bool left_alone(const FilterP& p, int row) { return p.only && p.only[row] == 0; }
 
 // NaN becomes -inf (never kept)
 __device__ __forceinline__ float clean(float z) { return z > -INFINITY ? z : -INFINITY; }
@@ -577,6 +579,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __shared__ RowOpts opts;
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (left_alone(p, row)) return;
     float v[kPer];
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
     if (w == 0) {  // (divisions in 64 bits: for all waves they were an eighth of the work)
@@ -687,6 +690,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     __shared__ int sfound;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int bk = tid % kBuckets, part = tid / kBuckets;
+    if (left_alone(p, row)) return;
     ChunkRec* recs = wk.recs + (size_t)row * nch;
     const RowOpts o = row_opts(p, row);
     if (tid < nch) {
@@ -881,6 +885,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
     __shared__ uint32_t sc[NG][kChunkWaves];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (left_alone(p, row)) return;
     const RowRec& rr = wk.rows[row];
     const int mode = rr.mode;
     if (mode != kModeBorder) return;
@@ -962,6 +967,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
     __shared__ uint2 tab[kTab];
     ResolveShared& s = sh.s;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (left_alone(p, row)) return;
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
     // (wave 0 holds the chunks' weights from here to the draw)
     u64 cabove[kLaneChunks];
@@ -1301,6 +1307,7 @@ template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T);
     const int c = blockIdx.x, row = blockIdx.y;
+    if (left_alone(p, row)) return;
     const RowRec& rr = wk.rows[row];
     const int mode = rr.mode;
     if (mode == kModeRow) return;  // written by k_filter_resolve
@@ -1344,7 +1351,33 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work 
     }
 }
 
+// Rows as sd_filter_logits writes them without options, z - max; rows of `own`
+// (filtered already: their largest is 0) as they are.  Not-a-numbers stay.  A
+// diagnostic's copy, one workgroup a row.
+__global__ __launch_bounds__(1024) void k_shown_rows(const float* z, const int32_t* own, int V, float* out) {
+    __shared__ float sm[16];
+    const size_t at = (size_t)blockIdx.x * V;
+    float m = -INFINITY;
+    if (own[blockIdx.x]) {
+        m = 0.f;
+    } else {
+        for (int i = threadIdx.x; i < V; i += 1024) m = fmaxf(m, clean(z[at + i]));
+        m = wave_top(m);
+        if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
+        __syncthreads();
+        for (int i = 0; i < 16; ++i) m = fmaxf(m, sm[i]);
+    }
+    for (int i = threadIdx.x; i < V; i += 1024) {
+        const float x = z[at + i];
+        out[at + i] = x == -INFINITY ? x : x == m ? 0.f : (float)((double)x - (double)m);
+    }
+}
+
 }  // namespace
+
+void launch_shown_rows(int T, int V, const float* logits, const int32_t* own, float* out, hipStream_t s) {
+    hipLaunchKernelGGL(k_shown_rows, dim3(T), dim3(1024), 0, s, logits, own, V, out);
+}
 
 size_t filter_workspace(int n_rows, int V) { return layout(n_rows, V, nullptr, nullptr); }
 
@@ -1378,6 +1411,7 @@ void launch_filter(const FilterCall& c, hipStream_t s) {
     p.temp = c.temp; p.topk = c.topk; p.topp = c.topp; p.minp = c.minp;
     p.u = c.u; p.token = c.token; p.prob = c.prob; p.kept = c.kept;
     p.out = c.out; p.ostride = c.ostride;
+    p.only = c.only;
     if (c.bf16) launch_typed<bf16_t>(c, p, s);
     else launch_typed<float>(c, p, s);
 }

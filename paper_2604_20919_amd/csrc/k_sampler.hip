@@ -41,7 +41,13 @@ struct SampP {
     const VStat* lstat;
     const float* zd;
     int groups;
+    OwnRows own;          // slots with logits of their own
+    bool own_only;        // phase A takes only those (the others have their epilogue's statistics)
 };
+// the logits of slot t
+__device__ __forceinline__ const float* row_of(const SampP& p, int t) {
+    return (p.own.own && p.own.own[t] ? p.own.rows : p.logits) + (size_t)t * p.V;
+}
 
 // Batch tables of the context-free sampler call, built on the device from
 // the kernel argument (nothing is copied from the host): user ids and draft
@@ -98,12 +104,13 @@ __global__ __launch_bounds__(256) void k_samp_a1(SampP p, NoallocMeta nm, Noallo
     __shared__ float sm[4], ss[4];
     __shared__ int si[4];
     const int t = blockIdx.x, c = blockIdx.y;
-    const float* z = p.logits + (size_t)t * p.V;
+    if (p.own_only && p.own.own[t] == 0) return;
+    const float* z = row_of(p, t);
     const int k0 = c * p.cwa, k1 = min(p.V, k0 + p.cwa);
     if (STAGE && t == 0 && c == 0) noalloc_stage(nm, nt, p.bv.drafts);
     float m = -INFINITY, s = 0.f;  // m: this thread's maximum and, at bi, first argmax
     int bi = 0x7fffffff;
-    const bool vec = (p.V & 3) == 0 && ((uintptr_t)p.logits & 15) == 0;
+    const bool vec = (p.V & 3) == 0 && ((uintptr_t)z & 15) == 0;
     for (int kt = k0; kt < k1; kt += 4096) {
         float v[16];
         // element e of the tile: increasing k per thread
@@ -180,6 +187,7 @@ __global__ __launch_bounds__(256) void k_samp_a2(SampP p, int chunks) {
     const BatchView& bv = p.bv;
     const int t = FUSED ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= bv.T) return;  // (unfused: a wave past the last slot)
+    if (!FUSED && p.own_only && p.own.own[t] == 0) return;
     // what the accept test reads besides the statistics, requested before the
     // merge: the draft that follows this slot, its logit and its q
     const int b = bv.slot_b[t], j = bv.slot_j[t];
@@ -189,7 +197,7 @@ __global__ __launch_bounds__(256) void k_samp_a2(SampP p, int chunks) {
     if (d < 0 || d >= p.V) d = 0;  // flagged by the prepare kernel
     float zdv = 0.f, qd = 0.f;
     if (test && bv.mode == 1) {
-        zdv = FUSED ? p.zd[t] : p.logits[(size_t)t * p.V + d];
+        zdv = FUSED ? p.zd[t] : row_of(p, t)[d];
         if (bv.qk == 0) qd = bv.q[(size_t)di * p.V + d];
     }
     float M = -INFINITY, S = 0.f;
@@ -304,7 +312,7 @@ __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
     const int row = bv.slot_off[b] + a;
     const float* st4 = p.sstat + (size_t)row * 4;
     const float M = st4[0], S = st4[1];
-    const float* z = p.logits + (size_t)row * p.V;
+    const float* z = row_of(p, row);
     const bool resid = a < Lb;
     const int k0 = c * p.cw, k1 = min(p.V, k0 + p.cw);
     const float* qr = nullptr;
@@ -460,7 +468,7 @@ void launch_probs(const Dims& D, const BatchView& bv, const SlotBufs& sb, const 
 }
 
 void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
-                    hipStream_t s, int groups, const NoallocMeta* nm, const NoallocTables* nt) {
+                    hipStream_t s, int groups, const NoallocMeta* nm, const NoallocTables* nt, OwnRows own) {
     SampP p;
     p.bv = bv;
     p.logits = logits;
@@ -474,10 +482,12 @@ void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, cons
     p.lstat = reinterpret_cast<const VStat*>(sb.lstat);
     p.zd = sb.zd;
     p.groups = groups;
+    p.own = own;
+    p.own_only = groups > 0;
     const int chunks = (D.V + p.cw - 1) / p.cw;
-    if (groups > 0) {
-        hipLaunchKernelGGL(k_samp_a2<true>, dim3(bv.T), dim3(256), 0, s, p, chunks);
-    } else {
+    // (slots with logits of their own are decided again from those)
+    if (groups > 0) hipLaunchKernelGGL(k_samp_a2<true>, dim3(bv.T), dim3(256), 0, s, p, chunks);
+    if (groups == 0 || own.own) {
         // phase A chunks: about 16 workgroups a CU in all (each pays its merge,
         // 64 chunks a slot cost 32 us for 108 slots of 151936 against 15),
         // at least one 4096-element tile each

@@ -36,7 +36,7 @@ int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 struct Layout {
     // staging block (int32 offsets within the block)
     size_t st_user, st_prefix, st_L, st_root, st_soff, st_doff, st_sb, st_sj, st_pt, st_items,
-        st_ioff, st_flags, st_prow, st_temp, st_topk, st_topp, st_minp, st_adapter, st_bytes;
+        st_ioff, st_flags, st_prow, st_temp, st_topk, st_topp, st_minp, st_own, st_adapter, st_bytes;
     // slot buffers (byte offsets within the slot)
     size_t stage, tok, cs, x, ssq, h, ffn, qbuf, attn, apart, aml, gpart, logits, sstat, spart,
         spartB, lstat, zd, dnext, skcnt, result, filter, lora, slot_bytes;
@@ -126,11 +126,12 @@ Layout plan(const sd_config& c) {
     L.st_ioff = take_i(L.Bmax + 1);
     L.st_flags = take_i(4);
     L.st_prow = take_i(L.Bmax);
-    // per slot: its user's sampling options and adapter
+    // per slot: its user's sampling options (st_own: there are some) and adapter
     L.st_temp = take_i(L.Tmax);
     L.st_topk = take_i(L.Tmax);
     L.st_topp = take_i(L.Tmax);
     L.st_minp = take_i(L.Tmax);
+    L.st_own = take_i(L.Tmax);
     L.st_adapter = take_i(L.Tmax);
     L.st_bytes = o;
     // slot
@@ -212,7 +213,7 @@ struct Slot {
     std::vector<int> users;  // global ids in batch order
     std::vector<int> L;
     std::vector<int> prow;   // decode steps: destination row of each user's probabilities
-    bool filtered = false;   // some user of a stochastic pass has sampling options
+    int filtered = 0;        // users of a stochastic pass with sampling options: none, some (1), all (2)
     bool adapted = false;    // some user of the pass has an adapter
     hipEvent_t done = nullptr;
     char* stage_host = nullptr;  // pinned
@@ -438,6 +439,7 @@ void build_stage(sd_ctx* c, Slot& s, int mode, bool with_items, int* n_items, in
             ((int32_t*)(st + L.st_topk))[t] = u.top_k;
             ((float*)(st + L.st_topp))[t] = u.top_p;
             ((float*)(st + L.st_minp))[t] = u.min_p;
+            ((int32_t*)(st + L.st_own))[t] = u.filtered();
             ((int32_t*)(st + L.st_adapter))[t] = u.adapter;
         }
         for (int i = 0; i < L.max_pages; ++i)
@@ -1030,8 +1032,10 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
                               hipStream_t st, float* probs = nullptr) {
     sd_status rs = hip_status(hipMemcpyAsync(s.base + c->lay.stage, s.stage_host, c->lay.st_bytes,
                                              hipMemcpyHostToDevice, st));
-    // users with sampling options: every slot's row of logits is filtered (into the
-    // slot's own rows), and the sampler takes its statistics from there
+    // users with sampling options: their slots' rows of logits are filtered (into the
+    // pass's own rows), and the sampler takes them and their statistics from there;
+    // slots of other users are decided as in a pass without such users
+    const OwnRows own{s.filtered ? (const int32_t*)(s.base + c->lay.stage + c->lay.st_own) : nullptr, s.bufs.logits};
     auto filter = [&](const float* from) {
         const char* stage = s.base + c->lay.stage;
         FilterCall f{};
@@ -1044,6 +1048,7 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
         f.topp = (const float*)(stage + c->lay.st_topp);
         f.minp = (const float*)(stage + c->lay.st_minp);
         f.out = s.bufs.logits;
+        f.only = own.own;
         f.ws = s.base + c->lay.filter;
         launch_filter(f, st);
     };
@@ -1051,18 +1056,16 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
         if (logits) {
             launch_prepare(c->D, bv, s.bufs, st);
             if (s.filtered) filter(logits);
-            launch_sampler(c->D, bv, s.bufs, s.filtered ? s.bufs.logits : logits, st);
+            launch_sampler(c->D, bv, s.bufs, logits, st, 0, nullptr, nullptr, own);
             rs = hip_status(hipGetLastError());
         } else {
             int groups = 0;
             rs = enqueue_forward(c, s, bv, st, pass_writes_logits(c, bv.mode, probs), &groups);
             if (rs == SD_OK) {
                 ProfScope ps(c, SD_K_SAMPLER, st);
-                if (s.filtered) {
-                    filter(s.bufs.logits);
-                    groups = 0;
-                }
-                launch_sampler(c->D, bv, s.bufs, s.bufs.logits, st, groups);
+                if (s.filtered) filter(s.bufs.logits);
+                if (s.filtered == 2) groups = 0;  // (no slot needs the epilogue's statistics)
+                launch_sampler(c->D, bv, s.bufs, s.bufs.logits, st, groups, nullptr, nullptr, own);
                 if (probs) launch_probs(c->D, bv, s.bufs, s.bufs.logits, probs, st);
                 rs = hip_status(hipGetLastError());
             }
@@ -1186,11 +1189,13 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     s.batch = batch;
     s.sample_only = sample_only;
     s.logits_ok = sample_only || pass_writes_logits(c, mode, probs);
-    s.filtered = s.adapted = false;
+    s.adapted = false;
+    int n_own = 0;
     for (int m : users) {
-        s.filtered |= mode == SD_STOCHASTIC && c->users[m].filtered();
+        n_own += c->users[m].filtered();
         s.adapted |= c->users[m].adapter >= 0;
     }
+    s.filtered = mode != SD_STOCHASTIC || n_own == 0 ? 0 : n_own < s.B ? 1 : 2;
     int n_items = 0, rows_max = 0, combine = 0, few = 0;
     build_stage(c, s, mode, !sample_only, &n_items, &rows_max, &combine, &few);
     BatchView bv = make_view(c, s);
@@ -1316,6 +1321,10 @@ sd_status sd_debug_logits(sd_ctx* c, int32_t batch, float* dst, sd_stream stream
     if (!s.pending || s.batch != batch || s.sample_only || !s.logits_ok) return SD_ESTATE;
     hipStream_t st = (hipStream_t)stream;
     SD_HIP(hipStreamWaitEvent(st, s.done, 0));
+    if (s.filtered) {
+        launch_shown_rows(s.T, c->D.V, s.bufs.logits, (const int32_t*)(s.base + c->lay.stage + c->lay.st_own), dst, st);
+        return hip_status(hipGetLastError());
+    }
     SD_HIP(hipMemcpyAsync(dst, s.bufs.logits, (size_t)s.T * c->D.V * 4, hipMemcpyDeviceToDevice, st));
     return SD_OK;
 }

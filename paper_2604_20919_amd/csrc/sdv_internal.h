@@ -203,9 +203,15 @@ void launch_pack(const void* s0, const void* s1, const void* s2, int seg1, int s
 // phase A's first kernel.
 struct NoallocMeta;
 struct NoallocTables;
+// Slots with logits of their own: slot t with own[t] != 0 takes row t of `rows`
+// and statistics from there, the others are as without (own null: none has).
+struct OwnRows {
+    const int32_t* own = nullptr;
+    const float* rows = nullptr;
+};
 void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
                     hipStream_t s, int groups = 0, const NoallocMeta* nm = nullptr,
-                    const NoallocTables* nt = nullptr);
+                    const NoallocTables* nt = nullptr, OwnRows own = OwnRows{});
 // probs[t][k] = exp(z[t][k] - m_t) / S_t from the sampler's per-slot
 // statistics (the same expression the race uses for p)
 void launch_probs(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
@@ -245,10 +251,13 @@ struct FilterCall {
     int32_t* kept;
     float* out;
     int64_t ostride;
+    const int32_t* only;  // [n_rows] or null (all): rows where it is 0 are left as they are (out)
     void* ws;  // filter_workspace bytes
 };
 size_t filter_workspace(int n_rows, int V);
 void launch_filter(const FilterCall& c, hipStream_t s);
+// a filtered pass's logits as sd_debug_logits shows them: all rows relative to their largest
+void launch_shown_rows(int T, int V, const float* logits, const int32_t* own, float* out, hipStream_t s);
 
 // Low-rank adapters: y_out[t] = y_in[t] + scale[a] B_a (A_a x[t]), a = ids[t]
 // (outside 0 .. n_adapters - 1: y_out[t] = y_in[t]).  Columns of segment s (seg[s] ..
