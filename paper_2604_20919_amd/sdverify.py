@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import Dict, Optional, Sequence
 
 import numpy as np
 
@@ -170,16 +170,30 @@ def sd_verify_query_sizes(cfg: sd_config):
     return kv.value, ws.value, wp.value
 
 
+class _Context:
+    """What sd_adapters_set needs to know of a context, and the adapters that the
+    library reads in place."""
+
+    def __init__(self, n_layers: int, device: int):
+        self.n_layers, self.device, self.adapters = n_layers, device, None
+
+
+_contexts: Dict[int, _Context] = {}
+
+
 def sd_verify_init(cfg: sd_config, weights: sd_weights, kv_pool, workspace, weight_pack=None) -> int:
+    import torch
     out = ctypes.c_void_p()
     _check("sd_verify_init", lib().sd_verify_init(ctypes.byref(cfg), ctypes.byref(weights),
                                                   _dev(kv_pool), _dev(workspace), _dev(weight_pack),
                                                   ctypes.byref(out)))
+    _contexts[out.value] = _Context(cfg.n_layers, torch.cuda.current_device())
     return out.value
 
 
 def sd_verify_destroy(ctx: int) -> None:
     _check("sd_verify_destroy", lib().sd_verify_destroy(ctx))
+    _contexts.pop(ctx, None)
 
 
 def sd_user_reset(ctx: int, user: int, prefix_len: int, root_token: int) -> None:
@@ -425,21 +439,33 @@ def sd_user_sampling(ctx: int, user: int, temperature: float = 1.0, top_k: int =
 
 
 def sd_adapters_set(ctx: int, layers) -> None:
-    """layers: per layer a dict of Lora under "qkv", "o", "down" (any of them
-    left out), or None to take all adapters away.  The caller keeps the
-    tensors alive until the next call or sd_verify_destroy."""
+    """layers: per layer of the context's model a dict of Lora under "qkv", "o",
+    "down" (any of them left out) on the context's GPU, or None to take all
+    adapters away.  Their tensors are kept alive until the next call that
+    succeeds or sd_verify_destroy; changing the list or its dicts
+    afterwards changes nothing."""
+    known = _contexts.get(ctx)
+    if known is None:
+        raise ValueError("not a context of sd_verify_init")
     if layers is None:
         _check("sd_adapters_set", lib().sd_adapters_set(ctx, 0, None))
+        known.adapters = None
         return
+    if len(layers) != known.n_layers:
+        raise ValueError(f"adapters of {len(layers)} layers, the model has {known.n_layers}")
     arr = (sd_layer_adapters * len(layers))()
-    n = 0
+    keep, n = [], 0
     for dst, src in zip(arr, layers):
         for name, w in src.items():
             if name not in ("qkv", "o", "down"):
                 raise ValueError(f"no adapters beside {name}")
+            if w.a.device.index != known.device:
+                raise ValueError(f"adapters beside {name} on {w.a.device}, the context on GPU {known.device}")
             setattr(dst, name, w.desc)
+            keep.append((w.a, w.b, w.scale))
             n = w.desc.n_adapters
     _check("sd_adapters_set", lib().sd_adapters_set(ctx, n, arr))
+    known.adapters = keep
 
 
 def sd_user_adapter(ctx: int, user: int, adapter: int) -> None:

@@ -72,10 +72,7 @@ class Verifier:
     def set_adapters(self, layers):
         """Adapters of every layer (sd_adapters_set): per layer a dict of
         sdverify.Lora under "qkv", "o", "down"; None: no adapters."""
-        if layers is not None and len(layers) != self.cfg.n_layers:
-            raise ValueError(f"adapters of {len(layers)} layers, the model has {self.cfg.n_layers}")
         sv.sd_adapters_set(self.ctx, layers)
-        self._adapters = layers  # the library reads them in place
 
     def user_adapter(self, user: int, adapter: int):
         """The adapter of a user's slots, -1: none (sd_user_adapter)."""
