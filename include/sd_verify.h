@@ -528,7 +528,7 @@ sd_status sd_lora_query_size(const sd_lora* w, int32_t n_rows, uint64_t* workspa
  *   y_in, y_out: rows of d_out elements of y_dtype, y_in_stride and
  *            y_out_stride apart; y_out may be y_in (same stride) and may not
  *            overlap it otherwise.  The output of the shared projection W x.
- * Sums are fp32 (bf16: A x is carried on in two bf16 planes, about 16 bits),
+ * Sums are fp32 (bf16: A x is carried on in three bf16 planes, all of its bits),
  * rounded once into y_out, in an order that depends on the sizes alone.
  * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, dtype,
  * stride, overlap, x_lo with SD_F32), SD_ELIMIT, SD_ENOMEM, SD_EHIP.

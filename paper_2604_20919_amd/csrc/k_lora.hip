@@ -185,11 +185,38 @@ __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h, int
 }
 
 // h of a row's segment as right operand: the sum of its planes, in bf16 carried
-// on in two planes of its own (hi + lo, about 16 bits, two products)
+// on in three planes of its own that hold all of its 24 bits (three products; two
+// planes, 16 bits, take as long at up to rank 64 with whole pieces: 21.3 against
+// 21.4 us for 229 rows, 99.7 against 99.9 for 8192; dearer for many rows of other
+// ranks, whose registers it is that bound them: 2000 rows of rank 12 25.5 against 26.2,
+// of rank 50 25.5 against 28.3, 1024 of rank 128 50 against 52, with y in bf16 43 against 49)
+template <typename T> constexpr int kInner = sizeof(T) == 2 ? 3 : 1;
 template <typename T> struct Inner {
-    typedef typename Mma<T>::Frag Frag;
-    Frag hi, lo;
+    typename Mma<T>::Frag p[kInner<T>];
 };
+// Each plane takes the eight highest bits that are left: nothing is rounded, and
+// numbers next to the largest do not become infinite.  (An infinity or a
+// not-a-number is in the first plane alone; inf - inf would make one of the other.)
+__device__ __forceinline__ Inner<bf16_t> inner_planes(const float (&v)[8]) {
+    Inner<bf16_t> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(v[i]);
+        float left = v[i] - __uint_as_float(a & 0xffff0000u);
+        left = (a & 0x7f800000u) != 0x7f800000u ? left : 0.f;
+        const uint32_t b = __float_as_uint(left);
+        const uint32_t c = __float_as_uint(left - __uint_as_float(b & 0xffff0000u));
+        r.p[0][i] = __builtin_bit_cast(__bf16, (uint16_t)(a >> 16));
+        r.p[1][i] = __builtin_bit_cast(__bf16, (uint16_t)(b >> 16));
+        r.p[2][i] = __builtin_bit_cast(__bf16, (uint16_t)(c >> 16));
+    }
+    return r;
+}
+__device__ __forceinline__ Inner<float> inner_planes(const float (&v)[4]) {
+    Inner<float> r;
+    __builtin_memcpy(&r.p[0], v, 16);
+    return r;
+}
 // (pieces may reach past the row, the last one past the planes: the workspace does too)
 template <typename T>
 __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank, size_t stride, int planes) {
@@ -207,17 +234,7 @@ __device__ __forceinline__ Inner<T> inner_piece(const float* hr, int k, int rank
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = k + i < rank ? v[i] : 0.f;
-    Inner<T> r;
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            r.hi[i] = (__bf16)v[i];
-            r.lo[i] = (__bf16)(v[i] - (float)r.hi[i]);
-        }
-    } else {
-        __builtin_memcpy(&r.hi, v, 16);
-    }
-    return r;
+    return inner_planes(v);
 }
 
 // y_out = y_in + scale B h: a wave takes 16 rows, `per` blocks of 16 CT columns
@@ -309,8 +326,8 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraCall c, const float* h, int
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     const Frag f = inside<WHOLE>(bf[r][q], (4 * r + g) * E, c.rank);
-                    acc[q] = Mma<T>::run(f, hv[r].hi, acc[q]);
-                    if constexpr (sizeof(T) == 2) acc[q] = Mma<T>::run(f, hv[r].lo, acc[q]);
+#pragma unroll
+                    for (int i = 0; i < kInner<T>; ++i) acc[q] = Mma<T>::run(f, hv[r].p[i], acc[q]);
                 }
             }
             if (next >= 0) fetch(next);
@@ -473,33 +490,26 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_down_wide(LoraCall c, 
     }
 }
 
-// The planes of h added up, into the first; in bf16 as two bf16 planes, hi and
-// lo, in the place of the float that they make (about 16 of its bits).
-template <typename T>
+// The planes of h added up, into the first.
 __global__ __launch_bounds__(256) void k_lora_join(float* h, size_t n, int planes) {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
     float v = 0.f;
 #pragma unroll 8
     for (int p = 0; p < planes; ++p) v += h[p * n + i];
-    if constexpr (sizeof(T) == 2) {
-        const __bf16 hi = (__bf16)v, lo = (__bf16)(v - (float)hi);
-        ((uint32_t*)h)[i] = (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16 | __builtin_bit_cast(uint16_t, lo);
-    } else {
-        h[i] = v;
-    }
+    h[i] = v;
 }
 
 // Workgroups next to each other in launch order take the same rows' next columns:
 // those that run together then have whole rows between them, not one piece of
 // each row (8192 rows of 5120 columns, rank 64: 66 -> 60 us), and y passes by what
-// the caches keep of B and h (60 -> 56 us).
+// the caches keep of B and h (60 -> 56 us).  Up to rank 64 two workgroups are on a
+// CU (2000 rows of rank 12 26.2 us, 28.5 with one).
 template <typename T, typename Y, int RB, bool WHOLE>
-__global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, const float* h, int per) {
+__global__ __launch_bounds__(64 * kWideWaves, RB * Mma<T>::kE <= 16 ? 4 : 2) void k_lora_up_wide(LoraCall c, const float* h, int per) {
     typedef typename Mma<T>::Frag Frag;
     constexpr int E = Mma<T>::kE, CT = 4;
     constexpr int W = 16 / sizeof(Y), JW = W / 4;
-    constexpr bool LO = sizeof(T) == 2;
     constexpr int P = 4 * RB * E + E;  // elements between the columns' rows of B in LDS
     __shared__ __align__(16) T bs[2][16 * CT * P];
     __shared__ int ids[kWideTile];
@@ -533,7 +543,7 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
     for (int a = -1; (a = next_id(ids, a, lane)) >= 0;) {
         const bool part = __ballot(mine == a) != 0;
         const float sc = c.scale ? c.scale[a] : 1.f;
-        Frag hf[RB], lf[RB];
+        Inner<T> hv[RB];
         // B of a block of columns: 16 CT rows of 4 RB pieces
         constexpr int N = 16 * CT * 4 * RB, PP = (N + 64 * kWideWaves - 1) / (64 * kWideWaves);
         Frag st[PP];
@@ -586,19 +596,11 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     const int k = (4 * r + g) * E;
-                    uint32_t v[E];
+                    float v[E];
                     __builtin_memcpy(v, hr + (k < c.rank ? k : 0), sizeof(v));
 #pragma unroll
-                    for (int i = 0; i < E; ++i) v[i] = k + i < c.rank ? v[i] : 0;
-                    if constexpr (LO) {
-#pragma unroll
-                        for (int i = 0; i < E; ++i) {
-                            hf[r][i] = __builtin_bit_cast(__bf16, (uint16_t)(v[i] >> 16));
-                            lf[r][i] = __builtin_bit_cast(__bf16, (uint16_t)v[i]);
-                        }
-                    } else {
-                        __builtin_memcpy(&hf[r], v, 16);
-                    }
+                    for (int i = 0; i < E; ++i) v[i] = k + i < c.rank ? v[i] : 0.f;
+                    hv[r] = inner_planes(v);
                 }
             }
             Y yc[CT / JW][W];
@@ -616,8 +618,8 @@ __global__ __launch_bounds__(64 * kWideWaves) void k_lora_up_wide(LoraCall c, co
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
                         const Frag bf = *(const Frag*)&bs[buf][lcol(q) * P + (4 * r + g) * E];
-                        acc[q] = Mma<T>::run(bf, hf[r], acc[q]);
-                        if constexpr (LO) acc[q] = Mma<T>::run(bf, lf[r], acc[q]);
+#pragma unroll
+                        for (int i = 0; i < kInner<T>; ++i) acc[q] = Mma<T>::run(bf, hv[r].p[i], acc[q]);
                     }
                 }
                 if (mine == a) {
@@ -727,7 +729,7 @@ void launch_up(const LoraCall& c, const Shape& sh, float* h, hipStream_t s) {
     const int64_t units = (int64_t)blocks * sh.tiles;
     if (sh.wide) {
         const size_t n = (size_t)c.T * c.n_seg * c.rank;
-        hipLaunchKernelGGL(k_lora_join<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, h, n, sh.planes);
+        hipLaunchKernelGGL(k_lora_join, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, h, n, sh.planes);
         // as many blocks a workgroup as leave about four workgroups a CU
         const int per = std::max(1, (int)std::min<int64_t>(units / (4 * cu_count()), 16));
         const dim3 g((blocks + per - 1) / per, sh.tiles);
