@@ -356,7 +356,8 @@ sd_status sd_sample_logits(sd_ctx* ctx, int32_t batch, int32_t n_users, const in
 
 /* Diagnostic: copy the logits of pending batch `batch` (device fp32
  * [sum(l_m+1)][vocab]) into dst (device), ordered after the batch on
- * `stream`.  SD_ESTATE if the batch is not pending or its pass stored no
+ * `stream`.  The copy has to be done before the batch's workspace slot takes
+ * its next batch.  SD_ESTATE if the batch is not pending or its pass stored no
  * logits (sd_config.logits_out). */
 sd_status sd_debug_logits(sd_ctx* ctx, int32_t batch, float* dst, sd_stream stream);
 

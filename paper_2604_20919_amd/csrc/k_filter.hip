@@ -433,7 +433,8 @@ struct Work {
     RowRec* rows;
     ChunkRec* recs;   // [n][chunks]
     u64* hist;        // [n][chunks][kBuckets]
-    uint2* list;      // [n][kList] (key, index)
+    uint2* list;      // [n][list_n] (key, index)
+    int list_n;       // kList, or the row where that is shorter
 };
 int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -444,8 +445,9 @@ size_t layout(int n, int V, void* base, Work* w) {
     char* a = take(n * sizeof(RowRec));
     char* b = take(nc * sizeof(ChunkRec));
     char* c = take(nc * kBuckets * 8);
-    char* d = take((size_t)n * kList * 8);
-    if (w) *w = Work{(RowRec*)a, (ChunkRec*)b, (u64*)c, (uint2*)d};
+    const int list_n = std::min(kList, V);
+    char* d = take((size_t)n * list_n * 8);
+    if (w) *w = Work{(RowRec*)a, (ChunkRec*)b, (u64*)c, (uint2*)d, list_n};
     return o;
 }
 
@@ -870,7 +872,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
         r.klo = su[10];
         r.khi = su[11] - 1;
         r.kmin = su[12];
-        r.mode = r.n_list > kList ? kModeRow : kModeBorder;
+        r.mode = r.n_list > (uint32_t)wk.list_n ? kModeRow : kModeBorder;
         wk.rows[row] = r;
     }
 }
@@ -922,7 +924,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
         if (lane == 0) sc[g][w] = tot;
     }
     __syncthreads();
-    uint2* list = wk.list + (size_t)row * kList + off;
+    const uint32_t room = (uint32_t)wk.list_n - off;
+    uint2* list = wk.list + (size_t)row * wk.list_n + off;
     uint32_t base = 0;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -934,7 +937,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Wor
 #pragma unroll
         for (int e = 0; e < W; ++e)
             // (there is room for every member; the bound holds if someone writes the logits meanwhile)
-            if ((mine >> (g * W + e) & 1) && at < kList - off)
+            if ((mine >> (g * W + e) & 1) && at < room)
                 list[at++] = uint2{key_of(v[g * W + e]), (uint32_t)(c * kChunk + elem_at<T>(tid, g * W + e))};
     }
 }
@@ -1056,7 +1059,7 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
         }
     }
     if (border) {
-        const uint2* list = wk.list + (size_t)row * kList;
+        const uint2* list = wk.list + (size_t)row * wk.list_n;
         const int n = (int)r.n_list, w0 = __builtin_amdgcn_readfirstlane(tid & ~63);
         uint2 held[kHeld];
         auto hold = [&](int i0) {
@@ -1380,6 +1383,14 @@ void launch_shown_rows(int T, int V, const float* logits, const int32_t* own, fl
 }
 
 size_t filter_workspace(int n_rows, int V) { return layout(n_rows, V, nullptr, nullptr); }
+int filter_rows(size_t bytes, int V, int most) {
+    if (filter_workspace(most, V) <= bytes) return most;
+    // (each of the four sections is rounded up once)
+    const size_t row = filter_workspace(256, V) / 256;
+    int n = (int)std::min<size_t>(bytes / row + 1, most);
+    while (n > 0 && filter_workspace(n, V) > bytes) --n;
+    return n;
+}
 
 template <typename T>
 static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {

@@ -772,9 +772,10 @@ void launch_typed(const LoraCall& c, hipStream_t s) {
 
 }  // namespace
 
-// (enough for every smaller T too: planes times rows, the rows rounded up to tiles)
-size_t lora_workspace(int T, int rank, int n_seg) {
-    const size_t rows = std::min((size_t)kWidePlanes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
+// (enough for every smaller T, rank and n_seg too: planes times rows, the rows rounded up to tiles)
+size_t lora_workspace(int T, int rank, int n_seg, int d_in, int bf16) {
+    const int planes = std::min(kWidePlanes, (d_in * (bf16 ? 2 : 4) + 255) / 256);
+    const size_t rows = std::min((size_t)planes * T, (size_t)kWideTile * (kGroups + (T + 15) / 16));
     // (and a piece of 32 bytes past the end)
     return (rows * rank * n_seg * 4 + 32 + 255) & ~(size_t)255;
 }
@@ -799,7 +800,7 @@ sd_status sd_lora_query_size(const sd_lora* w, int32_t n_rows, uint64_t* workspa
     if (w->seg_off[0] != 0 || w->seg_off[w->n_seg] != w->d_out) return SD_EINVAL;
     for (int i = 0; i < w->n_seg; ++i)
         if (w->seg_off[i] >= w->seg_off[i + 1]) return SD_EINVAL;
-    *workspace_bytes = sdv::lora_workspace(n_rows, w->rank, w->n_seg);
+    *workspace_bytes = sdv::lora_workspace(n_rows, w->rank, w->n_seg, w->d_in, w->dtype == SD_BF16);
     return SD_OK;
 }
 

@@ -41,6 +41,7 @@ struct Layout {
     size_t stage, tok, cs, x, ssq, h, ffn, qbuf, attn, apart, aml, gpart, logits, sstat, spart,
         spartB, lstat, zd, dnext, skcnt, result, filter, lora, slot_bytes;
     size_t lora_bytes;
+    int filter_rows;  // rows that the filter takes at once (0: none, see sd_user_sampling)
     size_t gpart_floats;
     int nsq;
     // global region after the slots
@@ -156,18 +157,31 @@ Layout plan(const sd_config& c) {
     L.aml = take(nparts * 2 * 4);
     L.gpart_floats = gemm_partial_floats(D, L.Tmax);
     L.gpart = take(std::max<size_t>(L.gpart_floats, 1) * 4);
+    // The filter of the users with sampling options works in the forward's
+    // buffers, which nothing reads once the logits are there; what does not fit
+    // is filtered a few rows at a time.
+    L.filter = L.x;
+    L.filter_rows = 0;
+    if (D.V <= SD_FILTER_MAX_VOCAB && L.Tmax <= SD_FILTER_MAX_ROWS) {
+        s = std::max(s, align_up(L.filter + filter_workspace(1, D.V)));
+        L.filter_rows = filter_rows(s - L.filter, D.V, L.Tmax);
+    }
     L.logits = take((size_t)L.Tmax * D.V * 4);
     L.sstat = take((size_t)L.Tmax * 4 * 4);
     L.spart = take((size_t)L.Tmax * kVocabChunks * 4 * 4);
     L.spartB = take((size_t)L.Bmax * kVocabChunks * 4 * 4);
     L.lstat = take(D.bf16 ? (size_t)lm_stat_groups_max(D.V) * L.Tmax * 4 * 4 : 16);
+    // The adapters' inner results lie where the lm_head leaves the logits and their
+    // statistics: every layer is done before.
+    L.lora = L.logits;
+    L.lora_bytes = 0;
+    for (int d_in : {D.d, D.nq(), D.F})
+        L.lora_bytes = std::max(L.lora_bytes, lora_workspace(L.Tmax, kLoraRank, kLoraSegs, d_in, D.bf16));
+    s = std::max(s, align_up(L.lora + L.lora_bytes));
     L.zd = take((size_t)L.Tmax * 4);
     L.dnext = take((size_t)L.Tmax * 4);
     L.skcnt = take((size_t)kSkCounters * 4);
     L.result = take((size_t)(2 * L.Bmax + 4) * 4);
-    L.filter = take(D.V > SD_FILTER_MAX_VOCAB || L.Tmax > SD_FILTER_MAX_ROWS ? 0 : filter_workspace(L.Tmax, D.V));
-    L.lora_bytes = lora_workspace(L.Tmax, kLoraRank, kLoraSegs);
-    L.lora = take(L.lora_bytes);
     L.slot_bytes = s;
     L.total = align_up(L.slot_bytes * (size_t)c.max_pending);
     return L;
@@ -915,7 +929,7 @@ sd_status sd_user_sampling(sd_ctx* c, int32_t user, float temperature, int32_t t
         !(min_p >= 0.f && min_p <= 1.f))
         return SD_EINVAL;
     // the filter's kernels hold a row's chunks in LDS, and rows in a grid's y
-    if (c->D.V > SD_FILTER_MAX_VOCAB || c->lay.Tmax > SD_FILTER_MAX_ROWS) return SD_ELIMIT;
+    if (c->lay.filter_rows == 0) return SD_ELIMIT;
     User& u = c->users[user];
     if (u.pending_slot >= 0) return SD_ESTATE;
     u.temperature = temperature;
@@ -1038,19 +1052,21 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
     const OwnRows own{s.filtered ? (const int32_t*)(s.base + c->lay.stage + c->lay.st_own) : nullptr, s.bufs.logits};
     auto filter = [&](const float* from) {
         const char* stage = s.base + c->lay.stage;
-        FilterCall f{};
-        f.n_rows = bv.T;
-        f.V = c->D.V;
-        f.logits = from;
-        f.stride = f.ostride = c->D.V;
-        f.temp = (const float*)(stage + c->lay.st_temp);
-        f.topk = (const int32_t*)(stage + c->lay.st_topk);
-        f.topp = (const float*)(stage + c->lay.st_topp);
-        f.minp = (const float*)(stage + c->lay.st_minp);
-        f.out = s.bufs.logits;
-        f.only = own.own;
-        f.ws = s.base + c->lay.filter;
-        launch_filter(f, st);
+        for (int t = 0; t < bv.T; t += c->lay.filter_rows) {
+            FilterCall f{};
+            f.n_rows = std::min(bv.T - t, c->lay.filter_rows);
+            f.V = c->D.V;
+            f.logits = from + (size_t)t * c->D.V;
+            f.stride = f.ostride = c->D.V;
+            f.temp = (const float*)(stage + c->lay.st_temp) + t;
+            f.topk = (const int32_t*)(stage + c->lay.st_topk) + t;
+            f.topp = (const float*)(stage + c->lay.st_topp) + t;
+            f.minp = (const float*)(stage + c->lay.st_minp) + t;
+            f.out = s.bufs.logits + (size_t)t * c->D.V;
+            f.only = own.own + t;
+            f.ws = s.base + c->lay.filter;
+            launch_filter(f, st);
+        }
     };
     if (rs == SD_OK) {
         if (logits) {

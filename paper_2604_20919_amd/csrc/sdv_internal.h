@@ -255,6 +255,8 @@ struct FilterCall {
     void* ws;  // filter_workspace bytes
 };
 size_t filter_workspace(int n_rows, int V);
+// most rows at once, up to `most`, that a workspace of so many bytes holds
+int filter_rows(size_t bytes, int V, int most);
 void launch_filter(const FilterCall& c, hipStream_t s);
 // a filtered pass's logits as sd_debug_logits shows them: all rows relative to their largest
 void launch_shown_rows(int T, int V, const float* logits, const int32_t* own, float* out, hipStream_t s);
@@ -278,7 +280,7 @@ struct LoraCall {
     int64_t ys, yos;
     void* ws;               // lora_workspace bytes
 };
-size_t lora_workspace(int T, int rank, int n_seg);
+size_t lora_workspace(int T, int rank, int n_seg, int d_in, int bf16);
 void launch_lora(const LoraCall& c, hipStream_t s);
 
 void launch_kv_copy(const Dims& D, const KVPool& kv, const KVCopyPages& pages, int layer,
