@@ -1063,7 +1063,7 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
             f.topp = (const float*)(stage + c->lay.st_topp) + t;
             f.minp = (const float*)(stage + c->lay.st_minp) + t;
             f.out = s.bufs.logits + (size_t)t * c->D.V;
-            f.only = own.own + t;
+            f.only = s.filtered == 1 ? own.own + t : nullptr;
             f.ws = s.base + c->lay.filter;
             launch_filter(f, st);
         }
