@@ -9,8 +9,9 @@
 // no larger.  So nothing is sorted: the end is found by histograms of counts
 // and weights, digit by digit of an order-preserving integer key of the logit.
 //
-// Weights are rounded to 64-bit fixed-point numbers, so sums of them are exact
-// and the same in every order, LDS atomics included.
+// Weights are rounded to 64-bit fixed-point numbers, so sums of them within a
+// workgroup are exact and the same in every order, LDS atomics included; the sums
+// of a row's chunks are merged in 64-bit floating point, in a fixed order.
 #include <algorithm>
 
 #include "../../include/sd_verify.h"
@@ -87,7 +88,8 @@ __device__ __forceinline__ RowOpts row_opts(const FilterP& p, int row) {
     o.c = o.greedy ? 0.0 : 1.4426950408889634 / (double)t;
     o.rc = o.greedy ? 0.0 : (double)t * 0.6931471805599453;
     // (the lower the temperature, the more octaves a logit makes: the buckets of a row
-    // together are 13 to 27 wide in logits from T = 0.6 down, 22 at T = 1.  With eighths
+    // together are 13 to 27 wide in logits from T = 0.6 down to 1.5e-4, where
+    // kMaxShift ends it (0.9 at 1e-5), and 22 T above.  With eighths
     // at every temperature the prefix of the 50 largest at T = 0.1 ended below them,
     // and the whole-row path took 600 us for one row of 151936 and 1220 for 416, against 26
     // and 104; the shift costs the first read 65 -> 68 us for 416 rows.)
@@ -170,9 +172,11 @@ __device__ __forceinline__ uint32_t wave_least(uint32_t v) {
 }
 
 // A whole row by one workgroup, whatever its values: the rows
-// that the chunked kernels below leave (see kModeRow).  Bound by its passes' latencies: 0.2 to
-// 0.9 ms for 1 to 32 rows of 151936 (equal logits, which meet in one bin, the
-// longest) against 0.03 ms for rows in chunks; such rows are rare.  Passes over the row:
+// that the chunked kernels below leave (see kModeRow).  Bound by its passes' latencies: 0.22 to
+// 1.2 ms for one row of 151936, 0.6 to 2.6 ms for 416 (many equal logits, which meet
+// in one bin, the longest) against 0.03 and 0.11 ms for rows in chunks; such rows are
+// rare, but at 2^20 tokens ordinary ones are among them: more than kList of 2^20 N(0, 1.43) logits
+// share the bucket in which top-p 0.95 ends, 4.6 ms a row.  Passes over the row:
 // maximum; weights' total; one a digit of the prefix's last key (9 bits
 // each); the last key's ties if not all of them are kept; the kept weights by
 // wave segments; the segment drawn from, or the rows written.

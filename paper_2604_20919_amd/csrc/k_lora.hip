@@ -108,8 +108,8 @@ __device__ __forceinline__ int tile_id(const LoraCall& c, int t0, int lane) {
 // of the rows in turn, their sums added in LDS and left as plane blockIdx.y of h
 // ([planes][T][R]) that the second product adds up.  Bound by what it reads: 80 rows of
 // 25600 in two planes with 16 adapters of rank 32, 34 MB, 16 us (one workgroup taking
-// all of a tile's adapters: 52 us), 229 rows of 5120, 11 us (19); a plain read of 29 MB takes 13 us
-// on the card, most of it to get under way.  Deeper unrolling, other orders of the
+// all of a tile's adapters: 52 us), 229 rows of 5120, 11 us (19); a plain read of 34 MB, one
+// after the other, takes 7.5 us on the card.  Deeper unrolling, other orders of the
 // pieces, twice the ranges of k or half the waves left both where they are.
 template <typename T, int NW, bool LO>
 __global__ __launch_bounds__(64 * NW) void k_lora_down(LoraCall c, float* h, int share) {
