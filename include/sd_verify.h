@@ -441,9 +441,9 @@ sd_status sd_sample_logits_noalloc(int32_t n_users, const int32_t* user_ids, con
  *   w_r >= min_p
  * hold: each filter looks at the whole distribution at temperature T, and a
  * token has to pass all.  Many servers apply top-k first and top-p to what it
- * leaves, renormalised, which keeps fewer where both are on (28 to 43 of the 50
- * that are kept here at k = 50, p = 0.9): for that order call sd_filter_logits
- * with temperature and top_k, and the second call on its rows with top_p.
+ * leaves, renormalised, which keeps fewer tokens where both are on: for that
+ * order call sd_filter_logits with temperature and top_k, and the second call
+ * on its rows with top_p.
  * Weights are computed to about 2^-30 of each, or 2^-36 of the row's largest
  * where that is more, and summed as 64-bit integers over 4096 tokens at a time,
  * whose sums are merged in 64-bit floating point in a fixed order: results are

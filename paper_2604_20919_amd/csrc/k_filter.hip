@@ -42,9 +42,11 @@ struct FilterP {
     int32_t* kept;
     float* out;          // [n][ostride] (filtered rows)
     int64_t ostride;
-    const int32_t* only; // [n] or null: rows where it is 0 are left as they are
+    const int32_t* only; // [n]: rows where it is 0 are left as they are (kernels with ONLY)
 };
-__device__ __forceinline__ bool left_alone(const FilterP& p, int row) { return p.only && p.only[row] == 0; }
+template <bool ONLY> __device__ __forceinline__ bool left_alone(const FilterP& p, int row) {
+    return ONLY && p.only[row] == 0;
+}
 
 // NaN becomes -inf (never kept)
 __device__ __forceinline__ float clean(float z) { return z > -INFINITY ? z : -INFINITY; }
@@ -574,7 +576,7 @@ __device__ __forceinline__ int bucket_shift(double G, double Gc, int sh) {
 // 68 us (3.7 TB/s; reading alone takes 40), rows without filters 35 us for 256 (4.4 TB/s).
 // One LDS atomic an element carries count and weight; copies of the histogram
 // against bank conflicts changed nothing (2 or 4 of them: -1 or +3 us).
-template <typename T>
+template <typename T, bool ONLY>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work wk) {
     __shared__ u64 hs[kBuckets];  // (the lightest first: one instruction less an element)
     __shared__ float sm[kChunkWaves];
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_filter_scan(FilterP p, Work w
     __shared__ RowOpts opts;
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if (left_alone(p, row)) return;
+    if (left_alone<ONLY>(p, row)) return;
     float v[kPer];
     load_chunk<T>((const T*)p.z + (size_t)row * p.stride, c * kChunk, p.V, v);
     if (w == 0) {  // (divisions in 64 bits: for all waves they were an eighth of the work)
@@ -687,7 +689,7 @@ __device__ __forceinline__ uint32_t first_key(F in, double edge, double off, uin
 // quarter of its chunks.  Bound by its chain of loads and barriers: 9 us for 1 to
 // 130 rows of 151936, 14 us for 416.
 constexpr int kFindThreads = 4 * kBuckets;
-template <bool DRAW>
+template <bool DRAW, bool ONLY>
 __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk, int nch) {
     __shared__ double cG[kMaxChunks], cS[kMaxChunks], unit[kMaxChunks], bsum[4][kBuckets], sd[16];
     __shared__ uint32_t bcnt[4][kBuckets], cn[kMaxChunks], cfirst[kMaxChunks], su[16];
@@ -696,7 +698,7 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
     __shared__ int sfound;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int bk = tid % kBuckets, part = tid / kBuckets;
-    if (left_alone(p, row)) return;
+    if (left_alone<ONLY>(p, row)) return;
     ChunkRec* recs = wk.recs + (size_t)row * nch;
     const RowOpts o = row_opts(p, row);
     if (tid < nch) {
@@ -885,13 +887,13 @@ __global__ __launch_bounds__(kFindThreads) void k_filter_find(FilterP p, Work wk
 // weights above it.  Chunks without members are not read: 4.5 us for one row of
 // 151936, 27 us for 416, whose chunks all have some (9.4 TB/s, most of it from the
 // caches).
-template <typename T, bool DRAW>
+template <typename T, bool DRAW, bool ONLY>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_collect(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T), NG = kPer / W;
     __shared__ uint32_t sc[NG][kChunkWaves];
     const int c = blockIdx.x, row = blockIdx.y, nch = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if (left_alone(p, row)) return;
+    if (left_alone<ONLY>(p, row)) return;
     const RowRec& rr = wk.rows[row];
     const int mode = rr.mode;
     if (mode != kModeBorder) return;
@@ -968,13 +970,13 @@ constexpr int kHeldAll = kHeld * kRowThreads;   // at once; longer lists are rea
 // members: 11 us for one row of 151936, 26 us for 416.  PLAIN: no row has a
 // filter, and the chunks are merged here: 6.5 us for 256 rows, against 15.5 us
 // of this kernel and the two before it.
-template <typename T, bool DRAW, bool PLAIN>
+template <typename T, bool DRAW, bool PLAIN, bool ONLY>
 __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Work wk, int nch) {
     __shared__ union { RowShared row; ResolveShared s; } sh;
     __shared__ uint2 tab[kTab];
     ResolveShared& s = sh.s;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if (left_alone(p, row)) return;
+    if (left_alone<ONLY>(p, row)) return;
     const ChunkRec* recs = wk.recs + (size_t)row * nch;
     // (wave 0 holds the chunks' weights from here to the draw)
     u64 cabove[kLaneChunks];
@@ -1310,11 +1312,11 @@ __global__ __launch_bounds__(kRowThreads, 4) void k_filter_resolve(FilterP p, Wo
 // read again, and what is written goes past the caches, which hold the rows of
 // the first read: 229 rows of 151936, 44 -> 38 us, and 44 -> 39 us for the first
 // read of the next rows, which then finds no lines to be written back.
-template <typename T>
+template <typename T, bool ONLY>
 __global__ __launch_bounds__(kChunkThreads) void k_filter_write(FilterP p, Work wk) {
     constexpr int W = 16 / sizeof(T);
     const int c = blockIdx.x, row = blockIdx.y;
-    if (left_alone(p, row)) return;
+    if (left_alone<ONLY>(p, row)) return;
     const RowRec& rr = wk.rows[row];
     const int mode = rr.mode;
     if (mode == kModeRow) return;  // written by k_filter_resolve
@@ -1396,25 +1398,29 @@ int filter_rows(size_t bytes, int V, int most) {
     return n;
 }
 
-template <typename T>
+// ONLY: rows may be left alone (fp32 rows that are rewritten)
+template <typename T, bool ONLY>
 static void launch_typed(const FilterCall& c, const FilterP& p, hipStream_t s) {
     Work wk;
     layout(c.n_rows, c.V, c.ws, &wk);
     const int nch = chunks_of(c.V);
-    const dim3 g(nch, c.n_rows);
-    hipLaunchKernelGGL(k_filter_scan<T>, g, dim3(kChunkThreads), 0, s, p, wk);
-    const dim3 rows(c.n_rows), of_row(kRowThreads);
-    if (c.out) {
-        hipLaunchKernelGGL(k_filter_find<false>, rows, dim3(kFindThreads), 0, s, p, wk, nch);
-        hipLaunchKernelGGL((k_filter_collect<T, false>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, false, false>), rows, of_row, 0, s, p, wk, nch);
-        hipLaunchKernelGGL(k_filter_write<T>, g, dim3(kChunkThreads), 0, s, p, wk);
-    } else if (!c.topk && !c.topp && !c.minp) {
-        hipLaunchKernelGGL((k_filter_resolve<T, true, true>), rows, of_row, 0, s, p, wk, nch);
-    } else {
-        hipLaunchKernelGGL(k_filter_find<true>, rows, dim3(kFindThreads), 0, s, p, wk, nch);
-        hipLaunchKernelGGL((k_filter_collect<T, true>), g, dim3(kChunkThreads), 0, s, p, wk);
-        hipLaunchKernelGGL((k_filter_resolve<T, true, false>), rows, of_row, 0, s, p, wk, nch);
+    const dim3 g(nch, c.n_rows), rows(c.n_rows), of_row(kRowThreads);
+    hipLaunchKernelGGL((k_filter_scan<T, ONLY>), g, dim3(kChunkThreads), 0, s, p, wk);
+    if (ONLY || c.out) {
+        hipLaunchKernelGGL((k_filter_find<false, ONLY>), rows, dim3(kFindThreads), 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_collect<T, false, ONLY>), g, dim3(kChunkThreads), 0, s, p, wk);
+        hipLaunchKernelGGL((k_filter_resolve<T, false, false, ONLY>), rows, of_row, 0, s, p, wk, nch);
+        hipLaunchKernelGGL((k_filter_write<T, ONLY>), g, dim3(kChunkThreads), 0, s, p, wk);
+        return;
+    }
+    if constexpr (!ONLY) {
+        if (!c.topk && !c.topp && !c.minp) {
+            hipLaunchKernelGGL((k_filter_resolve<T, true, true, false>), rows, of_row, 0, s, p, wk, nch);
+        } else {
+            hipLaunchKernelGGL((k_filter_find<true, false>), rows, dim3(kFindThreads), 0, s, p, wk, nch);
+            hipLaunchKernelGGL((k_filter_collect<T, true, false>), g, dim3(kChunkThreads), 0, s, p, wk);
+            hipLaunchKernelGGL((k_filter_resolve<T, true, false, false>), rows, of_row, 0, s, p, wk, nch);
+        }
     }
 }
 
@@ -1427,8 +1433,9 @@ void launch_filter(const FilterCall& c, hipStream_t s) {
     p.u = c.u; p.token = c.token; p.prob = c.prob; p.kept = c.kept;
     p.out = c.out; p.ostride = c.ostride;
     p.only = c.only;
-    if (c.bf16) launch_typed<bf16_t>(c, p, s);
-    else launch_typed<float>(c, p, s);
+    if (c.only) launch_typed<float, true>(c, p, s);
+    else if (c.bf16) launch_typed<bf16_t, false>(c, p, s);
+    else launch_typed<float, false>(c, p, s);
 }
 
 }  // namespace sdv

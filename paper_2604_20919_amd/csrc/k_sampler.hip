@@ -44,9 +44,10 @@ struct SampP {
     OwnRows own;          // slots with logits of their own
     bool own_only;        // phase A takes only those (the others have their epilogue's statistics)
 };
-// the logits of slot t
-__device__ __forceinline__ const float* row_of(const SampP& p, int t) {
-    return (p.own.own && p.own.own[t] ? p.own.rows : p.logits) + (size_t)t * p.V;
+// The logits of slot t.  OWN: some slots have their own (kernels of their own: with
+// the choice in all of them 16 users of 151936 tokens took 43.9 us, not 41.7).
+template <bool OWN> __device__ __forceinline__ const float* row_of(const SampP& p, int t) {
+    return (OWN && p.own.own[t] ? p.own.rows : p.logits) + (size_t)t * p.V;
 }
 
 // Batch tables of the context-free sampler call, built on the device from
@@ -99,13 +100,13 @@ __device__ __forceinline__ void noalloc_stage(const NoallocMeta& m, const Noallo
 // rows are not 16-byte aligned): their maximum first, then one exponential
 // per element; the workgroup's maximum is known before the sums are merged,
 // so the merge is a rescale and plain sums.  STAGE: the context-free call.
-template <bool STAGE>
+template <bool STAGE, bool OWN>
 __global__ __launch_bounds__(256) void k_samp_a1(SampP p, NoallocMeta nm, NoallocTables nt) {
     __shared__ float sm[4], ss[4];
     __shared__ int si[4];
     const int t = blockIdx.x, c = blockIdx.y;
-    if (p.own_only && p.own.own[t] == 0) return;
-    const float* z = row_of(p, t);
+    if (OWN && p.own_only && p.own.own[t] == 0) return;
+    const float* z = row_of<OWN>(p, t);
     const int k0 = c * p.cwa, k1 = min(p.V, k0 + p.cwa);
     if (STAGE && t == 0 && c == 0) noalloc_stage(nm, nt, p.bv.drafts);
     float m = -INFINITY, s = 0.f;  // m: this thread's maximum and, at bi, first argmax
@@ -180,14 +181,14 @@ __global__ __launch_bounds__(256) void k_samp_a1(SampP p, NoallocMeta nm, Noallo
 // records ([T][groups]); thread i merges records i, i + 256, ... in that
 // order, then the lanes and the four waves are merged.  Ties of the argmax
 // go to the lowest index either way.
-template <bool FUSED>
+template <bool FUSED, bool OWN>
 __global__ __launch_bounds__(256) void k_samp_a2(SampP p, int chunks) {
     __shared__ VStat wst[4];
     const int lane = threadIdx.x & 63;
     const BatchView& bv = p.bv;
     const int t = FUSED ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= bv.T) return;  // (unfused: a wave past the last slot)
-    if (!FUSED && p.own_only && p.own.own[t] == 0) return;
+    if (OWN && p.own_only && p.own.own[t] == 0) return;
     // what the accept test reads besides the statistics, requested before the
     // merge: the draft that follows this slot, its logit and its q
     const int b = bv.slot_b[t], j = bv.slot_j[t];
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(256) void k_samp_a2(SampP p, int chunks) {
     if (d < 0 || d >= p.V) d = 0;  // flagged by the prepare kernel
     float zdv = 0.f, qd = 0.f;
     if (test && bv.mode == 1) {
-        zdv = FUSED ? p.zd[t] : row_of(p, t)[d];
+        zdv = FUSED ? p.zd[t] : row_of<OWN>(p, t)[d];
         if (bv.qk == 0) qd = bv.q[(size_t)di * p.V + d];
     }
     float M = -INFINITY, S = 0.f;
@@ -299,7 +300,7 @@ __device__ __forceinline__ int leading_accepts(const SampP& p, int b) {
 // of the bounds and of log1pf (a few 2^-23), the added terms that of
 // subnormal keys.  (Every key exact, 256 threads: 1 / 16 / 32 users of 151936
 // tokens 11.2 / 23.9 / 44.2 us; this 9.7 / 20.6 / 37.8.)
-template <bool SPARSE>
+template <bool SPARSE, bool OWN>
 __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
     __shared__ float sk[2][16], sl[2][16];
     __shared__ int sidx[2][16];
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
     const int row = bv.slot_off[b] + a;
     const float* st4 = p.sstat + (size_t)row * 4;
     const float M = st4[0], S = st4[1];
-    const float* z = row_of(p, row);
+    const float* z = row_of<OWN>(p, row);
     const bool resid = a < Lb;
     const int k0 = c * p.cw, k1 = min(p.V, k0 + p.cw);
     const float* qr = nullptr;
@@ -486,7 +487,7 @@ void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, cons
     p.own_only = groups > 0;
     const int chunks = (D.V + p.cw - 1) / p.cw;
     // (slots with logits of their own are decided again from those)
-    if (groups > 0) hipLaunchKernelGGL(k_samp_a2<true>, dim3(bv.T), dim3(256), 0, s, p, chunks);
+    if (groups > 0) hipLaunchKernelGGL((k_samp_a2<true, false>), dim3(bv.T), dim3(256), 0, s, p, chunks);
     if (groups == 0 || own.own) {
         // phase A chunks: about 16 workgroups a CU in all (each pays its merge,
         // 64 chunks a slot cost 32 us for 108 slots of 151936 against 15),
@@ -496,11 +497,17 @@ void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, cons
         p.cwa = ((D.V + ca - 1) / ca + 3) & ~3;
         p.chunks_a = (D.V + p.cwa - 1) / p.cwa;
         const dim3 ga(bv.T, p.chunks_a);
+        const dim3 g4((bv.T + 3) / 4);
         if (nm)
-            hipLaunchKernelGGL(k_samp_a1<true>, ga, dim3(256), 0, s, p, *nm, *nt);
+            hipLaunchKernelGGL((k_samp_a1<true, false>), ga, dim3(256), 0, s, p, *nm, *nt);
+        else if (own.own)
+            hipLaunchKernelGGL((k_samp_a1<false, true>), ga, dim3(256), 0, s, p, NoallocMeta{}, NoallocTables{});
         else
-            hipLaunchKernelGGL(k_samp_a1<false>, ga, dim3(256), 0, s, p, NoallocMeta{}, NoallocTables{});
-        hipLaunchKernelGGL(k_samp_a2<false>, dim3((bv.T + 3) / 4), dim3(256), 0, s, p, p.chunks_a);
+            hipLaunchKernelGGL((k_samp_a1<false, false>), ga, dim3(256), 0, s, p, NoallocMeta{}, NoallocTables{});
+        if (own.own)
+            hipLaunchKernelGGL((k_samp_a2<false, true>), g4, dim3(256), 0, s, p, p.chunks_a);
+        else
+            hipLaunchKernelGGL((k_samp_a2<false, false>), g4, dim3(256), 0, s, p, p.chunks_a);
     }
     if (bv.mode == 1) {
         // whole waves, as many as are resident at once over all users (24 a
@@ -508,10 +515,9 @@ void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, cons
         const int quads = p.cw / 4, most = std::min(16, std::max(1, 24 * cu_count() / (bv.B * chunks))) * 64;
         const int tiles = (quads + most - 1) / most;
         const int nt = ((quads + tiles - 1) / tiles + 63) & ~63;
-        if (bv.qk > 0)
-            hipLaunchKernelGGL(k_samp_b1<true>, dim3(bv.B, chunks), dim3(nt), 0, s, p);
-        else
-            hipLaunchKernelGGL(k_samp_b1<false>, dim3(bv.B, chunks), dim3(nt), 0, s, p);
+        const auto race = bv.qk > 0 ? (own.own ? k_samp_b1<true, true> : k_samp_b1<true, false>)
+                                    : (own.own ? k_samp_b1<false, true> : k_samp_b1<false, false>);
+        hipLaunchKernelGGL(race, dim3(bv.B, chunks), dim3(nt), 0, s, p);
     }
     hipLaunchKernelGGL(k_samp_b2, dim3((bv.B + 3) / 4), dim3(256), 0, s, p, chunks);
 }

@@ -251,7 +251,7 @@ struct FilterCall {
     int32_t* kept;
     float* out;
     int64_t ostride;
-    const int32_t* only;  // [n_rows] or null (all): rows where it is 0 are left as they are (out)
+    const int32_t* only;  // [n_rows] or null (all): rows where it is 0 are left as they are (fp32 rows, out)
     void* ws;  // filter_workspace bytes
 };
 size_t filter_workspace(int n_rows, int V);
