@@ -593,6 +593,190 @@ typedef struct sd_layer_adapters {
 sd_status sd_adapters_set(sd_ctx* ctx, int32_t n_adapters, const sd_layer_adapters* layers);
 sd_status sd_user_adapter(sd_ctx* ctx, int32_t user, int32_t adapter);
 
+/*
+ * Trees of drafts.  A device that drafts several continuations sends them as a
+ * tree: the root token and its drafts are numbered breadth-first or in any
+ * order in which a draft follows its parent, each draft names its parent, and
+ * a slot attends to the cached prefix, to its ancestors and to itself.  The
+ * calls below work on a paged cache laid out as a context's KV pool; they need
+ * no context, and follow the rules of the context-free calls above.  Values in
+ * device arrays need no check: what a wrong one means is said with each, and no
+ * value leads to a read or write outside the arrays and the pool.
+ */
+
+/*
+ * A paged cache: n_layers x n_pages pages of 16 tokens, [layer][page][K | V][kv
+ * head] blocks of 16 * head_dim elements of `dtype`; a K block is [16][head_dim],
+ * a V block [head_dim][16].  This is the layout of the kv_pool that
+ * sd_verify_init takes (sd_user_pages gives a user's pages in it).
+ * SD_BF16: head_dim 64 or 128; SD_F32: even, up to 128 (SD_ENOTIMPL otherwise).
+ * At most 2^27 pages, 2^13 heads and 2^12 layers (SD_ELIMIT).  base is 256-byte
+ * aligned.
+ */
+typedef struct sd_kv_pool {
+    int32_t n_layers, n_pages, n_kv_heads, head_dim, dtype;
+    void* base;
+} sd_kv_pool;
+
+#define SD_TREE_MAX_SLOTS 256
+#define SD_TREE_MAX_USERS 16384
+
+/*
+ * The trees of n_users users, whose slots follow each other (device arrays):
+ *   slot_off:   int32 [n_users + 1], user b's slots are slot_off[b] ..
+ *               slot_off[b+1]-1 (values beyond 0 .. n_slots count as the
+ *               nearest of these; of more than max_slots slots the first
+ *               max_slots count, a user may have none)
+ *   prefix:     int32 [n_users], cached tokens before the user's first slot
+ *               (negative: 0); slot j's key and value are at position prefix + j
+ *   page_table: int32 [n_users][max_pages]: position p lies in page
+ *               page_table[b][p / 16], row p % 16.  Positions at or beyond 16 *
+ *               max_pages, and those on a page that the pool has not got, are
+ *               not attended to
+ *   parent:     int32 [n_slots]: the parent of slot j of its user, as a slot
+ *               number of that user below j; any other value: none, the slot
+ *               sees the prefix and itself.  NULL: slot j-1, a chain
+ * max_slots (host, 1 .. SD_TREE_MAX_SLOTS) and max_pages bound the work of a
+ * launch, whose shape depends on the host values alone: a captured call
+ * replays with other trees and longer contexts.
+ */
+typedef struct sd_tree {
+    int32_t n_users, n_slots, max_slots, max_pages;
+    const int32_t* slot_off;
+    const int32_t* prefix;
+    const int32_t* page_table;
+    const int32_t* parent;
+} sd_tree;
+
+/* Bytes of workspace (256-byte aligned) of sd_tree_attention.  Host only.
+ * SD_EINVAL: an inconsistent pool or tree, n_q_heads no multiple of the pool's
+ * n_kv_heads; SD_ENOTIMPL: a head_dim the kernels do not cover; SD_ELIMIT:
+ * max_slots or n_users beyond the limits above, more than 2^20 slots or 128
+ * query heads a KV head, or the pool's limits. */
+sd_status sd_tree_query_size(const sd_kv_pool* pool, const sd_tree* tree, int32_t n_q_heads,
+                             uint64_t* workspace_bytes);
+
+/*
+ * Attention of every slot of the trees in layer `layer`, grouped query heads:
+ *   out[t][h] = sum_p softmax_p(scale * q[t][h] . K[p][h / G]) V[p][h / G]
+ * over the positions p that the slot sees, G = n_q_heads / n_kv_heads.  A tree
+ * of one slot is a decoding step.
+ *   q:     [n_slots] rows of n_q_heads * head_dim elements of the pool's
+ *          dtype, q_stride elements apart
+ *   q_lo:  second plane of q (SD_BF16; q + q_lo is the value), or NULL
+ *   out:   rows like q's, out_stride apart; slots of no user are left as they
+ *          are, a slot that sees nothing becomes 0.  May not overlap q
+ *   out_lo: second plane of out (SD_BF16: out + out_lo has 16 bits), or NULL
+ *   scale: > 0 and finite
+ * Scores, maxima, sums and outputs are fp32 (the weights of the second product
+ * in two bf16 planes), in an order that depends on the sizes alone.  A cached
+ * infinity or not-a-number has no part in rows that do not see it.  Rows of
+ * q and out are 16-byte aligned (SD_BF16), elements otherwise.
+ * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, layer,
+ * stride, overlap, scale, a second plane with SD_F32), the above, SD_ENOMEM
+ * (workspace too small), SD_EHIP.
+ */
+sd_status sd_tree_attention(const sd_kv_pool* pool, int32_t layer, const sd_tree* tree, int32_t n_q_heads,
+                            const void* q, const void* q_lo, int64_t q_stride, void* out, void* out_lo,
+                            int64_t out_stride, float scale, void* workspace, uint64_t workspace_bytes,
+                            sd_stream stream);
+
+/*
+ * Pages dst[i] := pages src[i], i = 0 .. n-1, in every layer (src, dst: device
+ * int32 [n]).  A pair with a page that the pool has not got copies nothing.
+ * Destinations are distinct and no page is both a source and a destination
+ * (otherwise what they hold afterwards is undefined).
+ * Errors (nothing enqueued): SD_EINVAL (an inconsistent pool, NULL or misaligned
+ * pointer, n < 1), SD_ENOTIMPL (head_dim), SD_ELIMIT (n pages of a layer above 2^37
+ * bytes, or the pool's limits), SD_EHIP.
+ */
+sd_status sd_kv_copy_pages(const sd_kv_pool* pool, int32_t n, const int32_t* src, const int32_t* dst,
+                           sd_stream stream);
+
+#define SD_KV_COMPACT_MAX 256
+
+/*
+ * Rows moved together after the accepted path of a tree is known: for every
+ * user b, in every layer and KV head, the key and value of position prefix[b] + i
+ * become those that position prefix[b] + keep[b][i] had before the call, i = 0 ..
+ * n_keep[b]-1.  All rows are read before any is written, so keep may hold any
+ * numbers in any order, also one twice.
+ *   prefix, page_table, max_pages: as in sd_tree; a page belongs to one user
+ *   keep:   int32 [n_users][max_keep]; a negative number, or one whose position
+ *           or page does not exist, leaves row i as it is
+ *   n_keep: int32 [n_users], taken as 0 .. max_keep where it is beyond
+ * Errors (nothing enqueued): SD_EINVAL (an inconsistent pool, NULL or
+ * misaligned pointer, n_users, max_keep or max_pages < 1), SD_ENOTIMPL
+ * (head_dim), SD_ELIMIT (max_keep above SD_KV_COMPACT_MAX, n_users above
+ * SD_TREE_MAX_USERS, or the pool's limits), SD_EHIP.
+ */
+sd_status sd_kv_compact(const sd_kv_pool* pool, int32_t n_users, const int32_t* prefix, const int32_t* page_table,
+                        int32_t max_pages, const int32_t* keep, int32_t max_keep, const int32_t* n_keep,
+                        sd_stream stream);
+
+/*
+ * Rules that a request's logits pass before sampling options: penalties for
+ * repeated tokens, biases, and a grammar's mask.  All arrays are device arrays
+ * and may be NULL (off), tables of row t:
+ *   hist:    int32 [n_rows][3] begin, first, end: tokens[begin .. first-1] are
+ *            the prompt's, tokens[first .. end-1] the output's (n_tokens of
+ *            them in all; a number outside 0 .. n_tokens counts as the nearest,
+ *            and one below its predecessor as that).  Rows with the same
+ *            numbers one after the other share the reading
+ *   row_token, row_parent: int32 [n_rows]: drafts that belong to the output of
+ *            this row alone: row t's own token, its parent row's, and so on.
+ *            The parent is a row below t, any other value: none; rows more than
+ *            SD_TREE_MAX_SLOTS below the row itself do not count.  Both or none
+ *   repetition, presence, frequency: fp32 [n_rows]; a repetition that is not
+ *            positive and finite counts as 1, a presence or frequency that is
+ *            not finite as 0
+ *   bias:    int32 [n_rows][2] begin, end: bias_token[begin .. end-1] (int32)
+ *            have bias_value (fp32) added; of n_bias entries, clamped like hist.
+ *            Of one token listed twice the last entry counts
+ *   mask:    uint32 [n_masks][ceil(vocab / 32)], bit k % 32 of word k / 32 set:
+ *            token k is allowed;  mask_row: int32 [n_rows], which mask (outside
+ *            0 .. n_masks-1: none)
+ * With c the number of times a token is in the output and s whether it is in
+ * prompt or output, z becomes, in this order,
+ *   s:            z / repetition if z > 0, z * repetition otherwise
+ *   c > 0:        z - (frequency * c + presence)
+ *   listed:       z + bias
+ *   not allowed:  -inf
+ * Tokens outside 0 .. vocab-1 count for nothing.
+ */
+typedef struct sd_logit_rules {
+    const int32_t* tokens;
+    int64_t n_tokens;
+    const int32_t* hist;
+    const int32_t* row_token;
+    const int32_t* row_parent;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const int32_t* bias_token;
+    const float* bias_value;
+    int64_t n_bias;
+    const int32_t* bias;
+    const uint32_t* mask;
+    int32_t n_masks;
+    const int32_t* mask_row;
+} sd_logit_rules;
+
+/*
+ * out[t] = the rows of logits under the rules, fp32.  logits, dtype and
+ * row_stride as in sd_sample_filtered; out's rows are out_stride (>= vocab)
+ * apart, and it may be the logits themselves (SD_F32, same stride: only what
+ * changes is written) but not overlap them otherwise.  The result is what
+ * sd_sample_filtered, sd_filter_logits and sd_sample_logits take as logits; a
+ * row whose mask allows nothing is -inf throughout, which gives token -1 there.
+ * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, dtype,
+ * stride, overlap, one array of a pair without the other; a table of ranges of
+ * nothing needs no list), SD_ELIMIT (rows or
+ * vocab beyond SD_FILTER_MAX_*, n_tokens or n_bias beyond 2^31 - 1), SD_EHIP.
+ */
+sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                           const sd_logit_rules* rules, float* out, int64_t out_stride, sd_stream stream);
+
 /* Kernel classes for sd_profile_begin. */
 enum {
     SD_K_QKV = 1,      /* QKV projection GEMM + fused QK-norm/RoPE/KV append */

@@ -4,6 +4,9 @@
 #include <stdint.h>
 #include <stddef.h>
 
+struct sd_kv_pool;
+struct sd_logit_rules;
+
 namespace sdv {
 
 constexpr int kPageTokens = 16;   // tokens per KV page
@@ -282,6 +285,70 @@ struct LoraCall {
 };
 size_t lora_workspace(int T, int rank, int n_seg, int d_in, int bf16);
 void launch_lora(const LoraCall& c, hipStream_t s);
+
+// Attention of trees of drafts over a paged cache (sd_tree, sd_tree_attention).
+struct TreeCall {
+    KVPool kv;
+    int layer;
+    int n_users, n_slots, max_slots, max_pages, hq;
+    const int32_t *slot_off, *prefix, *page_table, *parent;
+    const void *q, *q_lo;  // [n_slots][qs]
+    void *out, *out_lo;    // [n_slots][os]
+    int64_t qs, os;
+    float scale;
+    void* ws;
+    size_t ws_bytes;
+};
+size_t tree_workspace(const TreeCall& c);
+void launch_tree_attention(const TreeCall& c, hipStream_t s);
+
+// A caller's paged cache as the kernels see it; SD_OK, or why not.
+int32_t pool_of(const ::sd_kv_pool* p, KVPool* kv);
+
+// Pages of a paged cache copied in every layer: page dst[i] := page src[i], from
+// device arrays, or (n <= kCopyPages) from the kernel's arguments.
+constexpr int kCopyPages = 120;
+struct CopyPages {
+    int32_t src[kCopyPages], dst[kCopyPages];
+};
+void launch_copy_pages(const KVPool& kv, int layers, int n, const int32_t* src, const int32_t* dst, hipStream_t s);
+void launch_copy_pages(const KVPool& kv, int layers, int n, const CopyPages& pages, hipStream_t s);
+
+// Rows moved together: position prefix[b] + i := position prefix[b] + keep[b][i], i
+// < n_keep[b], in every layer and KV head.  path (instead of keep): [B] bit masks of
+// the accepted drafts, row 0 (the root) stays and the i-th set bit p moves slot p + 1 to row i.
+struct CompactCall {
+    KVPool kv;
+    int layers, n_users, max_pages, max_keep;
+    const int32_t *prefix, *page_table, *keep, *n_keep;
+    const uint64_t* path;
+};
+void launch_compact(const CompactCall& c, hipStream_t s);
+
+// Rules on rows of logits (sd_logit_rules), out fp32 (out may be logits).
+// slot_j (instead of row_parent): rows of a user follow each other, row t's parent
+// is row t - 1 unless slot_j[t] is 0; parents of a user's own slots else (user-local,
+// where slot_j is given too).
+struct RulesCall {
+    int n_rows, V, bf16;
+    const void* logits;
+    int64_t stride;
+    float* out;
+    int64_t ostride;
+    const int32_t* tokens;
+    int n_tokens;
+    const int32_t *hist, *row_token, *row_parent, *slot_j;
+    const float *rep, *pres, *freq;
+    const int32_t* bias_token;
+    const float* bias_value;
+    int n_bias;
+    const int32_t* bias;
+    const uint32_t* mask;
+    int n_masks;
+    const int32_t* mask_row;
+};
+void launch_rules(const RulesCall& c, hipStream_t s);
+int32_t rules_of(const ::sd_logit_rules* r, RulesCall* c);
 
 void launch_kv_copy(const Dims& D, const KVPool& kv, const KVCopyPages& pages, int layer,
                     int pos0, int n, const void* k, const void* v, int to_pool, hipStream_t s);

@@ -29,9 +29,11 @@ EXPORTS = ("sd_verify_query_sizes", "sd_verify_init", "sd_verify_destroy", "sd_u
            "sd_verify_batch_graph", "sd_verify_batch_sparse", "sd_draft_batch", "sd_accept", "sd_sample_logits",
            "sd_sample_logits_noalloc", "sd_debug_logits", "sd_debug_wait_limit", "sd_profile_begin", "sd_profile_end",
            "sd_filter_query_size", "sd_sample_filtered", "sd_filter_logits", "sd_lora_query_size",
-           "sd_lora_apply", "sd_user_sampling", "sd_adapters_set", "sd_user_adapter", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
+           "sd_lora_apply", "sd_tree_query_size", "sd_tree_attention", "sd_kv_copy_pages", "sd_kv_compact",
+           "sd_adjust_logits", "sd_user_sampling", "sd_adapters_set", "sd_user_adapter", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
 SD_FILTER_MAX_ROWS, SD_FILTER_MAX_VOCAB = 65535, 1 << 20
 SD_LORA_MAX_RANK, SD_LORA_MAX_SEGS = 128, 4
+SD_TREE_MAX_SLOTS, SD_TREE_MAX_USERS, SD_KV_COMPACT_MAX = 256, 16384, 256
 SD_K_QKV, SD_K_ATTN, SD_K_O, SD_K_GATEUP, SD_K_DOWN, SD_K_LMHEAD, SD_K_SAMPLER, SD_K_SMALL = range(1, 9)
 
 
@@ -66,6 +68,23 @@ class sd_lora(ctypes.Structure):
 
 class sd_layer_adapters(ctypes.Structure):
     _fields_ = [(n, sd_lora) for n in ("qkv", "o", "down")]
+
+
+class sd_kv_pool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_pages", "n_kv_heads", "head_dim", "dtype")] + [
+        ("base", ctypes.c_void_p)]
+
+
+class sd_tree(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_users", "n_slots", "max_slots", "max_pages")] + [
+        (n, ctypes.c_void_p) for n in ("slot_off", "prefix", "page_table", "parent")]
+
+
+class sd_logit_rules(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("n_tokens", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in (
+        "hist", "row_token", "row_parent", "repetition", "presence", "frequency", "bias_token", "bias_value")] + [
+        ("n_bias", ctypes.c_int64), ("bias", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("n_masks", ctypes.c_int32),
+        ("mask_row", ctypes.c_void_p)]
 
 
 class SdError(RuntimeError):
@@ -114,6 +133,11 @@ def lib() -> ctypes.CDLL:
         L.sd_lora_query_size.argtypes = [P(sd_lora), i32, P(u64)]
         L.sd_lora_apply.argtypes = [P(sd_lora), i32, vp, vp, vp, i64, vp, i64, vp, i64, i32, vp, u64, vp]
         f32 = ctypes.c_float
+        L.sd_tree_query_size.argtypes = [P(sd_kv_pool), P(sd_tree), i32, P(u64)]
+        L.sd_tree_attention.argtypes = [P(sd_kv_pool), i32, P(sd_tree), i32, vp, vp, i64, vp, vp, i64, f32, vp, u64, vp]
+        L.sd_kv_copy_pages.argtypes = [P(sd_kv_pool), i32, vp, vp, vp]
+        L.sd_kv_compact.argtypes = [P(sd_kv_pool), i32, vp, vp, i32, vp, i32, vp, vp]
+        L.sd_adjust_logits.argtypes = [i32, i32, vp, i32, i64, P(sd_logit_rules), vp, i64, vp]
         L.sd_user_sampling.argtypes = [vp, i32, f32, i32, f32, f32]
         L.sd_adapters_set.argtypes = [vp, i32, P(sd_layer_adapters)]
         L.sd_user_adapter.argtypes = [vp, i32, i32]
@@ -430,6 +454,195 @@ def sd_lora_apply(w: Lora, adapter, x, y_in, y_out, workspace, x_lo=None, stream
     _check("sd_lora_apply", lib().sd_lora_apply(
         w.ref, n, _vec(adapter, n, "torch.int32", "adapter", at), xp, lo, xs, yi, ys, yo, yos, _dtype(y_in, "y_in"),
         ws, size, _stream(stream)))
+
+
+class KVPool:
+    """A paged cache (sd_kv_pool) with the tensor it lives in."""
+
+    def __init__(self, desc: sd_kv_pool, base):
+        self.desc, self.base, self.device = desc, base, base.device
+        self.ref = ctypes.byref(desc)
+
+
+def make_kv_pool(base, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, dtype: Optional[int] = None) -> KVPool:
+    """A paged cache in a contiguous tensor of n_layers * n_pages * 2 *
+    n_kv_heads * 16 * head_dim elements (float32 or bfloat16, or bytes
+    with dtype SD_F32 or SD_BF16, as Verifier.kv_pool is)."""
+    at = _on_current_device(base, "base")
+    dtype = _dtype(base, "base") if dtype is None else int(dtype)
+    es = 2 if dtype == SD_BF16 else 4
+    want = n_layers * n_pages * 2 * n_kv_heads * 16 * head_dim * es
+    if not base.is_contiguous() or base.numel() * base.element_size() != want:
+        raise ValueError(f"base: a contiguous tensor of {want} bytes on {at}, not {base.numel() * base.element_size()}")
+    return KVPool(sd_kv_pool(n_layers, n_pages, n_kv_heads, head_dim, dtype, base.data_ptr()), base)
+
+
+def _table(t, rows: Optional[int], what: str, at):
+    """(device pointer, columns) of a contiguous int32 matrix."""
+    if str(t.dtype) != "torch.int32" or t.dim() != 2 or not t.is_contiguous() or t.device != at or (
+            rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{what}: a contiguous int32 matrix{'' if rows is None else f' of {rows} rows'} on {at}, not "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), t.shape[1]
+
+
+class Tree:
+    """Users' trees of drafts (sd_tree) with the tensors they live in."""
+
+    def __init__(self, desc: sd_tree, tensors, device):
+        self.desc, self.tensors, self.device = desc, tensors, device
+        self.ref = ctypes.byref(desc)
+
+
+def make_tree(slot_off, prefix, page_table, parent=None, *, max_slots: int, n_slots: Optional[int] = None) -> Tree:
+    """Trees from device int32 slot_off [n + 1], prefix [n], page_table
+    [n][max_pages] and parent [n_slots] (None: chains; n_slots is then
+    needed).  max_slots: the most slots of a user."""
+    at = _on_current_device(slot_off, "slot_off")
+    n = slot_off.numel() - 1
+    table, max_pages = _table(page_table, n, "page_table", at)
+    if parent is not None:
+        if n_slots is not None and n_slots != parent.numel():
+            raise ValueError(f"parent of {parent.numel()} slots, not {n_slots}")
+        n_slots = parent.numel()
+    elif n_slots is None:
+        raise ValueError("n_slots is needed without parent")
+    d = sd_tree(n, int(n_slots), int(max_slots), max_pages, _vec(slot_off, n + 1, "torch.int32", "slot_off", at),
+                _vec(prefix, n, "torch.int32", "prefix", at), table, _vec(parent, n_slots, "torch.int32", "parent", at))
+    return Tree(d, (slot_off, prefix, page_table, parent), at)
+
+
+def sd_tree_query_size(pool: KVPool, tree: Tree, n_q_heads: int) -> int:
+    """Bytes of workspace of sd_tree_attention."""
+    b = ctypes.c_uint64()
+    _check("sd_tree_query_size", lib().sd_tree_query_size(pool.ref, tree.ref, int(n_q_heads), ctypes.byref(b)))
+    return b.value
+
+
+def _heads(t, like, what: str, at):
+    """(device pointer, row stride) of [n_slots][heads][head_dim] rows, each contiguous."""
+    if t.dim() != 3 or t.device != at or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+        raise ValueError(f"{what}: [slots][heads][head_dim] on {at}{'' if like is None else ' like q'}, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    n, h, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (n > 1 and t.stride(0) < h * d):
+        raise ValueError(f"{what}: a slot's heads must be contiguous and slots apart, strides are {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if n > 1 else h * d)
+
+
+def sd_tree_attention(pool: KVPool, layer: int, tree: Tree, q, out, workspace, q_lo=None, out_lo=None,
+                      scale: Optional[float] = None, stream=None) -> None:
+    """out[t][h] = attention of slot t's query head h over what it sees of its
+    user's cache: q, out [n_slots][heads][head_dim] of the pool's type (q_lo,
+    out_lo: second bf16 planes), scale 1 / sqrt(head_dim) by default."""
+    at = _on_current_device(q, "q")
+    if pool.device != at or tree.device != at:
+        raise ValueError(f"pool on {pool.device}, trees on {tree.device}, q on {at}")
+    qp, qs = _heads(q, None, "q", at)
+    op, os_ = _heads(out, q, "out", at)
+    if q.shape[0] != tree.desc.n_slots or q.shape[2] != pool.desc.head_dim or _dtype(q, "q") != pool.desc.dtype:
+        raise ValueError(f"q: {tree.desc.n_slots} slots of heads of {pool.desc.head_dim} in the pool's type, not {q.dtype} "
+                         f"{tuple(q.shape)}")
+    ql = ol = None
+    if q_lo is not None:
+        ql, s = _heads(q_lo, q, "q_lo", at)
+        if s != qs:
+            raise ValueError("q_lo: strides like q's")
+    if out_lo is not None:
+        ol, s = _heads(out_lo, q, "out_lo", at)
+        if s != os_:
+            raise ValueError("out_lo: strides like out's")
+    ws, size = _workspace(workspace, at)
+    _check("sd_tree_attention", lib().sd_tree_attention(
+        pool.ref, int(layer), tree.ref, q.shape[1], qp, ql, qs, op, ol, os_,
+        q.shape[2] ** -0.5 if scale is None else float(scale), ws, size, _stream(stream)))
+
+
+def sd_kv_copy_pages(pool: KVPool, src, dst, stream=None) -> None:
+    """Pages dst[i] := pages src[i] (device int32) in every layer."""
+    at = _on_current_device(src, "src")
+    if pool.device != at:
+        raise ValueError(f"pool on {pool.device}, src on {at}")
+    n = src.numel()
+    _check("sd_kv_copy_pages", lib().sd_kv_copy_pages(
+        pool.ref, n, _vec(src, n, "torch.int32", "src", at), _vec(dst, n, "torch.int32", "dst", at), _stream(stream)))
+
+
+def sd_kv_compact(pool: KVPool, prefix, page_table, keep, n_keep, stream=None) -> None:
+    """Position prefix[b] + i := position prefix[b] + keep[b][i], i < n_keep[b], in
+    every layer and head (device int32 [n], [n][max_pages], [n][max_keep], [n])."""
+    at = _on_current_device(prefix, "prefix")
+    if pool.device != at:
+        raise ValueError(f"pool on {pool.device}, prefix on {at}")
+    n = prefix.numel()
+    table, max_pages = _table(page_table, n, "page_table", at)
+    kp, max_keep = _table(keep, n, "keep", at)
+    _check("sd_kv_compact", lib().sd_kv_compact(
+        pool.ref, n, _vec(prefix, n, "torch.int32", "prefix", at), table, max_pages, kp, max_keep,
+        _vec(n_keep, n, "torch.int32", "n_keep", at), _stream(stream)))
+
+
+class LogitRules:
+    """Rules on rows of logits (sd_logit_rules) with the tensors they live in."""
+
+    def __init__(self, desc: sd_logit_rules, n_rows: int, vocab: int, tensors, device):
+        self.desc, self.n_rows, self.vocab, self.tensors, self.device = desc, n_rows, vocab, tensors, device
+        self.ref = ctypes.byref(desc)
+
+
+def make_logit_rules(n_rows: int, vocab: int, *, tokens=None, hist=None, repetition=None, presence=None, frequency=None,
+                     row_token=None, row_parent=None, bias_token=None, bias_value=None, bias=None, mask=None,
+                     mask_row=None) -> LogitRules:
+    """Rules for n_rows rows of `vocab` logits (device tensors, None: off):
+    tokens int32 [n] and hist int32 [n_rows][3]; repetition, presence, frequency
+    float32 [n_rows]; row_token, row_parent int32 [n_rows]; bias_token int32
+    [m], bias_value float32 [m] and bias int32 [n_rows][2]; mask int32 [k][ceil(vocab
+    / 32)] (bits of allowed tokens) and mask_row int32 [n_rows]."""
+    tensors = (tokens, hist, repetition, presence, frequency, row_token, row_parent, bias_token, bias_value, bias, mask,
+               mask_row)
+    given = [t for t in tensors if t is not None]
+    if not given:
+        raise ValueError("no rules")
+    at = _on_current_device(given[0], "rules")
+    for a, b, names in ((tokens, hist, "tokens and hist"), (row_token, row_parent, "row_token and row_parent"),
+                        (bias_token, bias, "bias_token and bias"), (bias_token, bias_value, "bias_token and bias_value"),
+                        (mask, mask_row, "mask and mask_row")):
+        if (a is None) != (b is None):
+            raise ValueError(f"{names} belong together")
+
+    def table(t, cols, what):
+        if t is None:
+            return None
+        p, c = _table(t, None if what == "mask" else n_rows, what, at)
+        if c != cols:
+            raise ValueError(f"{what}: {cols} columns, not {c}")
+        return p
+
+    i32, f32 = "torch.int32", "torch.float32"
+    size = lambda t: 0 if t is None else t.numel()  # noqa: E731
+    d = sd_logit_rules(
+        _vec(tokens, size(tokens), i32, "tokens", at), size(tokens), table(hist, 3, "hist"),
+        _vec(row_token, n_rows, i32, "row_token", at), _vec(row_parent, n_rows, i32, "row_parent", at),
+        _vec(repetition, n_rows, f32, "repetition", at), _vec(presence, n_rows, f32, "presence", at),
+        _vec(frequency, n_rows, f32, "frequency", at), _vec(bias_token, size(bias_token), i32, "bias_token", at),
+        _vec(bias_value, size(bias_token), f32, "bias_value", at), size(bias_token), table(bias, 2, "bias"),
+        table(mask, (vocab + 31) // 32, "mask"), 0 if mask is None else mask.shape[0],
+        _vec(mask_row, n_rows, i32, "mask_row", at))
+    return LogitRules(d, n_rows, vocab, tensors, at)
+
+
+def sd_adjust_logits(logits, rules: LogitRules, out, stream=None) -> None:
+    """out float32 [n][vocab] = the rows of logits (float32 or bfloat16) under the
+    rules.  out may be logits."""
+    at = _on_current_device(logits, "logits")
+    ptr, stride = _matrix(logits, rules.vocab, "logits", at)
+    optr, ostride = _matrix(out, rules.vocab, "out", at)
+    n = logits.shape[0]
+    if n != rules.n_rows or out.shape[0] != n or _dtype(out, "out") != SD_F32 or rules.device != at:
+        raise ValueError(f"logits and out: {rules.n_rows} rows, out float32, on the rules' {rules.device}, not {n} and "
+                         f"{out.dtype} of {out.shape[0]} on {at}")
+    _check("sd_adjust_logits", lib().sd_adjust_logits(
+        n, rules.vocab, ptr, _dtype(logits, "logits"), stride, rules.ref, optr, ostride, _stream(stream)))
 
 
 def sd_user_sampling(ctx: int, user: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
