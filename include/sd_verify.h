@@ -778,6 +778,66 @@ typedef struct sd_logit_rules {
 sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
                            const sd_logit_rules* rules, float* out, int64_t out_stride, sd_stream stream);
 
+/*
+ * The same inside a context.
+ *
+ * sd_verify_batch_tree: sd_verify_batch for trees of drafts.
+ *   parent: host int32 [sum l_m], in the order of draft_tokens: the parent of
+ *           the i-th draft of its user (i = 1 .. l_m), 0: the root, else the
+ *           number of an earlier draft of that user
+ * A slot's position is its depth, i_m for the root; slot j's key and value are
+ * first written at position i_m + j.  The target's token after each slot is
+ * its argmax (SD_GREEDY) or drawn from its distribution p (SD_STOCHASTIC, under
+ * the user's sampling options, race keyed by (seed, round, user, slot)).  From
+ * the root on, a draft below the current slot that equals that token is
+ * accepted and becomes the current slot (of equal ones the first); where there is
+ * none, that token is the user's out_token.  So the tokens are those of the
+ * target alone, whatever the drafts are and however they were chosen, and no
+ * draft probabilities are needed.  The accepted rows are moved together in the
+ * cache by the pass itself (positions i_m + 1 .. i_m + a_m).
+ * Complete with sd_accept or sd_accept_tree.  Errors as sd_verify_batch, and
+ * SD_EINVAL for SD_FORCE or a parent out of range, SD_ENOTIMPL for more than
+ * 800 slots.
+ *
+ * sd_accept_tree: sd_accept, and the drafts accepted: path, host int32
+ * [M][max_draft], receives for every user of the batch the numbers (1 .. l_m) of
+ * its accepted drafts in order, then -1 (1 .. a_m for a batch without trees).
+ *
+ * sd_user_fork: start user `user` with a copy of the first prefix_len cached
+ * tokens of user `from` (at most its length) and a root token of its own.
+ * Pages that `user` held are given back first.  The copy is enqueued on
+ * `stream` without waiting; passes of either user have to be ordered after it.
+ * Sampling options and adapter of `user` stay its own.
+ * Errors: SD_EINVAL (a user, length or token out of range, `from` not started,
+ * the same user), SD_ESTATE (one of them pending), SD_ENOMEM (pool exhausted;
+ * nothing has changed), SD_EHIP.
+ *
+ * sd_user_pages: the pages that a user holds, in order: pages, host int32
+ * [capacity] (may be NULL with capacity 0), receives the first of them, n_pages
+ * their number.
+ *
+ * sd_batch_rules: rules for the logits of the next pass of batch `batch`, of any
+ * kind, in every mode: n_rows rows, one a query slot of the batch in order.
+ * row_token and row_parent have to be NULL: the pass counts its own slots'
+ * tokens (root and drafts, along the tree), so hist ends before the root.  The
+ * rules come before sampling options; sd_debug_logits shows their result.
+ * The struct is copied, its arrays have to stay until sd_accept.  The pass takes
+ * the rules away, and so does a NULL rules.  A pass of another number of slots
+ * is refused (SD_EINVAL; the rules stay), and so is sd_sample_logits of a user
+ * never started, whose root token there is none of.
+ * Errors: SD_EINVAL, SD_ELIMIT as sd_adjust_logits, SD_ESTATE (the batch's
+ * workspace slot is pending).
+ */
+sd_status sd_verify_batch_tree(sd_ctx* ctx, int32_t batch, int32_t n_users, const int32_t* assign,
+                               const int32_t* draft_len, const int32_t* draft_tokens, const int32_t* parent,
+                               int32_t mode, uint64_t seed, uint64_t round, sd_stream stream);
+sd_status sd_accept_tree(sd_ctx* ctx, int32_t batch, int32_t* n_accepted, int32_t* out_token, int32_t* path,
+                         int32_t commit);
+sd_status sd_user_fork(sd_ctx* ctx, int32_t user, int32_t from, int32_t prefix_len, int32_t root_token,
+                       sd_stream stream);
+sd_status sd_user_pages(sd_ctx* ctx, int32_t user, int32_t* pages, int32_t capacity, int32_t* n_pages);
+sd_status sd_batch_rules(sd_ctx* ctx, int32_t batch, int32_t n_rows, const sd_logit_rules* rules);
+
 /* Kernel classes for sd_profile_begin. */
 enum {
     SD_K_QKV = 1,      /* QKV projection GEMM + fused QK-norm/RoPE/KV append */

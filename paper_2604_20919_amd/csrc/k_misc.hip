@@ -32,7 +32,7 @@ __global__ void k_prepare(BatchView bv, int32_t* tok, int32_t* dnext, float* cs,
         }
         dnext[t] = dn;
     }
-    const double pos = (double)(bv.prefix[b] + j);
+    const double pos = (double)(bv.prefix[b] + (bv.depth ? bv.depth[t] : j));
     for (int a = threadIdx.x; a < half; a += blockDim.x) {
         const double ang = pos * exp(-2.0 * a / hd * log_base);
         double sn, cn;

@@ -300,7 +300,7 @@ __device__ __forceinline__ int leading_accepts(const SampP& p, int b) {
 // of the bounds and of log1pf (a few 2^-23), the added terms that of
 // subnormal keys.  (Every key exact, 256 threads: 1 / 16 / 32 users of 151936
 // tokens 11.2 / 23.9 / 44.2 us; this 9.7 / 20.6 / 37.8.)
-template <bool SPARSE, bool OWN>
+template <bool SPARSE, bool OWN, bool SLOTS = false>
 __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
     __shared__ float sk[2][16], sl[2][16];
     __shared__ int sidx[2][16];
@@ -311,6 +311,7 @@ __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
     const int Lb = bv.L[b];
     const int a = leading_accepts(p, b);
     const int row = bv.slot_off[b] + a;
+    const int slot = SLOTS ? bv.slot_j[row] : a;
     const float* st4 = p.sstat + (size_t)row * 4;
     const float M = st4[0], S = st4[1];
     const float* z = row_of<OWN>(p, row);
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(1024) void k_samp_b1(SampP p) {
         float lp = 0.f, lr = 0.f;
         u64x4 rnd = u64x4{0, 0, 0, 0};
         if (k4 < k1) {
-            const u64x4 ctr = {bv.round, user, ((uint64_t)PURPOSE_RACE << 32) | (uint64_t)a, (uint64_t)(k4 >> 2)};
+            const u64x4 ctr = {bv.round, user, ((uint64_t)PURPOSE_RACE << 32) | (uint64_t)slot, (uint64_t)(k4 >> 2)};
             rnd = philox4x64_10(ctr, bv.seed, 0ull);
         }
 #pragma unroll
@@ -469,7 +470,8 @@ void launch_probs(const Dims& D, const BatchView& bv, const SlotBufs& sb, const 
 }
 
 void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
-                    hipStream_t s, int groups, const NoallocMeta* nm, const NoallocTables* nt, OwnRows own) {
+                    hipStream_t s, int groups, const NoallocMeta* nm, const NoallocTables* nt, OwnRows own,
+                    bool slots) {
     SampP p;
     p.bv = bv;
     p.logits = logits;
@@ -515,7 +517,8 @@ void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, cons
         const int quads = p.cw / 4, most = std::min(16, std::max(1, 24 * cu_count() / (bv.B * chunks))) * 64;
         const int tiles = (quads + most - 1) / most;
         const int nt = ((quads + tiles - 1) / tiles + 63) & ~63;
-        const auto race = bv.qk > 0 ? (own.own ? k_samp_b1<true, true> : k_samp_b1<true, false>)
+        const auto race = slots ? (own.own ? k_samp_b1<false, true, true> : k_samp_b1<false, false, true>)
+                        : bv.qk > 0 ? (own.own ? k_samp_b1<true, true> : k_samp_b1<true, false>)
                                     : (own.own ? k_samp_b1<false, true> : k_samp_b1<false, false>);
         hipLaunchKernelGGL(race, dim3(bv.B, chunks), dim3(nt), 0, s, p);
     }

@@ -642,6 +642,31 @@ template <int HD> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c
     if (c.out_lo) *(bf16x4*)((bf16_t*)c.out_lo + e) = lo;
 }
 
+// One wave a user: from the root along the drafts that equal the target's tokens, of
+// equal drafts below a slot the first.  At most 64 drafts, a lane each.
+__global__ __launch_bounds__(64) void k_tree_walk(BatchView bv, const int32_t* target, int32_t* result, int bmax,
+                                                  uint64_t* path) {
+    const int b = blockIdx.x, lane = threadIdx.x;
+    if (b == 0 && lane == 0) result[2 * bmax] = *bv.flags;
+    const int s0 = bv.slot_off[b], L = bv.L[b];
+    const bool mine = lane < L;
+    const int draft = mine ? bv.drafts[bv.draft_off[b] + lane] : -1, above = mine ? bv.parent[s0 + lane + 1] : -1;
+    uint64_t taken = 0;
+    int at = 0, n = 0, token = target[s0];
+    while (true) {
+        const uint64_t on = __ballot(mine && above == at && draft == token);
+        if (!on) break;
+        at = __ffsll((unsigned long long)on);  // draft number: lane + 1
+        taken |= on & -on;
+        ++n;
+        token = target[s0 + at];
+    }
+    if (lane != 0) return;
+    result[b] = n;
+    result[bmax + b] = token;
+    path[b] = taken;
+}
+
 // The plan's sizes: units times row groups aimed at, and the workspace it takes.
 struct TreeSizes {
     int cap, groups, units, rows;  // rows: partial rows
@@ -669,6 +694,13 @@ constexpr int kTreeCap = 256 * kResident;
 size_t tree_workspace(const TreeCall& c) {
     if (c.kv.esize != 2) return 256;
     return tree_sizes(c, kTreeCap).bytes;
+}
+
+size_t tree_workspace_least(const TreeCall& c) { return c.kv.esize == 2 ? tree_sizes(c, 1).bytes : 256; }
+
+void launch_tree_walk(const BatchView& bv, const int32_t* target, int32_t* result, int bmax, uint64_t* path,
+                      hipStream_t s) {
+    hipLaunchKernelGGL(k_tree_walk, dim3(bv.B), dim3(64), 0, s, bv, target, result, bmax, path);
 }
 
 // Whether a launch of this shape is possible.

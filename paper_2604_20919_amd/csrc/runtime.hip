@@ -39,8 +39,8 @@ struct Layout {
         st_ioff, st_flags, st_prow, st_temp, st_topk, st_topp, st_minp, st_own, st_adapter, st_bytes;
     // slot buffers (byte offsets within the slot)
     size_t stage, tok, cs, x, ssq, h, ffn, qbuf, attn, apart, aml, gpart, logits, sstat, spart,
-        spartB, lstat, zd, dnext, skcnt, result, filter, lora, slot_bytes;
-    size_t lora_bytes;
+        spartB, lstat, zd, dnext, skcnt, result, filter, lora, tree, slot_bytes;
+    size_t lora_bytes, tree_bytes;
     int filter_rows;  // rows that the filter takes at once (0: none, see sd_user_sampling)
     size_t gpart_floats;
     int nsq;
@@ -178,6 +178,17 @@ Layout plan(const sd_config& c) {
     for (int d_in : {D.d, D.nq(), D.F})
         L.lora_bytes = std::max(L.lora_bytes, lora_workspace(L.Tmax, kLoraRank, kLoraSegs, d_in, D.bf16));
     s = std::max(s, align_up(L.lora + L.lora_bytes));
+    // So do the partial outputs of a tree's attention, as many as there is room for.
+    L.tree = L.logits;
+    TreeCall tc{};
+    tc.kv.hkv = D.hkv;
+    tc.kv.hd = D.hd;
+    tc.kv.esize = (int)es;
+    tc.n_users = L.Bmax;
+    tc.max_slots = std::min(c.max_draft + 1, L.Tmax);
+    tc.hq = D.hq;
+    s = std::max(s, align_up(L.tree + tree_workspace_least(tc)));
+    L.tree_bytes = s - L.tree;
     L.zd = take((size_t)L.Tmax * 4);
     L.dnext = take((size_t)L.Tmax * 4);
     L.skcnt = take((size_t)kSkCounters * 4);
@@ -186,6 +197,9 @@ Layout plan(const sd_config& c) {
     L.total = align_up(L.slot_bytes * (size_t)c.max_pending);
     return L;
 }
+
+// A pass's results, rounded up to the alignment of the masks that follow them.
+size_t result_bytes(int Bmax) { return align_up((size_t)(2 * Bmax + 4) * 4); }
 
 // Element offsets of the packed GEMM weights (bf16): per layer QKV, O,
 // gate/up (interleaved), down; then lm_head.
@@ -229,9 +243,16 @@ struct Slot {
     std::vector<int> prow;   // decode steps: destination row of each user's probabilities
     int filtered = 0;        // users of a stochastic pass with sampling options: none, some (1), all (2)
     bool adapted = false;    // some user of the pass has an adapter
+    bool tree = false;       // a pass over trees of drafts
+    int max_slots = 0;       // most slots of a user of the pass
+    std::vector<int> parent; // trees: the drafts' parents, users in order
+    // rules for the logits of the next pass of batch rules_batch (sd_batch_rules)
+    bool has_rules = false, ruled = false;  // ruled: the pass in hand takes them
+    int rules_batch = -1, rules_rows = 0;
+    RulesCall rules{};
     hipEvent_t done = nullptr;
     char* stage_host = nullptr;  // pinned
-    int32_t* result_host = nullptr;  // pinned
+    int32_t* result_host = nullptr;  // pinned: results, then the masks of accepted drafts of trees
     char* base = nullptr;        // device slot base
     SlotBufs bufs{};
     // graph of the slot's last captured pass and the launch signature it
@@ -349,6 +370,13 @@ sd_status collect_batch(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     if ((int)users.size() > c->cfg.max_batch_users || T > c->cfg.max_batch_tokens) return SD_EINVAL;
     return SD_OK;
 }
+
+// Tables of a tree pass, T numbers each: the slots' parents and depths, and those by
+// which the sampler takes every slot as a user of its own without drafts.
+enum { kTreeParent, kTreeDepth, kTreeUser, kTreeZero, kTreeSelf };
+constexpr int kTreeTmax = 800;  // (five tables and one number in 4096)
+static_assert(5 * kTreeTmax + 1 <= 4 * kAttnItemsMax, "a tree's tables fit the table of attention items");
+template <class P> P tree_table(P items, int T, int which) { return items + (size_t)which * T; }
 
 // Write the staging block for the batch into the slot's pinned buffer.
 void build_stage(sd_ctx* c, Slot& s, int mode, bool with_items, int* n_items, int* rows_max,
@@ -477,6 +505,21 @@ void build_stage(sd_ctx* c, Slot& s, int mode, bool with_items, int* n_items, in
         }
         ioff[b + 1] = ni;
     }
+    if (s.tree) {
+        // (in the table of attention items, which a tree pass has none of)
+        int32_t* tp = tree_table(items, s.T, kTreeParent);
+        int32_t* td = tree_table(items, s.T, kTreeDepth);
+        for (int b = 0; b < s.B; ++b)
+            for (int j = 0; j <= s.L[b]; ++j) {
+                const int t = soff[b] + j;
+                tp[t] = j == 0 ? -1 : s.parent[doff[b] + j - 1];
+                td[t] = j == 0 ? 0 : td[soff[b] + tp[t]] + 1;
+                tree_table(items, s.T, kTreeUser)[t] = user[b];
+                tree_table(items, s.T, kTreeZero)[t] = 0;
+                tree_table(items, s.T, kTreeSelf)[t] = t;
+            }
+        tree_table(items, s.T, kTreeSelf)[s.T] = s.T;
+    }
     flags[0] = flags[1] = flags[2] = flags[3] = 0;
     int32_t* prow = (int32_t*)(st + L.st_prow);
     for (int b = 0; b < s.B; ++b) prow[b] = s.prow.empty() ? b : s.prow[b];
@@ -563,6 +606,32 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
         a.ws = s.base + c->lay.lora;
         launch_lora(a, st);
     };
+    auto tree_attention = [&](int layer) {
+        const size_t plane = (size_t)T * D.nq() * 2;
+        TreeCall a{};
+        a.kv = c->kv;
+        a.layer = layer;
+        a.n_users = bv.B;
+        a.n_slots = T;
+        a.max_slots = s.max_slots;
+        a.max_pages = bv.max_pages;
+        a.hq = D.hq;
+        a.slot_off = bv.slot_off;
+        a.prefix = bv.prefix;
+        a.page_table = bv.page_table;
+        a.parent = bv.parent;
+        a.q = sb.qbuf;
+        a.out = sb.attn;
+        if (D.bf16) {
+            a.q_lo = (const char*)sb.qbuf + plane;
+            a.out_lo = (char*)sb.attn + plane;
+        }
+        a.qs = a.os = D.nq();
+        a.scale = 1.0f / sqrtf((float)D.hd);
+        a.ws = s.base + c->lay.tree;
+        a.ws_bytes = c->lay.tree_bytes;
+        launch_tree_attention(a, st);
+    };
     for (int l = 0; l < D.L; ++l) {
         const sd_layer_weights& w = c->layers[l];
         const size_t lbase = (size_t)l * c->pl.layer * 2;
@@ -591,7 +660,8 @@ sd_status enqueue_forward(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t s
         }
         {
             ProfScope ps(c, SD_K_ATTN, st);
-            launch_attention(D, bv, sb, c->kv, l, st);
+            if (s.tree) tree_attention(l);
+            else launch_attention(D, bv, sb, c->kv, l, st);
         }
         {
             // output projection, then residual add fused with the pre-FFN norm
@@ -814,7 +884,7 @@ sd_status sd_verify_init(const sd_config* cfg, const sd_weights* w, void* kv_poo
         Slot& s = c->slots[i];
         s.base = c->ws + (size_t)i * L.slot_bytes;
         ok &= hipHostMalloc((void**)&s.stage_host, L.st_bytes, hipHostMallocDefault) == hipSuccess;
-        ok &= hipHostMalloc((void**)&s.result_host, (size_t)(2 * L.Bmax + 4) * 4,
+        ok &= hipHostMalloc((void**)&s.result_host, result_bytes(L.Bmax) + (size_t)L.Bmax * 8,
                             hipHostMallocDefault) == hipSuccess;
         ok &= hipEventCreateWithFlags(&s.done, hipEventDisableTiming) == hipSuccess;
         SlotBufs& b = s.bufs;
@@ -989,6 +1059,47 @@ sd_status sd_user_state(sd_ctx* c, int32_t user, int32_t* prefix_len, int32_t* r
     return SD_OK;
 }
 
+sd_status sd_user_pages(sd_ctx* c, int32_t user, int32_t* pages, int32_t capacity, int32_t* n_pages) {
+    if (!c || user < 0 || user >= c->cfg.max_users || capacity < 0 || (capacity > 0 && !pages) || !n_pages)
+        return SD_EINVAL;
+    const User& u = c->users[user];
+    if (!u.active) return SD_EINVAL;
+    *n_pages = (int32_t)u.pages.size();
+    std::copy_n(u.pages.begin(), std::min<size_t>(u.pages.size(), capacity), pages);
+    return SD_OK;
+}
+
+sd_status sd_user_fork(sd_ctx* c, int32_t user, int32_t from, int32_t prefix_len, int32_t root_token,
+                       sd_stream stream) {
+    if (!c || user < 0 || user >= c->cfg.max_users || from < 0 || from >= c->cfg.max_users || user == from)
+        return SD_EINVAL;
+    User &u = c->users[user], &f = c->users[from];
+    if (!f.active || prefix_len < 0 || prefix_len > f.prefix || prefix_len + 2 > c->cfg.max_ctx || root_token < 0 ||
+        root_token >= c->cfg.vocab)
+        return SD_EINVAL;
+    if (u.pending_slot >= 0 || f.pending_slot >= 0) return SD_ESTATE;
+    // its own pages first, then free ones
+    const int need = pages_for(prefix_len), own = (int)u.pages.size(), free_n = (int)c->free_pages.size();
+    if (need > own + free_n) return SD_ENOMEM;
+    CopyPages ids;
+    for (int p0 = 0; p0 < need; p0 += kCopyPages) {
+        const int n = std::min(kCopyPages, need - p0);
+        for (int i = 0; i < n; ++i) {
+            const int p = p0 + i;
+            ids.src[i] = f.pages[p];
+            ids.dst[i] = p < own ? u.pages[p] : c->free_pages[free_n - 1 - (p - own)];
+        }
+        launch_copy_pages(c->kv, c->D.L, n, ids, (hipStream_t)stream);
+        SD_HIP(hipGetLastError());
+    }
+    release_to(c, u, need);
+    reserve_to(c, u, need);  // (takes them from the back, as above)
+    u.active = true;
+    u.prefix = prefix_len;
+    u.root = root_token;
+    return SD_OK;
+}
+
 static sd_status kv_copy(sd_ctx* c, int32_t user, int32_t layer, int32_t pos0, int32_t n,
                          const void* k, const void* v, sd_stream stream, int to_pool) {
     if (!c || user < 0 || user >= c->cfg.max_users || layer < 0 || layer >= c->cfg.n_layers ||
@@ -1033,10 +1144,43 @@ sd_status sd_kv_read(sd_ctx* c, int32_t user, int32_t layer, int32_t pos0, int32
 // SD_LOGITS_ALL / SD_LOGITS_UNFUSED or the fp32 configuration; otherwise
 // only when something reads them after phase A -- the stochastic race of
 // phase B (the stop slot is known only once every slot's statistics are
-// complete) or the probabilities of a decode step.
-static bool pass_writes_logits(const sd_ctx* c, int mode, const float* probs) {
+// complete), the probabilities of a decode step, or rules on the logits.
+static bool pass_writes_logits(const sd_ctx* c, const Slot& s, int mode, const float* probs) {
     return !c->D.bf16 || c->cfg.logits_out != SD_LOGITS_AS_NEEDED || mode == SD_STOCHASTIC ||
-           probs != nullptr;
+           probs != nullptr || s.ruled;
+}
+
+// A tree pass after its logits: the target's token after every slot, the walk along
+// the drafts, the accepted rows moved together.  The tokens lie in the sampler's
+// phase-B partials, whose own lie in phase A's, and the masks of the accepted drafts in
+// the tokens of the lm_head's draft logits, which nothing reads any more.
+static void tree_result(sd_ctx* c, Slot& s, const BatchView& bv, hipStream_t st, int groups, const OwnRows& own) {
+    const int32_t* items = (const int32_t*)bv.items;
+    BatchView sv = bv;
+    sv.B = bv.T;
+    sv.nd = 0;
+    sv.user_id = tree_table(items, bv.T, kTreeUser);
+    sv.L = tree_table(items, bv.T, kTreeZero);
+    sv.draft_off = sv.L;
+    sv.slot_off = sv.slot_b = tree_table(items, bv.T, kTreeSelf);
+    SlotBufs sb = s.bufs;
+    int32_t* const results = (int32_t*)s.bufs.spartB;  // [2 T + 1] of Bmax * 256
+    sb.spartB = s.bufs.spart;
+    sb.result = results;
+    sb.bmax = bv.T;
+    launch_sampler(c->D, sv, sb, s.bufs.logits, st, groups, nullptr, nullptr, own, true);
+    uint64_t* const path = (uint64_t*)s.bufs.dnext;
+    launch_tree_walk(bv, results + bv.T, s.bufs.result, s.bufs.bmax, path, st);
+    CompactCall m{};
+    m.kv = c->kv;
+    m.layers = c->D.L;
+    m.n_users = bv.B;
+    m.max_pages = bv.max_pages;
+    m.max_keep = s.max_slots;
+    m.prefix = bv.prefix;
+    m.page_table = bv.page_table;
+    m.path = path;
+    launch_compact(m, st);
 }
 
 // Device work of one pass: staging upload, forward + sampler (or the
@@ -1068,20 +1212,40 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
             launch_filter(f, st);
         }
     };
+    // rules of the batch: the pass's rows are rewritten (caller's logits: into them)
+    // before anything looks at them, so their statistics are taken from there
+    auto rule = [&](const float* from) {
+        RulesCall r = s.rules;
+        r.n_rows = bv.T;
+        r.V = c->D.V;
+        r.logits = from;
+        r.stride = r.ostride = c->D.V;
+        r.out = s.bufs.logits;
+        r.row_token = s.bufs.tok;
+        r.row_parent = bv.parent;
+        r.slot_j = bv.slot_j;
+        launch_rules(r, st);
+    };
     if (rs == SD_OK) {
         if (logits) {
             launch_prepare(c->D, bv, s.bufs, st);
+            if (s.ruled) {
+                rule(logits);
+                logits = s.bufs.logits;
+            }
             if (s.filtered) filter(logits);
             launch_sampler(c->D, bv, s.bufs, logits, st, 0, nullptr, nullptr, own);
             rs = hip_status(hipGetLastError());
         } else {
             int groups = 0;
-            rs = enqueue_forward(c, s, bv, st, pass_writes_logits(c, bv.mode, probs), &groups);
+            rs = enqueue_forward(c, s, bv, st, pass_writes_logits(c, s, bv.mode, probs), &groups);
             if (rs == SD_OK) {
                 ProfScope ps(c, SD_K_SAMPLER, st);
+                if (s.ruled) rule(s.bufs.logits);
                 if (s.filtered) filter(s.bufs.logits);
-                if (s.filtered == 2) groups = 0;  // (no slot needs the epilogue's statistics)
-                launch_sampler(c->D, bv, s.bufs, s.bufs.logits, st, groups, nullptr, nullptr, own);
+                if (s.filtered == 2 || s.ruled) groups = 0;  // (no slot needs the epilogue's statistics)
+                if (s.tree) tree_result(c, s, bv, st, groups, own);
+                else launch_sampler(c->D, bv, s.bufs, s.bufs.logits, st, groups, nullptr, nullptr, own);
                 if (probs) launch_probs(c->D, bv, s.bufs, s.bufs.logits, probs, st);
                 rs = hip_status(hipGetLastError());
             }
@@ -1090,6 +1254,9 @@ static sd_status enqueue_pass(sd_ctx* c, Slot& s, const BatchView& bv, const flo
     if (rs == SD_OK)
         rs = hip_status(hipMemcpyAsync(s.result_host, s.bufs.result,
                                        (size_t)(2 * c->lay.Bmax + 4) * 4, hipMemcpyDeviceToHost, st));
+    if (rs == SD_OK && s.tree)
+        rs = hip_status(hipMemcpyAsync((char*)s.result_host + result_bytes(c->lay.Bmax), s.bufs.dnext, (size_t)bv.B * 8,
+                                       hipMemcpyDeviceToHost, st));
     return rs;
 }
 
@@ -1102,7 +1269,15 @@ static std::vector<int64_t> launch_key(sd_ctx* c, const Slot& s, const BatchView
                               bv.n_items, bv.rows_max, bv.combine, bv.few, (int64_t)(intptr_t)bv.drafts,
                               (int64_t)(intptr_t)bv.q, (int64_t)(intptr_t)bv.accept_u,
                               (int64_t)(intptr_t)st, c->sk_polls, s.filtered,
-                              s.adapted ? c->adapters_set : 0};
+                              s.adapted ? c->adapters_set : 0, s.ruled};
+    if (s.ruled) {
+        const RulesCall& r = s.rules;
+        for (const void* p : {(const void*)r.tokens, (const void*)r.hist, (const void*)r.rep, (const void*)r.pres,
+                              (const void*)r.freq, (const void*)r.bias_token, (const void*)r.bias_value,
+                              (const void*)r.bias, (const void*)r.mask, (const void*)r.mask_row})
+            k.push_back((int64_t)(intptr_t)p);
+        k.insert(k.end(), {r.n_tokens, r.n_bias, r.n_masks});
+    }
     for (int b = 0; b < s.B; ++b) {
         k.push_back(s.users[b]);
         k.push_back(s.L[b]);
@@ -1159,11 +1334,11 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
                         const float* logits, int32_t mode, uint64_t seed, uint64_t round,
                         const float* accept_u, sd_stream stream, bool graph = false,
                         float* probs = nullptr, const int32_t* probs_row = nullptr,
-                        SparseQ sq = SparseQ{}) {
+                        SparseQ sq = SparseQ{}, const int32_t* parent = nullptr) {
     if (!c) return SD_EINVAL;
     if (graph && (stream == nullptr || logits != nullptr)) return SD_EINVAL;
     if (mode != SD_GREEDY && mode != SD_STOCHASTIC && mode != SD_FORCE) return SD_EINVAL;
-    const bool need_q = mode == SD_STOCHASTIC && sq.k == 0;
+    const bool need_q = mode == SD_STOCHASTIC && sq.k == 0 && !parent;
     if (draft_len && (!draft_tokens || (need_q && !q))) return SD_EINVAL;
     const bool sample_only = logits != nullptr;
     if (batch < 0) return SD_EINVAL;
@@ -1171,8 +1346,17 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     if (s.pending) return SD_ESTATE;
     std::vector<int> users, Ls;
     int T = 0, nd = 0;
-    sd_status r = collect_batch(c, batch, n_users, assign, draft_len, !sample_only, users, Ls, T, nd);
+    const bool ruled = s.has_rules && s.rules_batch == batch;
+    // (rules count the users' root tokens, also on the caller's logits)
+    sd_status r = collect_batch(c, batch, n_users, assign, draft_len, !sample_only || ruled, users, Ls, T, nd);
     if (r != SD_OK) return r;
+    if (ruled && s.rules_rows != T) return SD_EINVAL;
+    if (parent) {
+        if (T > kTreeTmax) return SD_ENOTIMPL;
+        for (size_t b = 0, i = 0; b < users.size(); ++b)
+            for (int j = 1; j <= Ls[b]; ++j, ++i)
+                if (parent[i] < 0 || parent[i] >= j) return SD_EINVAL;
+    }
     if (!sample_only) {
         // page reservation for i_m + l_m + 1 tokens per user, all or nothing
         int need = 0;
@@ -1204,7 +1388,11 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     s.nd = nd;
     s.batch = batch;
     s.sample_only = sample_only;
-    s.logits_ok = sample_only || pass_writes_logits(c, mode, probs);
+    s.ruled = ruled;
+    s.tree = parent != nullptr;
+    if (parent) s.parent.assign(parent, parent + nd);
+    s.max_slots = *std::max_element(Ls.begin(), Ls.end()) + 1;
+    s.logits_ok = sample_only || pass_writes_logits(c, s, mode, probs);
     s.adapted = false;
     int n_own = 0;
     for (int m : users) {
@@ -1213,8 +1401,12 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     }
     s.filtered = mode != SD_STOCHASTIC || n_own == 0 ? 0 : n_own < s.B ? 1 : 2;
     int n_items = 0, rows_max = 0, combine = 0, few = 0;
-    build_stage(c, s, mode, !sample_only, &n_items, &rows_max, &combine, &few);
+    build_stage(c, s, mode, !sample_only && !s.tree, &n_items, &rows_max, &combine, &few);
     BatchView bv = make_view(c, s);
+    if (s.tree) {
+        bv.parent = tree_table((const int32_t*)bv.items, T, kTreeParent);
+        bv.depth = tree_table((const int32_t*)bv.items, T, kTreeDepth);
+    }
     bv.B = s.B;
     bv.T = T;
     bv.nd = nd;
@@ -1246,6 +1438,7 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
         return rs;
     }
     s.pending = true;
+    if (ruled) s.has_rules = false;
     const int slot_index = (int)(&s - c->slots);
     for (int m : users) c->users[m].pending_slot = slot_index;
     return SD_OK;
@@ -1285,6 +1478,14 @@ sd_status sd_verify_batch_sparse(sd_ctx* c, int32_t batch, int32_t n_users, cons
                   round, accept_u, stream, false, nullptr, nullptr, sq);
 }
 
+sd_status sd_verify_batch_tree(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t* assign,
+                               const int32_t* draft_len, const int32_t* draft_tokens, const int32_t* parent,
+                               int32_t mode, uint64_t seed, uint64_t round, sd_stream stream) {
+    if (!draft_len || !parent || mode == SD_FORCE) return SD_EINVAL;
+    return submit(c, batch, n_users, assign, draft_len, draft_tokens, nullptr, nullptr, mode, seed, round,
+                  nullptr, stream, false, nullptr, nullptr, SparseQ{}, parent);
+}
+
 sd_status sd_draft_batch(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t* assign,
                          int32_t mode, uint64_t seed, uint64_t round, float* probs,
                          const int32_t* probs_row, sd_stream stream) {
@@ -1302,8 +1503,8 @@ sd_status sd_sample_logits(sd_ctx* c, int32_t batch, int32_t n_users, const int3
                   accept_u, stream);
 }
 
-sd_status sd_accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_token,
-                    int32_t commit) {
+static sd_status accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_token, int32_t* path,
+                        int32_t commit) {
     if (!c || batch < 0 || !n_accepted || !out_token) return SD_EINVAL;
     Slot& s = c->slots[batch % c->cfg.max_pending];
     if (!s.pending || s.batch != batch) return SD_ESTATE;
@@ -1316,6 +1517,16 @@ sd_status sd_accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_
         if (ok) {
             n_accepted[s.users[b]] = s.result_host[b];
             out_token[s.users[b]] = s.result_host[Bmax + b];
+            if (path) {
+                int32_t* row = path + (size_t)s.users[b] * c->cfg.max_draft;
+                uint64_t taken = 0;  // of a tree: the accepted drafts
+                if (s.tree)
+                    std::memcpy(&taken, (const char*)s.result_host + result_bytes(Bmax) + (size_t)b * 8, 8);
+                int n = 0;
+                for (int i = 0; i < s.L[b]; ++i)
+                    if (s.tree ? (taken >> i) & 1 : i < s.result_host[b]) row[n++] = i + 1;
+                for (; n < c->cfg.max_draft; ++n) row[n] = -1;
+            }
         }
         if (!s.sample_only) {
             // (a user whose row gave no token stays where it is)
@@ -1329,6 +1540,37 @@ sd_status sd_accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_
     }
     s.pending = false;
     return ok ? SD_OK : SD_EDEVICE;
+}
+
+sd_status sd_accept(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_token,
+                    int32_t commit) {
+    return accept(c, batch, n_accepted, out_token, nullptr, commit);
+}
+
+sd_status sd_accept_tree(sd_ctx* c, int32_t batch, int32_t* n_accepted, int32_t* out_token, int32_t* path,
+                         int32_t commit) {
+    if (!path) return SD_EINVAL;
+    return accept(c, batch, n_accepted, out_token, path, commit);
+}
+
+sd_status sd_batch_rules(sd_ctx* c, int32_t batch, int32_t n_rows, const sd_logit_rules* rules) {
+    if (!c || batch < 0) return SD_EINVAL;
+    Slot& s = c->slots[batch % c->cfg.max_pending];
+    if (s.pending) return SD_ESTATE;
+    if (!rules) {
+        if (s.rules_batch == batch) s.has_rules = false;
+        return SD_OK;
+    }
+    if (n_rows < 1 || n_rows > c->cfg.max_batch_tokens || rules->row_token || rules->row_parent) return SD_EINVAL;
+    if (n_rows > SD_FILTER_MAX_ROWS || c->cfg.vocab > SD_FILTER_MAX_VOCAB) return SD_ELIMIT;
+    RulesCall r{};
+    const sd_status rs = rules_of(rules, &r);
+    if (rs != SD_OK) return rs;
+    s.rules = r;
+    s.rules_rows = n_rows;
+    s.rules_batch = batch;
+    s.has_rules = true;
+    return SD_OK;
 }
 
 sd_status sd_debug_logits(sd_ctx* c, int32_t batch, float* dst, sd_stream stream) {

@@ -84,6 +84,10 @@ struct BatchView {
     int qk;
     int32_t* flags;            // [1] device error bits, zeroed by the staging copy
     const int32_t* prow;       // [B] decode steps: output row of each user's probabilities
+    // trees of drafts: each slot's parent (a slot of its user, -1: none) and depth;
+    // null: chains, slot j below slot j - 1 at depth j
+    const int32_t* parent;     // [T]
+    const int32_t* depth;      // [T]
 };
 
 // Workspace buffers of one batch slot.
@@ -203,7 +207,8 @@ void launch_pack(const void* s0, const void* s1, const void* s2, int seg1, int s
 // > 0: phase A from the lm_head epilogue's statistics (sb.lstat, groups
 // partials per slot, and sb.zd); logits then only feed phase B (stochastic).
 // nm / nt (context-free call, groups = 0): the batch tables are built by
-// phase A's first kernel.
+// phase A's first kernel.  slots: every slot is a user of its own without drafts
+// (bv's tables say so) and draws with the key of its slot number.
 struct NoallocMeta;
 struct NoallocTables;
 // Slots with logits of their own: slot t with own[t] != 0 takes row t of `rows`
@@ -214,7 +219,7 @@ struct OwnRows {
 };
 void launch_sampler(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
                     hipStream_t s, int groups = 0, const NoallocMeta* nm = nullptr,
-                    const NoallocTables* nt = nullptr, OwnRows own = OwnRows{});
+                    const NoallocTables* nt = nullptr, OwnRows own = OwnRows{}, bool slots = false);
 // probs[t][k] = exp(z[t][k] - m_t) / S_t from the sampler's per-slot
 // statistics (the same expression the race uses for p)
 void launch_probs(const Dims& D, const BatchView& bv, const SlotBufs& sb, const float* logits,
@@ -300,6 +305,11 @@ struct TreeCall {
     size_t ws_bytes;
 };
 size_t tree_workspace(const TreeCall& c);
+size_t tree_workspace_least(const TreeCall& c);  // what a launch can do with
+// The walk of a tree pass: target [T] is the target's token after each slot; the
+// batch's results (n_acc, token, flags) and bit masks [B] of the accepted drafts.
+void launch_tree_walk(const BatchView& bv, const int32_t* target, int32_t* result, int bmax, uint64_t* path,
+                      hipStream_t s);
 void launch_tree_attention(const TreeCall& c, hipStream_t s);
 
 // A caller's paged cache as the kernels see it; SD_OK, or why not.

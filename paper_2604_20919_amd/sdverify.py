@@ -30,7 +30,8 @@ EXPORTS = ("sd_verify_query_sizes", "sd_verify_init", "sd_verify_destroy", "sd_u
            "sd_sample_logits_noalloc", "sd_debug_logits", "sd_debug_wait_limit", "sd_profile_begin", "sd_profile_end",
            "sd_filter_query_size", "sd_sample_filtered", "sd_filter_logits", "sd_lora_query_size",
            "sd_lora_apply", "sd_tree_query_size", "sd_tree_attention", "sd_kv_copy_pages", "sd_kv_compact",
-           "sd_adjust_logits", "sd_user_sampling", "sd_adapters_set", "sd_user_adapter", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
+           "sd_adjust_logits", "sd_verify_batch_tree", "sd_accept_tree", "sd_user_fork", "sd_user_pages",
+           "sd_batch_rules", "sd_user_sampling", "sd_adapters_set", "sd_user_adapter", "sd_calib_hbm", "sd_calib_mfma", "sd_status_str")
 SD_FILTER_MAX_ROWS, SD_FILTER_MAX_VOCAB = 65535, 1 << 20
 SD_LORA_MAX_RANK, SD_LORA_MAX_SEGS = 128, 4
 SD_TREE_MAX_SLOTS, SD_TREE_MAX_USERS, SD_KV_COMPACT_MAX = 256, 16384, 256
@@ -138,6 +139,11 @@ def lib() -> ctypes.CDLL:
         L.sd_kv_copy_pages.argtypes = [P(sd_kv_pool), i32, vp, vp, vp]
         L.sd_kv_compact.argtypes = [P(sd_kv_pool), i32, vp, vp, i32, vp, i32, vp, vp]
         L.sd_adjust_logits.argtypes = [i32, i32, vp, i32, i64, P(sd_logit_rules), vp, i64, vp]
+        L.sd_verify_batch_tree.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, u64, u64, vp]
+        L.sd_accept_tree.argtypes = [vp, i32, vp, vp, vp, i32]
+        L.sd_user_fork.argtypes = [vp, i32, i32, i32, i32, vp]
+        L.sd_user_pages.argtypes = [vp, i32, vp, i32, P(i32)]
+        L.sd_batch_rules.argtypes = [vp, i32, i32, P(sd_logit_rules)]
         L.sd_user_sampling.argtypes = [vp, i32, f32, i32, f32, f32]
         L.sd_adapters_set.argtypes = [vp, i32, P(sd_layer_adapters)]
         L.sd_user_adapter.argtypes = [vp, i32, i32]
@@ -195,11 +201,12 @@ def sd_verify_query_sizes(cfg: sd_config):
 
 
 class _Context:
-    """What sd_adapters_set needs to know of a context, and the adapters that the
-    library reads in place."""
+    """What sd_adapters_set and others need to know of a context, and the adapters
+    and batches' rules that the library reads in place."""
 
-    def __init__(self, n_layers: int, device: int):
+    def __init__(self, n_layers: int, device: int, vocab: int, max_draft: int):
         self.n_layers, self.device, self.adapters = n_layers, device, None
+        self.vocab, self.max_draft, self.rules = vocab, max_draft, {}
 
 
 _contexts: Dict[int, _Context] = {}
@@ -211,7 +218,7 @@ def sd_verify_init(cfg: sd_config, weights: sd_weights, kv_pool, workspace, weig
     _check("sd_verify_init", lib().sd_verify_init(ctypes.byref(cfg), ctypes.byref(weights),
                                                   _dev(kv_pool), _dev(workspace), _dev(weight_pack),
                                                   ctypes.byref(out)))
-    _contexts[out.value] = _Context(cfg.n_layers, torch.cuda.current_device())
+    _contexts[out.value] = _Context(cfg.n_layers, torch.cuda.current_device(), cfg.vocab, cfg.max_draft)
     return out.value
 
 
@@ -690,8 +697,74 @@ def sd_accept(ctx: int, batch: int, n_users: int, commit: bool = False):
     batch are -1."""
     n_acc = np.full(n_users, -1, np.int32)
     tok = np.full(n_users, -1, np.int32)
-    _check("sd_accept", lib().sd_accept(ctx, batch, n_acc.ctypes.data, tok.ctypes.data, int(commit)))
+    _done(ctx, batch, "sd_accept", lib().sd_accept(ctx, batch, n_acc.ctypes.data, tok.ctypes.data, int(commit)))
     return n_acc, tok
+
+
+def sd_verify_batch_tree(ctx: int, batch: int, assign: Sequence[int], draft_len: Sequence[int], draft_tokens,
+                         parent: Sequence[int], mode, seed: int = 0, round_: int = 0, stream=None) -> None:
+    """parent (host) [sum l_m]: the parent of each draft, 0 the root, else the
+    number (1 ..) of an earlier draft of its user."""
+    a, L, par = _host_i32(assign), _host_i32(draft_len), _host_i32(parent)
+    if a.size != L.size:
+        raise ValueError("assign and draft_len differ in length")
+    if par.size != int(L[a == batch].sum()):
+        raise ValueError(f"parent: {int(L[a == batch].sum())} drafts, not {par.size}")
+    mode = MODES[mode] if isinstance(mode, str) else int(mode)
+    _check("sd_verify_batch_tree", lib().sd_verify_batch_tree(
+        ctx, batch, a.size, a.ctypes.data, L.ctypes.data, _dev(draft_tokens), par.ctypes.data, mode,
+        int(seed), int(round_), _stream(stream)))
+
+
+def sd_accept_tree(ctx: int, batch: int, n_users: int, commit: bool = False):
+    """Returns (n_accepted[M], out_token[M], path[M][max_draft]); entries of users
+    outside the batch are -1."""
+    known = _contexts.get(ctx)
+    if known is None:
+        raise ValueError("not a context of sd_verify_init")
+    n_acc, tok = np.full(n_users, -1, np.int32), np.full(n_users, -1, np.int32)
+    path = np.full((n_users, known.max_draft), -1, np.int32)
+    _done(ctx, batch, "sd_accept_tree", lib().sd_accept_tree(ctx, batch, n_acc.ctypes.data, tok.ctypes.data,
+                                                             path.ctypes.data, int(commit)))
+    return n_acc, tok, path
+
+
+def sd_user_fork(ctx: int, user: int, from_: int, prefix_len: int, root_token: int, stream=None) -> None:
+    _check("sd_user_fork", lib().sd_user_fork(ctx, user, from_, prefix_len, root_token, _stream(stream)))
+
+
+def sd_user_pages(ctx: int, user: int) -> np.ndarray:
+    """The pages that a user holds, in order."""
+    n = ctypes.c_int32()
+    _check("sd_user_pages", lib().sd_user_pages(ctx, user, None, 0, ctypes.byref(n)))
+    pages = np.zeros(n.value, np.int32)
+    _check("sd_user_pages", lib().sd_user_pages(ctx, user, pages.ctypes.data, pages.size, ctypes.byref(n)))
+    return pages
+
+
+def sd_batch_rules(ctx: int, batch: int, rules: Optional[LogitRules]) -> None:
+    """Rules of the logits of the next pass of `batch` (None: none), one row a query
+    slot, without row_token and row_parent.  Their tensors are kept alive
+    until the pass is accepted."""
+    known = _contexts.get(ctx)
+    if known is None:
+        raise ValueError("not a context of sd_verify_init")
+    if rules is None:
+        _check("sd_batch_rules", lib().sd_batch_rules(ctx, batch, 0, None))
+        known.rules.pop(batch, None)
+        return
+    if rules.vocab != known.vocab or rules.device.index != known.device:
+        raise ValueError(f"rules for {rules.vocab} tokens on {rules.device}, the context has {known.vocab} on GPU {known.device}")
+    _check("sd_batch_rules", lib().sd_batch_rules(ctx, batch, rules.n_rows, rules.ref))
+    known.rules[batch] = rules
+
+
+def _done(ctx: int, batch: int, fn: str, status: int) -> None:
+    """A pass is over, with or without decisions: its rules are no longer read."""
+    known = _contexts.get(ctx)
+    if known is not None and status in (SD_OK, SD_EDEVICE):
+        known.rules.pop(batch, None)
+    _check(fn, status)
 
 
 def sd_debug_logits(ctx: int, batch: int, dst, stream=None) -> None:

@@ -78,6 +78,25 @@ class Verifier:
         """The adapter of a user's slots, -1: none (sd_user_adapter)."""
         sv.sd_user_adapter(self.ctx, user, adapter)
 
+    def fork_user(self, user: int, from_: int, prefix_len: int, root: int, stream=None):
+        """Start `user` with a copy of another user's first prefix_len cached
+        tokens (sd_user_fork)."""
+        sv.sd_user_fork(self.ctx, user, from_, prefix_len, root, stream)
+
+    def user_pages(self, user: int):
+        """The pages that a user holds, in order (sd_user_pages)."""
+        return sv.sd_user_pages(self.ctx, user)
+
+    def pool(self) -> sv.KVPool:
+        """The context's cache for the calls that take one (sd_tree_attention,
+        sd_kv_copy_pages, sd_kv_compact)."""
+        c = self.cfg
+        return sv.make_kv_pool(self.kv_pool, c.n_layers, c.n_pages, c.n_kv_heads, c.head_dim, c.dtype)
+
+    def batch_rules(self, batch: int, rules):
+        """Rules of the logits of the batch's next pass, None: none (sd_batch_rules)."""
+        sv.sd_batch_rules(self.ctx, batch, rules)
+
     def write_kv(self, user: int, layer: int, pos0: int, k: torch.Tensor, v: torch.Tensor, stream=None):
         sv.sd_kv_write(self.ctx, user, layer, pos0, k.shape[0], k, v, stream)
 
@@ -100,6 +119,12 @@ class Verifier:
         sv.sd_verify_batch_sparse(self.ctx, batch, assign, draft_len, drafts, q_idx, q_val, q_rest,
                                   mode, seed, round_, accept_u, stream)
 
+    def verify_tree(self, batch: int, assign: Sequence[int], draft_len: Sequence[int], drafts, parent,
+                    mode="stochastic", seed: int = 0, round_: int = 0, stream=None):
+        """Verification of trees of drafts (sd_verify_batch_tree); complete with
+        accept or accept_tree."""
+        sv.sd_verify_batch_tree(self.ctx, batch, assign, draft_len, drafts, parent, mode, seed, round_, stream)
+
     def draft(self, batch: int, assign: Sequence[int], mode="stochastic", seed: int = 0,
               round_: int = 0, probs=None, probs_row=None, stream=None):
         """One decode step of the users of `batch` (sd_draft_batch); complete
@@ -113,6 +138,10 @@ class Verifier:
 
     def accept(self, batch: int, n_users: int, commit: bool = False):
         return sv.sd_accept(self.ctx, batch, n_users, commit)
+
+    def accept_tree(self, batch: int, n_users: int, commit: bool = False):
+        """accept with the accepted drafts' numbers (sd_accept_tree)."""
+        return sv.sd_accept_tree(self.ctx, batch, n_users, commit)
 
     def wait_limit(self, max_polls: int) -> None:
         """Bound of the split gate/up product's waits (negative: default)."""

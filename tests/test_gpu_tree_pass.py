@@ -1,0 +1,562 @@
+"""Verification passes over trees of drafts (sd_verify_batch_tree), users forked
+(sd_user_fork) and rules on a pass's logits (sd_batch_rules).
+
+The logits of every slot of a tree are those of the oracle's forward over the path
+to it as a chain (1e-4 of the row's largest in fp32, 2e-3 in bf16: ten times what
+chains of these models measure); decisions are the walk of oracle.trees along the
+tokens that the oracle sampler takes from the GPU's own logits; and after a commit
+the next pass sees the accepted path as if it had always been a chain."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import workload as wl
+from gpu_harness import load_synthetic_kv, logit_rel_err, make_verifier
+from oracle import trees
+from paper_2604_20919_amd import sdverify as sv
+from test_gpu_requests import OPTIONS, Adapters, Merged, filtered
+from test_gpu_sampler import _case, _sampler_verifier
+from test_oracle_forward import torch_verify
+from workload.device import DeviceWeights
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"f32": 1e-4, "bf16": 2e-3}
+
+
+def dev(a, dtype=np.int32):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype)).cuda()
+
+
+def shown(v, T, stream=None):
+    lg = v.logits(0, T, stream)
+    torch.cuda.synchronize()
+    return lg.cpu().numpy()
+
+
+class Trees:
+    """Users' trees in a context with synthetic caches."""
+
+    def __init__(self, model, prefix, L, seed, spare=0, max_draft=None, **kw):
+        self.w = wl.custom_workload(model, list(prefix) + [0] * spare, list(L) + [1] * spare, seed=seed)
+        self.m = self.w.model
+        self.dw = DeviceWeights(self.m, self.w.seed)
+        self.v = make_verifier(self.w, self.dw, extra_ctx=80, max_draft=max_draft, **kw)
+        load_synthetic_kv(self.v, self.w, users=range(len(prefix)))
+        r = np.random.default_rng(seed)
+        self.B, self.L, self.prefix = len(prefix), list(L), list(prefix)
+        self.M = self.B + spare
+        self.roots = r.integers(0, self.m.vocab, self.B)
+        self.parent = [np.array([0] + [r.integers(max(0, j - 3), j) for j in range(2, n + 1)])[:n] for n in L]
+        self.drafts = [r.integers(0, self.m.vocab, n) for n in L]
+        self.past = [[] for _ in L]  # tokens committed on top of the synthetic cache
+        self.assign = np.array([0] * self.B + [-1] * spare, np.int32)
+        self.draft_len = np.array(list(L) + [1] * spare, np.int32)
+        for u in range(self.B):
+            self.v.reset_user(u, self.prefix[u], int(self.roots[u]))
+
+    def run(self, mode="greedy", seed=3, round_=0, commit=False, rules=None, stream=None):
+        if rules is not None:
+            self.v.batch_rules(0, rules)
+        self.v.verify_tree(0, self.assign, self.draft_len, dev(np.concatenate(self.drafts)), np.concatenate(self.parent), mode,
+                           seed, round_, stream)
+        lg = shown(self.v, sum(self.L) + self.B, stream)
+        acc, tok, path = self.v.accept_tree(0, self.M, commit)
+        return lg, acc, tok, path
+
+    def rows(self, u):
+        o = sum(self.L[:u]) + u
+        return slice(o, o + self.L[u] + 1)
+
+    def paths(self, u):
+        par = [-1] + list(self.parent[u])
+        return [trees.path_to(par, j)[::-1] for j in range(self.L[u] + 1)]
+
+    def plant(self, lg_of, depth):
+        """Makes the first drafts of paths what the target says, level by level."""
+        for _ in range(depth):
+            target = lg_of()
+            for u in range(self.B):
+                t = target[self.rows(u)]
+                at = 0
+                while True:
+                    below = [j for j in range(1, self.L[u] + 1) if self.parent[u][j - 1] == at]
+                    if not below:
+                        break
+                    hit = [j for j in below if self.drafts[u][j - 1] == t[at]]
+                    if not hit:
+                        self.drafts[u][below[-1] - 1] = t[at]
+                        break
+                    at = hit[0]
+
+    def check_logits(self, lg, label, weights=None):
+        ws = weights or oracle.WeightSource(self.m, self.w.seed)
+        worst = 0.0
+        for u in range(self.B):
+            ps = self.paths(u)
+            toks, n = [], []
+            for p in ps:
+                s = self.past[u] + [self.roots[u]] + [self.drafts[u][j - 1] for j in p[1:]]
+                toks += s
+                n.append(len(s))
+            k = len(ps)
+            kv = oracle.KVSource(self.m, self.w.seed, [u] * k, [self.prefix[u]] * k)
+            ref = oracle.forward(self.m, ws, kv, np.array([self.prefix[u]] * k, np.int32), np.array(n, np.int32),
+                                 np.array(toks, np.int32))
+            last = np.cumsum(n) - 1
+            worst = max(worst, float(logit_rel_err(lg[self.rows(u)], ref[last]).max()))
+        print(f"{label}: logit error {worst:.2e}", flush=True)
+        assert worst < TOL[self.m.dtype], label
+
+    def commit(self, acc, tok, path):
+        for u in range(self.B):
+            assert self.v.user_state(u) == (self.prefix[u] + len(self.past[u]) + 1 + acc[u], tok[u])
+            self.past[u] += [self.roots[u]] + [self.drafts[u][j - 1] for j in path[u][:acc[u]]]
+            self.roots[u] = tok[u]
+
+
+def targets(lg, t, mode, seed=3, round_=0):
+    """The target's token after every slot of user rows: argmax, or the oracle's race at that slot."""
+    if mode == "greedy":
+        return lg.argmax(axis=1), np.inf
+    out, gap = [], np.inf
+    for u in range(t.B):
+        for j, z in enumerate(lg[t.rows(u)]):
+            V = z.size
+            q = np.full((j, V), 0.0, np.float32)  # p / 0 accepts
+            d = np.full(j, int(z.argmax()), np.int32)
+            r = oracle.sample("stochastic", [u], [j], np.repeat(z[None], j + 1, 0), d, q, np.full(j, 0.5, np.float32), seed, round_)
+            assert r["n_acc"][0] == j
+            out.append(int(r["token"][0]))
+            gap = min(gap, float(r["race_gap"][0]))
+    return np.array(out), gap
+
+
+def check_walks(t, lg, acc, tok, path, mode, seed=3, round_=0):
+    target, gap = targets(lg, t, mode, seed, round_)
+    for u in range(t.B):
+        want, last = trees.walk(target[t.rows(u)], t.drafts[u], t.parent[u])
+        got = [int(x) for x in path[u] if x >= 0]
+        assert (got, int(acc[u]), int(tok[u])) == (want, len(want), last), (u, mode, gap)
+        assert (path[u][len(want):] == -1).all()
+
+
+@pytest.mark.parametrize("model", ["tiny", "tiny-qknorm", "tiny-bf16"])
+@pytest.mark.parametrize("mode", ["greedy", "stochastic"])
+def test_trees_over_committed_rounds(model, mode):
+    t = Trees(model, [40, 300, 0, 17, 90, 31], [1, 9, 20, 3, 30, 12], seed=61)
+    for rnd in range(3):
+        def lg_of():
+            lg, acc, tok, path = t.run(mode, round_=rnd)
+            return targets(lg, t, mode, round_=rnd)[0]
+        t.plant(lg_of, 2 + rnd)
+        lg, acc, tok, path = t.run(mode, round_=rnd, commit=True)
+        t.check_logits(lg, f"{model} {mode} round {rnd}")
+        check_walks(t, lg, acc, tok, path, mode, round_=rnd)
+        assert sum(acc) >= 4, acc
+        t.commit(acc, tok, path)
+    assert max(len(p) for p in t.past) >= 7
+    t.v.close()
+
+
+def test_a_chain_is_the_ordinary_greedy_pass():
+    t = Trees("tiny-bf16", [40, 300, 0, 17], [5, 9, 3, 12], seed=62)
+    t.parent = [np.arange(n) for n in t.L]
+    t.plant(lambda: t.run()[0].argmax(axis=1), 4)
+    lg, acc, tok, path = t.run()
+    assert sum(acc) >= 4
+    t.v.verify(0, t.assign, t.draft_len, dev(np.concatenate(t.drafts)), None, "greedy")
+    lg2 = t.v.logits(0, lg.shape[0]).cpu().numpy()
+    # (accept_tree on an ordinary batch: the leading drafts)
+    acc2, tok2, path2 = t.v.accept_tree(0, t.M)
+    assert np.array_equal(acc, acc2) and np.array_equal(tok, tok2) and np.array_equal(path, path2)
+    assert logit_rel_err(lg, lg2).max() < 2e-3
+    t.v.close()
+
+
+def test_the_widest_tree_and_equal_siblings():
+    t = Trees("tiny-bf16", [50], [64], seed=63)
+    t.parent = [np.array([0] * 20 + [1] * 20 + [5] * 24)]
+    lg, *_ = t.run()
+    top = lg.argmax(axis=1)
+    t.drafts[0][4] = t.drafts[0][7] = top[0]  # two equal drafts below the root: the first, slot 5, counts
+    lg, acc, tok, path = t.run()
+    t.drafts[0][45] = lg.argmax(axis=1)[5]
+    lg, acc, tok, path = t.run()
+    assert acc[0] == 2 and path[0][:2].tolist() == [5, 46] and tok[0] == lg[46].argmax()
+    t.check_logits(lg, "widest")
+    t.v.close()
+
+
+def test_passes_repeat_and_leave_the_context_alone():
+    """Without a commit a tree pass is repeatable bit for bit, also with an ordinary pass between and on another stream."""
+    t = Trees("tiny-bf16", [40, 300, 0], [6, 20, 9], seed=64)
+    t.plant(lambda: t.run()[0].argmax(axis=1), 3)
+    first = t.run()
+    for _ in range(3):
+        again = t.run()
+        assert all(np.array_equal(a, b) for a, b in zip(first, again))
+    d = dev(np.concatenate(t.drafts))
+    t.v.verify(0, t.assign, t.draft_len, d, None, "greedy")
+    t.v.accept(0, t.M)
+    again = t.run(stream=torch.cuda.Stream())
+    assert all(np.array_equal(a, b) for a, b in zip(first, again))
+    t.v.close()
+
+
+def test_two_batches_in_flight():
+    t = Trees("tiny-bf16", [40, 300, 17, 90], [6, 20, 9, 4], seed=65, max_batch_tokens=64)
+    parent, drafts = t.parent, t.drafts
+    t.plant(lambda: t.run()[0].argmax(axis=1), 3)
+    _, acc, tok, path = t.run()
+    assign = np.array([0, 1, 1, 0], np.int32)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ds = [dev(np.concatenate([drafts[u] for u in range(4) if assign[u] == n])) for n in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for n in range(2):
+            t.v.verify_tree(n, assign, t.draft_len, ds[n], np.concatenate([parent[u] for u in range(4) if assign[u] == n]),
+                            "greedy", stream=streams[n])
+        for n in range(2):
+            a, k, p = t.v.accept_tree(n, 4)
+            on = assign == n
+            assert np.array_equal(a[on], acc[on]) and np.array_equal(k[on], tok[on]) and np.array_equal(p[on], path[on])
+            assert (a[~on] == -1).all() and (p[~on] == -1).all()
+    t.v.close()
+
+
+def test_options_and_adapters_in_trees():
+    t = Trees("tiny-bf16", [33, 7, 90, 128, 0, 60], [9, 4, 12, 6, 20, 3], seed=66)
+    ad = Adapters(t.m, 3, 8, seed=11)
+    t.v.set_adapters(ad.layers)
+    which = (2, -1, 0, 1, -1, 1)
+    for u, a in enumerate(which):
+        t.v.user_adapter(u, a)
+    lg, *_ = t.run()
+    ws = oracle.WeightSource(t.m, t.w.seed)
+    for u in range(t.B):  # every path as a chain of the model with the adapter merged in
+        for j, p in enumerate(t.paths(u)):
+            toks = np.array([t.roots[u]] + [t.drafts[u][i - 1] for i in p[1:]], np.int32)
+            kv = oracle.KVSource(t.m, t.w.seed, [u], [t.prefix[u]])
+            src = Merged(ws, ad, which[u]) if which[u] >= 0 else ws
+            ref = torch_verify(t.m, src, kv, [t.prefix[u]], [toks.size], toks, kv_bf16=True)
+            assert logit_rel_err(lg[t.rows(u)][j:j + 1], ref[-1:]).max() < 2.3e-3, (u, j)
+    raw = t.run("stochastic")[0]
+    for u, o in enumerate(OPTIONS):
+        t.v.user_sampling(u, *o)
+    got = t.run("stochastic")
+    assert np.array_equal(got[0], filtered(raw, OPTIONS, np.array(t.L) + 1))
+    check_walks(t, *got, "stochastic")
+    t.v.close()
+
+
+@pytest.mark.parametrize("model", ["tiny", "tiny-bf16"])
+def test_forked_users(model):
+    t = Trees(model, [77, 300], [8, 5], seed=67, spare=2, max_batch_tokens=30)
+    assert len(t.v.user_pages(0)) == 5 and len(t.v.user_pages(1)) == 19
+    free = t.v.cfg.n_pages - 24
+    t.v.fork_user(2, 0, 77, int(t.roots[0]))
+    t.v.fork_user(3, 1, 130, int(t.roots[1]))
+    pages = [t.v.user_pages(u) for u in range(4)]
+    assert [len(p) for p in pages] == [5, 19, 5, 9] and len(set(np.concatenate(pages))) == 38 and free >= 14
+    assert t.v.user_state(2) == (77, t.roots[0]) and t.v.user_state(3) == (130, t.roots[1])
+    L = np.array([8, 5, 8, 5], np.int32)
+    d = dev(np.concatenate([t.drafts[0], t.drafts[1]] * 2))
+    par = np.concatenate([t.parent[0], t.parent[1]] * 2)
+
+    def run():
+        t.v.verify_tree(0, np.zeros(4, np.int32), L, d, par, "greedy")
+        lg = t.v.logits(0, 30).cpu().numpy()
+        t.v.accept(0, 4)
+        return lg
+
+    lg = run()
+    assert np.array_equal(lg[:9], lg[15:24])
+    assert not np.array_equal(lg[9:15], lg[24:])  # a shorter context
+    # what the copy's owner does is not seen by the other
+    z = torch.zeros((77, t.m.n_kv_heads, t.m.head_dim), dtype=torch.float32 if model == "tiny" else torch.int16, device="cuda")
+    for l in range(t.m.n_layers):
+        t.v.write_kv(2, l, 0, z, z)
+    torch.cuda.synchronize()
+    again = run()
+    assert np.array_equal(again[:15], lg[:15]) and not np.array_equal(again[15:24], lg[15:24])
+    # forked onto a user with pages of its own, and the pages given back
+    t.v.fork_user(3, 0, 40, 5)
+    assert len(t.v.user_pages(3)) == 3
+    t.v.fork_user(3, 1, 0, 5)
+    assert len(t.v.user_pages(3)) == 0 and t.v.user_state(3) == (0, 5)
+    t.v.fork_user(3, 1, 300, int(t.roots[1]))
+    again = run()
+    assert np.array_equal(again[9:15], again[24:])
+    for u in range(4):
+        sv.sd_user_release(t.v.ctx, u)
+    t.v.reset_user(0, min(16 * t.v.cfg.n_pages, t.v.cfg.max_ctx - 2), 0)
+    t.v.close()
+
+
+def test_fork_many_pages():
+    """More pages than one launch takes."""
+    w = wl.custom_workload("tiny-bf16", [2500, 0], [1, 1], seed=68)
+    dw = DeviceWeights(w.model, w.seed)
+    v = make_verifier(w, dw, extra_ctx=2600)
+    load_synthetic_kv(v, w, users=[0])
+    v.fork_user(1, 0, 2499, 7)
+    torch.cuda.synchronize()
+    m = w.model
+    for l in range(m.n_layers):
+        got = []
+        for u in (0, 1):
+            k = torch.empty((2499, m.n_kv_heads, m.head_dim), dtype=torch.int16, device="cuda")
+            x = torch.empty_like(k)
+            v.read_kv(u, l, 0, k, x)
+            got.append((k, x))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    v.close()
+
+
+class BatchRules:
+    """Penalties, biases and masks for the T slots of a batch of B users."""
+
+    def __init__(self, V, users_of, seed):
+        r = np.random.default_rng(seed)
+        T, B = len(users_of), max(users_of) + 1
+        self.V, self.T = V, T
+        size = r.integers(0, 60, B)
+        at = np.concatenate([[0], np.cumsum(size)])
+        self.tokens = r.integers(0, V, at[-1])
+        self.hist = np.array([[at[u], at[u] + size[u] // 2, at[u + 1]] for u in range(B)])[users_of]
+        self.rep, self.pres, self.freq = (r.choice(c, B).astype(np.float32)[users_of] for c in ([1.0, 1.4], [0.0, 0.6], [0.0, 0.3]))
+        self.bias_token = np.concatenate([r.choice(V, 9, replace=False) for _ in range(B)])
+        self.bias_value = (r.standard_normal(9 * B) * 2).astype(np.float32)
+        self.bias = np.array([[9 * u, 9 * u + 9] for u in range(B)])[users_of]
+        self.words = r.integers(-2 ** 31, 2 ** 31, (B, (V + 31) // 32)).astype(np.int32)
+        self.mask_row = np.array([u if u % 2 else -1 for u in range(B)])[users_of]
+
+    def make(self, **kw):
+        self.held = dict(tokens=dev(self.tokens), hist=dev(self.hist), repetition=dev(self.rep, np.float32),
+                         presence=dev(self.pres, np.float32), frequency=dev(self.freq, np.float32),
+                         bias_token=dev(self.bias_token), bias_value=dev(self.bias_value, np.float32), bias=dev(self.bias),
+                         mask=dev(self.words), mask_row=dev(self.mask_row))
+        return sv.make_logit_rules(self.T, self.V, **self.held, **kw)
+
+    def apply(self, raw, slot_tokens, parent):
+        """The same by the context-free call, the slots' tokens given."""
+        z = torch.from_numpy(raw).cuda()
+        out = torch.empty_like(z)
+        sv.sd_adjust_logits(z, self.make(row_token=dev(slot_tokens), row_parent=dev(parent)), out)
+        torch.cuda.synchronize()
+        return out.cpu().numpy()
+
+
+@pytest.mark.parametrize("model", ["tiny", "tiny-bf16"])
+def test_rules_in_tree_passes(model):
+    t = Trees(model, [40, 300, 0, 17], [5, 9, 12, 3], seed=71)
+    users = np.repeat(range(4), np.array(t.L) + 1)
+    R = BatchRules(t.m.vocab, users, 5)
+    slot_tokens = np.concatenate([[t.roots[u]] + list(t.drafts[u]) for u in range(4)])
+    first = np.cumsum([0] + [n + 1 for n in t.L])
+    parent = np.concatenate([[-1] + [first[u] + p for p in t.parent[u]] for u in range(4)])
+    for mode in ("greedy", "stochastic"):
+        raw = t.run(mode)[0]
+        got = t.run(mode, rules=R.make())
+        assert np.array_equal(got[0], R.apply(raw, slot_tokens, parent))
+        check_walks(t, *got, mode)
+        assert np.array_equal(t.run(mode)[0], raw)  # the rules were for one pass
+    for u, o in zip(range(4), OPTIONS):
+        t.v.user_sampling(u, *o)
+    got = t.run("stochastic", rules=R.make())
+    assert np.array_equal(got[0], filtered(R.apply(raw, slot_tokens, parent), OPTIONS[:4], np.array(t.L) + 1))
+    check_walks(t, *got, "stochastic")
+    t.v.close()
+
+
+@pytest.mark.parametrize("model,graph", [("tiny", False), ("tiny-bf16", False), ("tiny-bf16", True)])
+@pytest.mark.parametrize("logits_out", [sv.SD_LOGITS_AS_NEEDED, sv.SD_LOGITS_ALL])
+def test_rules_in_ordinary_passes(model, graph, logits_out):
+    prefix, L = [40, 300, 0, 17, 5], [1, 7, 3, 5, 2]
+    w = wl.custom_workload(model, prefix, L, seed=72)
+    dw = DeviceWeights(w.model, w.seed)
+    v = make_verifier(w, dw, logits_out=logits_out)
+    load_synthetic_kv(v, w)
+    b = w.batch(0)
+    from workload.device import batch_to_device
+    drafts, q, au = batch_to_device(b)
+    st = torch.cuda.Stream() if graph else None
+    users = np.repeat(range(5), b.n_slots)
+    R = BatchRules(w.model.vocab, users, 6)
+    j = np.concatenate([np.arange(n) for n in b.n_slots])
+    parent = np.where(j > 0, np.arange(b.T) - 1, -1)
+    for i, u in enumerate(b.users):
+        v.reset_user(int(u), prefix[i], int(b.root[i]))
+    raw = None
+    rules = R.make()
+    for mode in ("stochastic", "stochastic", "greedy", "force"):
+        if raw is None:
+            v.verify(0, w.assign, w.draft_len, drafts, q, mode, 3, 0, au, st, graph)
+            raw = shown(v, b.T, st)
+            v.accept(0, 5)
+            want = R.apply(raw, b.slot_tokens(), parent)
+        v.batch_rules(0, rules)
+        v.verify(0, w.assign, w.draft_len, drafts, q, mode, 3, 0, au, st, graph)
+        lg = shown(v, b.T, st)
+        acc, tok = v.accept(0, 5)
+        assert np.array_equal(lg, want), mode
+        ref = oracle.sample(mode, b.users, b.draft_len, want, b.drafts, b.q, b.accept_u, 3, 0)
+        assert np.array_equal(acc[b.users], ref["n_acc"]) and np.array_equal(tok[b.users], ref["token"]), mode
+    # another batch's rules wait for their pass
+    v.batch_rules(2, rules)
+    v.verify(0, w.assign, w.draft_len, drafts, q, "stochastic", 3, 0, au, st, graph)
+    assert np.array_equal(shown(v, b.T, st), raw)
+    v.accept(0, 5)
+    v.close()
+
+
+def test_rules_in_a_decoding_step_and_on_the_callers_logits():
+    prefix = [0, 17, 64, 129]
+    w = wl.custom_workload("tiny-bf16", prefix, [4] * 4, seed=73)
+    dw = DeviceWeights(w.model, w.seed)
+    v = make_verifier(w, dw, logits_out=sv.SD_LOGITS_AS_NEEDED)
+    load_synthetic_kv(v, w)
+    roots = np.array([5, 9, 100, 2000])
+    for u in range(4):
+        v.reset_user(u, prefix[u], int(roots[u]))
+    V = w.model.vocab
+    R = BatchRules(V, np.arange(4), 7)
+    probs = torch.zeros((4, V), device="cuda")
+    v.draft(0, np.zeros(4, np.int32), "stochastic", seed=2, probs=probs)
+    raw = v.logits(0, 4).cpu().numpy()
+    v.accept(0, 4)
+    want = R.apply(raw, roots, np.full(4, -1))
+    for mode in ("greedy", "stochastic"):
+        v.batch_rules(0, R.make())
+        v.draft(0, np.zeros(4, np.int32), mode, seed=2, probs=probs)
+        assert np.array_equal(v.logits(0, 4).cpu().numpy(), want)
+        _, tok = v.accept(0, 4)
+        z = want.astype(np.float64)
+        p = np.exp(z - z.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        assert np.abs(probs.cpu().numpy() - p).max() < 1e-5
+        if mode == "greedy":
+            assert np.array_equal(tok, want.argmax(1))
+    v.close()
+    Ls = [1, 4, 2, 8]
+    logits, q, drafts, au, users = _case(1024, Ls, "stochastic", 74, True)
+    v = _sampler_verifier(1024, 4, 8, sum(Ls) + 4)
+    R = BatchRules(1024, np.repeat(range(4), np.array(Ls) + 1), 8)
+    z = torch.from_numpy(logits).cuda()
+    a = np.zeros(4, np.int32)
+    v.batch_rules(0, R.make())
+    with pytest.raises(sv.SdError) as e:  # users without root tokens
+        v.sample(0, a, Ls, dev(drafts), dev(q, np.float32), z, "stochastic", 5, 1, dev(au, np.float32))
+    assert e.value.status == sv.SD_EINVAL
+    for u in range(4):
+        v.reset_user(u, 0, 11 * u)
+    v.sample(0, a, Ls, dev(drafts), dev(q, np.float32), z, "stochastic", 5, 1, dev(au, np.float32))
+    acc, tok = v.accept(0, 4)
+    assert np.array_equal(z.cpu().numpy(), logits)
+    toks, o = [], 0
+    for u, n in enumerate(Ls):
+        toks += [11 * u] + list(drafts[o:o + n])
+        o += n
+    j = np.concatenate([np.arange(n + 1) for n in Ls])
+    want = R.apply(logits, np.array(toks), np.where(j > 0, np.arange(j.size) - 1, -1))
+    ref = oracle.sample("stochastic", users, Ls, want, drafts, q, au, 5, 1)
+    assert np.array_equal(acc, ref["n_acc"]) and np.array_equal(tok, ref["token"])
+    v.close()
+
+
+def test_a_token_out_of_range_commits_nothing():
+    t = Trees("tiny-bf16", [40, 30], [4, 6], seed=75)
+    t.drafts[1][2] = t.m.vocab
+    with pytest.raises(sv.SdError) as e:
+        t.run(commit=True)
+    assert e.value.status == sv.SD_EDEVICE
+    assert [t.v.user_state(u)[0] for u in range(2)] == [40, 30]
+    t.drafts[1][2] = 3
+    lg, *_ = t.run()
+    t.check_logits(lg, "after a bad token")
+    t.v.close()
+
+
+def test_a_row_without_a_token_stops_its_user():
+    """A mask that allows nothing: token -1, and a commit leaves the user where it is."""
+    t = Trees("tiny-bf16", [40, 30], [4, 6], seed=76)
+    mask = np.zeros((1, t.m.vocab // 32), np.int32)
+    row = np.array([0] * 5 + [-1] * 7)
+    rules = sv.make_logit_rules(12, t.m.vocab, mask=dev(mask), mask_row=dev(row))
+    lg, acc, tok, path = t.run("stochastic", rules=rules, commit=True)
+    assert tok[0] == -1 and acc[0] == 0 and t.v.user_state(0)[0] == 40
+    assert tok[1] >= 0 and t.v.user_state(1)[0] == 31 + acc[1]
+    t.v.close()
+
+
+def test_refusals():
+    t = Trees("tiny-bf16", [40, 30, 9], [4, 6, 2], seed=77, spare=1, max_draft=6)
+    v, ctx = t.v, t.v.ctx
+    before = [v.user_state(u) for u in range(3)], [list(v.user_pages(u)) for u in range(3)]
+
+    def refused(status, f, *a, **k):
+        with pytest.raises(sv.SdError) as e:
+            f(*a, **k)
+        assert e.value.status == status
+
+    d, par = dev(np.concatenate(t.drafts)), np.concatenate(t.parent)
+    for i, p in ((0, 1), (0, -1), (5, 6), (3, 9)):
+        bad = par.copy()
+        bad[i] = p
+        refused(sv.SD_EINVAL, v.verify_tree, 0, t.assign, t.draft_len, d, bad, "greedy")
+    refused(sv.SD_EINVAL, v.verify_tree, 0, t.assign, t.draft_len, d, par, "force")
+    refused(sv.SD_EINVAL, v.verify_tree, 0, t.assign, t.draft_len, None, par, "greedy")
+    refused(sv.SD_EINVAL, v.verify_tree, 0, np.zeros(4, np.int32), t.draft_len, d, list(par) + [0], "greedy")  # user 3 not started
+    with pytest.raises(ValueError):
+        v.verify_tree(0, t.assign, t.draft_len, d, par[:-1], "greedy")
+    refused(sv.SD_ESTATE, v.accept_tree, 0, 4)
+    # forks
+    for user, frm, n, root in ((0, 0, 1, 0), (4, 0, 1, 0), (-1, 0, 1, 0), (1, 3, 0, 0), (3, 0, 41, 0), (3, 0, -1, 0),
+                               (3, 0, 1, -1), (3, 0, 1, t.m.vocab)):
+        refused(sv.SD_EINVAL, v.fork_user, user, frm, n, root)
+    refused(sv.SD_EINVAL, v.user_pages, 3)
+    # rules
+    one = torch.zeros(15, device="cuda")
+    r15 = sv.make_logit_rules(15, t.m.vocab, presence=one)
+    r9 = sv.make_logit_rules(9, t.m.vocab, presence=one[:9].contiguous())
+    i15 = torch.zeros(15, dtype=torch.int32, device="cuda")
+    refused(sv.SD_EINVAL, v.batch_rules, 0, sv.make_logit_rules(15, t.m.vocab, row_token=i15, row_parent=i15))
+    refused(sv.SD_EINVAL, v.batch_rules, -1, r15)
+    refused(sv.SD_EINVAL, v.batch_rules, 0, sv.make_logit_rules(1000, t.m.vocab, presence=torch.zeros(1000, device="cuda")))
+    with pytest.raises(ValueError):
+        v.batch_rules(0, sv.make_logit_rules(15, 100, presence=one))
+    v.batch_rules(0, r9)
+    refused(sv.SD_EINVAL, v.verify_tree, 0, t.assign, t.draft_len, d, par, "greedy")  # 15 slots
+    v.batch_rules(0, None)
+    assert before == ([v.user_state(u) for u in range(3)], [list(v.user_pages(u)) for u in range(3)])
+    v.verify_tree(0, t.assign, t.draft_len, d, par, "greedy")
+    refused(sv.SD_ESTATE, v.batch_rules, 0, r15)
+    refused(sv.SD_ESTATE, v.fork_user, 3, 0, 4, 1)
+    refused(sv.SD_ESTATE, v.verify_tree, 2, np.where(t.assign == 0, 2, -1), t.draft_len, d, par, "greedy")
+    v.accept(0, 4)
+    v.close()
+
+
+def test_a_fork_without_room_changes_nothing():
+    v = _sampler_verifier(64, 4, 2, 8)  # eight pages
+    v.reset_user(0, 62, 1)
+    v.reset_user(1, 62, 2)
+    for user in (2, 3):
+        with pytest.raises(sv.SdError) as e:
+            v.fork_user(user, 0, 40, 1)
+        assert e.value.status == sv.SD_ENOMEM
+        with pytest.raises(sv.SdError):
+            v.user_state(user)
+    held = list(v.user_pages(0)), list(v.user_pages(1))
+    v.fork_user(1, 0, 50, 7)  # its own pages do
+    assert [len(x) for x in held] == [4, 4] and list(v.user_pages(1)) == held[1] and v.user_state(1) == (50, 7)
+    v.reset_user(1, 16, 2)
+    v.fork_user(2, 0, 40, 1)
+    assert len(v.user_pages(2)) == 3 and set(v.user_pages(2)) < set(held[1])
+    torch.cuda.synchronize()
+    v.close()
