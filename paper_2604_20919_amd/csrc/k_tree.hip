@@ -130,98 +130,100 @@ __global__ __launch_bounds__(256) void k_tree_rows(TreeCall c) {
 //                      dim-major block; P in two bf16 planes.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(4))) const int32_t cint32_t;
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kRows = 128;   // query rows a workgroup
 constexpr int kBlock = 32;   // tokens a block
-constexpr int kBuffers = 3;  // LDS ring
-constexpr int kResident = 2; // workgroups a CU
 
+// All blocks of all units -- a user's query rows in groups, for every KV head --
+// stand in one line, and every workgroup takes `per` of them.  A unit that lies in
+// several workgroups' parts is merged afterwards from their partials: slot 2 w of
+// workgroup w is its first segment, 2 w + 1 its last.
 struct TreePlan {
-    int cap;       // units times row groups aimed at
-    int groups;    // row groups of the widest user
-    int units;     // most units
-    float* part;   // [rows][HD] outputs of chunks, not yet divided
-    float2* ml;    // [rows] their maxima (log2 domain) and sums
-    int2* table;   // [n_users] chunks, first row of the partials
+    int wgs;        // workgroups
+    int prows;      // rows of a partial slot
+    int64_t* per;   // blocks a workgroup, as the kernel found it
+    int64_t* base;  // [n_users] where a user's first unit begins
+    float* part;    // [2 wgs][prows][HD] outputs of segments, not yet divided
+    float2* ml;     // [2 wgs][prows] their maxima (log2 domain) and sums
 };
 
-// What one workgroup does: user, head, its chunk of blocks, its partials' first row.
-struct TreeUnit {
-    int b, g, chunk, chunks, blk0, blk1, row0;
+// A user in the line: its units (KV head by KV head, row group by row group) of nb
+// blocks each begin at base.
+struct TreeSpan {
+    int b, nb, units;
+    int64_t base;
 };
+struct TreeScan {
+    int64_t sum[8];
+    TreeSpan found;
+};
+template <int ROWS> __device__ __forceinline__ int64_t tree_weight(const TreeCall& c, int b, int* nb, int* units) {
+    *nb = *units = 0;
+    if (b >= c.n_users) return 0;
+    const TreeUser us = tree_user(c, b);
+    if (us.n <= 0) return 0;
+    *nb = (us.end + kBlock - 1) / kBlock;
+    *units = (us.n * (c.hq / c.kv.hkv) + ROWS - 1) / ROWS * c.kv.hkv;
+    return (int64_t)*nb * *units;
+}
 
-// The unit of number u: users in order, a user's chunks in order, heads.  Every
-// workgroup works this out for itself from the users' lengths (a launch less than a
-// plan made before).  A chunk has as many blocks as leave all units times row
-// groups within `cap`, evened out within a user.
-__device__ __forceinline__ bool tree_unit(const TreeCall& c, const TreePlan& pl, int u, TreeUnit* out) {
-    __shared__ int64_t wsum[4];
-    __shared__ int wu[4], wr[4];
-    __shared__ TreeUnit found;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, G = c.hq / c.kv.hkv;
-    auto blocks_of = [&](int b, int* rows) {
-        const TreeUser us = tree_user(c, b);
-        *rows = us.n * G;
-        return us.n > 0 ? (us.end + kBlock - 1) / kBlock : 0;
-    };
-    int64_t total = 0;
-    int rows = 0;
-    for (int b = tid; b < c.n_users; b += 256) {
-        const int nb = blocks_of(b, &rows);
-        total += (int64_t)nb * ((rows + kRows - 1) / kRows);
-    }
+// The length of the line, and the user at a position of it.  Every workgroup works
+// them out from the users' lengths (a launch less than a plan made before).
+template <int NW> __device__ __forceinline__ int64_t tree_total(const TreeCall& c, TreeScan& sc) {
+    const int tid = threadIdx.x, wave = tid >> 6;
+    int nb, units;
+    int64_t t = 0;
+    for (int b = tid; b < c.n_users; b += 64 * NW) t += tree_weight<32 * NW>(c, b, &nb, &units);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    if (lane == 0) wsum[wave] = total;
-    if (tid == 0) found.b = -1;
+    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+    if ((tid & 63) == 0) sc.sum[wave] = t;
     __syncthreads();
-    total = (wsum[0] + wsum[1] + wsum[2] + wsum[3]) * c.kv.hkv;
-    const int len = (int)min(max((total + pl.cap - 1) / pl.cap, (int64_t)1), (int64_t)1 << 30);
-    int u0 = 0, r0 = 0;  // units and partial rows of the users before
-    for (int b0 = 0; b0 < c.n_users; b0 += 256) {
-        const int b = b0 + tid;
-        const int nb = b < c.n_users ? blocks_of(b, &rows) : 0;
-        const int nc = (nb + len - 1) / len;
-        int su = nc, sr = nc > 1 ? nc * rows : 0;  // inclusive sums over the users
+    t = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) t += sc.sum[w];
+    __syncthreads();
+    return t;
+}
+template <int NW> __device__ __forceinline__ TreeSpan tree_find(const TreeCall& c, int64_t pos, TreeScan& sc) {
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    int64_t before = 0;
+    for (int b0 = 0; b0 < c.n_users; b0 += 64 * NW) {
+        int nb, units;
+        const int64_t own = tree_weight<32 * NW>(c, b0 + tid, &nb, &units);
+        int64_t t = own;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(su, o, 64), y = __shfl_up(sr, o, 64);
-            if (lane >= o) { su += x; sr += y; }
+            const int64_t x = __shfl_up(t, o, 64);
+            if (lane >= o) t += x;
         }
-        if (lane == 63) { wu[wave] = su; wr[wave] = sr; }
+        if (lane == 63) sc.sum[wave] = t;
         __syncthreads();
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) { su += wu[w]; sr += wr[w]; }
+        int64_t all = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w == wave) t += before + all;
+            all += sc.sum[w];
         }
-        const int first = (u0 + su - nc) * c.kv.hkv;
-        if (nc > 0 && u >= first && u < first + nc * c.kv.hkv) {
-            const int k = (u - first) / c.kv.hkv, each = (nb + nc - 1) / nc;
-            found.b = b;
-            found.g = (u - first) % c.kv.hkv;
-            found.chunk = k;
-            found.chunks = nc;
-            found.blk0 = min(nb, k * each);
-            found.blk1 = min(nb, (k + 1) * each);
-            found.row0 = (r0 + sr - (nc > 1 ? nc * rows : 0)) * c.kv.hkv;
-        }
-        u0 += wu[0] + wu[1] + wu[2] + wu[3];
-        r0 += wr[0] + wr[1] + wr[2] + wr[3];
+        if (own > 0 && pos >= t - own && pos < t) sc.found = TreeSpan{b0 + tid, nb, units, t - own};
+        before += all;
         __syncthreads();
-        if (found.b >= 0) break;
+        if (pos < before) break;
     }
     // (the same in every lane: kept in scalar registers)
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    *out = TreeUnit{same(found.b), same(found.g), same(found.chunk), same(found.chunks),
-                    same(found.blk0), same(found.blk1), same(found.row0)};
-    return out->b >= 0;
+    TreeSpan f = sc.found;
+    f = TreeSpan{same(f.b), same(f.nb), same(f.units),
+                 (int64_t)((uint64_t)(uint32_t)same((int)f.base) | (uint64_t)(uint32_t)same((int)(f.base >> 32)) << 32)};
+    __syncthreads();
+    return f;
 }
 
 // anc[j]: bits of slot j and its ancestors, by doubling: what a slot's furthest
 // known ancestor knows is added to it until nobody has one.
+template <int THREADS>
 __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser& us, uint32_t (*anc)[kMaskWords + 1],
                                                int* ptr) {
+    static_assert(THREADS >= kSlots, "a thread a slot");
     const int j = threadIdx.x;
     int p = -1;
     if (j < us.n) {
@@ -229,8 +231,8 @@ __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser
         p = p >= 0 && p < j ? p : -1;
 #pragma unroll
         for (int w = 0; w <= kMaskWords; ++w) anc[j][w] = w == j >> 5 ? 1u << (j & 31) : 0;
+        ptr[j] = p;
     }
-    ptr[j] = p;
     while (__syncthreads_or(p >= 0)) {
         uint32_t more[kMaskWords] = {};
         int next = -1;
@@ -243,9 +245,9 @@ __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser
         if (p >= 0) {
 #pragma unroll
             for (int w = 0; w < kMaskWords; ++w) anc[j][w] |= more[w];
+            ptr[j] = next;
         }
         p = next;
-        ptr[j] = p;
     }
 }
 
@@ -268,39 +270,46 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// The fragments of one block, K's waited for and V's on their way.  The reads are
-// not the compiler's: it cannot tell the buffer from the ones being loaded and
-// would wait for every load in flight.  ka: this lane's K pieces (four addresses, the
-// swizzle moves them apart), va: its V slot, in the block's buffer.
-template <int HD>
-__device__ __forceinline__ void read_block(bf16x8 (&k)[HD / 16], bf16x8 (&v)[HD / 16], const uint32_t (&ka)[4], uint32_t va) {
+// The fragments of one block.  The reads are not the compiler's: it cannot tell the
+// buffer from the ones being loaded and would wait for every load in flight.  K's
+// are waited for; V's are not (wait_v), and begin when the scores are there (s), so
+// that both can have the same registers.  ka: this lane's K pieces (four addresses,
+// the swizzle moves them apart), va: its V slot, in the block's buffer.
+template <int HD> __device__ __forceinline__ void read_k(bf16x8 (&k)[HD / 16], const uint32_t (&ka)[4]) {
     if constexpr (HD == 128) {
         asm volatile(
-            "ds_read_b128 %0, %16 offset:%21\n\tds_read_b128 %1, %17 offset:%21\n\t"
-            "ds_read_b128 %2, %18 offset:%21\n\tds_read_b128 %3, %19 offset:%21\n\t"
-            "ds_read_b128 %4, %16 offset:%22\n\tds_read_b128 %5, %17 offset:%22\n\t"
-            "ds_read_b128 %6, %18 offset:%22\n\tds_read_b128 %7, %19 offset:%22\n\t"
-            "ds_read_b128 %8, %20 offset:%23\n\tds_read_b128 %9, %20 offset:%24\n\t"
-            "ds_read_b128 %10, %20 offset:%25\n\tds_read_b128 %11, %20 offset:%26\n\t"
-            "ds_read_b128 %12, %20 offset:%27\n\tds_read_b128 %13, %20 offset:%28\n\t"
-            "ds_read_b128 %14, %20 offset:%29\n\tds_read_b128 %15, %20 offset:%30\n\t"
-            "s_waitcnt lgkmcnt(8)"
-            : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(k[4]), "=&v"(k[5]), "=&v"(k[6]), "=&v"(k[7]),
-              "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
-            : "v"(ka[0]), "v"(ka[1]), "v"(ka[2]), "v"(ka[3]), "v"(va), "n"(0), "n"(128), "n"(8192),
-              "n"(9216), "n"(10240), "n"(11264), "n"(12288), "n"(13312), "n"(14336),
-              "n"(15360)
+            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+            "ds_read_b128 %4, %8 offset:128\n\tds_read_b128 %5, %9 offset:128\n\t"
+            "ds_read_b128 %6, %10 offset:128\n\tds_read_b128 %7, %11 offset:128\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(k[4]), "=&v"(k[5]), "=&v"(k[6]), "=&v"(k[7])
+            : "v"(ka[0]), "v"(ka[1]), "v"(ka[2]), "v"(ka[3])
             : "memory");
     } else {
         asm volatile(
-            "ds_read_b128 %0, %8 offset:%13\n\tds_read_b128 %1, %9 offset:%13\n\t"
-            "ds_read_b128 %2, %10 offset:%13\n\tds_read_b128 %3, %11 offset:%13\n\t"
-            "ds_read_b128 %4, %12 offset:%14\n\tds_read_b128 %5, %12 offset:%15\n\t"
-            "ds_read_b128 %6, %12 offset:%16\n\tds_read_b128 %7, %12 offset:%17\n\t"
-            "s_waitcnt lgkmcnt(4)"
-            : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-            : "v"(ka[0]), "v"(ka[1]), "v"(ka[2]), "v"(ka[3]), "v"(va), "n"(0), "n"(4096), "n"(5120),
-              "n"(6144), "n"(7168)
+            "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3])
+            : "v"(ka[0]), "v"(ka[1]), "v"(ka[2]), "v"(ka[3])
+            : "memory");
+    }
+}
+template <int HD> __device__ __forceinline__ void read_v(bf16x8 (&v)[HD / 16], uint32_t va, f32x16& s) {
+    if constexpr (HD == 128) {
+        asm volatile(
+            "ds_read_b128 %0, %9 offset:8192\n\tds_read_b128 %1, %9 offset:9216\n\t"
+            "ds_read_b128 %2, %9 offset:10240\n\tds_read_b128 %3, %9 offset:11264\n\t"
+            "ds_read_b128 %4, %9 offset:12288\n\tds_read_b128 %5, %9 offset:13312\n\t"
+            "ds_read_b128 %6, %9 offset:14336\n\tds_read_b128 %7, %9 offset:15360"
+            : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]),
+              "+v"(s)
+            : "v"(va)
+            : "memory");
+    } else {
+        asm volatile(
+            "ds_read_b128 %0, %5 offset:4096\n\tds_read_b128 %1, %5 offset:5120\n\t"
+            "ds_read_b128 %2, %5 offset:6144\n\tds_read_b128 %3, %5 offset:7168"
+            : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "+v"(s)
+            : "v"(va)
             : "memory");
     }
 }
@@ -312,234 +321,276 @@ template <int N> __device__ __forceinline__ void wait_v(bf16x8 (&v)[N]) {
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
 }
 
-// Eight bf16 values: infinities and not-a-numbers taken out (fin), and where they
-// were: 1 in up for +inf and not-a-numbers, in down for -inf and not-a-numbers.
-__device__ __forceinline__ void split_odd(const bf16x8& v, bf16x8& fin, bf16x8& up, bf16x8& down) {
+// Eight bf16 values with infinities and not-a-numbers taken out; and where they are:
+// 1 for the infinity of one sign (0x7f80 or 0xff80) and for not-a-numbers.
+__device__ __forceinline__ bf16x8 only_finite(bf16x8 v) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint16_t x = __builtin_bit_cast(uint16_t, (__bf16)v[e]);
-        const bool odd = (x & 0x7f80) == 0x7f80, nan = odd && (x & 0x7f);
-        fin[e] = odd ? (__bf16)0.f : v[e];
-        up[e] = (__bf16)(nan || (odd && !(x >> 15)) ? 1.f : 0.f);
-        down[e] = (__bf16)(nan || (odd && (x >> 15)) ? 1.f : 0.f);
+        if ((x & 0x7f80) == 0x7f80) v[e] = (__bf16)0.f;
     }
+    return v;
+}
+__device__ __forceinline__ bf16x8 where_odd(bf16x8 v, uint32_t inf) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint16_t x = __builtin_bit_cast(uint16_t, (__bf16)v[e]);
+        v[e] = (__bf16)(x == inf || (x & 0x7fff) > 0x7f80 ? 1.f : 0.f);
+    }
+    return v;
 }
 
-template <int HD> struct TreeLds {
+// NW waves a workgroup, 32 rows each: 4 (two workgroups a CU) or 8.
+template <int HD, int NW> struct TreeLds {
     static constexpr int PB = kPageTokens * HD * 2;  // bytes of a page's K or V block
     static constexpr int BUF = 4 * PB;               // two pages of K, two of V
-    __attribute__((aligned(1024))) char ring[kBuffers * BUF];
+    static constexpr int N = NW == 8 ? 6 : 3;        // buffers
+    __attribute__((aligned(1024))) char ring[N * BUF];
     uint32_t anc[kSlots][kMaskWords + 1];
     int ptr[kSlots];
+    TreeScan scan;
 };
 
-template <int HD, bool QLO>
-__device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl, TreeLds<HD>& lds) {
+// A segment: blocks blk0 .. blk1-1 of a unit.
+struct TreeSeg {
+    int b, g, rg, blk0, blk1;
+};
+
+// What the waves of a workgroup hold of their rows, and where they read from.
+template <int HD, bool QLO> struct TreeWave {
+    bf16x8 qf[HD / 16], ql[QLO ? HD / 16 : 1];
+    uint32_t ka[4], va;      // this lane's K pieces and V slot of the first buffer
+    uint32_t ksrc, vsrc;     // its gather sources within a page's K and V blocks
+    const uint32_t* anc;     // its row's ancestors
+    bool act;                // the wave has rows
+};
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// One pass over a segment.  CAREFUL: the values' infinities and not-a-numbers are kept
+// apart: 0 times one is not 0 in a product, and rows that do not see such a value, or
+// see it with two weights of opposite sign, must not take part in that.
+template <int HD, bool QLO, int NW, bool CAREFUL>
+__device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, int prefix, const TreeWave<HD, QLO>& w,
+                                          char* ring, int wave, float sc2, float& m, float& l,
+                                          f32x16 (&o)[HD / 32]) {
+    constexpr int DS = HD / 16, DT = HD / 32;
+    constexpr int PB = TreeLds<HD, NW>::PB, BUF = TreeLds<HD, NW>::BUF, N = TreeLds<HD, NW>::N;
+    constexpr int LOADS = BUF / 1024 / NW;  // 1 KB loads a wave and block
+    constexpr int PD = N - 1;               // blocks in flight
+    const int lane = threadIdx.x & 63, H = lane >> 5;
+    const int last = un.blk1 - un.blk0 - 1;
+    // K and V of the KV head in a page: page_bytes apart, V vo behind K
+    const char* const kbase = (const char*)c.kv.base + c.kv.k_off(c.layer, 0, un.g) * 2;
+    const uint32_t page_bytes = (uint32_t)(c.kv.page_elems() * 2), vo = (uint32_t)c.kv.hkv * PB;
+    // the pages of 32 blocks, a lane each (-1: the pool has not got it), and of the next 32
+    const int32_t* const pt = c.page_table + (size_t)un.b * c.max_pages;
+    auto pages = [&](int blk) {
+        const int i = 2 * blk + lane, p = i < c.max_pages && blk < un.blk1 ? pt[i] : -1;
+        return p < c.kv.n_pages ? p : -1;
+    };
+    int pg = pages(un.blk0), pg_next = pages(un.blk0 + 32);
+    uint32_t there = 0;  // which pages of the last blocks issued exist, two bits a block
+    auto issue = [&](int i, int buf) __attribute__((always_inline)) {
+        // (missing pages are read as page 0 and not attended to)
+        const int p0 = __builtin_amdgcn_readlane(pg, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(pg, 2 * (i & 31) + 1);
+        there = there << 2 | (p1 >= 0) << 1 | (p0 >= 0);
+        auto rsrc = [&](int p) {
+            return __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + (uint64_t)(uint32_t)max(p, 0) * page_bytes), (short)0,
+                                                     (int)(vo + PB), 0x00020000);
+        };
+        char* dst = ring + buf * BUF;
+        auto load = [&](__amdgpu_buffer_rsrc_t r, int at, uint32_t src, uint32_t off) __attribute__((always_inline)) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + at), 16, (int)src, (int)off, 0, 0);
+        };
+        // (V fragments: [dim tile][page])
+        if constexpr (HD == 128 && NW == 4) {
+            const __amdgpu_buffer_rsrc_t r0 = rsrc(p0), r1 = rsrc(p1);
+            load(r0, wave * 1024, w.ksrc, 0);
+            load(r1, PB + wave * 1024, w.ksrc, 0);
+            load(r0, 2 * PB + wave * 2048, w.vsrc, vo);
+            load(r1, 2 * PB + wave * 2048 + 1024, w.vsrc, vo);
+        } else if constexpr (HD == 128) {
+            const __amdgpu_buffer_rsrc_t r0 = rsrc(p0), r1 = rsrc(p1);
+            const int part = wave & 3;
+            const bool v = wave >= 4;
+            const uint32_t src = v ? w.vsrc : w.ksrc, off = v ? vo : 0;
+            load(r0, v ? 2 * PB + part * 2048 : part * 1024, src, off);
+            load(r1, v ? 2 * PB + part * 2048 + 1024 : PB + part * 1024, src, off);
+        } else {
+            const int page = (wave >> 1) & 1, part = wave & 1;
+            const __amdgpu_buffer_rsrc_t r = rsrc(page ? p1 : p0);
+            if (NW == 4 || wave < 4) load(r, page * PB + part * 1024, w.ksrc, 0);
+            if (NW == 4 || wave >= 4) load(r, 2 * PB + part * 2048 + page * 1024, w.vsrc, vo);
+        }
+    };
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+    __syncthreads();  // (the ring is free, the ancestors are there)
+    wait_vm<0>();
+    for (int i = 0; i < PD; ++i) issue(min(i, last), i);
+    int buf = 0;  // of block i
+    for (int i = 0; i <= last; ++i, buf = buf + 1 == N ? 0 : buf + 1) {
+        const int t0 = (un.blk0 + i) * kBlock;
+        if (i + PD <= last) {
+            wait_vm<LOADS * (PD - 1), true>();
+            barrier_nofence();
+            if (((i + PD) & 31) == 0) {
+                pg = pg_next;
+                pg_next = pages(un.blk0 + i + PD + 32);
+            }
+            issue(i + PD, buf == 0 ? N - 1 : buf - 1);
+        } else {
+            // the tail: blocks i .. last are the only ones in flight
+            if (PD > 4 && last - i >= 4) wait_vm<4 * LOADS, true>();
+            else if (PD > 3 && last - i == 3) wait_vm<3 * LOADS, true>();
+            else if (PD > 2 && last - i == 2) wait_vm<2 * LOADS, true>();
+            else if (last - i == 1) wait_vm<LOADS, true>();
+            else wait_vm<0, true>();
+            barrier_nofence();
+            there <<= 2;
+        }
+        if (!w.act) continue;
+        bf16x8 kf[DS], vf[DS];
+        const uint32_t at = (uint32_t)(buf * BUF), kb[4] = {w.ka[0] + at, w.ka[1] + at, w.ka[2] + at, w.ka[3] + at};
+        read_k<HD>(kf, kb);
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int d = 0; d < DS; ++d) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.qf[d], s, 0, 0, 0);
+            if constexpr (QLO) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.ql[d], s, 0, 0, 0);
+        }
+        read_v<HD>(vf, w.va + at, s);
+        // lane: tokens t0 + 8 H + e (e < 8) and t0 + 16 + 8 H + e of its row
+        const uint32_t both = there >> (2 * PD) & 3;
+        uint32_t see = ~0u;
+        if (t0 + kBlock > prefix || both != 3) {
+            see = (both & 1 ? 0xffffu : 0u) | (both & 2 ? 0xffff0000u : 0u);
+            if (t0 + kBlock > prefix) see &= tree_bits(w.anc, t0, prefix);
+            see >>= 8 * H;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = (see >> (e < 8 ? e : e + 8)) & 1 ? s[e] : -INFINITY;
+        }
+        float bm = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int e = 2; e < 16; ++e) bm = fmaxf(bm, s[e]);
+        const float mn = fmaxf(m, half_max(bm));
+        const bool live = mn != -INFINITY;
+        const float ms = live ? mn * sc2 : 0.f;
+        const float alpha = live ? __builtin_amdgcn_exp2f((m - mn) * sc2) : 1.f;
+        // the weights as two bf16 planes: hi rounded, lo what that left
+        float rs[2] = {0.f, 0.f};
+        uint32_t ph[8], pl[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], sc2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], sc2, -ms));
+            rs[0] += p0;
+            rs[1] += p1;
+            const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
+            ph[e / 2] = hi;
+            pl[e / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(p0 - __uint_as_float(hi << 16)),
+                                                            (__bf16)(p1 - __uint_as_float(hi & 0xffff0000u))});
+        }
+        l = fmaf(l, alpha, rs[0] + rs[1]);
+        m = mn;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        }
+        wait_v(vf);
+        if constexpr (CAREFUL) {
+            bf16x8 z[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)((see >> (e < 8 ? e : e + 8)) & 1 ? 1.f : 0.f);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+#pragma unroll
+                for (int sign = 0; sign < 2; ++sign) {
+                    f32x16 hit = f32x16{};
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_odd(vf[2 * d + t], sign ? 0xff80 : 0x7f80), z[t],
+                                                                      hit, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] += hit[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+                }
+                vf[2 * d] = only_finite(vf[2 * d]);
+                vf[2 * d + 1] = only_finite(vf[2 * d + 1]);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const bf16x8 hi = __builtin_bit_cast(bf16x8, uint4{ph[4 * t], ph[4 * t + 1], ph[4 * t + 2], ph[4 * t + 3]});
+                const bf16x8 lo = __builtin_bit_cast(bf16x8, uint4{pl[4 * t], pl[4 * t + 1], pl[4 * t + 2], pl[4 * t + 3]});
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], hi, o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], lo, o[d], 0, 0, 0);
+            }
+    }
+    wait_vm<0>();
+    l = half_sum(l);
+}
+
+template <int HD, bool QLO, int NW>
+__device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& pl, TreeLds<HD, NW>& lds, const TreeSeg& un,
+                                             const TreeUser& us, bool whole, int slot) {
     constexpr int DS = HD / 16, DT = HD / 32;  // k steps of S, dim tiles of O
-    constexpr int PB = TreeLds<HD>::PB, BUF = TreeLds<HD>::BUF;
-    constexpr int LOADS = BUF / 4096;          // 1 KB loads a wave and block
-    char* const ring = lds.ring;
-    auto& anc = lds.anc;
-    auto& ptr = lds.ptr;
+    constexpr int PB = TreeLds<HD, NW>::PB, ROWS = 32 * NW;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int lr = lane & 31, H = lane >> 5;
-    // workgroups that share a chunk (row groups) on one die, one after the other
-    const int x = blockIdx.x & 7, k = blockIdx.x >> 3, rg = k % pl.groups, u = (k / pl.groups) * 8 + x;
-    TreeUnit un;
-    if (!tree_unit(c, pl, u, &un)) return;
-    TreeUser us = tree_user(c, un.b);
-    us = TreeUser{__builtin_amdgcn_readfirstlane(us.s0), __builtin_amdgcn_readfirstlane(us.n),
-                  __builtin_amdgcn_readfirstlane(us.prefix), __builtin_amdgcn_readfirstlane(us.end)};
     const int G = c.hq / c.kv.hkv, R = us.n * G;
-    if (rg * kRows >= R) return;
-    if (un.g == 0 && un.chunk == 0 && rg == 0 && tid == 0) pl.table[un.b] = int2{un.chunks, un.row0};
-    if (un.blk1 * kBlock > us.prefix) tree_ancestors(c, us, anc, ptr);
-    const cint32_t* pt = (const cint32_t*)(c.page_table + (size_t)un.b * c.max_pages);
-    const int row = rg * kRows + wave * 32 + lr;
-    const bool act = rg * kRows + wave * 32 < R, ok = row < R;
+    const int lrow = wave * 32 + lr, row = un.rg * ROWS + lrow;
+    const bool ok = row < R;
     const int j = ok ? row / G : 0, hh = ok ? row % G : 0;
-    bf16x8 qf[DS], ql[QLO ? DS : 1];
+    TreeWave<HD, QLO> w;
+    w.act = un.rg * ROWS + wave * 32 < R;
+    w.anc = lds.anc[j];
     {
         const size_t e = (size_t)(us.s0 + j) * c.qs + (size_t)(un.g * G + hh) * HD + 8 * H;
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
-            qf[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q + e + 16 * d) : bf16x8{};
-            if constexpr (QLO) ql[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q_lo + e + 16 * d) : bf16x8{};
+            w.qf[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q + e + 16 * d) : bf16x8{};
+            if constexpr (QLO) w.ql[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q_lo + e + 16 * d) : bf16x8{};
         }
     }
-    // this lane's gather sources within a page's K and V blocks, and what it reads of a buffer
-    constexpr int PIECES = HD / 8, TOK = 64 / PIECES;  // 16-byte pieces of a K row, rows a 1 KB load
-    auto swz = [](int t) { return (t & 3) | ((t >> 1) & 4); };  // of token t of a page
-    // load i of a wave (hd 128: K page 0, K page 1, V page 0, V page 1, a quarter each; hd 64:
-    // K, V, half a page each)
-    const int part = HD == 128 ? wave : wave & 1;
+    // A wave's loads of a block: head_dim 128: quarters of K of page 0, of page 1, of V of
+    // page 0, of page 1; 64: halves of K and of V of one page (with eight waves: four of
+    // them K, four V).  K rows lie in LDS as in the page, their 16-byte pieces exchanged
+    // so that 8 lanes that read a piece of 8 rows read 8 different ones; V as fragments.
+    constexpr int PIECES = HD / 8, TOK = 64 / PIECES;  // pieces of a K row, rows a 1 KB load
+    auto swz = [](int t) { return (t & 3) | ((t >> 1) & 4); };  // of row t of a page
+    const int part = HD == 128 ? wave & 3 : wave & 1;
     const int kt = part * TOK + lane / PIECES;
-    const uint32_t ksrc = (uint32_t)(kt * HD * 2 + ((lane % PIECES) ^ swz(kt)) * 16);
-    const uint32_t vsrc = (uint32_t)(part * 1024 + lr * 32 + H * 16);
-    uint32_t ka[4];
+    w.ksrc = (uint32_t)(kt * HD * 2 + ((lane % PIECES) ^ swz(kt)) * 16);
+    w.vsrc = (uint32_t)(part * 1024 + lr * 32 + H * 16);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.ring;
     {
         const int a = lr >> 3, tok = 8 * ((lr >> 2) & 1) + 4 * (a & 1) + (lr & 3);
-        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
-            ka[d] = base + (uint32_t)((a >> 1) * PB + tok * HD * 2 + ((H ^ swz(tok)) ^ (2 * d)) * 16);
+            w.ka[d] = base + (uint32_t)((a >> 1) * PB + tok * HD * 2 + ((H ^ swz(tok)) ^ (2 * d)) * 16);
     }
-    const uint32_t va = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring + lane * 16u;
-
-    auto page_at = [&](int i) { return i < c.max_pages ? pt[i] : -1; };
-    auto in_pool = [&](int p) { return p >= 0 && p < c.kv.n_pages; };
-    auto issue = [&](int p0, int p1, int buf) __attribute__((always_inline)) {
-        // (pages that the pool has not got are read as page 0 and not attended to)
-        p0 = in_pool(p0) ? p0 : 0;
-        p1 = in_pool(p1) ? p1 : 0;
-        const char* base = (const char*)c.kv.base;
-        auto rsrc = [&](size_t elems) {
-            return __builtin_amdgcn_make_buffer_rsrc((void*)(base + elems * 2), (short)0, PB, 0x00020000);
-        };
-        char* dst = ring + buf * BUF;
-        if constexpr (HD == 128) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.k_off(c.layer, p0, un.g)), (lds_void*)(dst + wave * 1024), 16, (int)ksrc, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.k_off(c.layer, p1, un.g)), (lds_void*)(dst + PB + wave * 1024), 16, (int)ksrc, 0, 0, 0);
-            // V fragments [dim tile][page]
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.v_off(c.layer, p0, un.g)), (lds_void*)(dst + 2 * PB + wave * 2048), 16, (int)vsrc, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.v_off(c.layer, p1, un.g)), (lds_void*)(dst + 2 * PB + wave * 2048 + 1024), 16, (int)vsrc, 0, 0, 0);
-        } else {
-            const int pg = wave >> 1, p = pg ? p1 : p0;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.k_off(c.layer, p, un.g)), (lds_void*)(dst + pg * PB + part * 1024), 16, (int)ksrc, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(c.kv.v_off(c.layer, p, un.g)), (lds_void*)(dst + 2 * PB + part * 2048 + pg * 1024), 16, (int)vsrc, 0, 0, 0);
-        }
-    };
+    w.va = base + lane * 16u;
 
     const float sc2 = c.scale * 1.4426950408889634f;
     float m, l;
     f32x16 o[DT];
-    // A chunk whose outputs are not finite is done again with the values' infinities
-    // and not-a-numbers apart: 0 times one is not 0 in a product, and rows that do
-    // not see such a value, or see it with two weights of opposite sign, must not
-    // take part in that.
-    for (int careful = 0; careful < 2; ++careful) {
-        m = -INFINITY;
-        l = 0.f;
+    tree_pass<HD, QLO, NW, false>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o);
+    // a segment whose outputs are not finite is done again, carefully
+    bool odd = false;
+    if (w.act) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-        const int nblk = un.blk1 - un.blk0, last = nblk - 1;
-        constexpr int PD = kBuffers - 1;
-        __syncthreads();  // (the ring is free, the ancestors are there)
-        wait_vm<0>();
-        int np0 = 0, np1 = 0;  // pages of the block to be loaded next
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < PD; ++i) {
-            const int blk = un.blk0 + min(i, last);
-            issue(page_at(2 * blk), page_at(2 * blk + 1), i);
-        }
-        np0 = page_at(2 * (un.blk0 + min(PD, last)));
-        np1 = page_at(2 * (un.blk0 + min(PD, last)) + 1);
-        auto block = [&](int BI, int i) __attribute__((always_inline)) {
-            const int blk = un.blk0 + i, t0 = blk * kBlock;
-            if (i + PD <= last) {
-                wait_vm<LOADS * (PD - 1), true>();
-                barrier_nofence();
-                issue(np0, np1, (BI + PD) % kBuffers);
-                const int nx = un.blk0 + min(i + PD + 1, last);
-                np0 = page_at(2 * nx);
-                np1 = page_at(2 * nx + 1);
-            } else {
-                if (last - i >= 1) wait_vm<LOADS, true>();
-                else wait_vm<0, true>();
-                barrier_nofence();
-            }
-            if (!act) return;
-            bf16x8 kf[DS], vf[DS];
-            const uint32_t at = (uint32_t)(BI * BUF), kb[4] = {ka[0] + at, ka[1] + at, ka[2] + at, ka[3] + at};
-            read_block<HD>(kf, vf, kb, va + at);
-            f32x16 s = f32x16{};
-#pragma unroll
-            for (int d = 0; d < DS; ++d) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], qf[d], s, 0, 0, 0);
-                if constexpr (QLO) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], ql[d], s, 0, 0, 0);
-            }
-            // lane: tokens t0 + 8 H + e (e < 8) and t0 + 16 + 8 H + e of its row
-            uint32_t see = ~0u;
-            const bool all = t0 + kBlock <= us.prefix && in_pool(page_at(2 * blk)) && in_pool(page_at(2 * blk + 1));
-            if (!all) {
-                see = (in_pool(page_at(2 * blk)) ? 0xffffu : 0u) | (in_pool(page_at(2 * blk + 1)) ? 0xffff0000u : 0u);
-                if (t0 + kBlock > us.prefix) see &= tree_bits(anc[j], t0, us.prefix);
-                see >>= 8 * H;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = (see >> (e < 8 ? e : e + 8)) & 1 ? s[e] : -INFINITY;
-            }
-            float bm = fmaxf(s[0], s[1]);
-#pragma unroll
-            for (int e = 2; e < 16; ++e) bm = fmaxf(bm, s[e]);
-            const float mn = fmaxf(m, half_max(bm));
-            const bool live = mn != -INFINITY;
-            const float ms = live ? mn * sc2 : 0.f;
-            const float alpha = live ? __builtin_amdgcn_exp2f((m - mn) * sc2) : 1.f;
-            float rs = 0.f;
-            bf16x8 ph[2], plo[2];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float pe = __builtin_amdgcn_exp2f(fmaf(s[e], sc2, -ms));
-                rs += pe;
-                ph[e >> 3][e & 7] = (__bf16)pe;
-                plo[e >> 3][e & 7] = (__bf16)(pe - (float)ph[e >> 3][e & 7]);
-            }
-            l = fmaf(l, alpha, rs);
-            m = mn;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= alpha;
-            }
-            wait_v(vf);
-            if (careful) {
-                bf16x8 z[2];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)((see >> (e < 8 ? e : e + 8)) & 1 ? 1.f : 0.f);
-                if (all) z[0] = z[1] = bf16x8{1, 1, 1, 1, 1, 1, 1, 1};
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    f32x16 up = f32x16{}, down = f32x16{};
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        bf16x8 fin, fu, fd;
-                        split_odd(vf[2 * d + t], fin, fu, fd);
-                        vf[2 * d + t] = fin;
-                        up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fu, z[t], up, 0, 0, 0);
-                        down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd, z[t], down, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        o[d][e] += (up[e] > 0.f ? INFINITY : 0.f) + (down[e] > 0.f ? -INFINITY : 0.f);
-                }
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], ph[t], o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], plo[t], o[d], 0, 0, 0);
-                }
-        };
-        for (int i0 = 0; i0 < nblk; i0 += kBuffers) {
-            block(0, i0);
-            if (i0 + 1 < nblk) block(1, i0 + 1);
-            if (i0 + 2 < nblk) block(2, i0 + 2);
-        }
-        wait_vm<0>();
-        l = half_sum(l);
-        if (careful) break;
-        bool odd = false;
-        if (act) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[d][e]) < INFINITY);
-        }
-        if (!__syncthreads_or(odd)) break;
+            for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[d][e]) < INFINITY);
     }
+    if (__syncthreads_or(odd)) tree_pass<HD, QLO, NW, true>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o);
     if (!ok) return;
     // lane: dims 32 d + 8 (e / 4) + 4 H + e % 4 of its row
-    if (un.chunks == 1) {
+    if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const size_t e0 = (size_t)(us.s0 + j) * c.os + (size_t)(un.g * G + hh) * HD + 4 * H;
         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -559,7 +610,7 @@ __device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl,
             }
         return;
     }
-    const size_t pr = un.row0 + ((size_t)un.chunk * c.kv.hkv + un.g) * R + row;
+    const size_t pr = (size_t)slot * pl.prows + lrow;
     if (H == 0) pl.ml[pr] = float2{m == -INFINITY ? -INFINITY : m * sc2, l};
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -569,59 +620,88 @@ __device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl,
                 f32x4{o[d][4 * q4], o[d][4 * q4 + 1], o[d][4 * q4 + 2], o[d][4 * q4 + 3]};
 }
 
-template <int HD, bool QLO>
-__global__ __launch_bounds__(256, kResident) void k_tree_mfma(TreeCall c, TreePlan pl) {
-    __shared__ TreeLds<HD> lds;
-    tree_mfma<HD, QLO>(c, pl, lds);
+template <int HD, bool QLO, int NW>
+__device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl, TreeLds<HD, NW>& lds) {
+    // neighbours in the line, which share users and heads, on one die
+    const int id = (blockIdx.x & 7) * (pl.wgs / 8) + (blockIdx.x >> 3);
+    const int64_t total = tree_total<NW>(c, lds.scan), per = max((total + pl.wgs - 1) / pl.wgs, (int64_t)1);
+    if (id == 0 && threadIdx.x == 0) *pl.per = per;
+    int64_t pos = id * per;
+    const int64_t first = pos, end = min(total, pos + per);
+    while (pos < end) {
+        const TreeSpan sp = tree_find<NW>(c, pos, lds.scan);
+        int unit = (int)((pos - sp.base) / sp.nb), off = (int)((pos - sp.base) - (int64_t)unit * sp.nb);
+        unit = __builtin_amdgcn_readfirstlane(unit);
+        off = __builtin_amdgcn_readfirstlane(off);
+        if (unit == 0 && off == 0 && threadIdx.x == 0) pl.base[sp.b] = sp.base;
+        TreeUser us = tree_user(c, sp.b);
+        us = TreeUser{__builtin_amdgcn_readfirstlane(us.s0), __builtin_amdgcn_readfirstlane(us.n),
+                      __builtin_amdgcn_readfirstlane(us.prefix), __builtin_amdgcn_readfirstlane(us.end)};
+        const int groups = sp.units / c.kv.hkv;
+        bool known = false;  // the user's ancestors are in LDS
+        for (; unit < sp.units && pos < end; ++unit, off = 0) {
+            const int len = (int)min((int64_t)(sp.nb - off), end - pos);
+            const TreeSeg un{sp.b, unit / groups, unit % groups, off, off + len};
+            if (!known && un.blk1 * kBlock > us.prefix) {
+                __syncthreads();  // (nobody reads the ones before)
+                tree_ancestors<64 * NW>(c, us, lds.anc, lds.ptr);
+                known = true;
+            }
+            tree_segment<HD, QLO, NW>(c, pl, lds, un, us, len == sp.nb, 2 * id + (pos == first ? 0 : 1));
+            pos += len;
+        }
+    }
 }
 
-// Merges the chunks of a user's rows in chunk order; HD / 4 lanes a row.
-template <int HD> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c, TreePlan pl) {
-    constexpr int LANES = HD / 4, ROWS = 256 / LANES;
+template <int HD, bool QLO, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_tree_mfma(TreeCall c, TreePlan pl) {
+    __shared__ TreeLds<HD, NW> lds;
+    tree_mfma<HD, QLO, NW>(c, pl, lds);
+}
+
+// Merges the segments of units that lie in several workgroups' parts, in their order.
+// HD / 4 lanes take a row's segments, eight at a time; SPLIT such groups share a row's
+// segments where there are few rows.
+template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c, TreePlan pl, int wrows) {
+    constexpr int LANES = HD / 4, GROUPS = 256 / LANES, ROWS = GROUPS / SPLIT;
+    __shared__ float2 sml[GROUPS];
+    __shared__ f32x4 spart[SPLIT > 1 ? GROUPS : 1][LANES];
     const int b = blockIdx.y;
     const TreeUser us = tree_user(c, b);
-    const int rid = blockIdx.x * ROWS + threadIdx.x / LANES, ln = threadIdx.x % LANES;
-    if (us.n == 0 || rid >= us.n * c.hq) return;
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const size_t e = (size_t)(us.s0 + rid / c.hq) * c.os + (size_t)(rid % c.hq) * HD + 4 * ln;
-    if (us.end == 0) {  // no position has a page: no unit either
-        *(bf16x4*)((bf16_t*)c.out + e) = bf16x4{};
-        if (c.out_lo) *(bf16x4*)((bf16_t*)c.out_lo + e) = bf16x4{};
-        return;
-    }
-    const int2 tb = pl.table[b];
-    if (tb.x <= 1) return;
-    const int G = c.hq / c.kv.hkv, R = us.n * G, h = rid % c.hq, row = rid / c.hq * G + h % G;
+    const int grp = threadIdx.x / LANES, ln = threadIdx.x % LANES, part = grp % SPLIT;
+    const int rid = blockIdx.x * ROWS + grp / SPLIT;
+    const bool on = us.n > 0 && rid < us.n * c.hq;
+    if (SPLIT == 1 && !on) return;
+    if (blockIdx.x * ROWS >= us.n * c.hq) return;
+    const int G = c.hq / c.kv.hkv, h = on ? rid % c.hq : 0, j = on ? rid / c.hq : 0, row = j * G + h % G;
+    const int nb = (us.end + kBlock - 1) / kBlock, groups = (us.n * G + wrows - 1) / wrows;
+    const int64_t per = *pl.per, u0 = pl.base[b] + ((int64_t)(h / G) * groups + row / wrows) * nb;
+    const int w0 = (int)(u0 / per), n = (int)((u0 + nb - 1) / per) - w0 + 1;
+    const bool mine = on && n > 1;
     float M = -INFINITY, L = 0.f;
     f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < tb.x; k0 += 8) {
+    for (int k0 = part; mine && k0 < n; k0 += 8 * SPLIT) {
         float2 v[8];
         f32x4 p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const size_t pr = tb.y + ((size_t)min(k0 + i, tb.x - 1) * c.kv.hkv + h / G) * R + row;
+            const int k = min(k0 + i * SPLIT, n - 1), w = w0 + k;
+            // (a workgroup's first segment, or its last)
+            const size_t pr = (size_t)(2 * w + (u0 > w * per)) * pl.prows + row % wrows;
             v[i] = pl.ml[pr];
             p[i] = *(const f32x4*)(pl.part + pr * HD + 4 * ln);
-            if (k0 + i >= tb.x) v[i].x = -INFINITY;
+            if (k0 + i * SPLIT >= n) v[i] = float2{-INFINITY, 0.f};
         }
         float mg = M;
 #pragma unroll
         for (int i = 0; i < 8; ++i) mg = fmaxf(mg, v[i].x);
-        if (mg == -INFINITY) {
-            // nothing seen so far -- or scores that are not numbers, which show in the sums
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k0 + i < tb.x) L += v[i].y;
-            continue;
-        }
         const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mg);
         L *= f0;
         a *= f0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (k0 + i >= tb.x) continue;
             if (v[i].x == -INFINITY) {
-                L += v[i].y;
+                L += v[i].y;  // 0, or not a number
                 continue;
             }
             const float f = __builtin_amdgcn_exp2f(v[i].x - mg);
@@ -630,7 +710,29 @@ template <int HD> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c
         }
         M = mg;
     }
+    if constexpr (SPLIT > 1) {
+        if (ln == 0) sml[grp] = float2{M, L};
+        spart[grp][ln] = a;
+        __syncthreads();
+        if (part != 0 || !mine) return;
+        float mg = M;
+#pragma unroll
+        for (int i = 1; i < SPLIT; ++i) mg = fmaxf(mg, sml[grp + i].x);
+        const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mg);
+        L *= f0;
+        a *= f0;
+#pragma unroll
+        for (int i = 1; i < SPLIT; ++i) {
+            const float2 v = sml[grp + i];
+            const float f = v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(v.x - mg);
+            L += v.y * f;
+            if (v.x != -INFINITY) a += spart[grp + i][ln] * f;
+        }
+    }
+    if (!mine) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const size_t e = (size_t)(us.s0 + j) * c.os + (size_t)h * HD + 4 * ln;
     bf16x4 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -667,36 +769,35 @@ __global__ __launch_bounds__(64) void k_tree_walk(BatchView bv, const int32_t* t
     path[b] = taken;
 }
 
-// The plan's sizes: units times row groups aimed at, and the workspace it takes.
+// The parts of the workspace for so many workgroups.
 struct TreeSizes {
-    int cap, groups, units, rows;  // rows: partial rows
-    size_t bytes;
+    int prows;
+    size_t head, ml, bytes;
 };
-TreeSizes tree_sizes(const TreeCall& c, int cap) {
+TreeSizes tree_sizes(const TreeCall& c, int nw, int wgs) {
     TreeSizes z;
-    const int G = c.hq / c.kv.hkv;
-    z.cap = cap;
-    z.groups = (c.max_slots * G + kRows - 1) / kRows;
-    const int64_t least = (int64_t)c.n_users * c.kv.hkv;  // one unit a user and head
-    z.units = (int)std::min<int64_t>(cap + least, INT32_MAX);
-    // a unit has one row group's rows for each of its row groups, at most
-    const int64_t rows = (cap + least * z.groups) * std::min(kRows, c.max_slots * G);
-    z.rows = (int)std::min<int64_t>(rows, INT32_MAX);
-    z.bytes = ((size_t)c.n_users * 8 + 255) / 256 * 256 + ((size_t)rows * 8 + 255) / 256 * 256 + (size_t)rows * c.kv.hd * 4;
+    z.prows = std::min(32 * nw, c.max_slots * (c.hq / c.kv.hkv));
+    z.head = ((size_t)c.n_users * 8 + 8 + 255) / 256 * 256;
+    z.ml = ((size_t)2 * wgs * z.prows * 8 + 255) / 256 * 256;
+    z.bytes = z.head + z.ml + (size_t)2 * wgs * z.prows * c.kv.hd * 4;
     return z;
 }
 
-}  // namespace
+// Users of more than 128 rows a KV head take workgroups of eight waves.
+int tree_waves(const TreeCall& c) { return c.max_slots * (c.hq / c.kv.hkv) > 128 ? 8 : 4; }
+// Workgroups that are resident at once.
+int tree_wgs(int nw) { return cu_count() / 8 * 8 * (8 / nw); }
 
-// Workgroups that are resident at once; fewer where the workspace is smaller.
-constexpr int kTreeCap = 256 * kResident;
+}  // namespace
 
 size_t tree_workspace(const TreeCall& c) {
     if (c.kv.esize != 2) return 256;
-    return tree_sizes(c, kTreeCap).bytes;
+    // (host only: 256 CUs)
+    return tree_sizes(c, tree_waves(c), 256 * (8 / tree_waves(c))).bytes;
 }
-
-size_t tree_workspace_least(const TreeCall& c) { return c.kv.esize == 2 ? tree_sizes(c, 1).bytes : 256; }
+size_t tree_workspace_least(const TreeCall& c) {
+    return c.kv.esize == 2 ? tree_sizes(c, tree_waves(c), 8).bytes : 256;
+}
 
 void launch_tree_walk(const BatchView& bv, const int32_t* target, int32_t* result, int bmax, uint64_t* path,
                       hipStream_t s) {
@@ -704,36 +805,37 @@ void launch_tree_walk(const BatchView& bv, const int32_t* target, int32_t* resul
 }
 
 // Whether a launch of this shape is possible.
-bool tree_fits(const TreeCall& c) {
-    const TreeSizes z = tree_sizes(c, kTreeCap);
-    return (int64_t)z.units * z.groups <= (1 << 23) && z.rows < INT32_MAX && (int64_t)c.max_slots * c.hq <= (1 << 24);
-}
+bool tree_fits(const TreeCall& c) { return (int64_t)c.max_slots * c.hq <= (1 << 24); }
 
-template <int HD> static void launch_tree_mfma(const TreeCall& c, hipStream_t s) {
-    int cap = kTreeCap;
-    while (cap > 1 && tree_sizes(c, cap).bytes > c.ws_bytes) cap /= 2;
-    const TreeSizes z = tree_sizes(c, cap);
+template <int HD, int NW> static void launch_tree_mfma(const TreeCall& c, hipStream_t s) {
+    int wgs = std::min(tree_wgs(NW), 256 * (8 / NW));
+    while (wgs > 8 && tree_sizes(c, NW, wgs).bytes > c.ws_bytes) wgs -= 8;
+    const TreeSizes z = tree_sizes(c, NW, wgs);
     TreePlan pl;
-    pl.cap = cap;
-    pl.groups = z.groups;
-    pl.units = z.units;
+    pl.wgs = wgs;
+    pl.prows = z.prows;
     char* w = (char*)c.ws;
-    pl.table = (int2*)w;
-    w += ((size_t)c.n_users * 8 + 255) / 256 * 256;
-    pl.ml = (float2*)w;
-    w += ((size_t)z.rows * 8 + 255) / 256 * 256;
-    pl.part = (float*)w;
-    const dim3 grid((z.units + 7) / 8 * 8 * z.groups);
-    if (c.q_lo) hipLaunchKernelGGL((k_tree_mfma<HD, true>), grid, dim3(256), 0, s, c, pl);
-    else hipLaunchKernelGGL((k_tree_mfma<HD, false>), grid, dim3(256), 0, s, c, pl);
-    constexpr int ROWS = 256 / (HD / 4);
-    hipLaunchKernelGGL(k_tree_merge<HD>, dim3((c.max_slots * c.hq + ROWS - 1) / ROWS, c.n_users), dim3(256), 0, s, c, pl);
+    pl.per = (int64_t*)w;
+    pl.base = pl.per + 1;
+    pl.ml = (float2*)(w + z.head);
+    pl.part = (float*)(w + z.head + z.ml);
+    if (c.q_lo) hipLaunchKernelGGL((k_tree_mfma<HD, true, NW>), dim3(wgs), dim3(64 * NW), 0, s, c, pl);
+    else hipLaunchKernelGGL((k_tree_mfma<HD, false, NW>), dim3(wgs), dim3(64 * NW), 0, s, c, pl);
+    constexpr int GROUPS = 256 / (HD / 4);
+    // few rows: a workgroup each
+    if ((int64_t)c.n_slots * c.hq <= 512) {
+        hipLaunchKernelGGL((k_tree_merge<HD, GROUPS>), dim3(c.max_slots * c.hq, c.n_users), dim3(256), 0, s, c, pl, 32 * NW);
+    } else {
+        hipLaunchKernelGGL((k_tree_merge<HD, 1>), dim3((c.max_slots * c.hq + GROUPS - 1) / GROUPS, c.n_users), dim3(256), 0, s,
+                           c, pl, 32 * NW);
+    }
 }
 
 void launch_tree_attention(const TreeCall& c, hipStream_t s) {
     if (c.kv.esize == 2) {
-        if (c.kv.hd == 128) launch_tree_mfma<128>(c, s);
-        else launch_tree_mfma<64>(c, s);
+        const bool eight = tree_waves(c) == 8;
+        if (c.kv.hd == 128) eight ? launch_tree_mfma<128, 8>(c, s) : launch_tree_mfma<128, 4>(c, s);
+        else eight ? launch_tree_mfma<64, 8>(c, s) : launch_tree_mfma<64, 4>(c, s);
         return;
     }
     hipLaunchKernelGGL(k_tree_rows<float>, dim3(c.hq, c.max_slots, c.n_users), dim3(256), 0, s, c);

@@ -273,16 +273,21 @@ def test_forked_users(model):
         t.v.accept(0, 4)
         return lg
 
+    # (where a user's context is split, and so the last bits, goes by its place in the
+    # batch: equal users are as near each other as to the oracle, others are not)
+    tol = TOL[t.m.dtype]
+    same = lambda a, b: logit_rel_err(a, b).max() < tol  # noqa: E731
+    other = lambda a, b: logit_rel_err(a, b).max() > 10 * tol  # noqa: E731
     lg = run()
-    assert np.array_equal(lg[:9], lg[15:24])
-    assert not np.array_equal(lg[9:15], lg[24:])  # a shorter context
+    assert same(lg[:9], lg[15:24])
+    assert other(lg[9:15], lg[24:])  # a shorter context
     # what the copy's owner does is not seen by the other
     z = torch.zeros((77, t.m.n_kv_heads, t.m.head_dim), dtype=torch.float32 if model == "tiny" else torch.int16, device="cuda")
     for l in range(t.m.n_layers):
         t.v.write_kv(2, l, 0, z, z)
     torch.cuda.synchronize()
     again = run()
-    assert np.array_equal(again[:15], lg[:15]) and not np.array_equal(again[15:24], lg[15:24])
+    assert np.array_equal(again[:15], lg[:15]) and other(again[15:24], lg[15:24])
     # forked onto a user with pages of its own, and the pages given back
     t.v.fork_user(3, 0, 40, 5)
     assert len(t.v.user_pages(3)) == 3
@@ -290,7 +295,7 @@ def test_forked_users(model):
     assert len(t.v.user_pages(3)) == 0 and t.v.user_state(3) == (0, 5)
     t.v.fork_user(3, 1, 300, int(t.roots[1]))
     again = run()
-    assert np.array_equal(again[9:15], again[24:])
+    assert same(again[9:15], again[24:])
     for u in range(4):
         sv.sd_user_release(t.v.ctx, u)
     t.v.reset_user(0, min(16 * t.v.cfg.n_pages, t.v.cfg.max_ctx - 2), 0)
