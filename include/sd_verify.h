@@ -652,8 +652,8 @@ typedef struct sd_tree {
  * SD_EINVAL: an inconsistent pool or tree, n_q_heads no multiple of the pool's
  * n_kv_heads; SD_ENOTIMPL: a head_dim the kernels do not cover; SD_ELIMIT:
  * max_slots or n_users beyond the limits above, more than 2^20 slots or 128
- * query heads a KV head, a launch of more than 2^23 workgroups, or the pool's
- * limits. */
+ * query heads a KV head, 2^31 blocks (32 tokens of one KV head for up to 128 or
+ * 256 of its query rows) of contexts as long as max_pages, or the pool's limits. */
 sd_status sd_tree_query_size(const sd_kv_pool* pool, const sd_tree* tree, int32_t n_q_heads,
                              uint64_t* workspace_bytes);
 

@@ -141,8 +141,8 @@ constexpr int kBlock = 32;   // tokens a block
 struct TreePlan {
     int wgs;        // workgroups
     int prows;      // rows of a partial slot
-    int64_t* per;   // blocks a workgroup, as the kernel found it
-    int64_t* base;  // [n_users] where a user's first unit begins
+    int* per;       // blocks a workgroup, as the kernel found it
+    int* base;      // [n_users] where a user's first unit begins
     float* part;    // [2 wgs][prows][HD] outputs of segments, not yet divided
     float2* ml;     // [2 wgs][prows] their maxima (log2 domain) and sums
 };
@@ -150,70 +150,70 @@ struct TreePlan {
 // A user in the line: its units (KV head by KV head, row group by row group) of nb
 // blocks each begin at base.
 struct TreeSpan {
-    int b, nb, units;
-    int64_t base;
+    int b, nb, units, base;
 };
 struct TreeScan {
-    int64_t sum[8];
+    int sum[8];
     TreeSpan found;
 };
-template <int ROWS> __device__ __forceinline__ int64_t tree_weight(const TreeCall& c, int b, int* nb, int* units) {
+template <int ROWS> __device__ __forceinline__ int tree_weight(const TreeCall& c, int b, int* nb, int* units) {
     *nb = *units = 0;
     if (b >= c.n_users) return 0;
     const TreeUser us = tree_user(c, b);
     if (us.n <= 0) return 0;
     *nb = (us.end + kBlock - 1) / kBlock;
     *units = (us.n * (c.hq / c.kv.hkv) + ROWS - 1) / ROWS * c.kv.hkv;
-    return (int64_t)*nb * *units;
+    return *nb * *units;
 }
 
-// The length of the line, and the user at a position of it.  Every workgroup works
-// them out from the users' lengths (a launch less than a plan made before).
-template <int NW> __device__ __forceinline__ int64_t tree_total(const TreeCall& c, TreeScan& sc) {
-    const int tid = threadIdx.x, wave = tid >> 6;
-    int nb, units;
-    int64_t t = 0;
-    for (int b = tid; b < c.n_users; b += 64 * NW) t += tree_weight<32 * NW>(c, b, &nb, &units);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
-    if ((tid & 63) == 0) sc.sum[wave] = t;
-    __syncthreads();
-    t = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) t += sc.sum[w];
-    __syncthreads();
-    return t;
-}
-template <int NW> __device__ __forceinline__ TreeSpan tree_find(const TreeCall& c, int64_t pos, TreeScan& sc) {
+// The users in the line, as every workgroup finds them from their lengths (a launch
+// less than a plan made before), as many at a time as it has threads: a thread's
+// user, and the blocks up to its end.
+struct TreeUsers {
+    int b0 = -1, nb = 0, units = 0, own = 0, upto = 0;
+    int before = 0, all = 0;  // before, all: the blocks up to user b0, and up to the last here
+};
+template <int NW> __device__ __forceinline__ void tree_scan(const TreeCall& c, int b0, int before, TreeUsers& t, TreeScan& sc) {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    int64_t before = 0;
-    for (int b0 = 0; b0 < c.n_users; b0 += 64 * NW) {
-        int nb, units;
-        const int64_t own = tree_weight<32 * NW>(c, b0 + tid, &nb, &units);
-        int64_t t = own;
+    t.b0 = b0;
+    t.before = before;
+    t.own = tree_weight<32 * NW>(c, b0 + tid, &t.nb, &t.units);
+    t.upto = t.own;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t x = __shfl_up(t, o, 64);
-            if (lane >= o) t += x;
-        }
-        if (lane == 63) sc.sum[wave] = t;
-        __syncthreads();
-        int64_t all = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (w == wave) t += before + all;
-            all += sc.sum[w];
-        }
-        if (own > 0 && pos >= t - own && pos < t) sc.found = TreeSpan{b0 + tid, nb, units, t - own};
-        before += all;
-        __syncthreads();
-        if (pos < before) break;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(t.upto, o, 64);
+        if (lane >= o) t.upto += x;
     }
+    if (lane == 63) sc.sum[wave] = t.upto;
+    __syncthreads();
+    t.all = before;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w == wave) t.upto += t.all;
+        t.all += sc.sum[w];
+    }
+    __syncthreads();
+}
+// The length of the line.
+template <int NW> __device__ __forceinline__ int tree_total(const TreeCall& c, TreeUsers& t, TreeScan& sc) {
+    int all = 0;
+    for (int b0 = 0; b0 < c.n_users; b0 += 64 * NW) {
+        tree_scan<NW>(c, b0, all, t, sc);
+        all = t.all;
+    }
+    return all;
+}
+// The user at a position of it.
+template <int NW> __device__ __forceinline__ TreeSpan tree_find(const TreeCall& c, int pos, TreeUsers& t, TreeScan& sc) {
+    if (pos < t.before) tree_scan<NW>(c, 0, 0, t, sc);
+    while (pos >= t.all) tree_scan<NW>(c, t.b0 + 64 * NW, t.all, t, sc);
+    if (t.own > 0 && pos >= t.upto - t.own && pos < t.upto)
+        sc.found = TreeSpan{t.b0 + (int)threadIdx.x, t.nb, t.units, t.upto - t.own};
+    __syncthreads();
     // (the same in every lane: kept in scalar registers)
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     TreeSpan f = sc.found;
-    f = TreeSpan{same(f.b), same(f.nb), same(f.units),
-                 (int64_t)((uint64_t)(uint32_t)same((int)f.base) | (uint64_t)(uint32_t)same((int)(f.base >> 32)) << 32)};
+    f = TreeSpan{same(f.b), same(f.nb), same(f.units), same(f.base)};
     __syncthreads();
     return f;
 }
@@ -344,7 +344,7 @@ __device__ __forceinline__ bf16x8 where_odd(bf16x8 v, uint32_t inf) {
 template <int HD, int NW> struct TreeLds {
     static constexpr int PB = kPageTokens * HD * 2;  // bytes of a page's K or V block
     static constexpr int BUF = 4 * PB;               // two pages of K, two of V
-    static constexpr int N = NW == 8 ? 6 : 3;        // buffers
+    static constexpr int N = NW == 8 ? 6 : 4;        // buffers
     __attribute__((aligned(1024))) char ring[N * BUF];
     uint32_t anc[kSlots][kMaskWords + 1];
     int ptr[kSlots];
@@ -363,6 +363,8 @@ template <int HD, bool QLO> struct TreeWave {
     uint32_t ksrc, vsrc;     // its gather sources within a page's K and V blocks
     const uint32_t* anc;     // its row's ancestors
     bool act;                // the wave has rows
+    // blocks are taken tw at a time, each by the waves of one token group (tg)
+    int tw, tg;
 };
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -370,14 +372,13 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // One pass over a segment.  CAREFUL: the values' infinities and not-a-numbers are kept
 // apart: 0 times one is not 0 in a product, and rows that do not see such a value, or
 // see it with two weights of opposite sign, must not take part in that.
-template <int HD, bool QLO, int NW, bool CAREFUL>
+template <int HD, bool QLO, int NW, bool CAREFUL, class Q, class F>
 __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, int prefix, const TreeWave<HD, QLO>& w,
                                           char* ring, int wave, float sc2, float& m, float& l,
-                                          f32x16 (&o)[HD / 32]) {
+                                          f32x16 (&o)[HD / 32], Q queries, F meanwhile) {
     constexpr int DS = HD / 16, DT = HD / 32;
     constexpr int PB = TreeLds<HD, NW>::PB, BUF = TreeLds<HD, NW>::BUF, N = TreeLds<HD, NW>::N;
     constexpr int LOADS = BUF / 1024 / NW;  // 1 KB loads a wave and block
-    constexpr int PD = N - 1;               // blocks in flight
     const int lane = threadIdx.x & 63, H = lane >> 5;
     const int last = un.blk1 - un.blk0 - 1;
     // K and V of the KV head in a page: page_bytes apart, V vo behind K
@@ -391,7 +392,18 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
     };
     int pg = pages(un.blk0), pg_next = pages(un.blk0 + 32);
     uint32_t there = 0;  // which pages of the last blocks issued exist, two bits a block
-    auto issue = [&](int i, int buf) __attribute__((always_inline)) {
+    int next = 0, next_buf = 0;  // the block to be loaded next, and into which buffer
+    auto issue = [&]() __attribute__((always_inline)) {
+        const int i = next++, buf = next_buf;
+        next_buf = buf + 1 == N ? 0 : buf + 1;
+        if (i > last) {
+            there <<= 2;
+            return;
+        }
+        if (i > 0 && (i & 31) == 0) {
+            pg = pg_next;
+            pg_next = pages(un.blk0 + i + 32);
+        }
         // (missing pages are read as page 0 and not attended to)
         const int p0 = __builtin_amdgcn_readlane(pg, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(pg, 2 * (i & 31) + 1);
         there = there << 2 | (p1 >= 0) << 1 | (p0 >= 0);
@@ -428,107 +440,108 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
     l = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-    __syncthreads();  // (the ring is free, the ancestors are there)
+    queries();
+    // (pages and queries are waited for here: a wait for them inside the loop would be
+    // one for every load in flight)
     wait_vm<0>();
-    for (int i = 0; i < PD; ++i) issue(min(i, last), i);
-    int buf = 0;  // of block i
-    for (int i = 0; i <= last; ++i, buf = buf + 1 == N ? 0 : buf + 1) {
-        const int t0 = (un.blk0 + i) * kBlock;
-        if (i + PD <= last) {
-            wait_vm<LOADS * (PD - 1), true>();
-            barrier_nofence();
-            if (((i + PD) & 31) == 0) {
-                pg = pg_next;
-                pg_next = pages(un.blk0 + i + PD + 32);
+    __syncthreads();  // (nobody reads the ring or the ancestors before)
+    constexpr int ST = 2;  // blocks a stage
+    for (int i = 0; i < N - ST; ++i) issue();
+    meanwhile();
+    int stage = 0;  // buffer of block i
+    for (int i = 0; i <= last; i += ST, stage = stage + ST >= N ? 0 : stage + ST) {
+        // Blocks i and i + 1 are waited for; those that follow may be in flight.  Then every
+        // wave is done with the two blocks before, whose buffers take the next.
+        if (N > 4 && min(last, i + N - ST - 1) - (i + ST - 1) >= 2) wait_vm<2 * LOADS, true>();
+        else wait_vm<0, true>();
+        barrier_nofence();
+#pragma unroll
+        for (int k = 0; k < ST; ++k) issue();
+        for (int k = w.tg; k < ST; k += w.tw) {
+            if (!w.act || i + k > last) break;
+            const int t0 = (un.blk0 + i + k) * kBlock, buf = stage + k;
+            bf16x8 kf[DS], vf[DS];
+            const uint32_t at = (uint32_t)(buf * BUF), kb[4] = {w.ka[0] + at, w.ka[1] + at, w.ka[2] + at, w.ka[3] + at};
+            read_k<HD>(kf, kb);
+            // (two sums: a product waits for the one before it in its own)
+            f32x16 s = f32x16{}, s2 = f32x16{};
+#pragma unroll
+            for (int d = 0; d < DS; d += QLO ? 1 : 2) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.qf[d], s, 0, 0, 0);
+                if constexpr (QLO) s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.ql[d], s2, 0, 0, 0);
+                else s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d + 1], w.qf[d + 1], s2, 0, 0, 0);
             }
-            issue(i + PD, buf == 0 ? N - 1 : buf - 1);
-        } else {
-            // the tail: blocks i .. last are the only ones in flight
-            if (PD > 4 && last - i >= 4) wait_vm<4 * LOADS, true>();
-            else if (PD > 3 && last - i == 3) wait_vm<3 * LOADS, true>();
-            else if (PD > 2 && last - i == 2) wait_vm<2 * LOADS, true>();
-            else if (last - i == 1) wait_vm<LOADS, true>();
-            else wait_vm<0, true>();
-            barrier_nofence();
-            there <<= 2;
-        }
-        if (!w.act) continue;
-        bf16x8 kf[DS], vf[DS];
-        const uint32_t at = (uint32_t)(buf * BUF), kb[4] = {w.ka[0] + at, w.ka[1] + at, w.ka[2] + at, w.ka[3] + at};
-        read_k<HD>(kf, kb);
-        f32x16 s = f32x16{};
+            s += s2;
+            read_v<HD>(vf, w.va + at, s);
+            // lane: tokens t0 + 8 H + e (e < 8) and t0 + 16 + 8 H + e of its row
+            const uint32_t both = there >> (2 * (N - 1 - k)) & 3;
+            uint32_t see = ~0u;
+            if (t0 + kBlock > prefix || both != 3) {
+                see = (both & 1 ? 0xffffu : 0u) | (both & 2 ? 0xffff0000u : 0u);
+                if (t0 + kBlock > prefix) see &= tree_bits(w.anc, t0, prefix);
+                see >>= 8 * H;
 #pragma unroll
-        for (int d = 0; d < DS; ++d) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.qf[d], s, 0, 0, 0);
-            if constexpr (QLO) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d], w.ql[d], s, 0, 0, 0);
-        }
-        read_v<HD>(vf, w.va + at, s);
-        // lane: tokens t0 + 8 H + e (e < 8) and t0 + 16 + 8 H + e of its row
-        const uint32_t both = there >> (2 * PD) & 3;
-        uint32_t see = ~0u;
-        if (t0 + kBlock > prefix || both != 3) {
-            see = (both & 1 ? 0xffffu : 0u) | (both & 2 ? 0xffff0000u : 0u);
-            if (t0 + kBlock > prefix) see &= tree_bits(w.anc, t0, prefix);
-            see >>= 8 * H;
+                for (int e = 0; e < 16; ++e) s[e] = (see >> (e < 8 ? e : e + 8)) & 1 ? s[e] : -INFINITY;
+            }
+            float bm = fmaxf(s[0], s[1]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = (see >> (e < 8 ? e : e + 8)) & 1 ? s[e] : -INFINITY;
-        }
-        float bm = fmaxf(s[0], s[1]);
+            for (int e = 2; e < 16; ++e) bm = fmaxf(bm, s[e]);
+            // The maximum that weights are relative to follows the rows' own only when
+            // one is 2^8 beyond it (rescaling the outputs costs as much as a product).
+            const float mn = fmaxf(m, half_max(bm));
+            if (__builtin_amdgcn_ballot_w64((mn - m) * sc2 > 8.f)) {
+                const float alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sc2);
 #pragma unroll
-        for (int e = 2; e < 16; ++e) bm = fmaxf(bm, s[e]);
-        const float mn = fmaxf(m, half_max(bm));
-        const bool live = mn != -INFINITY;
-        const float ms = live ? mn * sc2 : 0.f;
-        const float alpha = live ? __builtin_amdgcn_exp2f((m - mn) * sc2) : 1.f;
-        // the weights as two bf16 planes: hi rounded, lo what that left
-        float rs[2] = {0.f, 0.f};
-        uint32_t ph[8], pl[8];
+                for (int d = 0; d < DT; ++d) o[d] *= alpha;
+                l *= alpha;
+                m = mn;
+            }
+            const float ms = m == -INFINITY ? 0.f : m * sc2;
+            // the weights as two bf16 planes: hi rounded, lo what that left
+            float rs[2] = {0.f, 0.f};
+            uint32_t ph[8], pl[8];
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], sc2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], sc2, -ms));
-            rs[0] += p0;
-            rs[1] += p1;
-            const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
-            ph[e / 2] = hi;
-            pl[e / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(p0 - __uint_as_float(hi << 16)),
-                                                            (__bf16)(p1 - __uint_as_float(hi & 0xffff0000u))});
-        }
-        l = fmaf(l, alpha, rs[0] + rs[1]);
-        m = mn;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+            for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], sc2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], sc2, -ms));
+                rs[0] += p0;
+                rs[1] += p1;
+                const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
+                ph[e / 2] = hi;
+                pl[e / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(p0 - __uint_as_float(hi << 16)),
+                                                                (__bf16)(p1 - __uint_as_float(hi & 0xffff0000u))});
+            }
+            l += rs[0] + rs[1];
+            wait_v(vf);
+            if constexpr (CAREFUL) {
+                bf16x8 z[2];
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= alpha;
-        }
-        wait_v(vf);
-        if constexpr (CAREFUL) {
-            bf16x8 z[2];
+                for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)((see >> (e < 8 ? e : e + 8)) & 1 ? 1.f : 0.f);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)((see >> (e < 8 ? e : e + 8)) & 1 ? 1.f : 0.f);
+                for (int d = 0; d < DT; ++d) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
+                    for (int sign = 0; sign < 2; ++sign) {
+                        f32x16 hit = f32x16{};
 #pragma unroll
-                for (int sign = 0; sign < 2; ++sign) {
-                    f32x16 hit = f32x16{};
+                        for (int t = 0; t < 2; ++t)
+                            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_odd(vf[2 * d + t], sign ? 0xff80 : 0x7f80), z[t],
+                                                                          hit, 0, 0, 0);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_odd(vf[2 * d + t], sign ? 0xff80 : 0x7f80), z[t],
-                                                                      hit, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[d][e] += hit[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+                        for (int e = 0; e < 16; ++e) o[d][e] += hit[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+                    }
+                    vf[2 * d] = only_finite(vf[2 * d]);
+                    vf[2 * d + 1] = only_finite(vf[2 * d + 1]);
                 }
-                vf[2 * d] = only_finite(vf[2 * d]);
-                vf[2 * d + 1] = only_finite(vf[2 * d + 1]);
             }
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const bf16x8 hi = __builtin_bit_cast(bf16x8, uint4{ph[4 * t], ph[4 * t + 1], ph[4 * t + 2], ph[4 * t + 3]});
                 const bf16x8 lo = __builtin_bit_cast(bf16x8, uint4{pl[4 * t], pl[4 * t + 1], pl[4 * t + 2], pl[4 * t + 3]});
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], hi, o[d], 0, 0, 0);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], lo, o[d], 0, 0, 0);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], hi, o[d], 0, 0, 0);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], lo, o[d], 0, 0, 0);
             }
+        }
     }
     wait_vm<0>();
     l = half_sum(l);
@@ -536,26 +549,23 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
 
 template <int HD, bool QLO, int NW>
 __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& pl, TreeLds<HD, NW>& lds, const TreeSeg& un,
-                                             const TreeUser& us, bool whole, int slot) {
+                                             const TreeUser& us, bool learn, bool whole, int slot) {
     constexpr int DS = HD / 16, DT = HD / 32;  // k steps of S, dim tiles of O
     constexpr int PB = TreeLds<HD, NW>::PB, ROWS = 32 * NW;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int lr = lane & 31, H = lane >> 5;
     const int G = c.hq / c.kv.hkv, R = us.n * G;
-    const int lrow = wave * 32 + lr, row = un.rg * ROWS + lrow;
-    const bool ok = row < R;
+    // few rows: two token groups
+    const int tw = min(R - un.rg * ROWS, ROWS) <= ROWS / 2 ? 2 : 1;
+    const int tile = tw == 2 ? wave & (NW / 2 - 1) : wave;
+    const int lrow = tile * 32 + lr, row = un.rg * ROWS + lrow;
+    bool ok = row < R;
     const int j = ok ? row / G : 0, hh = ok ? row % G : 0;
     TreeWave<HD, QLO> w;
-    w.act = un.rg * ROWS + wave * 32 < R;
+    w.act = un.rg * ROWS + tile * 32 < R;
+    w.tw = tw;
+    w.tg = tw == 2 ? wave / (NW / 2) : 0;
     w.anc = lds.anc[j];
-    {
-        const size_t e = (size_t)(us.s0 + j) * c.qs + (size_t)(un.g * G + hh) * HD + 8 * H;
-#pragma unroll
-        for (int d = 0; d < DS; ++d) {
-            w.qf[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q + e + 16 * d) : bf16x8{};
-            if constexpr (QLO) w.ql[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q_lo + e + 16 * d) : bf16x8{};
-        }
-    }
     // A wave's loads of a block: head_dim 128: quarters of K of page 0, of page 1, of V of
     // page 0, of page 1; 64: halves of K and of V of one page (with eight waves: four of
     // them K, four V).  K rows lie in LDS as in the page, their 16-byte pieces exchanged
@@ -578,7 +588,20 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
     const float sc2 = c.scale * 1.4426950408889634f;
     float m, l;
     f32x16 o[DT];
-    tree_pass<HD, QLO, NW, false>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o);
+    auto queries = [&]() __attribute__((always_inline)) {
+        const size_t e = (size_t)(us.s0 + j) * c.qs + (size_t)(un.g * G + hh) * HD + 8 * H;
+#pragma unroll
+        for (int d = 0; d < DS; ++d) {
+            w.qf[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q + e + 16 * d) : bf16x8{};
+            if constexpr (QLO) w.ql[d] = ok ? *(const bf16x8*)((const bf16_t*)c.q_lo + e + 16 * d) : bf16x8{};
+        }
+    };
+    auto ancestors = [&]() __attribute__((always_inline)) {  // while the first blocks are on their way
+        if (!learn) return;
+        tree_ancestors<64 * NW>(c, us, lds.anc, lds.ptr);
+        __syncthreads();
+    };
+    tree_pass<HD, QLO, NW, false>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o, queries, ancestors);
     // a segment whose outputs are not finite is done again, carefully
     bool odd = false;
     if (w.act) {
@@ -587,7 +610,39 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
 #pragma unroll
             for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[d][e]) < INFINITY);
     }
-    if (__syncthreads_or(odd)) tree_pass<HD, QLO, NW, true>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o);
+    if (__syncthreads_or(odd)) tree_pass<HD, QLO, NW, true>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o, [] {}, [] {});
+    if (tw == 2) {
+        // the second token group's sums, through the ring: [tile][4 * dim tiles][lane]
+        f32x4* const sp = (f32x4*)lds.ring + tile * (4 * DT * 64);
+        float2* const sm = (float2*)((f32x4*)lds.ring + (NW / 2) * (4 * DT * 64)) + tile * 64;
+        __syncthreads();
+        if (w.tg == 1 && w.act) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    sp[(4 * d + q4) * 64 + lane] = f32x4{o[d][4 * q4], o[d][4 * q4 + 1], o[d][4 * q4 + 2], o[d][4 * q4 + 3]};
+            sm[lane] = float2{m, l};
+        }
+        __syncthreads();
+        if (w.tg == 0 && w.act) {
+            const float2 v = sm[lane];
+            const float mn = fmaxf(m, v.x);
+            const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sc2);
+            const float f1 = v.x == mn ? 1.f : __builtin_amdgcn_exp2f((v.x - mn) * sc2);
+            m = mn;
+            l = l * f0 + v.y * f1;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    const f32x4 p = sp[(4 * d + q4) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d][4 * q4 + e] = o[d][4 * q4 + e] * f0 + p[e] * f1;
+                }
+        }
+        ok &= w.tg == 0;
+    }
     if (!ok) return;
     // lane: dims 32 d + 8 (e / 4) + 4 H + e % 4 of its row
     if (whole) {
@@ -624,15 +679,16 @@ template <int HD, bool QLO, int NW>
 __device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl, TreeLds<HD, NW>& lds) {
     // neighbours in the line, which share users and heads, on one die
     const int id = (blockIdx.x & 7) * (pl.wgs / 8) + (blockIdx.x >> 3);
-    const int64_t total = tree_total<NW>(c, lds.scan), per = max((total + pl.wgs - 1) / pl.wgs, (int64_t)1);
+    TreeUsers users;
+    const int total = __builtin_amdgcn_readfirstlane(tree_total<NW>(c, users, lds.scan));
+    const int per = max((int)(((uint32_t)total + pl.wgs - 1) / (uint32_t)pl.wgs), 1);
     if (id == 0 && threadIdx.x == 0) *pl.per = per;
-    int64_t pos = id * per;
-    const int64_t first = pos, end = min(total, pos + per);
+    if (total <= id * (int64_t)per) return;
+    int pos = id * per;
+    const int first = pos, end = pos + min(total - pos, per);
     while (pos < end) {
-        const TreeSpan sp = tree_find<NW>(c, pos, lds.scan);
-        int unit = (int)((pos - sp.base) / sp.nb), off = (int)((pos - sp.base) - (int64_t)unit * sp.nb);
-        unit = __builtin_amdgcn_readfirstlane(unit);
-        off = __builtin_amdgcn_readfirstlane(off);
+        const TreeSpan sp = tree_find<NW>(c, pos, users, lds.scan);
+        int unit = (int)((uint32_t)(pos - sp.base) / (uint32_t)sp.nb), off = pos - sp.base - unit * sp.nb;
         if (unit == 0 && off == 0 && threadIdx.x == 0) pl.base[sp.b] = sp.base;
         TreeUser us = tree_user(c, sp.b);
         us = TreeUser{__builtin_amdgcn_readfirstlane(us.s0), __builtin_amdgcn_readfirstlane(us.n),
@@ -640,14 +696,11 @@ __device__ __forceinline__ void tree_mfma(const TreeCall& c, const TreePlan& pl,
         const int groups = sp.units / c.kv.hkv;
         bool known = false;  // the user's ancestors are in LDS
         for (; unit < sp.units && pos < end; ++unit, off = 0) {
-            const int len = (int)min((int64_t)(sp.nb - off), end - pos);
+            const int len = min(sp.nb - off, end - pos);
             const TreeSeg un{sp.b, unit / groups, unit % groups, off, off + len};
-            if (!known && un.blk1 * kBlock > us.prefix) {
-                __syncthreads();  // (nobody reads the ones before)
-                tree_ancestors<64 * NW>(c, us, lds.anc, lds.ptr);
-                known = true;
-            }
-            tree_segment<HD, QLO, NW>(c, pl, lds, un, us, len == sp.nb, 2 * id + (pos == first ? 0 : 1));
+            const bool tail = un.blk1 * kBlock > us.prefix;
+            tree_segment<HD, QLO, NW>(c, pl, lds, un, us, tail && !known, len == sp.nb, 2 * id + (pos == first ? 0 : 1));
+            known |= tail;
             pos += len;
         }
     }
@@ -660,8 +713,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_mfma(TreeCall c, TreePlan p
 }
 
 // Merges the segments of units that lie in several workgroups' parts, in their order.
-// HD / 4 lanes take a row's segments, eight at a time; SPLIT such groups share a row's
-// segments where there are few rows.
+// HD / 4 lanes take a row's segments, two at a time (a unit seldom lies in more than
+// three parts); where there are few rows SPLIT such groups share a row's, four at a time.
 template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c, TreePlan pl, int wrows) {
     constexpr int LANES = HD / 4, GROUPS = 256 / LANES, ROWS = GROUPS / SPLIT;
     __shared__ float2 sml[GROUPS];
@@ -675,16 +728,17 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
     if (blockIdx.x * ROWS >= us.n * c.hq) return;
     const int G = c.hq / c.kv.hkv, h = on ? rid % c.hq : 0, j = on ? rid / c.hq : 0, row = j * G + h % G;
     const int nb = (us.end + kBlock - 1) / kBlock, groups = (us.n * G + wrows - 1) / wrows;
-    const int64_t per = *pl.per, u0 = pl.base[b] + ((int64_t)(h / G) * groups + row / wrows) * nb;
-    const int w0 = (int)(u0 / per), n = (int)((u0 + nb - 1) / per) - w0 + 1;
+    const int per = *pl.per, u0 = pl.base[b] + ((h / G) * groups + row / wrows) * nb;
+    const int w0 = (int)((uint32_t)u0 / (uint32_t)per), n = (int)((uint32_t)(u0 + nb - 1) / (uint32_t)per) - w0 + 1;
     const bool mine = on && n > 1;
+    constexpr int CH = SPLIT > 1 ? 4 : 2;
     float M = -INFINITY, L = 0.f;
     f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = part; mine && k0 < n; k0 += 8 * SPLIT) {
-        float2 v[8];
-        f32x4 p[8];
+    for (int k0 = part; mine && k0 < n; k0 += CH * SPLIT) {
+        float2 v[CH];
+        f32x4 p[CH];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < CH; ++i) {
             const int k = min(k0 + i * SPLIT, n - 1), w = w0 + k;
             // (a workgroup's first segment, or its last)
             const size_t pr = (size_t)(2 * w + (u0 > w * per)) * pl.prows + row % wrows;
@@ -694,12 +748,12 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
         }
         float mg = M;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) mg = fmaxf(mg, v[i].x);
+        for (int i = 0; i < CH; ++i) mg = fmaxf(mg, v[i].x);
         const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mg);
         L *= f0;
         a *= f0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < CH; ++i) {
             if (v[i].x == -INFINITY) {
                 L += v[i].y;  // 0, or not a number
                 continue;
@@ -777,7 +831,7 @@ struct TreeSizes {
 TreeSizes tree_sizes(const TreeCall& c, int nw, int wgs) {
     TreeSizes z;
     z.prows = std::min(32 * nw, c.max_slots * (c.hq / c.kv.hkv));
-    z.head = ((size_t)c.n_users * 8 + 8 + 255) / 256 * 256;
+    z.head = ((size_t)c.n_users * 4 + 4 + 255) / 256 * 256;
     z.ml = ((size_t)2 * wgs * z.prows * 8 + 255) / 256 * 256;
     z.bytes = z.head + z.ml + (size_t)2 * wgs * z.prows * c.kv.hd * 4;
     return z;
@@ -805,7 +859,13 @@ void launch_tree_walk(const BatchView& bv, const int32_t* target, int32_t* resul
 }
 
 // Whether a launch of this shape is possible.
-bool tree_fits(const TreeCall& c) { return (int64_t)c.max_slots * c.hq <= (1 << 24); }
+bool tree_fits(const TreeCall& c) {
+    const int rows = 32 * tree_waves(c);
+    const int64_t units = (int64_t)c.kv.hkv * ((c.max_slots * (c.hq / c.kv.hkv) + rows - 1) / rows);
+    // (a block is counted in 31 bits)
+    return (int64_t)c.max_slots * c.hq <= (1 << 24) && c.n_users * units < (1ll << 31) &&
+           c.n_users * units * (((int64_t)c.max_pages + 1) / 2) < (1ll << 31);
+}
 
 template <int HD, int NW> static void launch_tree_mfma(const TreeCall& c, hipStream_t s) {
     int wgs = std::min(tree_wgs(NW), 256 * (8 / NW));
@@ -815,7 +875,7 @@ template <int HD, int NW> static void launch_tree_mfma(const TreeCall& c, hipStr
     pl.wgs = wgs;
     pl.prows = z.prows;
     char* w = (char*)c.ws;
-    pl.per = (int64_t*)w;
+    pl.per = (int*)w;
     pl.base = pl.per + 1;
     pl.ml = (float2*)(w + z.head);
     pl.part = (float*)(w + z.head + z.ml);
