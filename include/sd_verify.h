@@ -773,7 +773,7 @@ typedef struct sd_logit_rules {
  * Errors (nothing enqueued): SD_EINVAL (NULL or misaligned pointer, dtype,
  * stride, overlap, one array of a pair without the other; a table of ranges of
  * nothing needs no list), SD_ELIMIT (rows or
- * vocab beyond SD_FILTER_MAX_*, n_tokens or n_bias beyond 2^31 - 1), SD_EHIP.
+ * vocab beyond SD_FILTER_MAX_*, n_tokens or n_bias above 2^30 - 4096), SD_EHIP.
  */
 sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
                            const sd_logit_rules* rules, float* out, int64_t out_stride, sd_stream stream);

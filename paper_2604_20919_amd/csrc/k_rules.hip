@@ -4,10 +4,20 @@
 // in prompt or output:  s: z / r or z * r by z's sign;  c: z - (f c + p);  listed:
 // z + bias;  not allowed: -inf.
 //
-// A workgroup takes a chunk of the vocabulary and a few rows.  It counts the
-// chunk's tokens of a row's history in LDS (integers: the order does not matter),
-// keeps the counts while the next row has the same history, as the slots of a user
-// do, and adds the row's own drafts for that row alone.
+// What bounds it: the row read once and written once in 32 bits (6 bytes a token for
+// bfloat16 rows); history, biases and masks are a few percent of that, but every
+// workgroup of a row looks through the whole of its history and biases.  So a workgroup
+// takes kChunk tokens of up to kRowsMax rows: it counts the chunk's tokens of a history
+// in LDS (integers: the order does not matter), keeps the words while the next row has
+// the same history and biases, as the slots of a user do, and adds the row's own drafts
+// for that row alone.  The row's elements are loaded one row ahead, before the lists are
+// looked through.  Between short chunks (more workgroups a CU to hide the lists' loads)
+// and long ones (fewer looks through the lists), and between few and many rows, 416 bf16
+// rows of 155136 with histories, biases and masks (389 MB) took
+//     kChunk 2048, rows 2 / 4 / 8:  168 / 144 / 141 us;  229 such rows  73 / 69 / 70
+//     kChunk 4096, rows 2 / 4 / 8:  166 / 162 / 168 us   (an earlier form of the lists)
+// so 2048 and 4: 2.7 TB/s.  Of the 144 us the rows alone are 80 (4.8 TB/s, a copy's rate),
+// histories 17 to 22, masks 12 to 17, biases 22 to 31.
 #include <algorithm>
 
 #include "../../include/sd_verify.h"
@@ -17,27 +27,110 @@
 namespace sdv {
 namespace {
 
-constexpr int kChunk = 4096;         // tokens a workgroup
-constexpr int kRowsMax = 8;          // rows a workgroup
+constexpr int kChunk = 2048;         // tokens a workgroup
+constexpr int kRowsMax = 4;          // rows a workgroup
 constexpr int kBack = SD_TREE_MAX_SLOTS;  // rows below a row that its drafts may be in
-constexpr uint32_t kPrompt = 0x80000000u;  // count word: the token is in the prompt
+constexpr int kHeld = 2;             // biases a thread keeps in registers, the rest are read again
+// a token's word: in the prompt, with a bias, how often in the output
+constexpr uint32_t kPrompt = 0x80000000u, kBias = 0x40000000u, kCount = 0x3fffffffu;
 
 __device__ __forceinline__ float fin(const float* p, int t, float off) {
     const float v = p ? p[t] : off;
     return isfinite(v) ? v : off;
 }
 
-template <typename T, bool VEC>
+// A list's entries by the whole workgroup, kAhead loads in flight a thread.
+constexpr int kAhead = 8;
+template <class F> __device__ __forceinline__ void for_list(const int32_t* list, int begin, int end, F f) {
+    for (int i0 = begin + (int)threadIdx.x; i0 < end; i0 += 256 * kAhead) {
+        int k[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) k[u] = i0 + 256 * u < end ? list[i0 + 256 * u] : -1;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) f(i0 + 256 * u, k[u]);
+    }
+}
+
+// Four elements of a row as they lie in memory.
+template <typename T> struct Four;
+template <> struct Four<float> {
+    f32x4 v;
+    __device__ __forceinline__ void get(float (&o)[4]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = v[e];
+    }
+};
+template <> struct Four<bf16_t> {
+    uint2 v;
+    __device__ __forceinline__ void get(float (&o)[4]) const {
+        o[0] = __uint_as_float(v.x << 16);
+        o[1] = __uint_as_float(v.x & 0xffff0000u);
+        o[2] = __uint_as_float(v.y << 16);
+        o[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+};
+
+// What rules a row has.
+struct RowRules {
+    int nb, nf, ne, ob, oe;  // its history's begin, first output and end, its biases
+    float rep, pres, freq;
+    const uint32_t* mask;
+};
+__device__ __forceinline__ RowRules row_rules(const RulesCall& c, int t, int words) {
+    RowRules r{};
+    if (c.hist) {
+        r.nb = min(max(c.hist[3 * (size_t)t], 0), c.n_tokens);
+        r.nf = min(max(c.hist[3 * (size_t)t + 1], r.nb), c.n_tokens);
+        r.ne = min(max(c.hist[3 * (size_t)t + 2], r.nf), c.n_tokens);
+    }
+    if (c.bias) {
+        r.ob = min(max(c.bias[2 * (size_t)t], 0), c.n_bias);
+        r.oe = min(max(c.bias[2 * (size_t)t + 1], r.ob), c.n_bias);
+    }
+    r.rep = c.rep ? c.rep[t] : 1.f;
+    if (!(r.rep > 0.f && isfinite(r.rep))) r.rep = 1.f;
+    r.pres = fin(c.pres, t, 0.f);
+    r.freq = fin(c.freq, t, 0.f);
+    const int m = c.mask ? c.mask_row[t] : -1;
+    r.mask = m >= 0 && m < c.n_masks ? c.mask + (size_t)m * words : nullptr;
+    return r;
+}
+
+// VEC: four elements a load, rows of `out` apart from the logits, the next row's loads in
+// flight while one is written; otherwise one element a load, or in place, where only
+// what changes is read and written.
+template <typename T, bool VEC, bool PLACE>
 __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words) {
     extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
     __shared__ int par[kBack + kRowsMax], tokw[kBack + kRowsMax];
     __shared__ uint16_t own[kRowsMax][kBack + 1];  // a row's drafts in this chunk
     __shared__ int n_own[kRowsMax];
+    __shared__ RowRules rules[kRowsMax];
     uint32_t* const cnt = lds;            // [kChunk]
-    uint32_t* const bix = lds + kChunk;   // [kChunk] entry + 1 of the token's bias (with biases only)
+    // where a token's word says kBias: [kChunk] the bias's entry, [kChunk] its value
+    uint32_t* const bix = lds + kChunk;
+    float* const bval = (float*)(lds + 2 * kChunk);
     const int tid = threadIdx.x;
     const int k0 = blockIdx.x * kChunk, kn = min(kChunk, c.V - k0);
     const int r0 = blockIdx.y * rows, r1 = min(c.n_rows, r0 + rows);
+    constexpr int Q = kChunk / 1024;
+    Four<T> now[Q], next[Q];
+    uint32_t m[Q], mnext[Q];  // the mask's bits of the thread's elements
+    auto load = [&](int t, Four<T> (&q)[Q]) __attribute__((always_inline)) {
+        const T* z = (const T*)c.logits + (size_t)t * c.stride + k0;
+#pragma unroll
+        for (int u = 0; u < Q; ++u)
+            if (4 * tid + 1024 * u < kn) q[u] = *(const Four<T>*)(z + 4 * tid + 1024 * u);
+    };
+    auto load_mask = [&](const uint32_t* mask, uint32_t (&q)[Q]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < Q; ++u) {
+            const int k = 4 * tid + 1024 * u;
+            q[u] = mask && k < kn ? mask[(k0 + k) >> 5] >> ((k0 + k) & 31) : 0xfu;
+        }
+    };
+    if constexpr (VEC && !PLACE) load(r0, now);
+    if (tid < r1 - r0) rules[tid] = row_rules(c, r0 + tid, words);
     if (c.row_token) {
         const int w0 = r0 - kBack;
         for (int i = tid; i < kBack + r1 - r0; i += 256) {
@@ -65,92 +158,118 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
     } else if (tid < rows) {
         n_own[tid] = 0;
     }
+    __syncthreads();
+    if constexpr (VEC) load_mask(rules[0].mask, m);
+    // every entry of the row's biases whose token is in the chunk: those held, those beyond
+    auto for_biases = [&](int oe, int more, const int (&bk)[kHeld], const float (&bv)[kHeld], auto chunk_of, auto f) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (bk[u] >= 0) f(more - 256 * (kHeld - u) + tid, bk[u], bv[u]);
+        for (int i = more + tid; i < oe; i += 256) {
+            const int k = chunk_of(c.bias_token[i]);
+            if (k >= 0) f(i, k, c.bias_value[i]);
+        }
+    };
     int hb = -1, hf = -1, he = -1, bb = -1, be = -1;
     for (int t = r0; t < r1; ++t) {
-        int nb = 0, nf = 0, ne = 0, ob = 0, oe = 0;
-        if (c.hist) {
-            nb = min(max(c.hist[3 * (size_t)t], 0), c.n_tokens);
-            nf = min(max(c.hist[3 * (size_t)t + 1], nb), c.n_tokens);
-            ne = min(max(c.hist[3 * (size_t)t + 2], nf), c.n_tokens);
+        if (t + 1 < r1) {
+            if constexpr (VEC && !PLACE) load(t + 1, next);
+            if constexpr (VEC) load_mask(rules[t + 1 - r0].mask, mnext);
         }
-        if (c.bias) {
-            ob = min(max(c.bias[2 * (size_t)t], 0), c.n_bias);
-            oe = min(max(c.bias[2 * (size_t)t + 1], ob), c.n_bias);
-        }
-        __syncthreads();  // the previous row has been read
-        if (nb != hb || nf != hf || ne != he) {
-            for (int i = tid; i < kChunk; i += 256) cnt[i] = 0;
+        const RowRules r = rules[t - r0];
+        // the words: anew where history or biases are others, else as they are
+        if (r.nb != hb || r.nf != hf || r.ne != he || r.ob != bb || r.oe != be) {
+            // (the first biases in registers from here on)
+            int bk[kHeld];
+            float bv[kHeld];
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                const int i = r.ob + tid + 256 * u;
+                bk[u] = i < r.oe ? c.bias_token[i] - k0 : -1;
+                bv[u] = i < r.oe ? c.bias_value[i] : 0.f;
+                if (bk[u] >= kn) bk[u] = -1;
+            }
+            const int more = r.ob + 256 * kHeld;
+            __syncthreads();  // the previous row has been read
+            for (int i = 4 * tid; i < kChunk; i += 1024) *(uint4*)(cnt + i) = uint4{0, 0, 0, 0};
+            auto chunk_of = [&](int k) { return k >= k0 && k < k0 + kn ? k - k0 : -1; };
+            for_biases(r.oe, more, bk, bv, chunk_of, [&](int, int k, float) { bix[k] = 0; });
             __syncthreads();
-            for (int i = nb + tid; i < ne; i += 256) {
-                const int k = c.tokens[i] - k0;
-                if (k < 0 || k >= kn) continue;
-                if (i < nf) atomicOr(&cnt[k], kPrompt);
+            for_list(c.tokens, r.nb, r.ne, [&](int i, int k) {
+                k -= k0;
+                if (k < 0 || k >= kn) return;
+                if (i < r.nf) atomicOr(&cnt[k], kPrompt);
                 else atomicAdd(&cnt[k], 1u);
+            });
+            for_biases(r.oe, more, bk, bv, chunk_of, [&](int i, int k, float) {
+                atomicOr(&cnt[k], kBias);
+                atomicMax(&bix[k], (uint32_t)(i - r.ob));  // the last entry of a token
+            });
+            if (r.oe > r.ob) {
+                __syncthreads();
+                for_biases(r.oe, more, bk, bv, chunk_of, [&](int i, int k, float v) {
+                    if (bix[k] == (uint32_t)(i - r.ob)) bval[k] = v;
+                });
             }
-            hb = nb; hf = nf; he = ne;
-        }
-        if (c.bias && (ob != bb || oe != be)) {
-            for (int i = tid; i < kChunk; i += 256) bix[i] = 0;
+            hb = r.nb; hf = r.nf; he = r.ne;
+            bb = r.ob; be = r.oe;
             __syncthreads();
-            for (int i = ob + tid; i < oe; i += 256) {
-                const int k = c.bias_token[i] - k0;
-                if (k >= 0 && k < kn) atomicMax(&bix[k], (uint32_t)i + 1);  // the last entry of a token
-            }
-            bb = ob; be = oe;
         }
-        for (int i = tid; i < n_own[t - r0]; i += 256) atomicAdd(&cnt[own[t - r0][i]], 1u);
-        float rep = c.rep ? c.rep[t] : 1.f;
-        if (!(rep > 0.f && isfinite(rep))) rep = 1.f;
-        const float pres = fin(c.pres, t, 0.f), freq = fin(c.freq, t, 0.f);
-        const int mr = c.mask ? c.mask_row[t] : -1;
-        const uint32_t* mask = mr >= 0 && mr < c.n_masks ? c.mask + (size_t)mr * words : nullptr;
+        const int mine = n_own[t - r0];
+        if (mine) {
+            __syncthreads();
+            for (int i = tid; i < mine; i += 256) atomicAdd(&cnt[own[t - r0][i]], 1u);
+            __syncthreads();
+        }
         const T* z = (const T*)c.logits + (size_t)t * c.stride;
         float* o = c.out + (size_t)t * c.ostride;
-        const bool in_place = (const void*)z == (const void*)o;
-        __syncthreads();
-        auto rule = [&](int k, float v, uint32_t w, uint32_t bx, bool allowed) {
-            const uint32_t times = w & ~kPrompt;
-            if (w) v = v > 0.f ? v / rep : v * rep;
-            if (times) v -= freq * (float)times + pres;
-            if (bx) v += c.bias_value[bx - 1];
-            return allowed ? v : -INFINITY;
+        auto rule = [&](float v, uint32_t w, int k) {
+            const uint32_t times = w & kCount;
+            if (w & (kPrompt | kCount)) v = v > 0.f ? v / r.rep : v * r.rep;
+            if (times) v -= r.freq * (float)times + r.pres;
+            if (w & kBias) v += bval[k];
+            return v;
         };
-        if (VEC) {
-            for (int k = 4 * tid; k < kn; k += 1024) {
-                float v[4];
+        if constexpr (VEC) {
+#pragma unroll
+            for (int u = 0; u < Q; ++u) {
+                const int k = 4 * tid + 1024 * u;
+                if (k >= kn) break;
                 const uint4 w = *(const uint4*)(cnt + k);
-                uint4 bx = uint4{0, 0, 0, 0};
-                if (c.bias) bx = *(const uint4*)(bix + k);
-                const uint32_t m = mask ? mask[(k0 + k) >> 5] >> ((k0 + k) & 31) : 0xfu;
-                const bool touch = (w.x | w.y | w.z | w.w | bx.x | bx.y | bx.z | bx.w) || (~m & 0xf);
-                if (in_place && !touch) continue;
-                if constexpr (sizeof(T) == 2) {
-                    const uint2 u = *(const uint2*)(z + k0 + k);
-                    v[0] = bf16_to_f32(u.x & 0xffff); v[1] = bf16_to_f32(u.x >> 16);
-                    v[2] = bf16_to_f32(u.y & 0xffff); v[3] = bf16_to_f32(u.y >> 16);
-                } else {
-                    const float4 u = *(const float4*)(z + k0 + k);
-                    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+                if constexpr (PLACE) {
+                    if (!(w.x | w.y | w.z | w.w) && !(~m[u] & 0xf)) continue;
+                    now[u] = *(const Four<T>*)(z + k0 + k);
                 }
-                if (touch) {
-                    v[0] = rule(k, v[0], w.x, bx.x, m & 1);
-                    v[1] = rule(k + 1, v[1], w.y, bx.y, m & 2);
-                    v[2] = rule(k + 2, v[2], w.z, bx.z, m & 4);
-                    v[3] = rule(k + 3, v[3], w.w, bx.w, m & 8);
+                float v[4];
+                now[u].get(v);
+                if (w.x | w.y | w.z | w.w) {
+                    v[0] = rule(v[0], w.x, k);
+                    v[1] = rule(v[1], w.y, k + 1);
+                    v[2] = rule(v[2], w.z, k + 2);
+                    v[3] = rule(v[3], w.w, k + 3);
                 }
-                *(float4*)(o + k0 + k) = float4{v[0], v[1], v[2], v[3]};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = m[u] >> e & 1 ? v[e] : -INFINITY;
+                *(f32x4*)(o + k0 + k) = f32x4{v[0], v[1], v[2], v[3]};
+            }
+#pragma unroll
+            for (int u = 0; u < Q; ++u) {
+                if constexpr (!PLACE) now[u] = next[u];
+                m[u] = mnext[u];
             }
         } else {
             for (int k = tid; k < kn; k += 256) {
-                const uint32_t w = cnt[k], bx = c.bias ? bix[k] : 0;
-                const bool ok = !mask || ((mask[(k0 + k) >> 5] >> ((k0 + k) & 31)) & 1);
-                if (in_place && !w && !bx && ok) continue;
-                o[k0 + k] = rule(k, ld<T>(z, k0 + k), w, bx, ok);
+                const uint32_t w = cnt[k];
+                const bool ok = !r.mask || ((r.mask[(k0 + k) >> 5] >> ((k0 + k) & 31)) & 1);
+                if (PLACE && !w && ok) continue;
+                const float v = rule(ld<T>(z, k0 + k), w, k);
+                o[k0 + k] = ok ? v : -INFINITY;
             }
         }
-        if (n_own[t - r0]) {
+        if (mine && t + 1 < r1) {
             __syncthreads();
-            for (int i = tid; i < n_own[t - r0]; i += 256) atomicSub(&cnt[own[t - r0][i]], 1u);
+            for (int i = tid; i < mine; i += 256) atomicSub(&cnt[own[t - r0][i]], 1u);
+            __syncthreads();
         }
     }
 }
@@ -162,20 +281,18 @@ void launch_rules(const RulesCall& c, hipStream_t s) {
     // rows that share their histories' counts, while there are workgroups for every CU
     int rows = kRowsMax;
     while (rows > 1 && (int64_t)((c.n_rows + rows - 1) / rows) * chunks < 4 * cu_count()) rows /= 2;
-    const size_t lds = (size_t)kChunk * 4 * (c.bias ? 2 : 1);
+    const size_t lds = (size_t)kChunk * 4 * (c.bias ? 3 : 1);
     const int words = (c.V + 31) / 32;
     const dim3 grid(chunks, (c.n_rows + rows - 1) / rows);
     // four elements a load where every row starts on that
     const uintptr_t es = c.bf16 ? 2 : 4;
     const bool vec = c.V % 4 == 0 && c.stride % 4 == 0 && c.ostride % 4 == 0 && (uintptr_t)c.logits % (4 * es) == 0 &&
                      (uintptr_t)c.out % 16 == 0;
-    if (c.bf16) {
-        if (vec) hipLaunchKernelGGL((k_rules<bf16_t, true>), grid, dim3(256), lds, s, c, rows, words);
-        else hipLaunchKernelGGL((k_rules<bf16_t, false>), grid, dim3(256), lds, s, c, rows, words);
-    } else {
-        if (vec) hipLaunchKernelGGL((k_rules<float, true>), grid, dim3(256), lds, s, c, rows, words);
-        else hipLaunchKernelGGL((k_rules<float, false>), grid, dim3(256), lds, s, c, rows, words);
-    }
+    const bool place = c.logits == (const void*)c.out;  // (fp32)
+    const auto run = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(256), lds, s, c, rows, words); };
+    if (c.bf16) vec ? run(k_rules<bf16_t, true, false>) : run(k_rules<bf16_t, false, false>);
+    else if (place) vec ? run(k_rules<float, true, true>) : run(k_rules<float, false, true>);
+    else vec ? run(k_rules<float, true, false>) : run(k_rules<float, false, false>);
 }
 
 // The rules' arrays; out is left to the caller.
@@ -195,7 +312,8 @@ int32_t rules_of(const sd_logit_rules* r, RulesCall* c) {
          (uintptr_t)r->repetition | (uintptr_t)r->presence | (uintptr_t)r->frequency | (uintptr_t)r->bias_token |
          (uintptr_t)r->bias_value | (uintptr_t)r->bias | (uintptr_t)r->mask | (uintptr_t)r->mask_row) % 4)
         return SD_EINVAL;
-    if (r->n_tokens > 0x7fffffff || r->n_bias > 0x7fffffff) return SD_ELIMIT;
+    // (a token's word counts to 2^30, and a list's index runs past its end by a step)
+    if (r->n_tokens > (1 << 30) - 4096 || r->n_bias > (1 << 30) - 4096) return SD_ELIMIT;
     c->tokens = r->tokens;
     c->n_tokens = (int)r->n_tokens;
     c->hist = r->hist;
