@@ -29,94 +29,187 @@ __device__ __forceinline__ TreeUser tree_user(const TreeCall& c, int b) {
     return u;
 }
 
-// One workgroup per (user, slot, query head); its waves take every fourth block of 64
-// tokens and are merged in wave order.  Scores: lane = token; outputs: lane = dim.
-template <typename T>
-__global__ __launch_bounds__(256) void k_tree_rows(TreeCall c) {
-    __shared__ float qs[128];
-    __shared__ int par[kSlots];
-    __shared__ uint32_t anc[kMaskWords];
-    __shared__ float ps[4][64];
-    __shared__ float ms[4], ls[4], os[4][128];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int h = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
-    const TreeUser u = tree_user(c, b);
-    if (j >= u.n) return;
-    const int hd = c.kv.hd, g = h / (c.hq / c.kv.hkv);
-    const size_t t = u.s0 + j;
-    if (tid < kMaskWords) anc[tid] = 0;
-    if (tid <= j) {
-        const int p = c.parent ? c.parent[u.s0 + tid] : tid - 1;
-        par[tid] = p < tid ? p : -1;
+// anc[j]: bits of slot j and its ancestors, by doubling: what a slot's furthest
+// known ancestor knows is added to it until nobody has one.
+template <int THREADS>
+__device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser& us, uint32_t (*anc)[kMaskWords + 1],
+                                               int* ptr) {
+    static_assert(THREADS >= kSlots, "a thread a slot");
+    const int j = threadIdx.x;
+    int p = -1;
+    if (j < us.n) {
+        p = c.parent ? c.parent[us.s0 + j] : j - 1;
+        p = p >= 0 && p < j ? p : -1;
+#pragma unroll
+        for (int w = 0; w <= kMaskWords; ++w) anc[j][w] = w == j >> 5 ? 1u << (j & 31) : 0;
+        ptr[j] = p;
     }
-    if (tid < hd) {
-        const size_t e = t * c.qs + (size_t)h * hd + tid;
-        qs[tid] = ld<T>((const T*)c.q, e) + (c.q_lo ? ld<T>((const T*)c.q_lo, e) : 0.f);
-    }
-    __syncthreads();
-    if (tid == 0)
-        for (int a = j; a >= 0; a = par[a]) anc[a >> 5] |= 1u << (a & 31);
-    __syncthreads();
-    const int n = min(u.prefix + j + 1, u.end);
-    const int32_t* pt = c.page_table + (size_t)b * c.max_pages;
-    const T* base = (const T*)c.kv.base;
-    float m = -INFINITY, l = 0.f, a0 = 0.f, a1 = 0.f;
-    for (int c0 = wave * 64; c0 < n; c0 += 256) {
-        const int tok = c0 + lane, r = tok - u.prefix;
-        float d = -INFINITY;
-        const int page = tok < n ? pt[tok >> 4] : -1;
-        const bool sees = page >= 0 && page < c.kv.n_pages && (r < 0 || ((anc[r >> 5] >> (r & 31)) & 1));
-        if (sees) {
-            const T* kr = base + c.kv.k_off(c.layer, page, g) + (size_t)(tok & 15) * hd;
-            float s = 0.f;
-            for (int a = 0; a < hd; ++a) s = fmaf(qs[a], ld<T>(kr, a), s);
-            d = s * c.scale;
+    while (__syncthreads_or(p >= 0)) {
+        uint32_t more[kMaskWords] = {};
+        int next = -1;
+        if (p >= 0) {
+#pragma unroll
+            for (int w = 0; w < kMaskWords; ++w) more[w] = anc[p][w];
+            next = ptr[p];
         }
-        const float mn = fmaxf(m, wave_max(d));
-        const float al = mn == -INFINITY ? 1.f : expf(m - mn), pe = sees ? expf(d - mn) : 0.f;
-        l = l * al + wave_sum(pe);
-        m = mn;
-        a0 *= al;
-        a1 *= al;
-        const unsigned long long on = __ballot(sees);
-        wave_lds_order();
-        ps[wave][lane] = pe;
-        wave_lds_order();
-        for (int p = 0; p < 64; ++p) {
-            if (!((on >> p) & 1)) continue;  // (what a row does not see may hold anything)
-            const T* vb = base + c.kv.v_off(c.layer, pt[(c0 + p) >> 4], g) + (p & 15);
-            const float w = ps[wave][p];
-            if (lane < hd) a0 = fmaf(w, ld<T>(vb, (size_t)lane * kPageTokens), a0);
-            if (lane + 64 < hd) a1 = fmaf(w, ld<T>(vb, (size_t)(lane + 64) * kPageTokens), a1);
+        __syncthreads();
+        if (p >= 0) {
+#pragma unroll
+            for (int w = 0; w < kMaskWords; ++w) anc[j][w] |= more[w];
+            ptr[j] = next;
         }
-    }
-    if (lane == 0) {
-        ms[wave] = m;
-        ls[wave] = l;
-    }
-    os[wave][lane] = a0;
-    os[wave][lane + 64] = a1;
-    __syncthreads();
-    if (tid >= hd) return;
-    const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-    float L = 0.f, o = 0.f;
-    for (int w = 0; w < 4; ++w) {
-        if (ms[w] == -INFINITY) continue;
-        const float f = expf(ms[w] - M);
-        L += ls[w] * f;
-        o += os[w][tid] * f;
-    }
-    const size_t e = t * c.os + (size_t)h * hd + tid;
-    const float v = M == -INFINITY ? 0.f : o / L;
-    if constexpr (sizeof(T) == 2) {
-        const __bf16 hi = (__bf16)v;
-        ((__bf16*)c.out)[e] = hi;
-        if (c.out_lo) ((__bf16*)c.out_lo)[e] = (__bf16)(v - (float)hi);
-    } else {
-        ((float*)c.out)[e] = v;
+        p = next;
     }
 }
 
+// fp32: no matrix instruction multiplies in full fp32 precision at more than the vector
+// units' rate, and the contexts of such models are short, so this kernel is the plain
+// one.  A workgroup takes kRows of a user's query rows (slot by slot, the heads of a KV
+// head together), its waves every eighth block of 64 tokens, and their sums are merged
+// in wave order.  Scores: lane = token, W elements of its key a load, each used for all
+// rows (the rows' queries are read from LDS, one 16-byte word for a dim of all rows);
+// outputs: lane = dim, a page's 16 values a load.  Five users of 3 to 17 slots over 63 to
+// 900 tokens, 12 heads of 64 over 4 KV heads: 29.5 us (one row a workgroup, four waves,
+// one element a load: 147).
+constexpr int kRows = 4, kRowWaves = 8;
+template <int W, int DT>
+__global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
+    typedef float fw __attribute__((ext_vector_type(W)));
+    __shared__ f32x4 qs[128];                                            // [dim], a row each element
+    __shared__ __attribute__((aligned(16))) float ps[kRowWaves][64][kRows];
+    __shared__ float ms[kRowWaves][kRows], ls[kRowWaves][kRows], os[kRowWaves][kRows][64 * DT];
+    __shared__ uint32_t anc[kSlots][kMaskWords + 1];
+    __shared__ int ptr[kSlots];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int b = blockIdx.z, g = blockIdx.y, row0 = blockIdx.x * kRows;
+    const TreeUser u = tree_user(c, b);
+    const int hd = c.kv.hd, G = c.hq / c.kv.hkv, R = u.n * G;
+    if (row0 >= R) return;
+    // element of a row's dim 0 in queries (stride c.qs) and outputs (c.os)
+    auto place = [&](int row, int64_t stride) { return (size_t)(u.s0 + row / G) * stride + (size_t)(g * G + row % G) * hd; };
+    if (tid < hd) {
+        f32x4 q;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) q[r] = row0 + r < R ? ((const float*)c.q)[place(row0 + r, c.qs) + tid] : 0.f;
+        qs[tid] = q;
+    }
+    tree_ancestors<64 * kRowWaves>(c, u, anc, ptr);
+    __syncthreads();
+    const int slot1 = min(row0 + kRows - 1, R - 1) / G;  // the last row's
+    const int n = min(u.prefix + slot1 + 1, u.end);
+    const int32_t* pt = c.page_table + (size_t)b * c.max_pages;
+    const float* base = (const float*)c.kv.base;
+    float m[kRows], l[kRows], o[DT][kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d][r] = 0.f;
+    }
+    for (int c0 = wave * 64; c0 < n; c0 += 64 * kRowWaves) {
+        const int tok = c0 + lane, rel = tok - u.prefix;
+        int page = tok < n ? pt[tok >> 4] : -1;
+        if (page >= c.kv.n_pages) page = -1;
+        float s[kRows] = {};
+        if (page >= 0) {
+            const float* kr = base + c.kv.k_off(c.layer, page, g) + (size_t)(tok & 15) * hd;
+#pragma unroll 8
+            for (int a = 0; a < hd; a += W) {
+                const fw k = *(const fw*)(kr + a);
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const f32x4 q = qs[a + e];
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) s[r] = fmaf(q[r], k[e], s[r]);
+                }
+            }
+        }
+        unsigned long long on[kRows], any = 0;
+        f32x4 pe;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int j = (row0 + r) / G;
+            const bool sees = page >= 0 && row0 + r < R && (rel < 0 || (rel <= j && ((anc[j][rel >> 5] >> (rel & 31)) & 1)));
+            on[r] = __ballot(sees);
+            any |= on[r];
+            const float d = sees ? s[r] * c.scale : -INFINITY;
+            const float mn = fmaxf(m[r], wave_max(d));
+            const float al = mn == -INFINITY ? 1.f : expf(m[r] - mn);
+            pe[r] = d == -INFINITY ? 0.f : expf(d - mn);  // (not a number where d is)
+            l[r] = l[r] * al + wave_sum(pe[r]);
+            m[r] = mn;
+#pragma unroll
+            for (int d2 = 0; d2 < DT; ++d2) o[d2][r] *= al;
+        }
+        wave_lds_order();
+        *(f32x4*)ps[wave][lane] = pe;
+        wave_lds_order();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t some = (uint32_t)(any >> (16 * i)) & 0xffff;
+            if (!some) continue;
+            const float* vb = base + c.kv.v_off(c.layer, __builtin_amdgcn_readlane(page, 16 * i), g);
+            f32x4 v[DT][4];
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                if (lane + 64 * d < hd)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[d][x] = *(const f32x4*)(vb + (size_t)(lane + 64 * d) * kPageTokens + 4 * x);
+            uint32_t all = 0xffff;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (row0 + r < R) all &= (uint32_t)(on[r] >> (16 * i));
+            if (all == 0xffff) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const f32x4 w = *(const f32x4*)ps[wave][16 * i + e];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) o[d][r] = fmaf(w[r], v[d][e >> 2][e & 3], o[d][r]);
+                }
+            } else {  // (what a row does not see may hold anything)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const f32x4 w = *(const f32x4*)ps[wave][16 * i + e];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r)
+                            o[d][r] = fmaf(w[r], (on[r] >> (16 * i + e)) & 1 ? v[d][e >> 2][e & 3] : 0.f, o[d][r]);
+                }
+            }
+        }
+    }
+    if (lane == 0) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            ms[wave][r] = m[r];
+            ls[wave][r] = l[r];
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) os[wave][r][lane + 64 * d] = o[d][r];
+    __syncthreads();
+    for (int i = tid; i < kRows * hd; i += 64 * kRowWaves) {
+        const int r = i / hd, a = i % hd;
+        if (row0 + r >= R) break;
+        float M = ms[0][r];
+#pragma unroll
+        for (int w = 1; w < kRowWaves; ++w) M = fmaxf(M, ms[w][r]);
+        float L = 0.f, out = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) {
+            const float f = ms[w][r] == M ? 1.f : expf(ms[w][r] - M);
+            L += ls[w][r] * f;
+            out += os[w][r][a] * f;
+        }
+        ((float*)c.out)[place(row0 + r, c.os) + a] = L == 0.f ? 0.f : out / L;
+    }
+}
 
 // ---------------------------------------------------------------------------
 // bf16, matrix cores.  A workgroup takes one unit -- a chunk of one user's context
@@ -216,39 +309,6 @@ template <int NW> __device__ __forceinline__ TreeSpan tree_find(const TreeCall& 
     f = TreeSpan{same(f.b), same(f.nb), same(f.units), same(f.base)};
     __syncthreads();
     return f;
-}
-
-// anc[j]: bits of slot j and its ancestors, by doubling: what a slot's furthest
-// known ancestor knows is added to it until nobody has one.
-template <int THREADS>
-__device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser& us, uint32_t (*anc)[kMaskWords + 1],
-                                               int* ptr) {
-    static_assert(THREADS >= kSlots, "a thread a slot");
-    const int j = threadIdx.x;
-    int p = -1;
-    if (j < us.n) {
-        p = c.parent ? c.parent[us.s0 + j] : j - 1;
-        p = p >= 0 && p < j ? p : -1;
-#pragma unroll
-        for (int w = 0; w <= kMaskWords; ++w) anc[j][w] = w == j >> 5 ? 1u << (j & 31) : 0;
-        ptr[j] = p;
-    }
-    while (__syncthreads_or(p >= 0)) {
-        uint32_t more[kMaskWords] = {};
-        int next = -1;
-        if (p >= 0) {
-#pragma unroll
-            for (int w = 0; w < kMaskWords; ++w) more[w] = anc[p][w];
-            next = ptr[p];
-        }
-        __syncthreads();
-        if (p >= 0) {
-#pragma unroll
-            for (int w = 0; w < kMaskWords; ++w) anc[j][w] |= more[w];
-            ptr[j] = next;
-        }
-        p = next;
-    }
 }
 
 // Which of the tokens t0 .. t0+31 the slot with ancestors `a` sees.
@@ -898,7 +958,12 @@ void launch_tree_attention(const TreeCall& c, hipStream_t s) {
         else eight ? launch_tree_mfma<64, 8>(c, s) : launch_tree_mfma<64, 4>(c, s);
         return;
     }
-    hipLaunchKernelGGL(k_tree_rows<float>, dim3(c.hq, c.max_slots, c.n_users), dim3(256), 0, s, c);
+    const int rows = c.max_slots * (c.hq / c.kv.hkv);
+    const dim3 grid((rows + kRows - 1) / kRows, c.kv.hkv, c.n_users);
+    const auto run = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(64 * kRowWaves), 0, s, c); };
+    // (a key begins on 16 bytes where four elements divide the head)
+    if (c.kv.hd > 64) c.kv.hd % 4 == 0 ? run(k_tree_rows<4, 2>) : run(k_tree_rows<2, 2>);
+    else c.kv.hd % 4 == 0 ? run(k_tree_rows<4, 1>) : run(k_tree_rows<2, 1>);
 }
 
 }  // namespace sdv
