@@ -688,8 +688,8 @@ sd_status sd_tree_attention(const sd_kv_pool* pool, int32_t layer, const sd_tree
  * Destinations are distinct and no page is both a source and a destination
  * (otherwise what they hold afterwards is undefined).
  * Errors (nothing enqueued): SD_EINVAL (an inconsistent pool, NULL or misaligned
- * pointer, n < 1), SD_ENOTIMPL (head_dim), SD_ELIMIT (n pages of a layer above 2^37
- * bytes, or the pool's limits), SD_EHIP.
+ * pointer, n < 1), SD_ENOTIMPL (head_dim), SD_ELIMIT (n pages of a layer of 2^36
+ * bytes or more, or the pool's limits), SD_EHIP.
  */
 sd_status sd_kv_copy_pages(const sd_kv_pool* pool, int32_t n, const int32_t* src, const int32_t* dst,
                            sd_stream stream);

@@ -101,7 +101,7 @@ def test_page_refusals():
     assert call(n=0) == sv.SD_EINVAL and call(s=None) == sv.SD_EINVAL and call(d=None) == sv.SD_EINVAL
     assert call(s=odd) == sv.SD_EINVAL and call(d=odd) == sv.SD_EINVAL
     assert call(p=pool(base=None)) == sv.SD_EINVAL and call(p=pool(base=64)) == sv.SD_EINVAL
-    assert call(n=(1 << 22) + 1) == sv.SD_ELIMIT  # two pieces of 16 KB a page
+    assert call(n=1 << 21) == sv.SD_ELIMIT  # pages of 32 KB
     assert sv.lib().sd_kv_copy_pages(None, 1, P, P, None) == sv.SD_EINVAL
 
 
@@ -134,6 +134,8 @@ def rules(**kw):
     (dict(n_tokens=-1), sv.SD_EINVAL), (dict(n_bias=-1), sv.SD_EINVAL), (dict(n_masks=-1), sv.SD_EINVAL),
     (dict(repetition=4097), sv.SD_EINVAL), (dict(presence=4097), sv.SD_EINVAL), (dict(frequency=4098), sv.SD_EINVAL),
     (dict(tokens=4097, hist=4096, n_tokens=4), sv.SD_EINVAL), (dict(tokens=4096, hist=4096, n_tokens=1 << 31), sv.SD_ELIMIT),
+    (dict(tokens=4096, hist=4096, n_tokens=(1 << 30) - 4095), sv.SD_ELIMIT),
+    (dict(bias=4096, bias_token=4096, bias_value=4096, n_bias=(1 << 30) - 4095), sv.SD_ELIMIT),
     (dict(bias=4096, bias_token=4096, bias_value=4096, n_bias=1 << 31), sv.SD_ELIMIT),
 ])
 def test_rules_refusals(bad, status):
