@@ -68,7 +68,7 @@ __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser
 // head together), its waves every eighth block of 64 tokens, and their sums are merged
 // in wave order.  Scores: lane = token, W elements of its key a load, each used for all
 // rows (the rows' queries are read from LDS, one 16-byte word for a dim of all rows);
-// outputs: lane = dim, a page's 16 values a load.  Five users of 3 to 17 slots over 63 to
+// outputs: lane = dim, a page's 16 values a load.  Six users of 3 to 17 slots over 63 to
 // 900 tokens, 12 heads of 64 over 4 KV heads: 29.5 us (one row a workgroup, four waves,
 // one element a load: 147).
 constexpr int kRows = 4, kRowWaves = 8;
@@ -429,7 +429,8 @@ template <int HD, bool QLO> struct TreeWave {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// One pass over a segment.  CAREFUL: the values' infinities and not-a-numbers are kept
+// One pass over a segment.  CAREFUL: scores are taken relative to the maximum before they
+// are scaled, and the values' infinities and not-a-numbers are kept
 // apart: 0 times one is not 0 in a product, and rows that do not see such a value, or
 // see it with two weights of opposite sign, must not take part in that.
 template <int HD, bool QLO, int NW, bool CAREFUL, class Q, class F>
@@ -556,13 +557,15 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
                 l *= alpha;
                 m = mn;
             }
-            const float ms = m == -INFINITY ? 0.f : m * sc2;
+            const float m0 = m == -INFINITY ? 0.f : m, ms = m0 * sc2;
+            // (rounding m * sc2 is a common factor of all weights, unless m is huge)
+            auto weight = [&](float v) { return __builtin_amdgcn_exp2f(CAREFUL ? (v - m0) * sc2 : fmaf(v, sc2, -ms)); };
             // the weights as two bf16 planes: hi rounded, lo what that left
             float rs[2] = {0.f, 0.f};
             uint32_t ph[8], pl[8];
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], sc2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], sc2, -ms));
+                const float p0 = weight(s[e]), p1 = weight(s[e + 1]);
                 rs[0] += p0;
                 rs[1] += p1;
                 const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
@@ -662,9 +665,10 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
         __syncthreads();
     };
     tree_pass<HD, QLO, NW, false>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o, queries, ancestors);
-    // a segment whose outputs are not finite is done again, carefully
+    // a segment whose outputs are not finite or whose scores are huge is done again, carefully
     bool odd = false;
     if (w.act) {
+        odd = m != -INFINITY && fabsf(m) * sc2 >= 1048576.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll

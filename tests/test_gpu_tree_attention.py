@@ -85,13 +85,16 @@ class Case:
         sv.sd_tree_attention(self.kv, self.layer, self.tree, self.d_q, self.out, self.ws, q_lo=self.d_lo, out_lo=self.out_lo,
                              scale=scale, stream=stream)
 
-    def check(self, label, scale=None, out=None, out_lo=None):
+    def check(self, label, scale=None, out=None, out_lo=None, scores_of=None):
         torch.cuda.synchronize()
         sc = self.hd ** -0.5 if scale is None else scale
         q = self.q.double().numpy() + (0 if self.q_lo is None else self.q_lo.double().numpy())
         with np.errstate(invalid="ignore", over="ignore"):
             ref, size, score = trees.tree_attention(self.pool.double().numpy(), self.layer, self.off, self.prefix, self.table,
                                                     None if self.no_parent else self.parent, q, sc, self.hkv, self.max_slots)
+            if scores_of is not None:  # a pool without the keys that weigh nothing: no error of theirs counts
+                score = trees.tree_attention(scores_of.double().numpy(), self.layer, self.off, self.prefix, self.table,
+                                             None if self.no_parent else self.parent, q, sc, self.hkv, self.max_slots)[2]
         got = (self.out if out is None else out).double().cpu().numpy()
         lo = self.out_lo if out_lo is None else out_lo
         nobody = np.isnan(ref) & (size == 0)
@@ -241,6 +244,48 @@ def test_values_that_are_seen_pass_on_their_infinities(dtype):
     c.pool[:, int(c.table[1, 0]), 1, 1, 20 * 16 + x] = float("inf")
     c.to_gpu().call()
     c.check(f"{dtype} seen")
+
+
+@pytest.mark.parametrize("dtype,G,planes", [("bf16", 4, 1), ("bf16", 40, 2), ("f32", 4, 1)])
+def test_scores_of_minus_infinity_weigh_nothing(dtype, G, planes):
+    """Whole blocks whose scores are minus infinity or hugely negative, before and between others.  Their weights are
+    0 exactly, so what the other keys' scores allow is the tolerance."""
+    for val in (float("-inf"), -(2.0 ** 100)):
+        c = Case([(1300, 9), (40, 3)], dtype, 64, 1, G, planes=planes, seed=21)
+        c.q[:, :, 3] = 1.0
+        if planes == 2:
+            c.q_lo[:, :, 3] = 2.0 ** -10
+        plain = c.pool.clone()
+        for x in [*range(0, 600), *range(640, 900), 1301]:
+            at = int(c.table[0, x // 16]), 0, slice(None), (x % 16) * 64 + 3
+            c.pool[:, at[0], at[1], at[2], at[3]] = val
+            plain[:, at[0], at[1], at[2], at[3]] = 0
+        c.to_gpu().call()
+        c.check(f"{dtype} {val}", scores_of=plain)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_huge_scores_pick_the_largest(dtype, sign):
+    """Scores of +-2^60 (1 + i): all weight on one token, whose value is the output."""
+    c = Case([(70, 5), (16, 1)], dtype, 64, 1, 4, kind="chain", seed=22)
+    c.q[:] = 0
+    c.q[:, :, 3] = 1.5  # (so that a score times the scale is rounded)
+    for b in range(2):
+        for x in range(int(c.prefix[b]) + int(np.diff(c.off)[b])):
+            c.pool[:, int(c.table[b, x // 16]), 0, :, (x % 16) * 64 + 3] = sign * 2.0 ** 60 * (1 + x % 61)
+    c.to_gpu().call(scale=0.7)
+    got = c.out.cpu().reshape(c.T, c.hq, 64)
+    for b in range(2):
+        for j in range(int(np.diff(c.off)[b])):
+            keys = [x % 61 for x in range(int(c.prefix[b]) + j + 1)]
+            x = [i for i, k in enumerate(keys) if k == (max(keys) if sign > 0 else min(keys))]
+            pages = [c.pool[c.layer, int(c.table[b, i // 16]), 1, 0, i % 16::16] for i in x]
+            want = torch.stack(pages).double().mean(0)
+            assert len(x) <= 2
+            err = (got[int(c.off[b]) + j].double() - want).abs().max().item()
+            # (two equal weights: half of a sum of two bf16 values, rounded once to the output's type)
+            assert err <= want.abs().max().item() * 2.0 ** (-8 if dtype == "bf16" else -22), (b, j, err)
 
 
 def test_large_and_equal_scores():
