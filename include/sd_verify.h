@@ -826,7 +826,8 @@ sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, in
  * is refused (SD_EINVAL; the rules stay), and so is sd_sample_logits of a user
  * never started, whose root token there is none of.
  * Errors: SD_EINVAL, SD_ELIMIT as sd_adjust_logits, SD_ESTATE (the batch's
- * workspace slot is pending).
+ * workspace slot is pending, or has rules for another batch whose pass has not
+ * come; a NULL rules for that batch takes them away).
  */
 sd_status sd_verify_batch_tree(sd_ctx* ctx, int32_t batch, int32_t n_users, const int32_t* assign,
                                const int32_t* draft_len, const int32_t* draft_tokens, const int32_t* parent,

@@ -1561,6 +1561,7 @@ sd_status sd_batch_rules(sd_ctx* c, int32_t batch, int32_t n_rows, const sd_logi
         if (s.rules_batch == batch) s.has_rules = false;
         return SD_OK;
     }
+    if (s.has_rules && s.rules_batch != batch) return SD_ESTATE;  // (that batch's pass would go without)
     if (n_rows < 1 || n_rows > c->cfg.max_batch_tokens || rules->row_token || rules->row_parent) return SD_EINVAL;
     if (n_rows > SD_FILTER_MAX_ROWS || c->cfg.vocab > SD_FILTER_MAX_VOCAB) return SD_ELIMIT;
     RulesCall r{};

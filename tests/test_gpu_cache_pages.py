@@ -92,6 +92,29 @@ def test_the_most_rows(dtype, hd):
         assert np.array_equal(dev.double().cpu().numpy(), host), n
 
 
+def test_a_pool_beyond_32_bits():
+    """Pages whose elements are counted beyond 32 bits in the second of two layers."""
+    r = np.random.default_rng(9)
+    pages, page = 70000, 2 * 8 * 16 * 128
+    big = torch.empty(2 * pages * page, dtype=torch.bfloat16, device="cuda")
+    assert big.numel() > 1 << 32
+    rows = big.view(2, pages, 2, 8, 16 * 128)
+    at = np.array([0, 3, 34000, 51111, 65535, 65536, 69998, 69999])  # the small pool's pages in the large one
+    host, dev, _ = make("bf16", 2, at.size, 8, 128, 9)
+    where = torch.from_numpy(at).cuda()
+    rows[:, where] = dev
+    pool = sv.make_kv_pool(big, 2, pages, 8, 128)
+    src, dst = [1, 6, 3], [7, 0, 4]
+    sv.sd_kv_copy_pages(pool, ints(at[src]), ints(at[dst]))
+    torch.cuda.synchronize()
+    host = trees.copy_pages(host, src, dst)
+    assert np.array_equal(rows[:, where].double().cpu().numpy(), host)
+    table, prefix, keep, n_keep = r.permutation(at.size).reshape(2, 4), [11, 30], r.integers(0, 33, (2, 9)), [9, 7]
+    sv.sd_kv_compact(pool, ints(prefix), ints(at[table]), ints(keep), ints(n_keep))
+    torch.cuda.synchronize()
+    assert np.array_equal(rows[:, where].double().cpu().numpy(), trees.compact(host, prefix, table, keep, n_keep, 128))
+
+
 def test_bits_are_kept():
     """Not-a-numbers with payloads, infinities and subnormals move as they are."""
     r = np.random.default_rng(6)

@@ -182,6 +182,31 @@ def test_in_place(V, pad):
     check(R, before, z, f"in place {V}")
 
 
+@pytest.mark.parametrize("n,V,users", [(1, 3000, 1), (17, 9001, 5), (40, 6000, 13)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_biases(n, V, users, dtype):
+    """More biases than a workgroup has threads, many of one token, next to users of few."""
+    R = Rules(n, V, n, users=users, hist=7000, biases=3500)
+    z = logits(n, V, dtype, n)
+    out = torch.empty((n, V), device="cuda")
+    sv.sd_adjust_logits(z, R.make(), out)
+    check(R, z, out, f"{n}x{V} {dtype}")
+
+
+def test_rows_far_apart():
+    """Rows of logits and results whose elements are counted beyond 32 bits."""
+    R = Rules(5, 700, 3)
+    z = logits(5, 700, "f32", 3)
+    step = (1 << 30) + 4
+    far = torch.empty(4 * step + 700, device="cuda").as_strided((5, 700), (step, 1))
+    far.copy_(z)
+    out = torch.empty(4 * step + 704, device="cuda").as_strided((5, 700), (step + 1, 1))
+    sv.sd_adjust_logits(far, R.make(), out)
+    check(R, z, out, "apart")
+    sv.sd_adjust_logits(far, R.make(), far)
+    check(R, z, far, "in place")
+
+
 def test_long_histories_and_deep_paths():
     R = Rules(260, 2000, 4, users=1, hist=20000, biases=300)
     R.row_parent = np.arange(-1, 259)  # a chain of 260: the first rows are too far below the last

@@ -300,6 +300,21 @@ def test_large_and_equal_scores():
     c.check("equal scores")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_pool_beyond_32_bits(dtype):
+    """Pages whose elements are counted beyond 32 bits in the second of two layers."""
+    c = Case([(300, 9), (17, 4), (64, 1)], dtype, 128, 8, 2, seed=23).to_gpu()
+    pages, n = 70000, c.pool.shape[1]
+    at = np.concatenate([[0, 3], np.linspace(30000, pages - 1, n - 2).astype(int)])
+    big = torch.empty(2 * pages * 2 * 8 * 16 * 128, dtype=DT[dtype], device="cuda")
+    assert big.numel() > 1 << 32
+    big.view(2, pages, 2, 8, 16 * 128)[:, torch.from_numpy(at).cuda()] = c.d_pool
+    c.kv = sv.make_kv_pool(big, 2, pages, 8, 128)
+    c.d[2].copy_(torch.from_numpy(np.where(c.table >= 0, at[c.table], -1).astype(np.int32)))
+    c.call()
+    c.check(f"{dtype} beyond 32 bits")
+
+
 def test_runs_are_equal_and_do_not_depend_on_the_workspace():
     c = Case([(900, 13), (40, 2), (300, 30)], "bf16", 128, 2, 8, planes=2, seed=15).to_gpu()
     c.call()

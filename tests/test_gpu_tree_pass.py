@@ -547,6 +547,31 @@ def test_refusals():
     v.close()
 
 
+def test_rules_wait_for_their_own_batch():
+    """Batches 0 and 2 share a workspace slot: rules for one are not lost to rules for the other."""
+    t = Trees("tiny", [40, 30], [4, 6], seed=78)
+    r = np.random.default_rng(1)
+    raw = t.run()[0]
+    bias = dev(np.stack([np.arange(12), np.arange(1, 13)], 1))  # a token each
+    rules = sv.make_logit_rules(12, t.m.vocab, bias_token=dev(r.permutation(t.m.vocab)[:12]), bias=bias,
+                                bias_value=dev(np.ones(12), np.float32))
+    t.v.batch_rules(0, rules)
+    with pytest.raises(sv.SdError) as e:
+        t.v.batch_rules(2, rules)
+    assert e.value.status == sv.SD_ESTATE
+    t.v.batch_rules(2, None)
+    d, par = dev(np.concatenate(t.drafts)), np.concatenate(t.parent)
+    t.v.verify_tree(2, np.where(t.assign == 0, 2, -1), t.draft_len, d, par, "greedy")  # without
+    t.v.accept(2, 2)
+    assert (t.run()[0] != raw).sum() == 12  # the rules were kept
+    t.v.batch_rules(0, rules)
+    t.v.batch_rules(0, None)
+    t.v.batch_rules(2, rules)
+    t.v.batch_rules(2, None)
+    assert np.array_equal(t.run()[0], raw)
+    t.v.close()
+
+
 def test_a_fork_without_room_changes_nothing():
     v = _sampler_verifier(64, 4, 2, 8)  # eight pages
     v.reset_user(0, 62, 1)
