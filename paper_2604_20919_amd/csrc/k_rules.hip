@@ -51,17 +51,33 @@ template <class F> __device__ __forceinline__ void for_list(const int32_t* list,
     }
 }
 
-// Four elements of a row as they lie in memory.
+// Four elements of a row as they lie in memory, where a row may begin at any element:
+// the hardware takes a wide access at any address (229 rows of 155133 fp32 logits take
+// 71 us where those of 155136 take 69; one element a load took 127).
+typedef float f32x4e __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2e __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T> struct Four;
 template <> struct Four<float> {
-    f32x4 v;
+    f32x4e v;
+    __device__ __forceinline__ void load(const float* z) { v = *(const f32x4e*)z; }
+    __device__ __forceinline__ void some(const float* z, int n) {  // the first n < 4
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) v[e] = z[e];
+    }
     __device__ __forceinline__ void get(float (&o)[4]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = v[e];
     }
 };
 template <> struct Four<bf16_t> {
-    uint2 v;
+    u32x2e v;
+    __device__ __forceinline__ void load(const bf16_t* z) { v = *(const u32x2e*)z; }
+    __device__ __forceinline__ void some(const bf16_t* z, int n) {
+        const uint16_t* h = (const uint16_t*)z;
+        v[0] = h[0] | (n > 1 ? (uint32_t)h[1] << 16 : 0u);
+        v[1] = n > 2 ? h[2] : 0u;
+    }
     __device__ __forceinline__ void get(float (&o)[4]) const {
         o[0] = __uint_as_float(v.x << 16);
         o[1] = __uint_as_float(v.x & 0xffff0000u);
@@ -96,10 +112,9 @@ __device__ __forceinline__ RowRules row_rules(const RulesCall& c, int t, int wor
     return r;
 }
 
-// VEC: four elements a load, rows of `out` apart from the logits, the next row's loads in
-// flight while one is written; otherwise one element a load, or in place, where only
-// what changes is read and written.
-template <typename T, bool VEC, bool PLACE>
+// Rows of `out` apart from the logits: the next row's loads are in flight while one is
+// written.  PLACE: in place, where only what changes is read and written.
+template <typename T, bool PLACE>
 __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words) {
     extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
     __shared__ int par[kBack + kRowsMax], tokw[kBack + kRowsMax];
@@ -119,8 +134,11 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
     auto load = [&](int t, Four<T> (&q)[Q]) __attribute__((always_inline)) {
         const T* z = (const T*)c.logits + (size_t)t * c.stride + k0;
 #pragma unroll
-        for (int u = 0; u < Q; ++u)
-            if (4 * tid + 1024 * u < kn) q[u] = *(const Four<T>*)(z + 4 * tid + 1024 * u);
+        for (int u = 0; u < Q; ++u) {
+            const int k = 4 * tid + 1024 * u;
+            if (k + 4 <= kn) q[u].load(z + k);
+            else if (k < kn) q[u].some(z + k, kn - k);
+        }
     };
     auto load_mask = [&](const uint32_t* mask, uint32_t (&q)[Q]) __attribute__((always_inline)) {
 #pragma unroll
@@ -129,7 +147,7 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
             q[u] = mask && k < kn ? mask[(k0 + k) >> 5] >> ((k0 + k) & 31) : 0xfu;
         }
     };
-    if constexpr (VEC && !PLACE) load(r0, now);
+    if constexpr (!PLACE) load(r0, now);
     if (tid < r1 - r0) rules[tid] = row_rules(c, r0 + tid, words);
     if (c.row_token) {
         const int w0 = r0 - kBack;
@@ -159,7 +177,7 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
         n_own[tid] = 0;
     }
     __syncthreads();
-    if constexpr (VEC) load_mask(rules[0].mask, m);
+    load_mask(rules[0].mask, m);
     // every entry of the row's biases whose token is in the chunk: those held, those beyond
     auto for_biases = [&](int oe, int more, const int (&bk)[kHeld], const float (&bv)[kHeld], auto chunk_of, auto f) {
 #pragma unroll
@@ -173,8 +191,8 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
     int hb = -1, hf = -1, he = -1, bb = -1, be = -1;
     for (int t = r0; t < r1; ++t) {
         if (t + 1 < r1) {
-            if constexpr (VEC && !PLACE) load(t + 1, next);
-            if constexpr (VEC) load_mask(rules[t + 1 - r0].mask, mnext);
+            if constexpr (!PLACE) load(t + 1, next);
+            load_mask(rules[t + 1 - r0].mask, mnext);
         }
         const RowRules r = rules[t - r0];
         // the words: anew where history or biases are others, else as they are
@@ -230,41 +248,38 @@ __global__ __launch_bounds__(256) void k_rules(RulesCall c, int rows, int words)
             if (w & kBias) v += bval[k];
             return v;
         };
-        if constexpr (VEC) {
 #pragma unroll
-            for (int u = 0; u < Q; ++u) {
-                const int k = 4 * tid + 1024 * u;
-                if (k >= kn) break;
-                const uint4 w = *(const uint4*)(cnt + k);
-                if constexpr (PLACE) {
-                    if (!(w.x | w.y | w.z | w.w) && !(~m[u] & 0xf)) continue;
-                    now[u] = *(const Four<T>*)(z + k0 + k);
-                }
-                float v[4];
-                now[u].get(v);
-                if (w.x | w.y | w.z | w.w) {
-                    v[0] = rule(v[0], w.x, k);
-                    v[1] = rule(v[1], w.y, k + 1);
-                    v[2] = rule(v[2], w.z, k + 2);
-                    v[3] = rule(v[3], w.w, k + 3);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = m[u] >> e & 1 ? v[e] : -INFINITY;
-                *(f32x4*)(o + k0 + k) = f32x4{v[0], v[1], v[2], v[3]};
+        for (int u = 0; u < Q; ++u) {
+            const int k = 4 * tid + 1024 * u;
+            if (k >= kn) break;
+            const uint4 w = *(const uint4*)(cnt + k);
+            if constexpr (PLACE) {
+                if (!(w.x | w.y | w.z | w.w) && !(~m[u] & 0xf)) continue;
+                if (k + 4 <= kn) now[u].load(z + k0 + k);
+                else now[u].some(z + k0 + k, kn - k);
+            }
+            float v[4];
+            now[u].get(v);
+            if (w.x | w.y | w.z | w.w) {
+                v[0] = rule(v[0], w.x, k);
+                v[1] = rule(v[1], w.y, k + 1);
+                v[2] = rule(v[2], w.z, k + 2);
+                v[3] = rule(v[3], w.w, k + 3);
             }
 #pragma unroll
-            for (int u = 0; u < Q; ++u) {
-                if constexpr (!PLACE) now[u] = next[u];
-                m[u] = mnext[u];
+            for (int e = 0; e < 4; ++e) v[e] = m[u] >> e & 1 ? v[e] : -INFINITY;
+            if (k + 4 <= kn) {
+                *(f32x4e*)(o + k0 + k) = f32x4e{v[0], v[1], v[2], v[3]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (k + e < kn) o[k0 + k + e] = v[e];
             }
-        } else {
-            for (int k = tid; k < kn; k += 256) {
-                const uint32_t w = cnt[k];
-                const bool ok = !r.mask || ((r.mask[(k0 + k) >> 5] >> ((k0 + k) & 31)) & 1);
-                if (PLACE && !w && ok) continue;
-                const float v = rule(ld<T>(z, k0 + k), w, k);
-                o[k0 + k] = ok ? v : -INFINITY;
-            }
+        }
+#pragma unroll
+        for (int u = 0; u < Q; ++u) {
+            if constexpr (!PLACE) now[u] = next[u];
+            m[u] = mnext[u];
         }
         if (mine && t + 1 < r1) {
             __syncthreads();
@@ -284,15 +299,10 @@ void launch_rules(const RulesCall& c, hipStream_t s) {
     const size_t lds = (size_t)kChunk * 4 * (c.bias ? 3 : 1);
     const int words = (c.V + 31) / 32;
     const dim3 grid(chunks, (c.n_rows + rows - 1) / rows);
-    // four elements a load where every row starts on that
-    const uintptr_t es = c.bf16 ? 2 : 4;
-    const bool vec = c.V % 4 == 0 && c.stride % 4 == 0 && c.ostride % 4 == 0 && (uintptr_t)c.logits % (4 * es) == 0 &&
-                     (uintptr_t)c.out % 16 == 0;
     const bool place = c.logits == (const void*)c.out;  // (fp32)
     const auto run = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(256), lds, s, c, rows, words); };
-    if (c.bf16) vec ? run(k_rules<bf16_t, true, false>) : run(k_rules<bf16_t, false, false>);
-    else if (place) vec ? run(k_rules<float, true, true>) : run(k_rules<float, false, true>);
-    else vec ? run(k_rules<float, true, false>) : run(k_rules<float, false, false>);
+    if (c.bf16) run(k_rules<bf16_t, false>);
+    else place ? run(k_rules<float, true>) : run(k_rules<float, false>);
 }
 
 // The rules' arrays; out is left to the caller.

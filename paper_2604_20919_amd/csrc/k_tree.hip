@@ -212,20 +212,36 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
 }
 
 // ---------------------------------------------------------------------------
-// bf16, matrix cores.  A workgroup takes one unit -- a chunk of one user's context
-// for one KV head -- and up to 128 of the user's query rows (slots times the G
-// heads that share the KV head), a wave 32 of them.  The chunk streams through a
-// ring of LDS buffers in blocks of 32 tokens (two pages, K and V), loaded straight
-// from global memory, and per block
+// bf16, matrix cores.  A unit is a group of up to 32 NW of a user's query rows (slots
+// times the G heads that share a KV head) with the user's context for that head.  The
+// context streams through a ring of LDS buffers in blocks of 32 tokens (two pages, K and
+// V), loaded straight from global memory, and per block a wave takes 32 rows through
 //   S^T = K Q^T        K rows as the A operand, in a token order that leaves a lane
 //                      with 8 consecutive tokens of its row twice over, which is
 //   O^T += V^T P^T     the B operand of the second product, V^T from the page's
-//                      dim-major block; P in two bf16 planes.
+//                      dim-major block; P in two bf16 planes (one would save 18 % of a
+//                      wide tree's time and cost 1.4 times the error).
+//
+// What bounds it.  Few rows: the cache, read once a row group.  The layout keeps whole
+// pages together for that (4 KB of K and of V, loaded in 1 KB pieces), all blocks are
+// shared out evenly (below), and two blocks are loaded while two are used: 32 users of
+// 2292 tokens, 8 KV heads of 128, 4 / 8 / 13 slots of 8 heads: 61 / 67 / 97 us for 300 MB,
+// 5.0 / 4.5 / 3.1 TB/s; with two planes of queries 77 us at 8 slots.  One token over 131072
+// tokens, 4 heads of 64 (134 MB): 32 us + 6 for the merge.  Many rows: the parts add up,
+// since all of them draw on the same power and registers hold one block's fragments a
+// wave: 16 trees of 64 slots, 64 heads, 1024 to 8192 tokens take 295 us; without the second
+// product 209, without the softmax 247, without the first product 249, without all three 166.
+// The same instructions interleaved by hand over two blocks took 359.
+//
+// Two blocks a stage, two token groups for few rows, a maximum followed only when it is
+// far off, and merges two segments at a time together brought the ragged users (2 to 13
+// slots over 256 to 4096 tokens, two planes) from 142 to 105 us, the one token from 59 to
+// 38 and the wide trees from 369 to 303.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kBlock = 32;   // tokens a block
+constexpr int kBlock = 32;  // tokens a block
 
 // All blocks of all units -- a user's query rows in groups, for every KV head --
 // stand in one line, and every workgroup takes `per` of them.  A unit that lies in
@@ -779,6 +795,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_mfma(TreeCall c, TreePlan p
 // Merges the segments of units that lie in several workgroups' parts, in their order.
 // HD / 4 lanes take a row's segments, two at a time (a unit seldom lies in more than
 // three parts); where there are few rows SPLIT such groups share a row's, four at a time.
+// 4 us (8 slots of 16 heads, one user), 8 (32 ragged users, 64 heads), 17 (16 trees of 64).
 template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge(TreeCall c, TreePlan pl, int wrows) {
     constexpr int LANES = HD / 4, GROUPS = 256 / LANES, ROWS = GROUPS / SPLIT;
     __shared__ float2 sml[GROUPS];
