@@ -963,8 +963,11 @@ template <int HD, int NW> static void launch_tree_mfma(const TreeCall& c, hipStr
     if (c.q_lo) hipLaunchKernelGGL((k_tree_mfma<HD, true, NW>), dim3(wgs), dim3(64 * NW), 0, s, c, pl);
     else hipLaunchKernelGGL((k_tree_mfma<HD, false, NW>), dim3(wgs), dim3(64 * NW), 0, s, c, pl);
     constexpr int GROUPS = 256 / (HD / 4);
-    // few rows: a workgroup each
-    if ((int64_t)c.n_slots * c.hq <= 512) {
+    // Few rows, or rows in 16 parts or more: a workgroup each.  (2 users of 8 slots of 64
+    // heads over 2000 tokens, units in 32 parts: 40 -> 32 us; 4 users, 16 parts: 42 -> 39;
+    // 8 users, 8 parts: 44 -> 47)
+    const int64_t units = (int64_t)c.n_users * c.kv.hkv * ((c.max_slots * (c.hq / c.kv.hkv) + 32 * NW - 1) / (32 * NW));
+    if ((int64_t)c.n_slots * c.hq <= 512 || wgs >= 16 * units) {
         hipLaunchKernelGGL((k_tree_merge<HD, GROUPS>), dim3(c.max_slots * c.hq, c.n_users), dim3(256), 0, s, c, pl, 32 * NW);
     } else {
         hipLaunchKernelGGL((k_tree_merge<HD, 1>), dim3((c.max_slots * c.hq + GROUPS - 1) / GROUPS, c.n_users), dim3(256), 0, s,
