@@ -204,7 +204,7 @@ class _Context:
     """What sd_adapters_set and others need to know of a context, and the adapters
     and batches' rules that the library reads in place."""
 
-    def __init__(self, n_layers: int, device: int, vocab: int, max_draft: int):
+    def __init__(self, n_layers: int, device: int, vocab: int = 0, max_draft: int = 0):
         self.n_layers, self.device, self.adapters = n_layers, device, None
         self.vocab, self.max_draft, self.rules = vocab, max_draft, {}
 
