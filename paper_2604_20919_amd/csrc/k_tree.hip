@@ -65,19 +65,19 @@ __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser
 // fp32: no matrix instruction multiplies in full fp32 precision at more than the vector
 // units' rate, and the contexts of such models are short, so this kernel is the plain
 // one.  A workgroup takes kRows of a user's query rows (slot by slot, the heads of a KV
-// head together), its waves every eighth block of 64 tokens, and their sums are merged
+// head together), its NW waves every NW-th block of 64 tokens, and their sums are merged
 // in wave order.  Scores: lane = token, W elements of its key a load, each used for all
 // rows (the rows' queries are read from LDS, one 16-byte word for a dim of all rows);
 // outputs: lane = dim, a page's 16 values a load.  Six users of 3 to 17 slots over 63 to
 // 900 tokens, 12 heads of 64 over 4 KV heads: 29.5 us (one row a workgroup, four waves,
 // one element a load: 147).
-constexpr int kRows = 4, kRowWaves = 8;
-template <int W, int DT>
-__global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
+constexpr int kRows = 4;
+template <int W, int DT, int NW>
+__global__ __launch_bounds__(64 * NW) void k_tree_rows(TreeCall c) {
     typedef float fw __attribute__((ext_vector_type(W)));
     __shared__ f32x4 qs[128];                                            // [dim], a row each element
-    __shared__ __attribute__((aligned(16))) float ps[kRowWaves][64][kRows];
-    __shared__ float ms[kRowWaves][kRows], ls[kRowWaves][kRows], os[kRowWaves][kRows][64 * DT];
+    __shared__ __attribute__((aligned(16))) float ps[NW][64][kRows];
+    __shared__ float ms[NW][kRows], ls[NW][kRows], os[NW][kRows][64 * DT];
     __shared__ uint32_t anc[kSlots][kMaskWords + 1];
     __shared__ int ptr[kSlots];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
         for (int r = 0; r < kRows; ++r) q[r] = row0 + r < R ? ((const float*)c.q)[place(row0 + r, c.qs) + tid] : 0.f;
         qs[tid] = q;
     }
-    tree_ancestors<64 * kRowWaves>(c, u, anc, ptr);
+    tree_ancestors<64 * NW>(c, u, anc, ptr);
     __syncthreads();
     const int slot1 = min(row0 + kRows - 1, R - 1) / G;  // the last row's
     const int n = min(u.prefix + slot1 + 1, u.end);
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d][r] = 0.f;
     }
-    for (int c0 = wave * 64; c0 < n; c0 += 64 * kRowWaves) {
+    for (int c0 = wave * 64; c0 < n; c0 += 64 * NW) {
         const int tok = c0 + lane, rel = tok - u.prefix;
         int page = tok < n ? pt[tok >> 4] : -1;
         if (page >= c.kv.n_pages) page = -1;
@@ -194,15 +194,15 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_tree_rows(TreeCall c) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) os[wave][r][lane + 64 * d] = o[d][r];
     __syncthreads();
-    for (int i = tid; i < kRows * hd; i += 64 * kRowWaves) {
+    for (int i = tid; i < kRows * hd; i += 64 * NW) {
         const int r = i / hd, a = i % hd;
         if (row0 + r >= R) break;
         float M = ms[0][r];
 #pragma unroll
-        for (int w = 1; w < kRowWaves; ++w) M = fmaxf(M, ms[w][r]);
+        for (int w = 1; w < NW; ++w) M = fmaxf(M, ms[w][r]);
         float L = 0.f, out = 0.f;
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float f = ms[w][r] == M ? 1.f : expf(ms[w][r] - M);
             L += ls[w][r] * f;
             out += os[w][r][a] * f;
@@ -984,10 +984,23 @@ void launch_tree_attention(const TreeCall& c, hipStream_t s) {
     }
     const int rows = c.max_slots * (c.hq / c.kv.hkv);
     const dim3 grid((rows + kRows - 1) / kRows, c.kv.hkv, c.n_users);
-    const auto run = [&](auto fn) { hipLaunchKernelGGL(fn, grid, dim3(64 * kRowWaves), 0, s, c); };
+    // Eight waves a workgroup, or four where contexts have no more than four blocks, or no
+    // more than 16 and there are more workgroups than two a CU.  (8 / 4 waves: 10 users of 6
+    // slots of 40 heads over 25 tokens, 640 workgroups, 31 / 17 us; six users of 3 to 17 slots
+    // over 63 to 900 tokens, 312, 29 / 36; 32 such users, 1664, 54 / 51; 32 over 2000, 162 / 172)
+    const bool few = c.max_pages <= 16 || (c.max_pages <= 64 && (int64_t)grid.x * grid.y * grid.z > 2 * cu_count());
+    const auto run = [&](auto eight, auto four) {
+        if (few) hipLaunchKernelGGL(four, grid, dim3(256), 0, s, c);
+        else hipLaunchKernelGGL(eight, grid, dim3(512), 0, s, c);
+    };
     // (a key begins on 16 bytes where four elements divide the head)
-    if (c.kv.hd > 64) c.kv.hd % 4 == 0 ? run(k_tree_rows<4, 2>) : run(k_tree_rows<2, 2>);
-    else c.kv.hd % 4 == 0 ? run(k_tree_rows<4, 1>) : run(k_tree_rows<2, 1>);
+    if (c.kv.hd > 64) {
+        if (c.kv.hd % 4 == 0) run(k_tree_rows<4, 2, 8>, k_tree_rows<4, 2, 4>);
+        else run(k_tree_rows<2, 2, 8>, k_tree_rows<2, 2, 4>);
+    } else {
+        if (c.kv.hd % 4 == 0) run(k_tree_rows<4, 1, 8>, k_tree_rows<4, 1, 4>);
+        else run(k_tree_rows<2, 1, 8>, k_tree_rows<2, 1, 4>);
+    }
 }
 
 }  // namespace sdv

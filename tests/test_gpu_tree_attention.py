@@ -125,6 +125,16 @@ def test_ragged_users(dtype, hd, kind):
     c.check(f"{dtype} {hd} {kind}")
 
 
+@pytest.mark.parametrize("hd", [2, 34, 64, 70, 100, 128])
+@pytest.mark.parametrize("users", [[(0, 1), (1, 9), (63, 2), (64, 3), (200, 17), (255, 1)], [(700, 4)] + [(90, 5)] * 70,
+                                   [(1100, 3), (0, 2)]])
+def test_fp32_contexts(hd, users):
+    """Short contexts, many workgroups, and neither."""
+    c = Case(users, "f32", hd, 2, 5, seed=hd).to_gpu()
+    c.call()
+    c.check(f"f32 {hd}")
+
+
 @pytest.mark.parametrize("hkv,G", [(1, 1), (1, 5), (3, 1), (2, 8), (1, 16), (1, 40), (4, 3), (1, 128)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_head_layouts(hkv, G, dtype):
