@@ -806,7 +806,14 @@ sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, in
  * sd_user_fork: start user `user` with a copy of the first prefix_len cached
  * tokens of user `from` (at most its length) and a root token of its own.
  * Pages that `user` held are given back first.  The copy is enqueued on
- * `stream` without waiting; passes of either user have to be ordered after it.
+ * `stream` without waiting.  Passes, sd_kv_write, sd_kv_read and forks on other
+ * streams come after it by themselves where they take pages that it reads or
+ * writes, whoever holds these by then: either user may be released, reset or
+ * forked again at once.  The caller orders what the context does not see:
+ * what fills the cache of `from` before the copy, sd_kv_write and sd_kv_read that
+ * earlier owners of the pages still have running, the context-free calls on the pool,
+ * and captured work (a fork, pass or write on a stream under capture runs when its
+ * graph is launched).
  * Sampling options and adapter of `user` stay its own.
  * Errors: SD_EINVAL (a user, length or token out of range, `from` not started,
  * the same user), SD_ESTATE (one of them pending), SD_ENOMEM (pool exhausted;

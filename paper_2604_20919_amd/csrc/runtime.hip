@@ -261,6 +261,14 @@ struct Slot {
     std::vector<int64_t> gkey;
 };
 
+// A fork's copy of pages: its number, an event behind it, and whether the call in hand
+// has to come after it.
+struct PageCopy {
+    int64_t number;
+    hipEvent_t done;
+    bool wanted;
+};
+
 }  // namespace
 
 struct sd_ctx {
@@ -275,6 +283,12 @@ struct sd_ctx {
     PackLayout pl{};
     std::vector<User> users;
     std::vector<int> free_pages;  // stack: back is allocated first
+    // The copies of forks that may still run, oldest first, and for every page the
+    // number of the last copy that read or wrote it (see wait_copies).
+    std::vector<PageCopy> copies;
+    std::vector<int64_t> page_copy;
+    int64_t n_copies = 0;
+    std::vector<hipEvent_t> spare_events;
     Slot slots[kMaxPending];
     int device = 0;
     int attn_cap = 512;  // attention work items that run in one wave of workgroups
@@ -316,6 +330,60 @@ bool reserve_to(sd_ctx* c, User& u, int want) {
         c->free_pages.pop_back();
     }
     return true;
+}
+
+// Pages outlive their owners: a fork's copy may still read or write pages that were given
+// back and handed out again since.  So whatever is enqueued on pages waits, on its own
+// stream, for the copies that had a part in them:
+//   want_copies   marks the copies that the pages p[0 .. n-1] have been in,
+//   wait_copies   lets the stream wait for those marked.
+// A copy itself waits for the earlier ones of its pages, so a page's last copy stands
+// for all of them.  Streams under capture do not wait: their work runs when their
+// graph is launched, which the caller orders.  Nothing here costs a context without copies
+// in flight anything.
+
+// The thread may ask events while other streams are captured.
+struct AnyCapture {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    AnyCapture() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+    ~AnyCapture() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+};
+
+bool is_capturing(hipStream_t st) {
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    return st && hipStreamIsCapturing(st, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone;
+}
+
+// Forgets the copies that are done.
+void retire_copies(sd_ctx* c) {
+    if (c->copies.empty()) return;
+    AnyCapture any;
+    size_t n = 0;
+    for (const PageCopy& p : c->copies) {
+        if (hipEventQuery(p.done) == hipSuccess) c->spare_events.push_back(p.done);  // (room: sd_user_fork)
+        else c->copies[n++] = p;
+    }
+    (void)hipGetLastError();  // (an event that is not done is no error of a launch)
+    c->copies.resize(n);
+    for (PageCopy& p : c->copies) p.wanted = false;
+}
+
+void want_copies(sd_ctx* c, const int* pages, int n) {
+    if (c->copies.empty()) return;
+    for (int i = 0; i < n; ++i) {
+        const int64_t number = c->page_copy[pages[i]];
+        if (number < c->copies.front().number) continue;
+        const auto at = std::lower_bound(c->copies.begin(), c->copies.end(), number,
+                                         [](const PageCopy& p, int64_t v) { return p.number < v; });
+        if (at != c->copies.end() && at->number == number) at->wanted = true;
+    }
+}
+
+sd_status wait_copies(sd_ctx* c, hipStream_t st) {
+    if (c->copies.empty() || is_capturing(st)) return SD_OK;
+    for (const PageCopy& p : c->copies)
+        if (p.wanted) SD_HIP(hipStreamWaitEvent(st, p.done, 0));
+    return SD_OK;
 }
 
 BatchView make_view(sd_ctx* c, Slot& s) {
@@ -878,6 +946,7 @@ sd_status sd_verify_init(const sd_config* cfg, const sd_weights* w, void* kv_poo
     c->users.resize(cfg->max_users);
     c->free_pages.reserve(cfg->n_pages);
     for (int p = cfg->n_pages - 1; p >= 0; --p) c->free_pages.push_back(p);
+    c->page_copy.assign(cfg->n_pages, 0);
     const Layout& L = c->lay;
     bool ok = true;
     for (int i = 0; i < cfg->max_pending && ok; ++i) {
@@ -962,6 +1031,11 @@ sd_status sd_verify_destroy(sd_ctx* c) {
         if (s.result_host) (void)hipHostFree(s.result_host);
     }
     for (hipEvent_t e : c->prof_ev) (void)hipEventDestroy(e);
+    for (const PageCopy& p : c->copies) {
+        (void)hipEventSynchronize(p.done);
+        (void)hipEventDestroy(p.done);
+    }
+    for (hipEvent_t e : c->spare_events) (void)hipEventDestroy(e);
     delete c;
     return SD_OK;
 }
@@ -1081,17 +1155,57 @@ sd_status sd_user_fork(sd_ctx* c, int32_t user, int32_t from, int32_t prefix_len
     // its own pages first, then free ones
     const int need = pages_for(prefix_len), own = (int)u.pages.size(), free_n = (int)c->free_pages.size();
     if (need > own + free_n) return SD_ENOMEM;
+    const hipStream_t st = (hipStream_t)stream;
+    hipEvent_t done = nullptr;
+    retire_copies(c);
+    if (need > 0) {
+        try {
+            u.pages.reserve(need);
+            c->copies.reserve(c->copies.size() + 1);
+            c->spare_events.reserve(c->spare_events.size() + c->copies.size() + 1);
+        } catch (const std::bad_alloc&) {
+            return SD_ENOMEM;
+        }
+        want_copies(c, f.pages.data(), need);
+        want_copies(c, u.pages.data(), std::min(own, need));
+        if (need > own) want_copies(c, c->free_pages.data() + free_n - (need - own), need - own);
+        const sd_status rs = wait_copies(c, st);
+        if (rs != SD_OK) return rs;
+        if (!is_capturing(st)) {
+            if (!c->spare_events.empty()) {
+                done = c->spare_events.back();
+                c->spare_events.pop_back();
+            } else {
+                SD_HIP(hipEventCreateWithFlags(&done, hipEventDisableTiming));
+            }
+        }
+    }
     CopyPages ids;
-    for (int p0 = 0; p0 < need; p0 += kCopyPages) {
+    hipError_t e = hipSuccess;
+    for (int p0 = 0; p0 < need && e == hipSuccess; p0 += kCopyPages) {
         const int n = std::min(kCopyPages, need - p0);
         for (int i = 0; i < n; ++i) {
             const int p = p0 + i;
             ids.src[i] = f.pages[p];
             ids.dst[i] = p < own ? u.pages[p] : c->free_pages[free_n - 1 - (p - own)];
         }
-        launch_copy_pages(c->kv, c->D.L, n, ids, (hipStream_t)stream);
-        SD_HIP(hipGetLastError());
+        launch_copy_pages(c->kv, c->D.L, n, ids, st);
+        e = hipGetLastError();
     }
+    if (done) {
+        // (also behind a copy that was enqueued in part; without an event it is waited for)
+        ++c->n_copies;
+        for (int p = 0; p < need; ++p) {
+            c->page_copy[f.pages[p]] = c->n_copies;
+            c->page_copy[p < own ? u.pages[p] : c->free_pages[free_n - 1 - (p - own)]] = c->n_copies;
+        }
+        if (hipEventRecord(done, st) != hipSuccess) {
+            e = hipErrorUnknown;
+            (void)hipStreamSynchronize(st);
+        }
+        c->copies.push_back(PageCopy{c->n_copies, done, false});
+    }
+    if (e != hipSuccess) return SD_EHIP;
     release_to(c, u, need);
     reserve_to(c, u, need);  // (takes them from the back, as above)
     u.active = true;
@@ -1112,6 +1226,12 @@ static sd_status kv_copy(sd_ctx* c, int32_t user, int32_t layer, int32_t pos0, i
     if (n == 0) return SD_OK;
     if (to_pool && u.pending_slot >= 0) return SD_ESTATE;
     hipStream_t st = (hipStream_t)stream;
+    if (!c->copies.empty()) {
+        retire_copies(c);
+        want_copies(c, u.pages.data() + pos0 / kPageTokens, pages_for(pos0 + n) - pos0 / kPageTokens);
+        const sd_status rs = wait_copies(c, st);
+        if (rs != SD_OK) return rs;
+    }
     // one launch per kKVCopyPages pages; the page ids ride in the kernel
     // arguments, so nothing is staged and the call does not wait
     const size_t row = (size_t)c->D.hkv * c->D.hd * (c->D.bf16 ? 2 : 4);
@@ -1425,9 +1545,15 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     bv.q_rest = sq.rest;
     bv.qk = sq.k;
     hipStream_t st = (hipStream_t)stream;
+    sd_status rs = SD_OK;
+    if (!sample_only && !c->copies.empty()) {
+        retire_copies(c);
+        for (int m : users) want_copies(c, c->users[m].pages.data(), (int)c->users[m].pages.size());
+        rs = wait_copies(c, st);
+    }
     // an open profiling window records events between launches: eager path
-    sd_status rs = graph && c->prof_class == 0 ? enqueue_graph(c, s, bv, st)
-                                               : enqueue_pass(c, s, bv, logits, st, probs);
+    if (rs == SD_OK)
+        rs = graph && c->prof_class == 0 ? enqueue_graph(c, s, bv, st) : enqueue_pass(c, s, bv, logits, st, probs);
     if (rs == SD_OK) rs = hip_status(hipEventRecord(s.done, st));
     if (rs != SD_OK) {
         if (!sample_only)
