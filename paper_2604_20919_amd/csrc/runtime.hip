@@ -410,9 +410,10 @@ BatchView make_view(sd_ctx* c, Slot& s) {
 // Collect the users of batch `batch` and validate every argument that does
 // not need the device.  Fills users / Ls / T / nd.
 // draft_len == NULL: a decode step, every batch user contributes its root
-// alone (l_m = 0, one query slot).
+// alone (l_m = 0, one query slot).  need_active: every user has been started;
+// in_cache: its slots get keys and values, for which its context has to have room.
 sd_status collect_batch(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t* assign,
-                        const int32_t* draft_len, bool need_active, std::vector<int>& users,
+                        const int32_t* draft_len, bool need_active, bool in_cache, std::vector<int>& users,
                         std::vector<int>& Ls, int& T, int& nd) {
     if (batch < 0 || n_users < 1 || n_users > c->cfg.max_users || !assign) return SD_EINVAL;
     users.clear();
@@ -424,10 +425,8 @@ sd_status collect_batch(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
         const int L = draft_len ? draft_len[m] : 0;
         if (draft_len && (L < 1 || L > c->cfg.max_draft)) return SD_EINVAL;
         const User& u = c->users[m];
-        if (need_active) {
-            if (!u.active) return SD_EINVAL;
-            if (u.prefix + L + 1 > c->cfg.max_ctx) return SD_EINVAL;
-        }
+        if (need_active && !u.active) return SD_EINVAL;
+        if (in_cache && u.prefix + L + 1 > c->cfg.max_ctx) return SD_EINVAL;
         if (u.pending_slot >= 0) return SD_ESTATE;
         users.push_back(m);
         Ls.push_back(L);
@@ -1468,7 +1467,8 @@ static sd_status submit(sd_ctx* c, int32_t batch, int32_t n_users, const int32_t
     int T = 0, nd = 0;
     const bool ruled = s.has_rules && s.rules_batch == batch;
     // (rules count the users' root tokens, also on the caller's logits)
-    sd_status r = collect_batch(c, batch, n_users, assign, draft_len, !sample_only || ruled, users, Ls, T, nd);
+    sd_status r = collect_batch(c, batch, n_users, assign, draft_len, !sample_only || ruled, !sample_only, users, Ls, T,
+                                nd);
     if (r != SD_OK) return r;
     if (ruled && s.rules_rows != T) return SD_EINVAL;
     if (parent) {
