@@ -253,7 +253,7 @@ struct TreePlan {
     int* per;       // blocks a workgroup, as the kernel found it
     int* base;      // [n_users] where a user's first unit begins
     float* part;    // [2 wgs][prows][HD] outputs of segments, not yet divided
-    float2* ml;     // [2 wgs][prows] their maxima (log2 domain) and sums
+    float2* ml;     // [2 wgs][prows] their maxima (before scaling) and sums
 };
 
 // A user in the line: its units (KV head by KV head, row group by row group) of nb
@@ -335,6 +335,19 @@ __device__ __forceinline__ uint32_t tree_bits(const uint32_t* a, int t0, int pre
     if (r >= kSlots) return 0;
     const uint64_t two = (uint64_t)a[r >> 5] | ((uint64_t)a[(r >> 5) + 1] << 32);
     return (uint32_t)(two >> (r & 31));
+}
+
+// A maximum in the log2 domain, rounded.  (Never fused into what uses it: every use has
+// to see the same rounding.)
+__device__ __forceinline__ float log2_max(float m, float sc2) {
+#pragma clang fp contract(off)
+    return m * sc2;
+}
+// What the ordinary pass's weights, which are relative to that rounded product, are
+// multiplied by to be relative to m itself.
+__device__ __forceinline__ float to_exact_max(float m, float sc2) {
+    const float lo = fmaf(m, sc2, -log2_max(m, sc2));
+    return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-lo);
 }
 
 __device__ __forceinline__ float half_max(float v) {  // of lanes l and l ^ 32
@@ -445,8 +458,10 @@ template <int HD, bool QLO> struct TreeWave {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// One pass over a segment.  CAREFUL: scores are taken relative to the maximum before they
-// are scaled, and the values' infinities and not-a-numbers are kept
+// One pass over a segment.  The weights are relative to the scaled and rounded maximum
+// (one operation each), so whatever changes the maximum takes the difference of two such
+// products; to_exact_max leads from there to m.  CAREFUL: scores are taken relative to the
+// maximum before they are scaled, and the values' infinities and not-a-numbers are kept
 // apart: 0 times one is not 0 in a product, and rows that do not see such a value, or
 // see it with two weights of opposite sign, must not take part in that.
 template <int HD, bool QLO, int NW, bool CAREFUL, class Q, class F>
@@ -567,14 +582,15 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
             // one is 2^8 beyond it (rescaling the outputs costs as much as a product).
             const float mn = fmaxf(m, half_max(bm));
             if (__builtin_amdgcn_ballot_w64((mn - m) * sc2 > 8.f)) {
-                const float alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sc2);
+                const float alpha =
+                    mn == m ? 1.f
+                            : __builtin_amdgcn_exp2f(CAREFUL ? (m - mn) * sc2 : log2_max(m, sc2) - log2_max(mn, sc2));
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= alpha;
                 l *= alpha;
                 m = mn;
             }
-            const float m0 = m == -INFINITY ? 0.f : m, ms = m0 * sc2;
-            // (rounding m * sc2 is a common factor of all weights, unless m is huge)
+            const float m0 = m == -INFINITY ? 0.f : m, ms = log2_max(m0, sc2);
             auto weight = [&](float v) { return __builtin_amdgcn_exp2f(CAREFUL ? (v - m0) * sc2 : fmaf(v, sc2, -ms)); };
             // the weights as two bf16 planes: hi rounded, lo what that left
             float rs[2] = {0.f, 0.f};
@@ -690,7 +706,9 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
 #pragma unroll
             for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[d][e]) < INFINITY);
     }
-    if (__syncthreads_or(odd)) tree_pass<HD, QLO, NW, true>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o, [] {}, [] {});
+    const bool careful = __syncthreads_or(odd);
+    if (careful) tree_pass<HD, QLO, NW, true>(c, un, us.prefix, w, lds.ring, wave, sc2, m, l, o, [] {}, [] {});
+    auto to_exact = [&](float max) { return careful ? 1.f : to_exact_max(max, sc2); };
     if (tw == 2) {
         // the second token group's sums, through the ring: [tile][4 * dim tiles][lane]
         f32x4* const sp = (f32x4*)lds.ring + tile * (4 * DT * 64);
@@ -708,8 +726,8 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
         if (w.tg == 0 && w.act) {
             const float2 v = sm[lane];
             const float mn = fmaxf(m, v.x);
-            const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sc2);
-            const float f1 = v.x == mn ? 1.f : __builtin_amdgcn_exp2f((v.x - mn) * sc2);
+            const float f0 = to_exact(m) * (m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sc2));
+            const float f1 = to_exact(v.x) * (v.x == mn ? 1.f : __builtin_amdgcn_exp2f((v.x - mn) * sc2));
             m = mn;
             l = l * f0 + v.y * f1;
 #pragma unroll
@@ -746,13 +764,14 @@ __device__ __forceinline__ void tree_segment(const TreeCall& c, const TreePlan& 
         return;
     }
     const size_t pr = (size_t)slot * pl.prows + lrow;
-    if (H == 0) pl.ml[pr] = float2{m == -INFINITY ? -INFINITY : m * sc2, l};
+    const float f = tw == 2 ? 1.f : to_exact(m);
+    if (H == 0) pl.ml[pr] = float2{m, l * f};
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
             *(f32x4*)(pl.part + pr * HD + 32 * d + 8 * q4 + 4 * H) =
-                f32x4{o[d][4 * q4], o[d][4 * q4 + 1], o[d][4 * q4 + 2], o[d][4 * q4 + 3]};
+                f32x4{o[d][4 * q4] * f, o[d][4 * q4 + 1] * f, o[d][4 * q4 + 2] * f, o[d][4 * q4 + 3] * f};
 }
 
 template <int HD, bool QLO, int NW>
@@ -812,6 +831,7 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
     const int per = *pl.per, u0 = pl.base[b] + ((h / G) * groups + row / wrows) * nb;
     const int w0 = (int)((uint32_t)u0 / (uint32_t)per), n = (int)((uint32_t)(u0 + nb - 1) / (uint32_t)per) - w0 + 1;
     const bool mine = on && n > 1;
+    const float sc2 = c.scale * 1.4426950408889634f;
     constexpr int CH = SPLIT > 1 ? 4 : 2;
     float M = -INFINITY, L = 0.f;
     f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -830,7 +850,7 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
         float mg = M;
 #pragma unroll
         for (int i = 0; i < CH; ++i) mg = fmaxf(mg, v[i].x);
-        const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mg);
+        const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((M - mg) * sc2);
         L *= f0;
         a *= f0;
 #pragma unroll
@@ -839,7 +859,7 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
                 L += v[i].y;  // 0, or not a number
                 continue;
             }
-            const float f = __builtin_amdgcn_exp2f(v[i].x - mg);
+            const float f = __builtin_amdgcn_exp2f((v[i].x - mg) * sc2);
             L += v[i].y * f;
             a += p[i] * f;
         }
@@ -853,13 +873,13 @@ template <int HD, int SPLIT> __global__ __launch_bounds__(256) void k_tree_merge
         float mg = M;
 #pragma unroll
         for (int i = 1; i < SPLIT; ++i) mg = fmaxf(mg, sml[grp + i].x);
-        const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mg);
+        const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((M - mg) * sc2);
         L *= f0;
         a *= f0;
 #pragma unroll
         for (int i = 1; i < SPLIT; ++i) {
             const float2 v = sml[grp + i];
-            const float f = v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(v.x - mg);
+            const float f = v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v.x - mg) * sc2);
             L += v.y * f;
             if (v.x != -INFINITY) a += spart[grp + i][ln] * f;
         }
