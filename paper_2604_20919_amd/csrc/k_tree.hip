@@ -4,6 +4,7 @@
 // prefix, its ancestors and itself:  out = sum_p softmax_p(scale q . k_p) v_p.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/sd_verify.h"
 #include "sdv_device.h"
@@ -360,10 +361,14 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 
 // The fragments of one block.  The reads are not the compiler's: it cannot tell the
-// buffer from the ones being loaded and would wait for every load in flight.  K's
-// are waited for; V's are not (wait_v), and begin when the scores are there (s), so
-// that both can have the same registers.  ka: this lane's K pieces (four addresses,
-// the swizzle moves them apart), va: its V slot, in the block's buffer.
+// buffer from the ones being loaded and would wait for every load in flight (as it does
+// for the ancestors' words, in the blocks that reach into a tree).  A statement's
+// registers count as written when it is, so each waits for its own reads: between a
+// read and a later wait the compiler could copy, spill or reuse them.  V's come two
+// dim tiles at a time, the second two while the products of the first run; with all of
+// them read and waited for at once 32 ragged users took 106 us instead of 104.  ka:
+// this lane's K pieces (four addresses, the swizzle moves them apart), va: its V slot,
+// in the block's buffer; AT: of two V tiles within it.
 template <int HD> __device__ __forceinline__ void read_k(bf16x8 (&k)[HD / 16], const uint32_t (&ka)[4]) {
     if constexpr (HD == 128) {
         asm volatile(
@@ -382,32 +387,13 @@ template <int HD> __device__ __forceinline__ void read_k(bf16x8 (&k)[HD / 16], c
             : "memory");
     }
 }
-template <int HD> __device__ __forceinline__ void read_v(bf16x8 (&v)[HD / 16], uint32_t va, f32x16& s) {
-    if constexpr (HD == 128) {
-        asm volatile(
-            "ds_read_b128 %0, %9 offset:8192\n\tds_read_b128 %1, %9 offset:9216\n\t"
-            "ds_read_b128 %2, %9 offset:10240\n\tds_read_b128 %3, %9 offset:11264\n\t"
-            "ds_read_b128 %4, %9 offset:12288\n\tds_read_b128 %5, %9 offset:13312\n\t"
-            "ds_read_b128 %6, %9 offset:14336\n\tds_read_b128 %7, %9 offset:15360"
-            : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]),
-              "+v"(s)
-            : "v"(va)
-            : "memory");
-    } else {
-        asm volatile(
-            "ds_read_b128 %0, %5 offset:4096\n\tds_read_b128 %1, %5 offset:5120\n\t"
-            "ds_read_b128 %2, %5 offset:6144\n\tds_read_b128 %3, %5 offset:7168"
-            : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "+v"(s)
-            : "v"(va)
-            : "memory");
-    }
-}
-template <int N> __device__ __forceinline__ void wait_v(bf16x8 (&v)[N]) {
-    if constexpr (N == 8)
-        asm volatile("s_waitcnt lgkmcnt(0)"
-                     : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
-    else
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+template <int AT> __device__ __forceinline__ void read_v(bf16x8 (&v)[4], uint32_t va) {
+    asm volatile(
+        "ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%5+1024\n\t"
+        "ds_read_b128 %2, %4 offset:%5+2048\n\tds_read_b128 %3, %4 offset:%5+3072\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+        : "v"(va), "n"(AT)
+        : "memory");
 }
 
 // Eight bf16 values with infinities and not-a-numbers taken out; and where they are:
@@ -552,7 +538,7 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
         for (int k = w.tg; k < ST; k += w.tw) {
             if (!w.act || i + k > last) break;
             const int t0 = (un.blk0 + i + k) * kBlock, buf = stage + k;
-            bf16x8 kf[DS], vf[DS];
+            bf16x8 kf[DS];
             const uint32_t at = (uint32_t)(buf * BUF), kb[4] = {w.ka[0] + at, w.ka[1] + at, w.ka[2] + at, w.ka[3] + at};
             read_k<HD>(kf, kb);
             // (two sums: a product waits for the one before it in its own)
@@ -564,7 +550,6 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
                 else s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[d + 1], w.qf[d + 1], s2, 0, 0, 0);
             }
             s += s2;
-            read_v<HD>(vf, w.va + at, s);
             // lane: tokens t0 + 8 H + e (e < 8) and t0 + 16 + 8 H + e of its row
             const uint32_t both = there >> (2 * (N - 1 - k)) & 3;
             uint32_t see = ~0u;
@@ -606,13 +591,23 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
                                                                 (__bf16)(p1 - __uint_as_float(hi & 0xffff0000u))});
             }
             l += rs[0] + rs[1];
-            wait_v(vf);
+            bf16x8 hi[2], lo[2], z[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                hi[t] = __builtin_bit_cast(bf16x8, uint4{ph[4 * t], ph[4 * t + 1], ph[4 * t + 2], ph[4 * t + 3]});
+                lo[t] = __builtin_bit_cast(bf16x8, uint4{pl[4 * t], pl[4 * t + 1], pl[4 * t + 2], pl[4 * t + 3]});
+            }
             if constexpr (CAREFUL) {
-                bf16x8 z[2];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) z[e >> 3][e & 7] = (__bf16)((see >> (e < 8 ? e : e + 8)) & 1 ? 1.f : 0.f);
+            }
+            // two dim tiles at a time
+            auto tiles = [&](auto first) __attribute__((always_inline)) {
+                constexpr int D0 = decltype(first)::value;
+                bf16x8 vf[4];
+                read_v<2 * PB + 2048 * D0>(vf, w.va + at);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
+                for (int d = 0; CAREFUL && d < 2; ++d) {
 #pragma unroll
                     for (int sign = 0; sign < 2; ++sign) {
                         f32x16 hit = f32x16{};
@@ -621,21 +616,23 @@ __device__ __forceinline__ void tree_pass(const TreeCall& c, const TreeSeg& un, 
                             hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_odd(vf[2 * d + t], sign ? 0xff80 : 0x7f80), z[t],
                                                                           hit, 0, 0, 0);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[d][e] += hit[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+                        for (int e = 0; e < 16; ++e) o[D0 + d][e] += hit[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
                     }
                     vf[2 * d] = only_finite(vf[2 * d]);
                     vf[2 * d + 1] = only_finite(vf[2 * d + 1]);
                 }
-            }
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bf16x8 hi = __builtin_bit_cast(bf16x8, uint4{ph[4 * t], ph[4 * t + 1], ph[4 * t + 2], ph[4 * t + 3]});
-                const bf16x8 lo = __builtin_bit_cast(bf16x8, uint4{pl[4 * t], pl[4 * t + 1], pl[4 * t + 2], pl[4 * t + 3]});
+                for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], hi, o[d], 0, 0, 0);
+                    for (int d = 0; d < 2; ++d)
+                        o[D0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], hi[t], o[D0 + d], 0, 0, 0);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], lo, o[d], 0, 0, 0);
-            }
+                    for (int d = 0; d < 2; ++d)
+                        o[D0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * d + t], lo[t], o[D0 + d], 0, 0, 0);
+                }
+            };
+            tiles(std::integral_constant<int, 0>{});
+            if constexpr (DT == 4) tiles(std::integral_constant<int, 2>{});
         }
     }
     wait_vm<0>();
