@@ -795,7 +795,8 @@ sd_status sd_adjust_logits(int32_t n_rows, int32_t vocab, const void* logits, in
  * target alone, whatever the drafts are and however they were chosen, and no
  * draft probabilities are needed.  The accepted rows are moved together in the
  * cache by the pass itself (positions i_m + 1 .. i_m + a_m).
- * Complete with sd_accept or sd_accept_tree.  Errors as sd_verify_batch, and
+ * Complete with sd_accept or sd_accept_tree.  There is no graph form
+ * (sd_verify_batch_graph takes chains).  Errors as sd_verify_batch, and
  * SD_EINVAL for SD_FORCE or a parent out of range, SD_ENOTIMPL for more than
  * 800 slots.
  *

@@ -11,7 +11,7 @@ namespace {
 
 // A copy is bound by memory: every page read once and written once.  A workgroup copies
 // 4 KB of one page of one layer, 16 bytes a thread, and the stores go past the cache (a
-// user's copy is not read by what follows it at once).  80 pages of 128 KB in 64 layers
+// user's copy is not read by what follows it at once).  80 pages of 64 KB in 64 layers
 // (2 x 335 MB) take 110 us, 6.1 TB/s; with cached stores 114, with 8 or 16 KB a workgroup
 // 123 to 135, and three pages in 28 layers 17 us instead of 6.6.
 constexpr int kCopyPiece = 4096;

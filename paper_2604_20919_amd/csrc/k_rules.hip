@@ -17,7 +17,11 @@
 //     kChunk 2048, rows 2 / 4 / 8:  168 / 144 / 141 us;  229 such rows  73 / 69 / 70
 //     kChunk 4096, rows 2 / 4 / 8:  166 / 162 / 168 us   (an earlier form of the lists)
 // so 2048 and 4: 2.7 TB/s.  Of the 144 us the rows alone are 80 (4.8 TB/s, a copy's rate),
-// histories 17 to 22, masks 12 to 17, biases 22 to 31.
+// histories 17 to 22, masks 12 to 17, biases 22 to 31.  In place the rows are read and
+// written only where something changes them, but looked through the same: 229 fp32 rows
+// with histories and biases 51 us instead of 65 of their own, 416 with masks 126 of 146.
+// A row's drafts are found by one thread, parent after parent: 256 rows of 151936 tokens
+// take 56 us as 256 roots, 95 as one path of 256.
 #include <algorithm>
 
 #include "../../include/sd_verify.h"

@@ -63,15 +63,20 @@ __device__ __forceinline__ void tree_ancestors(const TreeCall& c, const TreeUser
     }
 }
 
-// fp32: no matrix instruction multiplies in full fp32 precision at more than the vector
-// units' rate, and the contexts of such models are short, so this kernel is the plain
-// one.  A workgroup takes kRows of a user's query rows (slot by slot, the heads of a KV
+// fp32, on the vector units: fp32 caches are those of small models with short contexts.  A
+// workgroup takes kRows of a user's query rows (slot by slot, the heads of a KV
 // head together), its NW waves every NW-th block of 64 tokens, and their sums are merged
 // in wave order.  Scores: lane = token, W elements of its key a load, each used for all
 // rows (the rows' queries are read from LDS, one 16-byte word for a dim of all rows);
 // outputs: lane = dim, a page's 16 values a load.  Six users of 3 to 17 slots over 63 to
-// 900 tokens, 12 heads of 64 over 4 KV heads: 29.5 us (one row a workgroup, four waves,
-// one element a load: 147).
+// 900 tokens, 12 heads of 64 over 4 KV heads: 29 us (one row a workgroup, four waves,
+// one element a load: 147).  What bounds it is latency, not the 1.7 us of its products at
+// the vector units' rate (half that of v_mfma_f32_16x16x4_f32, which the fp32 weights'
+// products use: packed fp32 is left out of this build): a wave's blocks follow each
+// other, their page numbers and keys are asked for when the block before is done, a
+// block's four pages of values after its softmax one after the other, and a row's
+// maximum and sum go through twelve shuffles.  A context is not split over workgroups, so
+// one user has no more than a workgroup for kRows rows of a KV head, however long it is.
 constexpr int kRows = 4;
 template <int W, int DT, int NW>
 __global__ __launch_bounds__(64 * NW) void k_tree_rows(TreeCall c) {
@@ -225,19 +230,25 @@ __global__ __launch_bounds__(64 * NW) void k_tree_rows(TreeCall c) {
 //
 // What bounds it.  Few rows: the cache, read once a row group.  The layout keeps whole
 // pages together for that (4 KB of K and of V, loaded in 1 KB pieces), all blocks are
-// shared out evenly (below), and two blocks are loaded while two are used: 32 users of
+// shared out evenly (below), and two blocks are loaded while two are used (but for those that
+// reach into a tree, where the ancestors' words wait for every load): 32 users of
 // 2292 tokens, 8 KV heads of 128, 4 / 8 / 13 slots of 8 heads: 61 / 67 / 97 us for 300 MB,
 // 5.0 / 4.5 / 3.1 TB/s; with two planes of queries 77 us at 8 slots.  One token over 131072
 // tokens, 4 heads of 64 (134 MB): 32 us + 6 for the merge.  Many rows: the parts add up,
 // since all of them draw on the same power and registers hold one block's fragments a
-// wave: 16 trees of 64 slots, 64 heads, 1024 to 8192 tokens take 295 us; without the second
+// wave: 16 trees of 64 slots, 64 heads, 1024 to 8192 tokens take 292 us and 18 for the merge
+// (317 in the first 10 ms after a pause; one call after the other 300 in all, since the
+// merge's start overlaps).  Of that, in a build that took 295: without the second
 // product 209, without the softmax 247, without the first product 249, without all three 166.
 // The same instructions interleaved by hand over two blocks took 359.
 //
 // Two blocks a stage, two token groups for few rows, a maximum followed only when it is
 // far off, and merges two segments at a time together brought the ragged users (2 to 13
 // slots over 256 to 4096 tokens, two planes) from 142 to 105 us, the one token from 59 to
-// 38 and the wide trees from 369 to 303.
+// 38 and the wide trees from 369 to 303 (calls, merges among them).
+//
+// head_dim 128 with two planes of queries takes all 256 registers and spills 18, outside
+// the loop over blocks; the careful pass brings most of them.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
