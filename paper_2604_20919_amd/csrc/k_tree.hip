@@ -401,7 +401,7 @@ template <int HD> __device__ __forceinline__ void read_k(bf16x8 (&k)[HD / 16], c
 template <int AT> __device__ __forceinline__ void read_v(bf16x8 (&v)[4], uint32_t va) {
     asm volatile(
         "ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%5+1024\n\t"
-        "ds_read_b128 %2, %4 offset:%5+2048\n\tds_read_b128 %3, %4 offset:%5+3072\n\ts_waitcnt lgkmcnt(0)"
+        "ds_read_b128 %2, %4 offset:%5+2*1024\n\tds_read_b128 %3, %4 offset:%5+3*1024\n\ts_waitcnt lgkmcnt(0)"
         : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
         : "v"(va), "n"(AT)
         : "memory");
